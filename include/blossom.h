@@ -367,6 +367,87 @@ int blossom_dense_causal_fwd(const blossom_params *p, const void *Q, const void 
                              void *ws, size_t ws_bytes, void *hip_stream);
 
 /*
+ * ---- Serving from a paged key/value cache ----
+ *
+ * A program that answers online keeps each history's keys and values between requests: a prompt's once, then one more for every
+ * new item.  Three entry points work on such a cache: blossom_kv_append puts new tokens into it, blossom_attn_prompt attends
+ * with a run of new tokens, blossom_attn_decode with one new token per sequence.
+ *
+ *   K_cache, V_cache  [n_pages, G, page, d], contiguous: a page holds `page` positions of one sequence, each key/value head's
+ *                     rows together.  The caller owns the pages and hands them out.
+ *   page_table        int32 [S, max_pages]: entry i of row s is the page of positions i*page .. (i+1)*page - 1 of sequence s.
+ *                     With table_per_head (decode only) [S, G, max_pages]: each key/value head lists pages of its own, such as
+ *                     those that a block selection chose (Sec. 3.4, Eq. 14; a page being a selection block); positions then
+ *                     count along the list.  Entries that no visible position needs are not used and may hold anything; a page
+ *                     whose entry is outside [0, n_pages) is skipped: nothing is stored there, its keys are masked.
+ *   kv_len            int32 [S]: positions of each sequence in the cache, the new tokens included: new token i of the n that
+ *                     sequence s brings stands at position kv_len[s] - n + i.
+ *   cu_seqlens        int32 [S+1], ascending from 0: new tokens cu_seqlens[s] .. cu_seqlens[s+1] - 1 of the packed rows are
+ *                     sequence s's (none is allowed).  Rows at and beyond cu_seqlens[S] are left as they are.
+ *   Capacity          a sequence holds at most max_len positions (0: max_pages * page; never more than that).  What would lie
+ *                     beyond, or before position 0, is neither stored nor attended.
+ * Heads are grouped as in Eq. 4-5: H query heads share G key/value heads, head h uses h / (H/G).  Packed rows are tokens:
+ * Q [T,H,d], K and V [T,G,d] with heads and channels contiguous and `*_stride` elements from one token to the next (0: packed
+ * tightly), so that slices of one fused projection can be passed as they are.  Types, ownership, streams and errors as above;
+ * pointers and strides are multiples of 16 bytes.  Everything the cache holds outside the visible positions (older rows of a
+ * page, pages nobody lists) may be any bits.  A value that is not finite at a cached position may reach every new token of
+ * its sequence.  No call synchronises, so all may be captured into a graph.
+ */
+typedef struct {
+  int32_t S;              /* sequences                                                             */
+  int32_t T;              /* packed rows of new tokens (append, prompt); decode has one row per sequence */
+  int32_t H, G, d;        /* query heads, key/value heads (G | H), head dimension in {8,16,32,64,128} */
+  int32_t page;           /* positions a page holds: 8, 16, 32, 64, 128 or 256                     */
+  int32_t n_pages;        /* pages of each cache                                                   */
+  int32_t max_pages;      /* entries of a page-table row                                           */
+  int32_t dtype;          /* BLOSSOM_F32 or BLOSSOM_BF16: Q, K, V, caches and O                    */
+  float softmax_scale;    /* 0.0f means 1/sqrt(d)                                                  */
+  int32_t window;         /* a query at position i sees keys j <= i with i - j < window; 0: all    */
+  int32_t max_len;        /* positions a sequence may hold; 0: max_pages * page                    */
+  int32_t table_per_head; /* decode only: page_table is [S,G,max_pages]                            */
+} blossom_paged_params;
+
+/* Bytes of device workspace of blossom_attn_decode (BLOSSOM_WS_DECODE) and blossom_attn_prompt (BLOSSOM_WS_PROMPT): partial
+ * results where a row's keys are split over workgroups.  Host call, no HIP; 0 for invalid params or when none is needed. */
+enum { BLOSSOM_WS_DECODE = 4, BLOSSOM_WS_PROMPT = 5 };
+size_t blossom_paged_workspace_bytes(const blossom_paged_params *p, int which);
+
+/*
+ * Stores the new tokens' keys and values in the cache, the keys rotated by their positions (Sec. 3.3, the recipe and the channel
+ * pairs of blossom_rope_select_blocks), and writes the rotated queries, in one pass.
+ *   K, V                in   [T,G,d] rows;  Q in [T,H,d] rows, or NULL (then Q_rot is NULL too)
+ *   rope_cos, rope_sin  in   fp32 [max_len (or max_pages*page), d/2], or both NULL: keys are stored as they are (Q NULL then)
+ *   K_cache, V_cache    in/out: the new tokens' rows are written, everything else stays
+ *   Q_rot               out  [T,H,d], packed tightly; zeros for a token without a place (position outside the capacity)
+ */
+int blossom_kv_append(const blossom_paged_params *p, const void *Q, int64_t q_stride, const void *K, int64_t k_stride,
+                      const void *V, int64_t v_stride, const float *rope_cos, const float *rope_sin,
+                      const int32_t *page_table, const int32_t *cu_seqlens, const int32_t *kv_len, void *K_cache,
+                      void *V_cache, void *Q_rot, void *hip_stream);
+
+/*
+ * Attention of one new token per sequence over its cached positions (Eq. 1; the token's own key among them, at kv_len[s] - 1):
+ *   O[s,h] = sum_j p_j V_j, p = softmax over the visible j of softmax_scale * Q[s,h].K_j;  lse[s,h] = log sum exp (natural)
+ * A query that sees no key (kv_len 0, all its pages skipped) gives O = 0 and lse = -inf.
+ *   Q    in   [S,H,d] rows;  O  out  [S,H,d];  lse  out  fp32 [S,H] or NULL
+ *   ws   scratch, >= blossom_paged_workspace_bytes(p, BLOSSOM_WS_DECODE), 16-byte aligned (NULL when that is 0)
+ * With lse, results over disjoint keys (two branches, a cache and a shared prefix) can be joined or gated by the caller.
+ */
+int blossom_attn_decode(const blossom_paged_params *p, const void *Q, int64_t q_stride, const void *K_cache,
+                        const void *V_cache, const int32_t *page_table, const int32_t *kv_len, void *O, float *lse,
+                        void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * The same for runs of new tokens that the cache already holds: whole prompts (kv_len[s] = new tokens of s) or chunks over a
+ * longer past, causal, packed without padding.
+ *   Q    in   [T,H,d] rows;  O  out  [T,H,d];  lse  out  fp32 [T,H] or NULL
+ *   ws   scratch, >= blossom_paged_workspace_bytes(p, BLOSSOM_WS_PROMPT), 16-byte aligned (NULL when that is 0)
+ */
+int blossom_attn_prompt(const blossom_paged_params *p, const void *Q, int64_t q_stride, const void *K_cache,
+                        const void *V_cache, const int32_t *page_table, const int32_t *cu_seqlens, const int32_t *kv_len,
+                        void *O, float *lse, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
  * Measured ceilings of the matrix-core forward (Eq. 1 as tiled QK^T / softmax / PV for the
  * long-term and short-term branches, Eq. 16-17) on the GPU at hand: a stripped copy of its
  * steady-state tile loop for block size 64 and d = 64, with the same instruction mix and memory

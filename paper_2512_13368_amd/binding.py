@@ -15,12 +15,13 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libblossom.so")
 
 F32, BF16 = 0, 1
-WS_SELECT, WS_FWD, WS_BWD, WS_DENSE = 0, 1, 2, 3
+WS_SELECT, WS_FWD, WS_BWD, WS_DENSE, WS_DECODE, WS_PROMPT = 0, 1, 2, 3, 4, 5
 
 EXPORTS = ("blossom_workspace_bytes", "blossom_select_blocks", "blossom_select_blocks_static", "blossom_select_blocks_cmp",
            "blossom_rope_select_blocks", "blossom_attn_bwd_rope", "blossom_select_positions_workspace_bytes",
            "blossom_select_positions", "blossom_attn_fwd_positions", "blossom_attn_bwd_positions", "blossom_out_proj_ln", "blossom_attn_fwd", "blossom_attn_bwd",
-           "blossom_attn_bwd_stages", "blossom_dense_causal_fwd", "blossom_probe_bytes", "blossom_probe", "blossom_strerror", "blossom_version")
+           "blossom_attn_bwd_stages", "blossom_paged_workspace_bytes", "blossom_kv_append", "blossom_attn_decode", "blossom_attn_prompt",
+           "blossom_dense_causal_fwd", "blossom_probe_bytes", "blossom_probe", "blossom_strerror", "blossom_version")
 PROBE_WORKGROUPS = 4096
 BWD_GATE, BWD_INVERSE, BWD_DQ, BWD_DKV, BWD_ALL = 1, 2, 4, 8, 15
 
@@ -31,6 +32,12 @@ class BlossomParams(ctypes.Structure):
                 ("dtype", ctypes.c_int32), ("softmax_scale", ctypes.c_float),
                 ("stis_mode", ctypes.c_int32), ("save_for_bwd", ctypes.c_int32),
                 ("stis_block", ctypes.c_int32), ("last_block_only", ctypes.c_int32)]
+
+
+class BlossomPagedParams(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_float if name == "softmax_scale" else ctypes.c_int32)
+                for name in ("S", "T", "H", "G", "d", "page", "n_pages", "max_pages", "dtype", "softmax_scale", "window", "max_len",
+                             "table_per_head")]
 
 
 class BlossomError(RuntimeError):
@@ -87,6 +94,15 @@ def lib() -> ctypes.CDLL:
                                             fp, fp, vp, ctypes.c_size_t, vp]
         L.blossom_attn_bwd_stages.restype = ctypes.c_int
         L.blossom_attn_bwd_stages.argtypes = L.blossom_attn_bwd.argtypes + [ctypes.c_uint]
+        gp, i64 = ctypes.POINTER(BlossomPagedParams), ctypes.c_int64
+        L.blossom_paged_workspace_bytes.restype = ctypes.c_size_t
+        L.blossom_paged_workspace_bytes.argtypes = [gp, ctypes.c_int]
+        L.blossom_kv_append.restype = ctypes.c_int
+        L.blossom_kv_append.argtypes = [gp, vp, i64, vp, i64, vp, i64, fp, fp, i32p, i32p, i32p, vp, vp, vp, vp]
+        L.blossom_attn_decode.restype = ctypes.c_int
+        L.blossom_attn_decode.argtypes = [gp, vp, i64, vp, vp, i32p, i32p, vp, fp, vp, ctypes.c_size_t, vp]
+        L.blossom_attn_prompt.restype = ctypes.c_int
+        L.blossom_attn_prompt.argtypes = [gp, vp, i64, vp, vp, i32p, i32p, i32p, vp, fp, vp, ctypes.c_size_t, vp]
         L.blossom_dense_causal_fwd.restype = ctypes.c_int
         L.blossom_dense_causal_fwd.argtypes = [pp, vp, vp, vp, i32p, vp, fp, vp, ctypes.c_size_t, vp]
         L.blossom_probe_bytes.restype = ctypes.c_size_t
@@ -600,3 +616,143 @@ def out_proj_ln(p: Params, d_model: int, O, W_O_t, H_prev, ln_gamma, ln_beta, ln
     if rc:
         raise BlossomError(rc, "blossom_out_proj_ln")
     return (S, mean, rstd) if want_stats else S
+
+
+@dataclass
+class PagedParams:
+    """blossom_paged_params: a batch of S sequences in a paged key/value cache, bringing T new tokens together."""
+    S: int
+    T: int
+    H: int
+    G: int
+    d: int
+    page: int
+    n_pages: int
+    max_pages: int
+    dtype: int = F32
+    softmax_scale: float = 0.0
+    window: int = 0
+    max_len: int = 0
+    table_per_head: int = 0
+
+    def c(self) -> BlossomPagedParams:
+        return BlossomPagedParams(self.S, self.T, self.H, self.G, self.d, self.page, self.n_pages, self.max_pages, self.dtype,
+                                  self.softmax_scale, self.window, self.max_len, self.table_per_head)
+
+    @property
+    def capacity(self) -> int:
+        """Positions that a sequence may hold: rows of the rotary tables."""
+        held = self.max_pages * self.page
+        return min(self.max_len, held) if self.max_len > 0 else held
+
+
+def paged_workspace_bytes(p: PagedParams, which: int) -> int:
+    cp = p.c()
+    return int(lib().blossom_paged_workspace_bytes(ctypes.byref(cp), which))
+
+
+def _token_stride(t, rows, heads, d, dtype, name) -> int:
+    """Elements from a token's row to the next of a [rows, heads, d] tensor whose heads and channels are contiguous."""
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if tuple(t.shape) != (rows, heads, d) or t.dtype != dtype or not t.is_cuda or t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
+        raise ValueError(f"{name}: expected cuda tensor {(rows, heads, d)} {dtype} with contiguous heads and channels, got "
+                         f"{tuple(t.shape)} {t.dtype} strides={tuple(t.stride())} cuda={t.is_cuda}")
+    return t.stride(0) if rows > 1 else 0
+
+
+def _check_cache(p: PagedParams, K_cache, V_cache, page_table, cu_seqlens, kv_len):
+    import torch
+    for t, nm in ((K_cache, "K_cache"), (V_cache, "V_cache"), (page_table, "page_table"), (kv_len, "kv_len")):
+        if t is None:
+            raise ValueError(f"{nm} is required")
+    shp = (p.n_pages, p.G, p.page, p.d)
+    _check_tensor(K_cache, shp, _torch_dtype(p), "K_cache")
+    _check_tensor(V_cache, shp, _torch_dtype(p), "V_cache")
+    _check_tensor(page_table, (p.S, p.G, p.max_pages) if p.table_per_head else (p.S, p.max_pages), torch.int32, "page_table")
+    _check_tensor(cu_seqlens, (p.S + 1,), torch.int32, "cu_seqlens")
+    _check_tensor(kv_len, (p.S,), torch.int32, "kv_len")
+
+
+def kv_append(p: PagedParams, K, V, K_cache, V_cache, page_table, cu_seqlens, kv_len, Q=None, rope=None, Q_rot=None, stream=None):
+    """blossom_kv_append: the new tokens' K and V [T,G,d] go into the cache, K rotated with rope=(cos, sin).  Returns Q_rot
+    [T,H,d], the rotated Q (None without Q).  K, V and Q may be slices of one projection: a token's heads are contiguous."""
+    cos, sin = rope if rope is not None else (None, None)
+    if Q is None or Q_rot is not None:
+        rc = (_fast or fastcall()).kv_append(p, Q, K, V, cos, sin, page_table, cu_seqlens, kv_len, K_cache, V_cache, Q_rot, stream)
+        if rc is not None:
+            if rc:
+                raise BlossomError(rc, "blossom_kv_append")
+            return Q_rot
+    import torch
+    dt = _torch_dtype(p)
+    ks, vs = _token_stride(K, p.T, p.G, p.d, dt, "K"), _token_stride(V, p.T, p.G, p.d, dt, "V")
+    qs = 0
+    if Q is not None:
+        qs = _token_stride(Q, p.T, p.H, p.d, dt, "Q")
+        if Q_rot is None:
+            Q_rot = torch.empty((p.T, p.H, p.d), dtype=dt, device=Q.device)
+    _check_tensor(Q_rot, (p.T, p.H, p.d), dt, "Q_rot")
+    if cu_seqlens is None:
+        raise ValueError("cu_seqlens is required")
+    _check_cache(p, K_cache, V_cache, page_table, cu_seqlens, kv_len)
+    _check_tensor(cos, (p.capacity, p.d // 2), torch.float32, "rope_cos")
+    _check_tensor(sin, (p.capacity, p.d // 2), torch.float32, "rope_sin")
+    cp = p.c()
+    rc = lib().blossom_kv_append(ctypes.byref(cp), _ptr(Q), qs, _ptr(K), ks, _ptr(V), vs, _ptr(cos), _ptr(sin), _ptr(page_table),
+                                 _ptr(cu_seqlens), _ptr(kv_len), _ptr(K_cache), _ptr(V_cache), _ptr(Q_rot), _stream(stream))
+    if rc:
+        raise BlossomError(rc, "blossom_kv_append")
+    return Q_rot
+
+
+def _paged_attn(p: PagedParams, which, rows, Q, K_cache, V_cache, page_table, cu_seqlens, kv_len, O, lse, ws, stream):
+    """The Python path of attn_decode and attn_prompt: allocates what is missing, names what is wrong."""
+    import torch
+    dt = _torch_dtype(p)
+    qs = _token_stride(Q, rows, p.H, p.d, dt, "Q")
+    _check_cache(p, K_cache, V_cache, page_table, cu_seqlens, kv_len)
+    if O is None:
+        O = torch.empty((rows, p.H, p.d), dtype=dt, device=Q.device)
+    _check_tensor(O, (rows, p.H, p.d), dt, "O")
+    _check_tensor(lse, (rows, p.H), torch.float32, "lse")
+    need = paged_workspace_bytes(p, which)
+    if ws is None and need > 0:
+        ws = torch.empty(need, dtype=torch.uint8, device=Q.device)
+    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
+    cp = p.c()
+    head = (ctypes.byref(cp), _ptr(Q), qs, _ptr(K_cache), _ptr(V_cache), _ptr(page_table))
+    tail = (_ptr(kv_len), _ptr(O), _ptr(lse), _ptr(ws), nbytes, _stream(stream))
+    if which == WS_DECODE:
+        name, rc = "blossom_attn_decode", lib().blossom_attn_decode(*head, *tail)
+    else:
+        name, rc = "blossom_attn_prompt", lib().blossom_attn_prompt(*head, _ptr(cu_seqlens), *tail)
+    if rc:
+        raise BlossomError(rc, name)
+    return O, lse
+
+
+def attn_decode(p: PagedParams, Q, K_cache, V_cache, page_table, kv_len, O=None, lse=None, ws=None, stream=None):
+    """blossom_attn_decode: one new token a sequence (Q [S,H,d]) over its cached positions.  Returns (O, lse); lse is written
+    where given."""
+    if O is not None:
+        rc = (_fast or fastcall()).attn_decode(p, Q, K_cache, V_cache, page_table, kv_len, O, lse, ws, stream)
+        if rc is not None:
+            if rc:
+                raise BlossomError(rc, "blossom_attn_decode")
+            return O, lse
+    return _paged_attn(p, WS_DECODE, p.S, Q, K_cache, V_cache, page_table, None, kv_len, O, lse, ws, stream)
+
+
+def attn_prompt(p: PagedParams, Q, K_cache, V_cache, page_table, cu_seqlens, kv_len, O=None, lse=None, ws=None, stream=None):
+    """blossom_attn_prompt: causal attention of packed new tokens (Q [T,H,d]) over their sequences' cached positions, their own
+    among them.  Returns (O, lse); lse is written where given."""
+    if O is not None:
+        rc = (_fast or fastcall()).attn_prompt(p, Q, K_cache, V_cache, page_table, cu_seqlens, kv_len, O, lse, ws, stream)
+        if rc is not None:
+            if rc:
+                raise BlossomError(rc, "blossom_attn_prompt")
+            return O, lse
+    if cu_seqlens is None:
+        raise ValueError("cu_seqlens is required")
+    return _paged_attn(p, WS_PROMPT, p.T, Q, K_cache, V_cache, page_table, cu_seqlens, kv_len, O, lse, ws, stream)

@@ -28,6 +28,9 @@ SOURCES = {
     "mfma_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "probe.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "out_proj.hip": ["-fno-strict-aliasing"],
+    "paged_api.hip": [],
+    "paged_append.hip": [],
+    "paged_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }
 
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",

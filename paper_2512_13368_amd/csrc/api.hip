@@ -378,10 +378,10 @@ const char *blossom_strerror(int code)
   switch (code) {
     case BLOSSOM_OK: return "ok";
     case BLOSSOM_ERR_NULL: return "a required pointer is NULL";
-    case BLOSSOM_ERR_SHAPE: return "bad shape: B, H, L must be >= 1 and ceil(L/block) <= 4096";
-    case BLOSSOM_ERR_UNSUPPORTED: return "unsupported d, block, dtype or stis_mode, or backward in serving mode";
-    case BLOSSOM_ERR_PARAM: return "bad parameter: topk >= 1, window >= 1, stis_block >= 0, finite softmax_scale >= 0";
-    case BLOSSOM_ERR_ALIGN: return "tensor or workspace pointer not 16-byte aligned";
+    case BLOSSOM_ERR_SHAPE: return "bad shape: every count must be >= 1 and ceil(L/block) <= 4096 (a paged cache: fewer than 2^31 positions, rows)";
+    case BLOSSOM_ERR_UNSUPPORTED: return "unsupported d, block, page, dtype or stis_mode, backward in serving mode, or page tables per head outside decode";
+    case BLOSSOM_ERR_PARAM: return "bad parameter: topk >= 1, window >= 1 (a paged cache: >= 0), stis_block >= 0, finite softmax_scale >= 0, G divides H, strides hold a row";
+    case BLOSSOM_ERR_ALIGN: return "tensor or workspace pointer, or stride, not a multiple of 16 bytes";
     case BLOSSOM_ERR_WORKSPACE: return "workspace missing or too small";
     case BLOSSOM_ERR_LAUNCH: return "kernel launch failed";
     case BLOSSOM_ERR_TOO_LARGE: return "problem too large for the static scratch array (B*H*ceil(L/block)*d*8 bytes must be <= 16 MiB)";

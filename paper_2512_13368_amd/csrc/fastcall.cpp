@@ -20,37 +20,32 @@ PyObject *g_cuda_stream;
 const char *kFields[13] = {"B", "H", "L", "d", "block", "topk", "window", "dtype", "softmax_scale", "stis_mode", "save_for_bwd", "stis_block",
                            "last_block_only"};
 
+PyObject *g_paged_fields[13];
+const char *kPagedFields[13] = {"S", "T", "H", "G", "d", "page", "n_pages", "max_pages", "dtype", "softmax_scale", "window", "max_len",
+                                "table_per_head"};
+
 // One call's arguments, read in order; `ok` falls at the first that is not as expected.
-struct Call {
+struct Arguments {
   PyObject *const *arg;
   bool ok = true;
-  blossom_params p{};
   at::ScalarType T{};
-  int64_t NB = 0;
   void *stream = nullptr;
 
-  explicit Call(PyObject *const *a) : arg(a) {}
+  explicit Arguments(PyObject *const *a) : arg(a) {}
 
-  bool params()
+  // the 13 fields of a parameter block, the one at `real` a number, the others whole
+  bool fields(PyObject *const *names, int real, long (&v)[13], float *number)
   {
     PyObject *obj = *arg++;
-    long v[13];
     for (int i = 0; i < 13 && ok; ++i) {
-      PyObject *x = PyObject_GetAttr(obj, g_fields[i]);
+      PyObject *x = PyObject_GetAttr(obj, names[i]);
       if (!x) return ok = false;
-      if (i == 8) p.softmax_scale = (float)PyFloat_AsDouble(x);
+      if (i == real) *number = (float)PyFloat_AsDouble(x);
       else v[i] = PyLong_AsLong(x);
       Py_DECREF(x);
-      ok = !PyErr_Occurred() && (i == 8 || v[i] == (int32_t)v[i]);
+      ok = !PyErr_Occurred() && (i == real || v[i] == (int32_t)v[i]);
     }
-    if (!ok) return false;
-    p.B = (int32_t)v[0]; p.H = (int32_t)v[1]; p.L = (int32_t)v[2]; p.d = (int32_t)v[3]; p.block = (int32_t)v[4];
-    p.topk = (int32_t)v[5]; p.window = (int32_t)v[6]; p.dtype = (int32_t)v[7]; p.stis_mode = (int32_t)v[9];
-    p.save_for_bwd = (int32_t)v[10]; p.stis_block = (int32_t)v[11]; p.last_block_only = (int32_t)v[12];
-    if (p.block < 1) return ok = false;
-    NB = ((int64_t)p.L + p.block - 1) / p.block;
-    T = p.dtype == 0 ? at::kFloat : at::kBFloat16;
-    return true;
+    return ok;
   }
   int32_t whole()
   {
@@ -129,7 +124,66 @@ struct Call {
   }
 };
 
-#define FASTCALL(name, count)                                                     \
+// Arguments that begin with the attention layer's parameter block.
+struct Call : Arguments {
+  blossom_params p{};
+  int64_t NB = 0;
+
+  using Arguments::Arguments;
+
+  bool params()
+  {
+    long v[13];
+    if (!fields(g_fields, 8, v, &p.softmax_scale)) return false;
+    p.B = (int32_t)v[0]; p.H = (int32_t)v[1]; p.L = (int32_t)v[2]; p.d = (int32_t)v[3]; p.block = (int32_t)v[4];
+    p.topk = (int32_t)v[5]; p.window = (int32_t)v[6]; p.dtype = (int32_t)v[7]; p.stis_mode = (int32_t)v[9];
+    p.save_for_bwd = (int32_t)v[10]; p.stis_block = (int32_t)v[11]; p.last_block_only = (int32_t)v[12];
+    if (p.block < 1) return ok = false;
+    NB = ((int64_t)p.L + p.block - 1) / p.block;
+    T = p.dtype == 0 ? at::kFloat : at::kBFloat16;
+    return true;
+  }
+};
+
+// Arguments that begin with a paged cache's parameter block.
+struct PagedCall : Arguments {
+  blossom_paged_params p{};
+
+  using Arguments::Arguments;
+
+  bool params()
+  {
+    long v[13];
+    if (!fields(g_paged_fields, 9, v, &p.softmax_scale)) return false;
+    p.S = (int32_t)v[0]; p.T = (int32_t)v[1]; p.H = (int32_t)v[2]; p.G = (int32_t)v[3]; p.d = (int32_t)v[4];
+    p.page = (int32_t)v[5]; p.n_pages = (int32_t)v[6]; p.max_pages = (int32_t)v[7]; p.dtype = (int32_t)v[8];
+    p.window = (int32_t)v[10]; p.max_len = (int32_t)v[11]; p.table_per_head = (int32_t)v[12];
+    T = p.dtype == 0 ? at::kFloat : at::kBFloat16;
+    return true;
+  }
+  // [rows, heads, d] with contiguous heads and channels; *stride: elements from a row to the next
+  void *rows(int64_t count, int64_t heads, int64_t *stride, bool optional = false)
+  {
+    PyObject *obj = *arg++;
+    *stride = 0;
+    if (obj == Py_None) {
+      ok = ok && optional;
+      return nullptr;
+    }
+    if (!ok || !THPVariable_Check(obj)) {
+      ok = false;
+      return nullptr;
+    }
+    const at::Tensor &t = THPVariable_Unpack(obj);
+    ok = t.is_cuda() && t.scalar_type() == T && t.dim() == 3 && t.size(0) == count && t.size(1) == heads && t.size(2) == p.d &&
+         t.stride(2) == 1 && (heads == 1 || t.stride(1) == p.d);
+    if (!ok) return nullptr;
+    if (count > 1) *stride = t.stride(0);
+    return t.data_ptr();
+  }
+};
+
+#define FASTCALL_OF(Call, name, count)                                            \
   PyObject *name##_body(Call &c);                                                 \
   PyObject *name(PyObject *, PyObject *const *args, Py_ssize_t n)                 \
   {                                                                               \
@@ -150,6 +204,7 @@ struct Call {
     }                                                                             \
   }                                                                               \
   PyObject *name##_body(Call &c)
+#define FASTCALL(name, count) FASTCALL_OF(Call, name, count)
 
 // select_blocks(p, Q, K, valid_len, sel, ws, stream)
 FASTCALL(select_blocks, 7)
@@ -337,9 +392,89 @@ FASTCALL(out_proj_ln, 13)
   return c.run([&] { return blossom_out_proj_ln(&p, dm, O, W, bias, prev, gamma, beta, eps, S, mean, rstd, c.stream); });
 }
 
+// The cache's tensors as every paged call has them.
+struct CacheTensors {
+  int32_t *table, *cu = nullptr, *len;
+  void *K, *V;
+  int32_t *get_table(PagedCall &c)
+  {
+    const blossom_paged_params &p = c.p;
+    const int64_t per_head[3] = {p.S, p.G, p.max_pages}, one[2] = {p.S, p.max_pages};
+    return c.tensor<int32_t>(p.table_per_head ? at::IntArrayRef(per_head, 3) : at::IntArrayRef(one, 2), at::kInt);
+  }
+  void *get_cache(PagedCall &c)
+  {
+    const int64_t x[4] = {c.p.n_pages, c.p.G, c.p.page, c.p.d};
+    return c.tensor(x, c.T);
+  }
+  int32_t *get_counts(PagedCall &c, int64_t n) { return c.tensor<int32_t>(at::IntArrayRef(&n, 1), at::kInt); }
+};
+
+// kv_append(p, Q, K, V, rope_cos, rope_sin, page_table, cu_seqlens, kv_len, K_cache, V_cache, Q_rot, stream)
+FASTCALL_OF(PagedCall, kv_append, 13)
+{
+  const blossom_paged_params &p = c.p;
+  const int64_t held = (int64_t)p.max_pages * p.page, cap = p.max_len > 0 && p.max_len < held ? p.max_len : held;
+  const int64_t x[3] = {p.T, p.H, p.d}, r[2] = {cap, p.d / 2};
+  int64_t qs, ks, vs;
+  void *Q = c.rows(p.T, p.H, &qs, true), *K = c.rows(p.T, p.G, &ks), *V = c.rows(p.T, p.G, &vs);
+  float *cos = c.tensor<float>(r, at::kFloat, true), *sin = c.tensor<float>(r, at::kFloat, true);
+  CacheTensors t;
+  t.table = t.get_table(c);
+  t.cu = t.get_counts(c, (int64_t)p.S + 1);
+  t.len = t.get_counts(c, p.S);
+  t.K = t.get_cache(c);
+  t.V = t.get_cache(c);
+  void *Q_rot = c.tensor(x, c.T, true);
+  c.on_stream();
+  return c.run([&] { return blossom_kv_append(&p, Q, qs, K, ks, V, vs, cos, sin, t.table, t.cu, t.len, t.K, t.V, Q_rot, c.stream); });
+}
+
+// attn_decode(p, Q, K_cache, V_cache, page_table, kv_len, O, lse, ws, stream)
+FASTCALL_OF(PagedCall, attn_decode, 10)
+{
+  const blossom_paged_params &p = c.p;
+  const int64_t x[3] = {p.S, p.H, p.d};
+  int64_t qs;
+  void *Q = c.rows(p.S, p.H, &qs);
+  CacheTensors t;
+  t.K = t.get_cache(c);
+  t.V = t.get_cache(c);
+  t.table = t.get_table(c);
+  t.len = t.get_counts(c, p.S);
+  void *O = c.tensor(x, c.T);
+  float *lse = c.tensor<float>(at::IntArrayRef(x, 2), at::kFloat, true);
+  size_t bytes;
+  void *ws = c.workspace(blossom_paged_workspace_bytes(&p, BLOSSOM_WS_DECODE), &bytes);
+  c.on_stream();
+  return c.run([&] { return blossom_attn_decode(&p, Q, qs, t.K, t.V, t.table, t.len, O, lse, ws, bytes, c.stream); });
+}
+
+// attn_prompt(p, Q, K_cache, V_cache, page_table, cu_seqlens, kv_len, O, lse, ws, stream)
+FASTCALL_OF(PagedCall, attn_prompt, 11)
+{
+  const blossom_paged_params &p = c.p;
+  const int64_t x[3] = {p.T, p.H, p.d};
+  int64_t qs;
+  void *Q = c.rows(p.T, p.H, &qs);
+  CacheTensors t;
+  t.K = t.get_cache(c);
+  t.V = t.get_cache(c);
+  t.table = t.get_table(c);
+  t.cu = t.get_counts(c, (int64_t)p.S + 1);
+  t.len = t.get_counts(c, p.S);
+  void *O = c.tensor(x, c.T);
+  float *lse = c.tensor<float>(at::IntArrayRef(x, 2), at::kFloat, true);
+  size_t bytes;
+  void *ws = c.workspace(blossom_paged_workspace_bytes(&p, BLOSSOM_WS_PROMPT), &bytes);
+  c.on_stream();
+  return c.run([&] { return blossom_attn_prompt(&p, Q, qs, t.K, t.V, t.table, t.cu, t.len, O, lse, ws, bytes, c.stream); });
+}
+
 #define ENTRY(name) {#name, (PyCFunction)(void *)name, METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {ENTRY(select_blocks), ENTRY(rope_select_blocks), ENTRY(select_positions), ENTRY(attn_fwd),
                           ENTRY(attn_fwd_positions), ENTRY(attn_bwd), ENTRY(attn_bwd_positions), ENTRY(out_proj_ln),
+                          ENTRY(kv_append), ENTRY(attn_decode), ENTRY(attn_prompt),
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
@@ -348,7 +483,8 @@ PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, kMethods
 PyMODINIT_FUNC PyInit__fastcall()
 {
   for (int i = 0; i < 13; ++i)
-    if (!(g_fields[i] = PyUnicode_InternFromString(kFields[i]))) return nullptr;
+    if (!(g_fields[i] = PyUnicode_InternFromString(kFields[i])) || !(g_paged_fields[i] = PyUnicode_InternFromString(kPagedFields[i])))
+      return nullptr;
   if (!(g_cuda_stream = PyUnicode_InternFromString("cuda_stream"))) return nullptr;
   return PyModule_Create(&kModule);
 }

@@ -1,0 +1,59 @@
+// The paged key/value cache's operators: kernel-side description and what their kernels share (gfx950 only).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace blossom {
+namespace paged {
+
+// One call (passed to kernels by value; device pointers).  Element type of Q, K, V, the caches and O: `dtype`.
+struct Args {
+  int S, T, H, G, R, d;        // sequences, packed new tokens, heads, key/value heads, H / G, head size
+  int page_shift;              // log2 of the positions a page holds
+  int n_pages, max_pages;      // pages of a cache, entries of a page-table row
+  int cap;                     // positions a sequence may have: keys at or beyond are never read or written
+  int window;                  // a query sees that many positions up to its own; 0x7FFFFFFF: all
+  int dtype;
+  float scale2;                // softmax scale * log2(e)
+  int64_t table_seq, table_group;  // page-table steps from a sequence and from a key/value head to the next
+  const void *Q, *K, *V;
+  int64_t q_stride, k_stride, v_stride;  // elements from a token's row to the next's
+  void *K_cache, *V_cache;     // [n_pages, G, page, d]
+  const int *page_table, *cu, *kv_len;
+  const float *rope_cos, *rope_sin;  // [cap, d/2] or nullptr
+  void *Q_rot;                 // [T,H,d] or nullptr
+  void *O;                     // [T,H,d] (decode: [S,H,d])
+  float *lse;                  // [T,H] or nullptr
+  int nsplit;                  // parts that a row's keys are split into; > 1: partial results go to the workspace
+  float *part_o, *part_ml;     // [rows, nsplit, d] and [rows, nsplit, 2]: sums, and (reference in log2 units, sum of exponentials)
+};
+
+// append: paged_append.hip
+void launch_append(const Args &a, hipStream_t st);
+// one-token and prompt attention: paged_attn.hip.  `splits` is the number of parts for this shape.
+int attn_splits(const Args &a, bool prompt);
+void launch_decode(const Args &a, hipStream_t st);
+void launch_prompt(const Args &a, hipStream_t st);
+
+// The sequence whose new tokens' tiles hold tile `t`, where sequence s's tiles begin at first(s), which grows with s: all 64 lanes
+// of a wavefront look at one sequence each.
+template <typename F>
+__device__ __forceinline__ int find_sequence(int S, int lane, F &&starts_by)
+{
+  int s = 0;
+  for (int at = 1; at < S; at += 64) {
+    const int mine = at + lane;
+    const unsigned long long in = __ballot(mine < S && starts_by(mine));
+    s += __builtin_popcountll(in);
+    if (in != ~0ull) break;
+  }
+  return __builtin_amdgcn_readfirstlane(s);
+}
+
+// cu[s] inside [0, T], whatever the caller's array holds
+__device__ __forceinline__ int token_at(const Args &a, int s) { return min(max(a.cu[s], 0), a.T); }
+
+}  // namespace paged
+}  // namespace blossom

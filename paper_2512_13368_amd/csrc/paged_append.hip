@@ -1,0 +1,136 @@
+// New tokens' keys and values into a paged cache, with the rotary position embedding on the way (Sec. 3.3), Q rotated too.
+//
+// A wavefront takes one token, or a share of its rows where there are few tokens: rows of Q, K and V are d elements each, a lane
+// moves 16 bytes, and a lane's place inside a row is the same in every row it moves, so that the token's angles are read once.
+// Nothing is read twice and nothing needs LDS: the kernel is bound by memory.
+#include "common.h"
+#include "launch.h"
+#include "paged.h"
+
+namespace blossom {
+namespace paged {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+// 16 bytes of a row, as floats
+template <typename T>
+struct Chunk;
+template <>
+struct Chunk<float> {
+  static constexpr int E = 4;
+  static __device__ __forceinline__ void get(const uint4 &v, float (&x)[4])
+  {
+    x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
+  }
+  static __device__ __forceinline__ uint4 put(const float (&x)[4])
+  {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  }
+};
+template <>
+struct Chunk<bf16_t> {
+  static constexpr int E = 8;
+  static __device__ __forceinline__ void get(const uint4 &v, float (&x)[8])
+  {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+  // (round to nearest even by the hardware's conversion, which keeps NaN a NaN)
+  static __device__ __forceinline__ uint4 put(const float (&x)[8])
+  {
+    typedef __bf16 pair __attribute__((ext_vector_type(2)));
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const pair p = {(__bf16)x[2 * i], (__bf16)x[2 * i + 1]};
+      w[i] = __builtin_bit_cast(uint32_t, p);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+
+}  // namespace
+
+// `share`: wavefronts that divide a token's rows (a power of two)
+template <typename T>
+__global__ __launch_bounds__(kThreads) void append_kernel(Args a, int share)
+{
+  constexpr int E = Chunk<T>::E;
+  const int lane = threadIdx.x & 63;
+  const long wave = (long)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int t = (int)(wave / share), part = (int)(wave % share);
+  if (t >= a.T) return;
+  const int s = find_sequence(a.S, lane, [&](int i) { return token_at(a, i) <= t; });
+  const int lo = token_at(a, s), hi = token_at(a, s + 1);
+  if (t < lo || t >= hi) return;  // a row that no sequence owns
+  const int n = a.kv_len[s];
+  const long pos = (long)n - (hi - lo) + (t - lo);
+  const bool placed = pos >= 0 && pos < a.cap;
+  int id = -1;
+  if (placed) id = a.page_table[s * a.table_seq + (pos >> a.page_shift)];
+  const bool stored = id >= 0 && id < a.n_pages;
+  const int page = 1 << a.page_shift, slot = (int)(pos & (page - 1));
+
+  const int lanes = a.d / E;            // lanes of a row
+  const int at = (lane % lanes) * E;    // this lane's channels in every row it moves
+  float c[E / 2], sn[E / 2];
+#pragma unroll
+  for (int i = 0; i < E / 2; ++i) { c[i] = 1.0f; sn[i] = 0.0f; }
+  if (a.rope_cos && placed) {
+    const float *pc = a.rope_cos + pos * (a.d / 2) + at / 2, *ps = a.rope_sin + pos * (a.d / 2) + at / 2;
+#pragma unroll
+    for (int i = 0; i < E / 2; i += 2) {
+      const float2 x = *reinterpret_cast<const float2 *>(pc + i), y = *reinterpret_cast<const float2 *>(ps + i);
+      c[i] = x.x; c[i + 1] = x.y;
+      sn[i] = y.x; sn[i + 1] = y.y;
+    }
+  }
+  auto turn = [&](const uint4 &v) __attribute__((always_inline)) -> uint4 {
+    float x[E];
+    Chunk<T>::get(v, x);
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) {  // the recipe of the selection's rotation
+      const float p = x[2 * i + 1] * sn[i], u = x[2 * i + 1] * c[i];
+      x[2 * i + 1] = fmaf(x[2 * i], sn[i], u);
+      x[2 * i] = fmaf(x[2 * i], c[i], -p);
+    }
+    return Chunk<T>::put(x);
+  };
+
+  const int per = 64 / lanes;  // rows that a wavefront moves at a time
+  const int nq = a.Q ? a.H : 0, rows = nq + 2 * a.G;
+  const T *Q = static_cast<const T *>(a.Q), *K = static_cast<const T *>(a.K), *V = static_cast<const T *>(a.V);
+  T *Kc = static_cast<T *>(a.K_cache), *Vc = static_cast<T *>(a.V_cache), *Qr = static_cast<T *>(a.Q_rot);
+  const size_t cell = (size_t)(stored ? id : 0) * a.G * page * a.d + (size_t)slot * a.d + at;
+  for (int r = part * per + lane / lanes; r < rows; r += share * per) {
+    if (r < nq) {
+      uint4 v = *reinterpret_cast<const uint4 *>(Q + t * a.q_stride + (size_t)r * a.d + at);
+      v = placed ? turn(v) : make_uint4(0, 0, 0, 0);
+      *reinterpret_cast<uint4 *>(Qr + ((size_t)t * a.H + r) * a.d + at) = v;
+    } else if (stored) {
+      const bool key = r < nq + a.G;
+      const int g = r - nq - (key ? 0 : a.G);
+      uint4 v = *reinterpret_cast<const uint4 *>((key ? K + t * a.k_stride : V + t * a.v_stride) + (size_t)g * a.d + at);
+      if (key && a.rope_cos) v = turn(v);
+      *reinterpret_cast<uint4 *>((key ? Kc : Vc) + cell + (size_t)g * page * a.d) = v;
+    }
+  }
+}
+
+void launch_append(const Args &a, hipStream_t st)
+{
+  int share = 1;
+  const long waves = (long)a.T * share;
+  const unsigned blocks = (unsigned)((waves + kThreads / 64 - 1) / (kThreads / 64));
+  if (a.dtype == 0) BLOSSOM_LAUNCH(append_kernel<float>, dim3(blocks), dim3(kThreads), 0, st, a, share);
+  else BLOSSOM_LAUNCH(append_kernel<bf16_t>, dim3(blocks), dim3(kThreads), 0, st, a, share);
+}
+
+}  // namespace paged
+}  // namespace blossom
