@@ -36,6 +36,20 @@ void launch_append(const Args &a, hipStream_t st);
 int attn_splits(const Args &a, bool prompt);
 void launch_decode(const Args &a, hipStream_t st);
 void launch_prompt(const Args &a, hipStream_t st);
+// prompt attention for bf16, d = 64 or 128: paged_prompt.hip
+constexpr int kPromptRows = 128;  // query rows of a workgroup
+bool prompt_mfma_supported(const Args &a);
+void launch_prompt_mfma(const Args &a, hipStream_t st);
+
+// Keys lo .. hi that a query at `pos` sees, of a sequence with n keys (hi < lo: none).
+struct Range {
+  int lo, hi;
+};
+__device__ __forceinline__ Range seen_by(const Args &a, int pos, int n)
+{
+  if (pos < 0) return {0, -1};
+  return {max(pos - a.window + 1, 0), min(pos, min(n, a.cap) - 1)};
+}
 
 // The sequence whose new tokens' tiles hold tile `t`, where sequence s's tiles begin at first(s), which grows with s: all 64 lanes
 // of a wavefront look at one sequence each.

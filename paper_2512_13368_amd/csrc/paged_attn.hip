@@ -158,16 +158,6 @@ struct Ops<float, D> {
 __device__ __forceinline__ void store_out(float *p, float x) { *p = x; }
 __device__ __forceinline__ void store_out(bf16_t *p, float x) { p->bits = __builtin_bit_cast(uint16_t, (__bf16)x); }
 
-// Keys lo .. hi that a query at `pos` sees, of a sequence with n keys (hi < lo: none).
-struct Range {
-  int lo, hi;
-};
-__device__ __forceinline__ Range seen_by(const Args &a, int pos, int n)
-{
-  if (pos < 0) return {0, -1};
-  return {max(pos - a.window + 1, 0), min(pos, min(n, a.cap) - 1)};
-}
-
 }  // namespace
 
 template <typename T, int D, bool PROMPT>
@@ -423,6 +413,7 @@ void launch_decode(const Args &a, hipStream_t st)
 
 void launch_prompt(const Args &a, hipStream_t st)
 {
+  if (prompt_mfma_supported(a)) return launch_prompt_mfma(a, st);
   if (a.dtype == 0) launch_rows_d<float>(a, true, st);
   else launch_rows_d<bf16_t>(a, true, st);
 }

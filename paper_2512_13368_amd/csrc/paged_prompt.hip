@@ -1,0 +1,284 @@
+// Prompt attention on the matrix cores for bf16, d = 64 or 128 (formulas: paged_attn.hip, which serves everything else).
+//
+// A workgroup of four wavefronts takes 128 query rows of one key/value head, 32 a wavefront, and walks the 64-key tiles that any of
+// them sees.  Rows are (token, head of the group) pairs, R = H/G of them a token, so that heads that share keys share the tiles too
+// and a short prompt fills its workgroups.  K and V tiles go from the pages straight to LDS (eight or four rows an instruction: always
+// of one page), one tile ahead or two; every wavefront reads them whole.
+//  - S^T = K Q^T on v_mfma_f32_32x32x16_bf16: a lane owns one query row and 16 of a half tile's 32 logits.
+//  - softmax in fp32, base 2: p = exp2(scale2 * s - ref).  The reference is a row's maximum over the first keys it meets; it is
+//    raised only when a lane's probabilities of a half tile pass 4096 in sum, so the usual half tile takes no maximum.
+//  - O^T += V^T P^T with P^T straight from the accumulator registers (rounded to bf16, as the matrix instruction wants them; the
+//    sum is of the unrounded ones) and V^T through the transposing LDS read.
+#include "common.h"
+#include "launch.h"
+#include "mfma_common.h"
+#include "paged.h"
+
+namespace blossom {
+namespace paged {
+
+using mfma::bf16x8;
+using mfma::f32x16;
+using mfma::kLn2;
+using mfma::kNegInf;
+using mfma::lds_s16x4;
+using mfma::s16x4;
+using mfma::u32x2;
+
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kKeys = 64;                  // keys of a tile
+constexpr float kSumLimit = 4096.0f;       // a lane's 16 probabilities of a half tile may sum to this
+
+// what stands in for rows that nobody may see
+__device__ const uint4 kZeros[64] = {};
+
+// One direct global->LDS load of 16 bytes a lane (see load_to_lds in mfma_common.h).
+__device__ __forceinline__ void row_to_lds(const void *base, unsigned off, unsigned lds)
+{
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(lds), "v"(off), "s"(base) : "memory");
+}
+
+}  // namespace
+
+template <int D, int STAGES, int WAVES_EU>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAVES_EU, WAVES_EU))) void prompt_kernel(Args a)
+{
+  constexpr int CH = D / 8;              // 16-byte chunks of a row
+  constexpr int RPI = 64 / CH;           // rows that a wavefront's load moves
+  constexpr int LOADS = kKeys / (RPI * kWaves);  // such loads of K a wavefront and tile (and as many of V)
+  constexpr int TILE = kKeys * D;
+  constexpr int NB = D / 32;             // blocks of 32 channels
+  __shared__ __attribute__((aligned(1024))) uint16_t Ks[STAGES][TILE];
+  __shared__ __attribute__((aligned(1024))) uint16_t Vs[STAGES][TILE];
+
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lq = lane & 31, lh = lane >> 5;
+
+  // ---- this workgroup's rows: the last tiles, which see most keys, first ----
+  const int g = blockIdx.x % a.G;
+  const int tile = (int)(gridDim.x / a.G) - 1 - (int)(blockIdx.x / a.G);
+  const int s = find_sequence(a.S, lane, [&](int i) { return (int)((long)token_at(a, i) * a.R / kPromptRows) + i <= tile; });
+  const int tok0 = __builtin_amdgcn_readfirstlane(token_at(a, s));
+  const int new_tokens = max(__builtin_amdgcn_readfirstlane(token_at(a, s + 1)) - tok0, 0);
+  const int wg_row = (tile - (int)((long)tok0 * a.R / kPromptRows) - s) * kPromptRows;
+  const int rows = new_tokens * a.R;
+  if (wg_row < 0 || wg_row >= rows) return;
+  const int len = max(__builtin_amdgcn_readfirstlane(a.kv_len[s]), 0);
+  const int first_pos = len - new_tokens;
+
+  const Range all_first = seen_by(a, first_pos + wg_row / a.R, len);
+  const Range all_last = seen_by(a, first_pos + (min(wg_row + kPromptRows, rows) - 1) / a.R, len);
+  const int lo = all_first.lo, hi = all_last.hi;  // keys that any row of the workgroup sees
+
+  const int row0 = wg_row + 32 * wv, row = row0 + lq;
+  const bool row_ok = row < rows;
+  const int tok = (row_ok ? row : rows - 1) / a.R;
+  const int head = g * a.R + (row_ok ? row : rows - 1) - tok * a.R;
+  Range my = seen_by(a, first_pos + tok, len);
+  if (!row_ok) my.hi = -1;
+  // keys that all rows of the wavefront see, and that any does (rows ascend with positions)
+  const bool wave_on = row0 < rows;
+  const int w_first = first_pos + min(row0, rows - 1) / a.R, w_last = first_pos + min(row0 + 31, rows - 1) / a.R;
+  const Range r_first = seen_by(a, w_first, len), r_last = seen_by(a, w_last, len);
+  const int every_lo = row0 + 31 < rows ? r_last.lo : 0x7FFFFFFF, every_hi = r_first.hi;
+  const int any_lo = r_first.lo, any_hi = wave_on ? r_last.hi : -1;
+
+  bf16x8 qf[D / 16];
+  {
+    const uint16_t *q = static_cast<const uint16_t *>(a.Q) + (tok0 + tok) * a.q_stride + (size_t)head * D;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) qf[kk] = *reinterpret_cast<const bf16x8 *>(q + 16 * kk + 8 * lh);
+  }
+
+  // ---- page list: 64 entries at a time, one a lane ----
+  const int *table = a.page_table + s * a.table_seq + g * a.table_group;
+  const int shift = a.page_shift;
+  const int t_lo = lo / kKeys, t_hi = hi >= lo ? hi / kKeys : t_lo - 1;
+  const int last_page = min(hi >> shift, a.max_pages - 1);
+  int list0 = (t_lo * kKeys) >> shift;  // first page of the chunk
+  auto entries = [&](int first) __attribute__((always_inline)) -> int {
+    if (hi < lo || first + lane > last_page) return 0;  // (a page that no key of the walk needs: anything)
+    const int id = table[first + lane];
+    return id >= 0 && id < a.n_pages ? id : -1;
+  };
+  int ids = entries(list0), ids_next = entries(list0 + 64);
+  unsigned long long missing = __ballot(ids < 0);  // pages out of range
+  auto advance = [&](int page) __attribute__((always_inline)) {
+    while (page >= list0 + 64) {
+      list0 += 64;
+      ids = ids_next;
+      ids_next = entries(list0 + 64);
+      missing = __ballot(ids < 0);
+    }
+  };
+
+  const size_t page_bytes = ((size_t)a.G << shift) * (D * 2), group_bytes = ((size_t)g << shift) * (D * 2);
+  const char *Kc = static_cast<const char *>(a.K_cache) + group_bytes, *Vc = static_cast<const char *>(a.V_cache) + group_bytes;
+  // LDS position of chunk c of row r: c ^ swz(r); K: its low bits of r or of r / 2, V: (r & 3) blocks of 64 or 32 bytes: both the
+  // row-per-lane 16-byte reads and the transposing reads of four rows then meet every bank once
+  const int l_row = lane / CH, l_ch = lane % CH;
+  const unsigned k_chunk = D == 128 ? (l_ch ^ ((RPI * wv + l_row) & 15)) : (l_ch ^ (((RPI * wv + l_row) >> 1) & 7));
+  const unsigned v_chunk = D == 128 ? (l_ch ^ (4 * (l_row & 3))) : (l_ch ^ (2 * (l_row & 3)));
+  const unsigned k_lane = l_row * (D * 2) + k_chunk * 16, v_lane = l_row * (D * 2) + v_chunk * 16;
+
+  auto stage = [&](int t, uint16_t *ks, uint16_t *vs) __attribute__((always_inline)) {
+    advance((t * kKeys + kKeys - 1) >> shift);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int r0 = RPI * (kWaves * i + wv), key0 = t * kKeys + r0;
+      const int page = key0 >> shift;
+      // (the chunk that holds the tile's last page holds its first too, or the one before does: pages of 8 make a tile of 8)
+      const int id = __builtin_amdgcn_readlane(ids, (page - list0) & 63);
+      const size_t off = (size_t)max(id, 0) * page_bytes + (size_t)(key0 & ((1 << shift) - 1)) * (D * 2);
+      const bool none = id < 0 || key0 > hi || key0 + RPI - 1 < lo;
+      const char *kb = none ? reinterpret_cast<const char *>(kZeros) : Kc + off;
+      const char *vb = none ? reinterpret_cast<const char *>(kZeros) : Vc + off;
+      unsigned ko = k_lane, vo = v_lane;
+      if (!none && (key0 < lo || key0 + RPI - 1 > hi)) {  // rows of the group that nobody sees: a seen one in their place
+        const int shift_rows = min(max(l_row, lo - key0), hi - key0) - l_row;
+        ko += shift_rows * (D * 2);
+        vo += shift_rows * (D * 2);
+      }
+      row_to_lds(kb, ko, mfma::lds_address(ks + r0 * D));
+      row_to_lds(vb, vo, mfma::lds_address(vs + r0 * D));
+    }
+  };
+
+  // ---- LDS read offsets (elements) ----
+  int koff[D / 16];
+#pragma unroll
+  for (int kk = 0; kk < D / 16; ++kk)
+    koff[kk] = lq * D + (((2 * kk + lh) ^ (D == 128 ? lq & 15 : (lq >> 1) & 7)) * 8);
+  const int r16 = lane & 15;
+  int voff[NB];
+#pragma unroll
+  for (int mb = 0; mb < NB; ++mb)
+    voff[mb] = (4 * lh + (r16 >> 2)) * D +
+               (((4 * mb + 2 * ((lane >> 4) & 1) + ((r16 & 3) >> 1)) ^ ((D == 128 ? 4 : 2) * (r16 >> 2))) * 8) + 4 * (r16 & 1);
+
+  f32x16 oacc[NB];
+#pragma unroll
+  for (int mb = 0; mb < NB; ++mb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) oacc[mb][i] = 0.0f;
+  float ref = 0.0f, l_run = 0.0f;
+  bool fresh = row_ok;  // no visible key met yet
+
+  // raises the reference to the row's maximum of this half tile, or places it
+  auto move_ref = [&](const f32x16 &sc) __attribute__((always_inline)) {
+    float mx = sc[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[i]);
+    const u32x2 sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+    mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * a.scale2;
+    const bool up = mx != kNegInf && (fresh || mx > ref);
+    const float to = up ? mx : ref;
+    const float f = up && !fresh ? __builtin_amdgcn_exp2f(ref - to) : 1.0f;
+    l_run *= f;
+#pragma unroll
+    for (int mb = 0; mb < NB; ++mb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) oacc[mb][i] *= f;
+    ref = to;
+    fresh = fresh && !up;
+  };
+
+  auto half = [&](const uint16_t *ks, const uint16_t *vs, int base, unsigned pages_ok) __attribute__((always_inline)) {
+    if (base > any_hi || base + 31 < any_lo) return;
+    f32x16 sc;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk)
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(ks + koff[kk]), qf[kk], sc, 0, 0, 0);
+    if (base < every_lo || base + 31 > every_hi || pages_ok != 0xFFFFFFFFu)
+      mfma::keep_rows(sc, mfma::row_bits(my.lo - base, my.hi - base) & pages_ok, lh, kNegInf);
+    bf16x8 pf[2];
+    float sum;
+    bool placed = __any(fresh);
+#pragma unroll 1
+    for (;;) {
+      if (placed) move_ref(sc);
+      float sa = 0.0f, sb = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const float pa = __builtin_amdgcn_exp2f(fmaf(sc[i], a.scale2, -ref));
+        const float pb = __builtin_amdgcn_exp2f(fmaf(sc[i + 1], a.scale2, -ref));
+        pf[i >> 3][i & 7] = (__bf16)pa;
+        pf[i >> 3][(i & 7) + 1] = (__bf16)pb;
+        sa += pa;
+        sb += pb;
+      }
+      sum = sa + sb;
+      if (placed || !__any(!(sum <= kSumLimit))) break;
+      placed = true;
+    }
+    l_run += sum;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int mb = 0; mb < NB; ++mb) {
+        const uint16_t *v0 = vs + 16 * t * D + voff[mb];
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(v0));
+        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(v0 + 8 * D));
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+        oacc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[t], oacc[mb], 0, 0, 0);
+      }
+  };
+
+  // bit k: key base + k has a page
+  auto pages_of = [&](int base) __attribute__((always_inline)) -> unsigned {
+    unsigned bits = 0u;
+    for (int k = 0; k < 32; k += 8)
+      if ((missing >> ((((base + k) >> shift) - list0) & 63) & 1ull) == 0ull) bits |= 0xFFu << k;
+    return bits;
+  };
+
+  // ---- the walk ----
+  if (t_hi >= t_lo) stage(t_lo, Ks[0], Vs[0]);
+  mfma::arrived_all<0>();
+  for (int t = t_lo; t <= t_hi; ++t) {
+    const int cur = (t - t_lo) & 1;
+    unsigned ok0 = 0xFFFFFFFFu, ok1 = 0xFFFFFFFFu;
+    if (missing != 0ull) {  // (before the list moves on)
+      ok0 = pages_of(t * kKeys);
+      ok1 = pages_of(t * kKeys + 32);
+    }
+    if (t < t_hi) stage(t + 1, Ks[cur ^ 1], Vs[cur ^ 1]);
+    half(Ks[cur], Vs[cur], t * kKeys, ok0);
+    half(Ks[cur] + 32 * D, Vs[cur] + 32 * D, t * kKeys + 32, ok1);
+    mfma::arrived_all<0>();
+  }
+
+  // ---- results ----
+  l_run += __shfl_xor(l_run, 32);
+  if (!row_ok) return;
+  const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
+  const size_t out = (size_t)(tok0 + tok) * a.H + head;
+  uint16_t *O = static_cast<uint16_t *>(a.O) + out * D;
+#pragma unroll
+  for (int mb = 0; mb < NB; ++mb)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      uint2 w;
+      w.x = mfma::pack2_bf16(oacc[mb][4 * q] * inv, oacc[mb][4 * q + 1] * inv);
+      w.y = mfma::pack2_bf16(oacc[mb][4 * q + 2] * inv, oacc[mb][4 * q + 3] * inv);
+      *reinterpret_cast<uint2 *>(O + 32 * mb + 8 * q + 4 * lh) = w;
+    }
+  if (lh == 0 && a.lse) a.lse[out] = l_run == 0.0f ? kNegInf : (ref + __log2f(l_run)) * kLn2;
+}
+
+bool prompt_mfma_supported(const Args &a) { return a.dtype == 1 && (a.d == 64 || a.d == 128); }
+
+void launch_prompt_mfma(const Args &a, hipStream_t st)
+{
+  const long tiles = (long)a.T * a.R / kPromptRows + a.S;
+  const dim3 grid((unsigned)(tiles * a.G)), block(64 * kWaves);
+  if (a.d == 64) BLOSSOM_LAUNCH((prompt_kernel<64, 2, 3>), grid, block, 0, st, a);
+  else BLOSSOM_LAUNCH((prompt_kernel<128, 2, 2>), grid, block, 0, st, a);
+}
+
+}  // namespace paged
+}  // namespace blossom

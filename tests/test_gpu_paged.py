@@ -393,3 +393,28 @@ def test_the_python_path_gives_the_same(monkeypatch):
     monkeypatch.undo()
     q2 = B.kv_append(c.p, k, v, *caches, table, cu, kv_len, Q=dq, rope=(cos, sin), Q_rot=torch.empty_like(dq))
     assert torch.equal(q1, q2) and torch.equal(Kc.view(torch.int16), caches[0].view(torch.int16))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page,window", [(8, 0), (8, 700), (16, 0), (128, 0)])
+def test_prompt_long_page_lists(d, page, window):
+    # lists of more pages than a wavefront has lanes, some of them out of range, also where the list is first looked at
+    c = Cache([1500, 1111], 4, 2, d, page, "bf16", new=[90, 33], window=window, seed=d + page)
+    for i in {0, 3, 63, 64, 65, 127, 130, 150}:
+        if i * page < 1100:
+            c.table[0, 0, i], c.table[1, 0, i] = -1, c.p.n_pages + i
+    Q, O, lse = run_prompt(c)
+    check(O, lse, *c.want_prompt(Q), "bf16")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_prompt_logits_that_grow_along_the_keys(d):
+    # the softmax's reference has to rise many times, by a little and by a lot
+    c = Cache([900], 2, 1, d, 16, "bf16", new=[200], seed=d)
+    ids = c.table[0, 0].astype(np.int64)
+    for j in range(900):
+        c.K_cache[int(ids[j // 16]), 0, j % 16] = (j / 900.0) ** 2 * 40.0 * (1.0 if j % 7 else -1.0)
+    Q = (c.normal(200, 2, d).abs() * 0.5 + 0.5).to(torch.bfloat16)
+    Q, O, lse = run_prompt(c, Q=Q)
+    wO, wl = c.want_prompt(Q)
+    check(O, lse, wO, wl, "bf16")
