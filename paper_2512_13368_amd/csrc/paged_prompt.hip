@@ -104,18 +104,25 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
     return id >= 0 && id < a.n_pages ? id : -1;
   };
   int ids = entries(list0), ids_next = entries(list0 + 64);
-  unsigned long long missing = __ballot(ids < 0);  // pages out of range
+  unsigned long long missing;  // pages out of range
+  unsigned off_lo, off_hi;     // where a page's rows of this head begin in the caches
+  auto take = [&]() __attribute__((always_inline)) {
+    missing = __ballot(ids < 0);
+    const size_t off = (size_t)max(ids, 0) * (((size_t)a.G << shift) * (D * 2)) + ((size_t)g << shift) * (D * 2);
+    off_lo = (unsigned)off;
+    off_hi = (unsigned)(off >> 32);
+  };
+  take();
   auto advance = [&](int page) __attribute__((always_inline)) {
     while (page >= list0 + 64) {
       list0 += 64;
       ids = ids_next;
       ids_next = entries(list0 + 64);
-      missing = __ballot(ids < 0);
+      take();
     }
   };
 
-  const size_t page_bytes = ((size_t)a.G << shift) * (D * 2), group_bytes = ((size_t)g << shift) * (D * 2);
-  const char *Kc = static_cast<const char *>(a.K_cache) + group_bytes, *Vc = static_cast<const char *>(a.V_cache) + group_bytes;
+  const char *Kc = static_cast<const char *>(a.K_cache), *Vc = static_cast<const char *>(a.V_cache);
   // LDS position of chunk c of row r: c ^ swz(r); K: its low bits of r or of r / 2, V: (r & 3) blocks of 64 or 32 bytes: both the
   // row-per-lane 16-byte reads and the transposing reads of four rows then meet every bank once
   const int l_row = lane / CH, l_ch = lane % CH;
@@ -125,24 +132,27 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
 
   auto stage = [&](int t, uint16_t *ks, uint16_t *vs) __attribute__((always_inline)) {
     advance((t * kKeys + kKeys - 1) >> shift);
+    const unsigned k_to = mfma::lds_address(ks) + RPI * wv * (D * 2), v_to = mfma::lds_address(vs) + RPI * wv * (D * 2);
+    const bool plain = missing == 0ull && t * kKeys >= lo && t * kKeys + kKeys - 1 <= hi;  // every row is somebody's
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int r0 = RPI * (kWaves * i + wv), key0 = t * kKeys + r0;
-      const int page = key0 >> shift;
-      // (the chunk that holds the tile's last page holds its first too, or the one before does: pages of 8 make a tile of 8)
-      const int id = __builtin_amdgcn_readlane(ids, (page - list0) & 63);
-      const size_t off = (size_t)max(id, 0) * page_bytes + (size_t)(key0 & ((1 << shift) - 1)) * (D * 2);
-      const bool none = id < 0 || key0 > hi || key0 + RPI - 1 < lo;
-      const char *kb = none ? reinterpret_cast<const char *>(kZeros) : Kc + off;
-      const char *vb = none ? reinterpret_cast<const char *>(kZeros) : Vc + off;
+      const int key0 = t * kKeys + RPI * (kWaves * i + wv);
+      const int at = (key0 >> shift) - list0;  // (a tile's pages lie in one chunk of the list: pages of 8 make a tile of 8)
+      const size_t off = ((size_t)(unsigned)__builtin_amdgcn_readlane(off_hi, at) << 32 | (unsigned)__builtin_amdgcn_readlane(off_lo, at)) +
+                         (unsigned)((key0 & ((1 << shift) - 1)) * (D * 2));
+      const char *kb = Kc + off, *vb = Vc + off;
       unsigned ko = k_lane, vo = v_lane;
-      if (!none && (key0 < lo || key0 + RPI - 1 > hi)) {  // rows of the group that nobody sees: a seen one in their place
-        const int shift_rows = min(max(l_row, lo - key0), hi - key0) - l_row;
-        ko += shift_rows * (D * 2);
-        vo += shift_rows * (D * 2);
+      if (!plain) {
+        if ((missing >> at & 1ull) != 0ull || key0 > hi || key0 + RPI - 1 < lo) {
+          kb = vb = reinterpret_cast<const char *>(kZeros);
+        } else {  // rows of the group that nobody sees: a seen one in their place
+          const int rows_off = min(max(l_row, lo - key0), hi - key0) - l_row;
+          ko += rows_off * (D * 2);
+          vo += rows_off * (D * 2);
+        }
       }
-      row_to_lds(kb, ko, mfma::lds_address(ks + r0 * D));
-      row_to_lds(vb, vo, mfma::lds_address(vs + r0 * D));
+      row_to_lds(kb, ko, k_to + i * (RPI * kWaves * D * 2));
+      row_to_lds(vb, vo, v_to + i * (RPI * kWaves * D * 2));
     }
   };
 
@@ -195,6 +205,16 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
       sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(ks + koff[kk]), qf[kk], sc, 0, 0, 0);
     if (base < every_lo || base + 31 > every_hi || pages_ok != 0xFFFFFFFFu)
       mfma::keep_rows(sc, mfma::row_bits(my.lo - base, my.hi - base) & pages_ok, lh, kNegInf);
+    bf16x8 vf[2][NB];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int mb = 0; mb < NB; ++mb) {
+        const uint16_t *v0 = vs + 16 * t * D + voff[mb];
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(v0));
+        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(v0 + 8 * D));
+        vf[t][mb] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+      }
     bf16x8 pf[2];
     float sum;
     bool placed = __any(fresh);
@@ -219,13 +239,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int mb = 0; mb < NB; ++mb) {
-        const uint16_t *v0 = vs + 16 * t * D + voff[mb];
-        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(v0));
-        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(v0 + 8 * D));
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-        oacc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[t], oacc[mb], 0, 0, 0);
-      }
+      for (int mb = 0; mb < NB; ++mb) oacc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[t][mb], pf[t], oacc[mb], 0, 0, 0);
   };
 
   // bit k: key base + k has a page
@@ -276,7 +290,7 @@ void launch_prompt_mfma(const Args &a, hipStream_t st)
 {
   const long tiles = (long)a.T * a.R / kPromptRows + a.S;
   const dim3 grid((unsigned)(tiles * a.G)), block(64 * kWaves);
-  if (a.d == 64) BLOSSOM_LAUNCH((prompt_kernel<64, 2, 3>), grid, block, 0, st, a);
+  if (a.d == 64) BLOSSOM_LAUNCH((prompt_kernel<64, 2, 4>), grid, block, 0, st, a);
   else BLOSSOM_LAUNCH((prompt_kernel<128, 2, 2>), grid, block, 0, st, a);
 }
 
