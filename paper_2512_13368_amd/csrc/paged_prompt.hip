@@ -197,14 +197,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
 
   auto half = [&](const uint16_t *ks, const uint16_t *vs, int base, unsigned pages_ok) __attribute__((always_inline)) {
     if (base > any_hi || base + 31 < any_lo) return;
-    f32x16 sc;
+    bf16x8 kf[D / 16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
-#pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk)
-      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(ks + koff[kk]), qf[kk], sc, 0, 0, 0);
-    if (base < every_lo || base + 31 > every_hi || pages_ok != 0xFFFFFFFFu)
-      mfma::keep_rows(sc, mfma::row_bits(my.lo - base, my.hi - base) & pages_ok, lh, kNegInf);
+    for (int kk = 0; kk < D / 16; ++kk) kf[kk] = *reinterpret_cast<const bf16x8 *>(ks + koff[kk]);
+    __builtin_amdgcn_sched_barrier(0);  // keys' operands are requested together, values' between the products
     bf16x8 vf[2][NB];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -215,21 +211,33 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
         const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(v0 + 8 * D));
         vf[t][mb] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
       }
+    f32x16 sc;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk], qf[kk], sc, 0, 0, 0);
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    }
+    if (base < every_lo || base + 31 > every_hi || pages_ok != 0xFFFFFFFFu)
+      mfma::keep_rows(sc, mfma::row_bits(my.lo - base, my.hi - base) & pages_ok, lh, kNegInf);
     bf16x8 pf[2];
     float sum;
     bool placed = __any(fresh);
 #pragma unroll 1
     for (;;) {
       if (placed) move_ref(sc);
-      float sa = 0.0f, sb = 0.0f;
+      float sa, sb;
 #pragma unroll
       for (int i = 0; i < 16; i += 2) {
         const float pa = __builtin_amdgcn_exp2f(fmaf(sc[i], a.scale2, -ref));
         const float pb = __builtin_amdgcn_exp2f(fmaf(sc[i + 1], a.scale2, -ref));
         pf[i >> 3][i & 7] = (__bf16)pa;
         pf[i >> 3][(i & 7) + 1] = (__bf16)pb;
-        sa += pa;
-        sb += pb;
+        sa = i == 0 ? pa : sa + pa;
+        sb = i == 0 ? pb : sb + pb;
       }
       sum = sa + sb;
       if (placed || !__any(!(sum <= kSumLimit))) break;
@@ -252,9 +260,13 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
 
   // ---- the walk ----
   if (t_hi >= t_lo) stage(t_lo, Ks[0], Vs[0]);
+  // (the compiler has the queries arrive here: it would wait for them in the loop, and for the tiles on their way with them)
+#pragma unroll
+  for (int kk = 0; kk < D / 16; ++kk) asm volatile("" : "+v"(qf[kk]));
+  asm volatile("" : "+v"(ids_next));
   mfma::arrived_all<0>();
-  for (int t = t_lo; t <= t_hi; ++t) {
-    const int cur = (t - t_lo) & 1;
+  auto step = [&](int t, auto buffer) __attribute__((always_inline)) {
+    constexpr int cur = decltype(buffer)::value;
     unsigned ok0 = 0xFFFFFFFFu, ok1 = 0xFFFFFFFFu;
     if (missing != 0ull) {  // (before the list moves on)
       ok0 = pages_of(t * kKeys);
@@ -264,6 +276,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
     half(Ks[cur], Vs[cur], t * kKeys, ok0);
     half(Ks[cur] + 32 * D, Vs[cur] + 32 * D, t * kKeys + 32, ok1);
     mfma::arrived_all<0>();
+  };
+  for (int t = t_lo; t <= t_hi; t += 2) {
+    step(t, std::integral_constant<int, 0>{});
+    if (t + 1 > t_hi) break;
+    step(t + 1, std::integral_constant<int, 1>{});
   }
 
   // ---- results ----
