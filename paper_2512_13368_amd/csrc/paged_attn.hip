@@ -31,6 +31,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int kRows = 16;   // query rows of a workgroup
 constexpr int kTile = 32;   // keys of a step
 constexpr int kWaves = 4;
+constexpr int kMostSplits = 256;
 
 // Operands of one step in registers, by storage type and head size.
 template <typename T, int D>
@@ -336,34 +337,52 @@ __global__ __launch_bounds__(64 * kWaves) void rows_kernel(Args a)
   }
 }
 
-// Joins a row's parts: a wavefront a row.
+// Joins a row's parts: a workgroup a row, whose threads take a part each for the weights, and then, 4 channels each, every
+// (256 / (d / 4))-th part's sums.  Parts that met no key have weight 0 and finite sums.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void join_kernel(Args a, long rows)
+__global__ __launch_bounds__(256) void join_kernel(Args a, int tokens)
 {
-  const int lane = threadIdx.x & 63;
-  const long row = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= rows) return;
-  const float *ml = a.part_ml + row * a.nsplit * 2;
-  float m = kNegInf;
-  for (int i = lane; i < a.nsplit; i += 64) m = fmaxf(m, ml[2 * i]);
+  constexpr int LANES = D / 4, GROUPS = 256 / LANES;
+  __shared__ float red_s[4], l_s[4], w_s[kMostSplits];
+  __shared__ __attribute__((aligned(16))) float4 o_s[GROUPS][LANES];
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const int row = blockIdx.x;
+  if (tokens && row / a.H >= token_at(a, a.S)) return;  // (a row that no sequence owns stays as it is)
+  const float *ml = a.part_ml + (size_t)row * a.nsplit * 2;
+  const float4 *po = reinterpret_cast<const float4 *>(a.part_o + (size_t)row * a.nsplit * D);
+  const bool mine = tid < a.nsplit;
+  const float2 x = mine ? *reinterpret_cast<const float2 *>(ml + 2 * tid) : make_float2(kNegInf, 0.0f);
+  float m = x.x;
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  const float ref = m == kNegInf ? 0.0f : m;
-  float l = 0.0f, o[(D + 63) / 64] = {};
-  for (int i = 0; i < a.nsplit; ++i) {
-    const float li = ml[2 * i + 1];
-    if (li == 0.0f) continue;
-    const float f = __builtin_amdgcn_exp2f(ml[2 * i] - ref);
-    l += li * f;
-    const float *po = a.part_o + (row * a.nsplit + i) * D;
+  if (lane == 0) red_s[wv] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(red_s[0], red_s[1]), fmaxf(red_s[2], red_s[3]));
+  const float w = __builtin_amdgcn_exp2f(x.x - (m == kNegInf ? 0.0f : m));
+  float l = x.y * w;
 #pragma unroll
-    for (int j = 0; j < (D + 63) / 64; ++j)
-      if (lane + 64 * j < D) o[j] += po[lane + 64 * j] * f;
+  for (int o = 32; o >= 1; o >>= 1) l += __shfl_xor(l, o);
+  if (mine) w_s[tid] = w;
+  if (lane == 0) l_s[wv] = l;
+  __syncthreads();
+  l = (l_s[0] + l_s[1]) + (l_s[2] + l_s[3]);
+  const int at = tid % LANES, grp = tid / LANES;
+  float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+  for (int i = grp; i < a.nsplit; i += GROUPS) {
+    const float4 v = po[(size_t)i * LANES + at];
+    const float f = w_s[i];
+    o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);
   }
+  o_s[grp][at] = o;
+  __syncthreads();
+  if (tid < D) {
+    float sum = 0.0f;
 #pragma unroll
-  for (int j = 0; j < (D + 63) / 64; ++j)
-    if (lane + 64 * j < D) store_out(static_cast<T *>(a.O) + row * D + lane + 64 * j, l == 0.0f ? 0.0f : o[j] / l);
-  if (lane == 0 && a.lse) a.lse[row] = l == 0.0f ? kNegInf : (m + __log2f(l)) * kLn2;
+    for (int i = 0; i < GROUPS; ++i) sum += reinterpret_cast<const float *>(&o_s[i][0])[tid];
+    store_out(static_cast<T *>(a.O) + (size_t)row * D + tid, l == 0.0f ? 0.0f : sum / l);
+  }
+  if (tid == 0 && a.lse) a.lse[row] = l == 0.0f ? kNegInf : (m + __log2f(l)) * kLn2;
 }
 
 int attn_splits(const Args &a, bool prompt)
@@ -373,7 +392,7 @@ int attn_splits(const Args &a, bool prompt)
   const long tiles = ((long)(a.window < a.cap ? a.window + kTile - 1 : a.cap) + kTile - 1) / kTile;
   const long want = (1024 + base - 1) / base, most = (tiles + 2 * kWaves - 1) / (2 * kWaves);
   const long n = want < most ? want : most;
-  return (int)(n < 1 ? 1 : n);
+  return (int)(n < 1 ? 1 : (n > kMostSplits ? kMostSplits : n));
 }
 
 namespace {
@@ -387,7 +406,7 @@ void launch_rows(const Args &a, bool prompt, hipStream_t st)
   else BLOSSOM_LAUNCH((rows_kernel<T, D, false>), grid, block, 0, st, a);
   if (a.nsplit > 1) {
     const long rows = (long)(prompt ? a.T : a.S) * a.H;
-    BLOSSOM_LAUNCH((join_kernel<T, D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a, rows);
+    BLOSSOM_LAUNCH((join_kernel<T, D>), dim3((unsigned)rows), dim3(256), 0, st, a, prompt ? a.T : 0);
   }
 }
 
