@@ -26,14 +26,15 @@ struct Args {
   void *Q_rot;                 // [T,H,d] or nullptr
   void *O;                     // [T,H,d] (decode: [S,H,d])
   float *lse;                  // [T,H] or nullptr
-  int nsplit;                  // parts that a row's keys are split into; > 1: partial results go to the workspace
-  float *part_o, *part_ml;     // [rows, nsplit, d] and [rows, nsplit, 2]: sums, and (reference in log2 units, sum of exponentials)
+  int parts;                   // decode: workgroups that share a key/value head's keys; 0: one a sequence
+  float *part_o, *part_ml;     // [H, parts, d] sums and [H, parts, 2] (reference in log2 units, sum of exponentials), in the workspace
+  int2 *part_of;               // [S] first part and parts of a sequence, there too
 };
 
 // append: paged_append.hip
 void launch_append(const Args &a, hipStream_t st);
-// one-token and prompt attention: paged_attn.hip.  `splits` is the number of parts for this shape.
-int attn_splits(const Args &a, bool prompt);
+// one-token and prompt attention: paged_attn.hip.  decode_parts: what `parts` is for this shape
+int decode_parts(const Args &a);
 void launch_decode(const Args &a, hipStream_t st);
 void launch_prompt(const Args &a, hipStream_t st);
 // prompt attention for bf16, d = 64 or 128: paged_prompt.hip

@@ -35,7 +35,6 @@ int check_params(const blossom_paged_params *p, Args *a)
   a->scale2 = (p->softmax_scale > 0.0f ? p->softmax_scale : 1.0f / std::sqrt((float)p->d)) * 1.4426950408889634f;
   a->table_group = p->table_per_head ? p->max_pages : 0;
   a->table_seq = (int64_t)p->max_pages * (p->table_per_head ? p->G : 1);
-  a->nsplit = 1;
   return BLOSSOM_OK;
 }
 
@@ -48,12 +47,10 @@ int check_stride(const Args &a, int64_t given, int heads, int64_t *stride)
   return *stride % (a.dtype == BLOSSOM_F32 ? 4 : 8) == 0 ? BLOSSOM_OK : BLOSSOM_ERR_ALIGN;
 }
 
-size_t part_rows(const Args &a, bool prompt) { return (size_t)(prompt ? a.T : a.S) * a.H * a.nsplit; }
-
 size_t attn_ws_bytes(Args &a, bool prompt)
 {
-  a.nsplit = attn_splits(a, prompt);
-  return a.nsplit > 1 ? part_rows(a, prompt) * (a.d + 2) * sizeof(float) : 0;
+  a.parts = prompt ? 0 : decode_parts(a);
+  return a.parts ? (size_t)a.H * a.parts * (a.d + 2) * sizeof(float) + (size_t)a.S * sizeof(int2) : 0;
 }
 
 int launch_status() { return hipGetLastError() == hipSuccess ? BLOSSOM_OK : BLOSSOM_ERR_LAUNCH; }
@@ -75,7 +72,8 @@ int attn(const blossom_paged_params *p, bool prompt, const void *Q, int64_t q_st
     if (!ws || ws_bytes < need) return BLOSSOM_ERR_WORKSPACE;
     if (!aligned16(ws)) return BLOSSOM_ERR_ALIGN;
     a.part_o = static_cast<float *>(ws);
-    a.part_ml = a.part_o + part_rows(a, prompt) * a.d;
+    a.part_ml = a.part_o + (size_t)a.H * a.parts * a.d;
+    a.part_of = reinterpret_cast<int2 *>(a.part_ml + (size_t)a.H * a.parts * 2);
   }
   a.Q = Q; a.K_cache = const_cast<void *>(K_cache); a.V_cache = const_cast<void *>(V_cache);
   a.page_table = page_table; a.cu = cu_seqlens; a.kv_len = kv_len;

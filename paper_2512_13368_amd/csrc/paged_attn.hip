@@ -31,7 +31,17 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int kRows = 16;   // query rows of a workgroup
 constexpr int kTile = 32;   // keys of a step
 constexpr int kWaves = 4;
-constexpr int kMostSplits = 256;
+constexpr int kMostParts = 256;   // parts of a key/value head's keys
+constexpr int kFillWaves = 2048;  // decode wavefronts that keep the memory busy: two a SIMD
+constexpr int kSplitTiles = 8;    // a wavefront's tiles from which splitting a sequence pays for the join
+
+// A load of cached rows; `ONCE`: past the caches, which hold none of them for a second reader.
+template <bool ONCE, typename V>
+__device__ __forceinline__ V cached(const V *p)
+{
+  if constexpr (ONCE) return load_once(p);
+  else return *p;
+}
 
 // Operands of one step in registers, by storage type and head size.
 template <typename T, int D>
@@ -41,29 +51,32 @@ template <int D>
 struct Ops<bf16_t, D> {
   static constexpr int NK = D >= 32 ? D / 32 : 1;  // matrix instructions for 16 keys' logits
   static constexpr int VPT = D >= 16 ? D / 16 : 1; // channels of V in a lane
-  uint4 q[NK], k[2][NK];
+  typedef uint4 Row[NK];
+  Row k[2];
   uint32_t v[8][VPT >= 2 ? VPT / 2 : 1];
   // d < 32: channels beyond the row are zeros
+  template <bool ONCE = false>
   static __device__ __forceinline__ void row(uint4 (&to)[NK], const bf16_t *p, int c)
   {
     if constexpr (D >= 32) {
 #pragma unroll
-      for (int i = 0; i < NK; ++i) to[i] = *reinterpret_cast<const uint4 *>(p + 32 * i + 8 * c);
+      for (int i = 0; i < NK; ++i) to[i] = cached<ONCE>(reinterpret_cast<const uint4 *>(p + 32 * i + 8 * c));
     } else {
       to[0] = make_uint4(0, 0, 0, 0);
-      if (8 * c < D) to[0] = *reinterpret_cast<const uint4 *>(p + 8 * c);
+      if (8 * c < D) to[0] = cached<ONCE>(reinterpret_cast<const uint4 *>(p + 8 * c));
     }
   }
+  template <bool ONCE = false>
   __device__ __forceinline__ void load_v(int slot, const bf16_t *p, int m)
   {
     if constexpr (VPT == 8) {
-      const uint4 x = *reinterpret_cast<const uint4 *>(p + 8 * m);
+      const uint4 x = cached<ONCE>(reinterpret_cast<const uint4 *>(p + 8 * m));
       v[slot][0] = x.x; v[slot][1] = x.y; v[slot][2] = x.z; v[slot][3] = x.w;
     } else if constexpr (VPT == 4) {
-      const uint2 x = *reinterpret_cast<const uint2 *>(p + 4 * m);
+      const uint2 x = cached<ONCE>(reinterpret_cast<const uint2 *>(p + 4 * m));
       v[slot][0] = x.x; v[slot][1] = x.y;
     } else if constexpr (VPT == 2) {
-      v[slot][0] = *reinterpret_cast<const uint32_t *>(p + 2 * m);
+      v[slot][0] = cached<ONCE>(reinterpret_cast<const uint32_t *>(p + 2 * m));
     } else {
       v[slot][0] = m < D ? (uint32_t)p[m].bits : 0u;
     }
@@ -73,7 +86,7 @@ struct Ops<bf16_t, D> {
 #pragma unroll
     for (int i = 0; i < (VPT >= 2 ? VPT / 2 : 1); ++i) v[slot][i] = 0u;
   }
-  __device__ __forceinline__ f32x4 logits(int t) const
+  __device__ __forceinline__ f32x4 logits(int t, const Row &q) const
   {
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -103,28 +116,31 @@ template <int D>
 struct Ops<float, D> {
   static constexpr int NK = D >= 16 ? D / 16 : 1;
   static constexpr int VPT = D >= 16 ? D / 16 : 1;
-  float4 q[NK], k[2][NK];
+  typedef float4 Row[NK];
+  Row k[2];
   float v[8][VPT];
+  template <bool ONCE = false>
   static __device__ __forceinline__ void row(float4 (&to)[NK], const float *p, int c)
   {
     if constexpr (D >= 16) {
 #pragma unroll
-      for (int i = 0; i < NK; ++i) to[i] = *reinterpret_cast<const float4 *>(p + 16 * i + 4 * c);
+      for (int i = 0; i < NK; ++i) to[i] = cached<ONCE>(reinterpret_cast<const float4 *>(p + 16 * i + 4 * c));
     } else {
       to[0] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      if (4 * c < D) to[0] = *reinterpret_cast<const float4 *>(p + 4 * c);
+      if (4 * c < D) to[0] = cached<ONCE>(reinterpret_cast<const float4 *>(p + 4 * c));
     }
   }
+  template <bool ONCE = false>
   __device__ __forceinline__ void load_v(int slot, const float *p, int m)
   {
     if constexpr (VPT >= 4) {
 #pragma unroll
       for (int j = 0; j < VPT; j += 4) {
-        const float4 x = *reinterpret_cast<const float4 *>(p + VPT * m + j);
+        const float4 x = cached<ONCE>(reinterpret_cast<const float4 *>(p + VPT * m + j));
         v[slot][j] = x.x; v[slot][j + 1] = x.y; v[slot][j + 2] = x.z; v[slot][j + 3] = x.w;
       }
     } else if constexpr (VPT == 2) {
-      const float2 x = *reinterpret_cast<const float2 *>(p + 2 * m);
+      const float2 x = cached<ONCE>(reinterpret_cast<const float2 *>(p + 2 * m));
       v[slot][0] = x.x; v[slot][1] = x.y;
     } else {
       v[slot][0] = m < D ? p[m] : 0.0f;
@@ -135,7 +151,7 @@ struct Ops<float, D> {
 #pragma unroll
     for (int i = 0; i < VPT; ++i) v[slot][i] = 0.0f;
   }
-  __device__ __forceinline__ f32x4 logits(int t) const
+  __device__ __forceinline__ f32x4 logits(int t, const Row &q) const
   {
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -159,9 +175,18 @@ struct Ops<float, D> {
 __device__ __forceinline__ void store_out(float *p, float x) { *p = x; }
 __device__ __forceinline__ void store_out(bf16_t *p, float x) { p->bits = __builtin_bit_cast(uint16_t, (__bf16)x); }
 
+__device__ __forceinline__ void store_four(float *p, const float4 &x, float f)
+{
+  *reinterpret_cast<float4 *>(p) = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
+}
+__device__ __forceinline__ void store_four(bf16_t *p, const float4 &x, float f)
+{
+  *reinterpret_cast<uint2 *>(p) = make_uint2(mfma::pack2_bf16(x.x * f, x.y * f), mfma::pack2_bf16(x.z * f, x.w * f));
+}
+
 }  // namespace
 
-template <typename T, int D, bool PROMPT>
+template <typename T, int D>
 __global__ __launch_bounds__(64 * kWaves) void rows_kernel(Args a)
 {
   typedef Ops<T, D> O_;
@@ -175,53 +200,32 @@ __global__ __launch_bounds__(64 * kWaves) void rows_kernel(Args a)
 
   // ---- this workgroup's rows ----
   const unsigned g = blockIdx.x % a.G;
-  const unsigned rest = blockIdx.x / a.G;
-  const int split = (int)(rest % a.nsplit);
-  const int tile = (int)(rest / a.nsplit);
+  const int tile = (int)(blockIdx.x / a.G);
   int s, row0, rows, tok0, new_tokens;
-  if constexpr (PROMPT) {
-    s = find_sequence(a.S, lane, [&](int i) { return (int)((long)token_at(a, i) * a.R / kRows) + i <= tile; });
-    tok0 = token_at(a, s);
-    new_tokens = max(token_at(a, s + 1) - tok0, 0);
-    row0 = (tile - (int)((long)tok0 * a.R / kRows) - s) * kRows;
-    rows = new_tokens * a.R;  // (T * R fits 31 bits: checked at the boundary)
-  } else {
-    const int tiles = (a.R + kRows - 1) / kRows;
-    s = tile / tiles;
-    tok0 = s;
-    new_tokens = 1;
-    row0 = (tile % tiles) * kRows;
-    rows = a.R;
-  }
+  s = find_sequence(a.S, lane, [&](int i) { return (int)((long)token_at(a, i) * a.R / kRows) + i <= tile; });
+  tok0 = token_at(a, s);
+  new_tokens = max(token_at(a, s + 1) - tok0, 0);
+  row0 = (tile - (int)((long)tok0 * a.R / kRows) - s) * kRows;
+  rows = new_tokens * a.R;  // (T * R fits 31 bits: checked at the boundary)
   if (row0 >= rows || row0 < 0) return;
   const int len = max(a.kv_len[s], 0);
   const int first_pos = len - new_tokens;
 
   const int row = row0 + n;
   const bool row_ok = row < rows;
-  const int tok = PROMPT ? (row_ok ? row : rows - 1) / a.R : 0;
+  const int tok = (row_ok ? row : rows - 1) / a.R;
   const int head = g * a.R + (row_ok ? row : rows - 1) - tok * a.R;
   Range my = seen_by(a, first_pos + tok, len);
   if (!row_ok) my.hi = -1;
-  int lo, hi;  // of all rows together
-  if constexpr (PROMPT) {
-    lo = seen_by(a, first_pos + row0 / a.R, len).lo;
-    hi = seen_by(a, first_pos + (min(row0 + kRows, rows) - 1) / a.R, len).hi;
-  } else {
-    lo = seen_by(a, first_pos, len).lo;
-    hi = seen_by(a, first_pos, len).hi;
-  }
+  // of all rows together
+  const int lo = seen_by(a, first_pos + row0 / a.R, len).lo;
+  const int hi = seen_by(a, first_pos + (min(row0 + kRows, rows) - 1) / a.R, len).hi;
 
   O_ x;
-  {
-    const T *q = static_cast<const T *>(a.Q) + (tok0 + tok) * a.q_stride + (size_t)head * D;
-    O_::row(x.q, q, c);
-  }
+  typename O_::Row q;
+  O_::row(q, static_cast<const T *>(a.Q) + (tok0 + tok) * a.q_stride + (size_t)head * D, c);
 
-  // ---- key tiles of this part ----
-  const int t_lo = lo / kTile, t_all = hi >= lo ? hi / kTile - t_lo + 1 : 0;
-  const int chunk = max((t_all + a.nsplit - 1) / a.nsplit, kWaves);
-  const int t_begin = t_lo + min(split * chunk, t_all), t_end = t_lo + min((split + 1) * chunk, t_all);
+  const int t_begin = lo / kTile, t_end = hi >= lo ? hi / kTile + 1 : t_begin;
 
   const int *table = a.page_table + s * a.table_seq + g * a.table_group;
   const int page_mask = (1 << a.page_shift) - 1;
@@ -267,7 +271,7 @@ __global__ __launch_bounds__(64 * kWaves) void rows_kernel(Args a)
     float p[8];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const f32x4 sc = x.logits(h);
+      const f32x4 sc = x.logits(h, q);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int key = base + 16 * h + 4 * c + i;
@@ -322,35 +326,292 @@ __global__ __launch_bounds__(64 * kWaves) void rows_kernel(Args a)
       ll += l_s[w][r] * f;
       o += acc_s[w][r][ch] * f;
     }
-    const int tk = PROMPT ? (row0 + r) / a.R : 0;
+    const int tk = (row0 + r) / a.R;
     const size_t out = (size_t)(tok0 + tk) * a.H + g * a.R + (row0 + r) - tk * a.R;
-    if (a.nsplit == 1) {
-      store_out(static_cast<T *>(a.O) + out * D + ch, ll == 0.0f ? 0.0f : o / ll);
-      if (ch == 0 && a.lse) a.lse[out] = ll == 0.0f ? kNegInf : (mm + __log2f(ll)) * kLn2;
-    } else {
-      a.part_o[(out * a.nsplit + split) * D + ch] = o;
-      if (ch == 0) {
-        a.part_ml[(out * a.nsplit + split) * 2] = mm;
-        a.part_ml[(out * a.nsplit + split) * 2 + 1] = ll;
+    store_out(static_cast<T *>(a.O) + out * D + ch, ll == 0.0f ? 0.0f : o / ll);
+    if (ch == 0 && a.lse) a.lse[out] = ll == 0.0f ? kNegInf : (mm + __log2f(ll)) * kLn2;
+  }
+}
+
+// Registers bound the wavefronts of a decode workgroup.
+constexpr int most_decode_waves(int d, int dtype) { return d == 128 ? 4 : (d == 64 && dtype == 0 ? 8 : 16); }
+
+// Maximum over the four lanes that hold a row's logits.
+__device__ __forceinline__ float row_max(float x)
+{
+  typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+  const u32x2 a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const u32x2 b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// ---- work of decode, split over a long cache ----
+__device__ __forceinline__ int tiles_of(const Args &a, int s)
+{
+  if (s >= a.S) return 0;
+  const int len = max(a.kv_len[s], 0);
+  const Range r = seen_by(a, len - 1, len);
+  return r.hi >= r.lo ? r.hi / kTile - r.lo / kTile + 1 : 0;
+}
+// inclusive sums over the lanes of a wavefront
+__device__ __forceinline__ int wave_scan(int x)
+{
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr:1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15 to the second and fourth row, 31 to the last two
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
+__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
+
+// The part of all sequences' keys that workgroup b of a key/value head takes: of a.parts workgroups, a sequence of t tiles is cut into
+// ceil(t / chunk), so that ragged lengths give parts of like size.  Every wavefront finds its own from the lengths, 64 sequences at a
+// time: a chunk of total / (parts - S / 2) nearly always makes few enough parts (half a part a sequence is lost to rounding up), one
+// of total / (parts - S) always does.
+struct Part {
+  int s = -1, first = 0, count = 0;  // sequence (-1: none), its first part, its parts
+  __device__ __forceinline__ Part(const Args &a, int lane, int b, int least)
+  {
+    const int t0 = tiles_of(a, lane);
+    auto tiles = [&](int s0) { return s0 == 0 ? t0 : tiles_of(a, s0 + lane); };
+    int total = 0;
+    for (int s0 = 0; s0 < a.S; s0 += 64) total += wave_sum(tiles(s0));
+    int chunk = max((total + a.parts - a.S / 2 - 1) / (a.parts - a.S / 2), least);
+    auto cut = [&](int t) { return (int)(((float)t + (float)(chunk - 1) + 0.5f) / (float)chunk); };  // ceil(t / chunk)
+    int need = 0;
+    for (int s0 = 0; s0 < a.S; s0 += 64) need += wave_sum(cut(tiles(s0)));
+    if (need > a.parts) chunk = max((total + a.parts - a.S - 1) / (a.parts - a.S), least);
+    int done = 0;
+    for (int s0 = 0; s0 < a.S; s0 += 64) {
+      const int mine = cut(tiles(s0)), upto = done + wave_scan(mine);
+      const int k = __builtin_popcountll(__ballot(upto <= b));
+      if (k < 64) {
+        s = s0 + k;
+        count = __builtin_amdgcn_readlane(mine, k);
+        first = __builtin_amdgcn_readlane(upto, k) - count;
+        return;
       }
+      done = __builtin_amdgcn_readlane(upto, 63);
+    }
+  }
+};
+
+// One new token a sequence: W wavefronts take the key tiles of up to 16 heads that share keys in turn.  SPLIT: a part of them.
+template <typename T, int D, int W, bool ONCE, bool SPLIT>
+__global__ __launch_bounds__(64 * W, D == 128 ? 2 : 4) void decode_kernel(Args a)
+{
+  typedef Ops<T, D> O_;
+  constexpr int VPT = O_::VPT;
+  constexpr int LDR = D + 4;  // floats of an LDS row
+  constexpr bool AHEAD = D == 128 && sizeof(T) == 2;  // the next tile is on its way while one is worked on
+  extern __shared__ __attribute__((aligned(16))) float lds_d[];
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 15, c = lane >> 4;
+
+  const int g = blockIdx.x % a.G;
+  const unsigned rest = blockIdx.x / a.G;
+  const int tiles = (a.R + kRows - 1) / kRows;
+  const int row0 = (int)(rest % tiles) * kRows, b = (int)(rest / tiles);
+  int s = b, part = 0, n_parts = 1;
+  if constexpr (SPLIT) {
+    const Part mine(a, lane, b, W);
+    if (mine.s < 0) return;
+    s = mine.s;
+    part = b - mine.first;
+    n_parts = mine.count;
+    if (part == 0 && g == 0 && row0 == 0 && threadIdx.x == 0) a.part_of[s] = make_int2(mine.first, n_parts);  // for the join
+  }
+  const int rows = min(a.R - row0, kRows), held = min(a.R, kRows);
+  const bool row_ok = n < rows;
+
+  // everything that hangs on nothing is requested before anything is waited for: the length, the query, and the page of what is
+  // this wavefront's first tile if keys are neither split nor windowed
+  const int *table = a.page_table + s * a.table_seq + g * a.table_group;
+  const int page_mask = (1 << a.page_shift) - 1;
+  auto entry = [&](int key) { return table[min(key >> a.page_shift, a.max_pages - 1)]; };
+  const int raw_len = a.kv_len[s];
+  int id[2] = {entry(wv * kTile + n), entry(wv * kTile + 16 + n)};
+  typename O_::Row q;
+  O_::row(q, static_cast<const T *>(a.Q) + s * a.q_stride + (size_t)(g * a.R + row0 + min(n, rows - 1)) * D, c);
+
+  const int len = max(__builtin_amdgcn_readfirstlane(raw_len), 0);
+  const Range my = seen_by(a, len - 1, len);
+  const int t_lo = my.lo / kTile, t_all = my.hi >= my.lo ? my.hi / kTile - t_lo + 1 : 0;
+  int t_begin = t_lo, t_end = t_lo + t_all;
+  if constexpr (SPLIT) {
+    const int each = (t_all + n_parts - 1) / n_parts;
+    t_begin = t_lo + min(part * each, t_all);
+    t_end = t_lo + min((part + 1) * each, t_all);
+  }
+  if (t_begin != 0) {
+    id[0] = entry((t_begin + wv) * kTile + n);
+    id[1] = entry((t_begin + wv) * kTile + 16 + n);
+  }
+
+  const T *Kc = static_cast<const T *>(a.K_cache), *Vc = static_cast<const T *>(a.V_cache);
+  const size_t page_step = ((size_t)a.G << a.page_shift) * D, group_off = ((size_t)g << a.page_shift) * D;
+
+  f32x4 acc[VPT];
+#pragma unroll
+  for (int j = 0; j < VPT; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  float m = kNegInf, l = 0.0f;
+
+  // requests a tile's rows, whose pages are in `id`, and the pages of the one after
+  auto request = [&](O_ &x, bool (&vok)[2], int t) __attribute__((always_inline)) {
+    const int base = t * kTile;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      id[h] = id[h] >= 0 && id[h] < a.n_pages ? id[h] : -1;
+      const int key = base + 16 * h + n;
+      O_::template row<ONCE>(x.k[h], Kc + max(id[h], 0) * page_step + group_off + (size_t)(key & page_mask) * D, c);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int vid = __shfl(id[h], 4 * c);  // (four keys of a lane group lie in one page: pages hold 8 positions or more)
+      vok[h] = vid >= 0;
+      const T *v = Vc + max(vid, 0) * page_step + group_off + (size_t)((base + 16 * h + 4 * c) & page_mask) * D;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x.template load_v<ONCE>(4 * h + i, v + i * D, n);
+    }
+    id[0] = entry(base + W * kTile + n);
+    id[1] = entry(base + W * kTile + 16 + n);
+  };
+  auto attend = [&](O_ &x, const bool (&vok)[2], int t) __attribute__((always_inline)) {
+    const int base = t * kTile;
+    float p[8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const f32x4 sc = x.logits(h, q);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[4 * h + i] = sc[i] * a.scale2;
+    }
+    if (!(__all(vok[0] && vok[1]) && base >= my.lo && base + kTile - 1 <= my.hi)) {  // what lies outside may hold anything
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int key = base + 16 * h + 4 * c + i;
+          if (!vok[h] || key < my.lo || key > my.hi) {
+            x.clear_v(4 * h + i);
+            p[4 * h + i] = kNegInf;
+          }
+        }
+    }
+    float mx = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
+    mx = fmaxf(m, row_max(mx));
+    const float ref = mx == kNegInf ? 0.0f : mx;  // no key seen yet: every exponential is 0
+    const float f = __builtin_amdgcn_exp2f(m - ref);
+    m = mx;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      p[i] = __builtin_amdgcn_exp2f(p[i] - ref);
+      sum += p[i];
+    }
+    l = l * f + sum;
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) acc[j] *= f;
+    x.product(p, acc);
+  };
+  if constexpr (AHEAD) {
+    O_ x0, x1;
+    bool v0[2], v1[2];
+    int t = t_begin + wv;
+    if (t < t_end) request(x0, v0, t);
+    while (t < t_end) {
+      if (t + W < t_end) request(x1, v1, t + W);
+      attend(x0, v0, t);
+      t += W;
+      if (t >= t_end) break;
+      if (t + W < t_end) request(x0, v0, t + W);
+      attend(x1, v1, t);
+      t += W;
+    }
+  } else {
+    for (int t = t_begin + wv; t < t_end; t += W) {
+      O_ x;
+      bool vok[2];
+      request(x, vok, t);
+      attend(x, vok, t);
+    }
+  }
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+
+  // ---- the wavefronts' results: [W][held] rows of sums, references, sums of exponentials ----
+  float *acc_s = lds_d, *m_s = lds_d + W * held * LDR, *l_s = m_s + W * held;
+  if (row_ok) {
+    if (c == 0) {
+      m_s[wv * held + n] = m;
+      l_s[wv * held + n] = l;
+    }
+    float *to = acc_s + (wv * held + n) * LDR;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < VPT; ++j)
+        if (VPT * (4 * c + i) + j < D) to[VPT * (4 * c + i) + j] = acc[j][i];
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < rows * (D / 4); e += 64 * W) {
+    const int r = e / (D / 4), ch = e % (D / 4) * 4;
+    float mm = kNegInf;
+#pragma unroll
+    for (int w = 0; w < W; ++w) mm = fmaxf(mm, m_s[w * held + r]);
+    const float ref = mm == kNegInf ? 0.0f : mm;
+    float ll = 0.0f;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const float f = __builtin_amdgcn_exp2f(m_s[w * held + r] - ref);
+      const float4 v = *reinterpret_cast<const float4 *>(acc_s + (w * held + r) * LDR + ch);
+      ll = fmaf(l_s[w * held + r], f, ll);
+      o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);
+    }
+    const size_t out = (size_t)s * a.H + g * a.R + row0 + r;
+    if (!SPLIT || n_parts == 1) {
+      const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
+      store_four(static_cast<T *>(a.O) + out * D + ch, o, inv);
+      if (ch == 0 && a.lse) a.lse[out] = ll == 0.0f ? kNegInf : (mm + __log2f(ll)) * kLn2;
+    } else {  // [H rows of the token's heads][parts]
+      const size_t at = (size_t)(g * a.R + row0 + r) * a.parts + b;
+      *reinterpret_cast<float4 *>(a.part_o + at * D + ch) = o;
+      if (ch == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(mm, ll);
     }
   }
 }
 
-// Joins a row's parts: a workgroup a row, whose threads take a part each for the weights, and then, 4 channels each, every
-// (256 / (d / 4))-th part's sums.  Parts that met no key have weight 0 and finite sums.
+// Joins the parts of a sequence's row, where it has more than one: a workgroup a row, whose threads take a part each for the weights
+// and then, 4 channels each, every (256 / (d / 4))-th part's sums.  Parts that met no key have weight 0 and finite sums.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void join_kernel(Args a, int tokens)
+__global__ __launch_bounds__(256) void join_kernel(Args a)
 {
   constexpr int LANES = D / 4, GROUPS = 256 / LANES;
-  __shared__ float red_s[4], l_s[4], w_s[kMostSplits];
-  __shared__ __attribute__((aligned(16))) float4 o_s[GROUPS][LANES];
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-  const int row = blockIdx.x;
-  if (tokens && row / a.H >= token_at(a, a.S)) return;  // (a row that no sequence owns stays as it is)
-  const float *ml = a.part_ml + (size_t)row * a.nsplit * 2;
-  const float4 *po = reinterpret_cast<const float4 *>(a.part_o + (size_t)row * a.nsplit * D);
-  const bool mine = tid < a.nsplit;
+  __shared__ float red_s[4], l_s[4], w_s[kMostParts];
+  __shared__ __attribute__((aligned(16))) float o_s[GROUPS][D];
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int s = blockIdx.x / a.H, h = blockIdx.x % a.H;
+  const int2 part = a.part_of[s];  // (of a sequence without keys: whatever the workspace held)
+  const int n = __builtin_amdgcn_readfirstlane(tiles_of(a, s) > 0 ? part.y : 0);
+  T *O = static_cast<T *>(a.O) + (size_t)blockIdx.x * D;
+  if (n <= 1) {
+    if (n == 1) return;  // (the part's workgroup wrote the row)
+    if (tid < D) store_out(O + tid, 0.0f);
+    if (tid == 0 && a.lse) a.lse[blockIdx.x] = kNegInf;
+    return;
+  }
+  const size_t at0 = (size_t)h * a.parts + part.x;
+  const float *ml = a.part_ml + at0 * 2;
+  const float4 *po = reinterpret_cast<const float4 *>(a.part_o + at0 * D);
+  const int at = tid % LANES, grp = tid / LANES;
+  float4 early[8];  // (requested with the weights)
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    early[k] = grp + k * GROUPS < n ? po[(size_t)(grp + k * GROUPS) * LANES + at] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  const bool mine = tid < n;
   const float2 x = mine ? *reinterpret_cast<const float2 *>(ml + 2 * tid) : make_float2(kNegInf, 0.0f);
   float m = x.x;
 #pragma unroll
@@ -362,79 +623,130 @@ __global__ __launch_bounds__(256) void join_kernel(Args a, int tokens)
   float l = x.y * w;
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) l += __shfl_xor(l, o);
-  if (mine) w_s[tid] = w;
+  w_s[tid] = mine ? w : 0.0f;
   if (lane == 0) l_s[wv] = l;
   __syncthreads();
   l = (l_s[0] + l_s[1]) + (l_s[2] + l_s[3]);
-  const int at = tid % LANES, grp = tid / LANES;
   float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 8
-  for (int i = grp; i < a.nsplit; i += GROUPS) {
-    const float4 v = po[(size_t)i * LANES + at];
-    const float f = w_s[i];
+  auto add = [&](const float4 &v, float f) __attribute__((always_inline)) {
     o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);
-  }
-  o_s[grp][at] = o;
+  };
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (grp + k * GROUPS < kMostParts) add(early[k], w_s[grp + k * GROUPS]);
+  for (int i = grp + 8 * GROUPS; i < n; i += GROUPS) add(po[(size_t)i * LANES + at], w_s[i]);
+  *reinterpret_cast<float4 *>(&o_s[grp][4 * at]) = o;
   __syncthreads();
   if (tid < D) {
     float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i) sum += reinterpret_cast<const float *>(&o_s[i][0])[tid];
-    store_out(static_cast<T *>(a.O) + (size_t)row * D + tid, l == 0.0f ? 0.0f : sum / l);
+    for (int i = 0; i < GROUPS; ++i) sum += o_s[i][tid];
+    store_out(O + tid, l == 0.0f ? 0.0f : sum / l);
   }
-  if (tid == 0 && a.lse) a.lse[row] = l == 0.0f ? kNegInf : (m + __log2f(l)) * kLn2;
-}
-
-int attn_splits(const Args &a, bool prompt)
-{
-  if (prompt) return 1;
-  const long base = (long)a.S * a.G * ((a.R + kRows - 1) / kRows);
-  const long tiles = ((long)(a.window < a.cap ? a.window + kTile - 1 : a.cap) + kTile - 1) / kTile;
-  const long want = (1024 + base - 1) / base, most = (tiles + 2 * kWaves - 1) / (2 * kWaves);
-  const long n = want < most ? want : most;
-  return (int)(n < 1 ? 1 : (n > kMostSplits ? kMostSplits : n));
+  if (tid == 0 && a.lse) a.lse[blockIdx.x] = l == 0.0f ? kNegInf : (m + __log2f(l)) * kLn2;
 }
 
 namespace {
 
-template <typename T, int D>
-void launch_rows(const Args &a, bool prompt, hipStream_t st)
+// Key tiles that a row may see: all that the host knows of the lengths.
+long most_tiles(const Args &a)
 {
-  const long tiles = prompt ? (long)a.T * a.R / kRows + a.S : (long)a.S * ((a.R + kRows - 1) / kRows);
-  const dim3 grid((unsigned)(tiles * a.nsplit * a.G)), block(64 * kWaves);
-  if (prompt) BLOSSOM_LAUNCH((rows_kernel<T, D, true>), grid, block, 0, st, a);
-  else BLOSSOM_LAUNCH((rows_kernel<T, D, false>), grid, block, 0, st, a);
-  if (a.nsplit > 1) {
-    const long rows = (long)(prompt ? a.T : a.S) * a.H;
-    BLOSSOM_LAUNCH((join_kernel<T, D>), dim3((unsigned)rows), dim3(256), 0, st, a, prompt ? a.T : 0);
-  }
+  return ((long)(a.window < a.cap ? a.window + kTile - 1 : a.cap) + kTile - 1) / kTile;
+}
+long decode_bases(const Args &a) { return (long)a.S * a.G * ((a.R + kRows - 1) / kRows); }
+
+// Wavefronts of a decode workgroup: more of them where workgroups are few, as far as registers and keys go.
+int decode_waves(const Args &a)
+{
+  const int most = most_decode_waves(a.d, a.dtype);
+  int w = 4;
+  while (w < most && decode_bases(a) * w < kFillWaves && most_tiles(a) >= 2 * w) w *= 2;
+  return w;
 }
 
-template <typename T>
-void launch_rows_d(const Args &a, bool prompt, hipStream_t st)
+}  // namespace
+
+int decode_parts(const Args &a)
 {
-  switch (a.d) {
-    case 8: launch_rows<T, 8>(a, prompt, st); break;
-    case 16: launch_rows<T, 16>(a, prompt, st); break;
-    case 32: launch_rows<T, 32>(a, prompt, st); break;
-    case 64: launch_rows<T, 64>(a, prompt, st); break;
-    default: launch_rows<T, 128>(a, prompt, st); break;
+  const int w = decode_waves(a);
+  const long heads = (long)a.G * ((a.R + kRows - 1) / kRows);
+  if (decode_bases(a) * w >= kFillWaves || most_tiles(a) < kSplitTiles * w) return 0;
+  if (a.S * most_tiles(a) > 1 << 22) return 0;  // (parts are counted in 32 bits and cut in fp32)
+  const long parts = kFillWaves / w / heads, most = a.S * ((most_tiles(a) + 2 * w - 1) / (2 * w));
+  const long n = parts < most ? parts : most;
+  return (int)(n >= 2 * a.S ? (n > kMostParts ? kMostParts : n) : 0);
+}
+
+namespace {
+
+template <typename T, int D, int W>
+void launch_decode_w(const Args &a, hipStream_t st)
+{
+  const dim3 grid((unsigned)(decode_bases(a) / a.S * (a.parts ? a.parts : a.S))), block(64 * W);
+  const size_t lds = (size_t)W * (a.R < kRows ? a.R : kRows) * (D + 6) * sizeof(float);
+  // what the last-level cache cannot hold until the next token's call is not kept in the caches at all
+  const bool once = a.R <= kRows && (double)a.S * most_tiles(a) * kTile * a.G * D * 2 * sizeof(T) > 256e6;
+  auto go = [&](auto kernel) {
+    if (lds > 65536)  // more than a launch gets unasked
+      (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    BLOSSOM_LAUNCH(kernel, grid, block, lds, st, a);
+  };
+  if (!a.parts) {
+    if (once) go(decode_kernel<T, D, W, true, false>);
+    else go(decode_kernel<T, D, W, false, false>);
+    return;
   }
+  if (once) go(decode_kernel<T, D, W, true, true>);
+  else go(decode_kernel<T, D, W, false, true>);
+  if (launch_failed()) return;
+  BLOSSOM_LAUNCH((join_kernel<T, D>), dim3((unsigned)(a.S * a.H)), dim3(256), 0, st, a);
+}
+
+template <typename T, int D>
+void launch_decode_d(const Args &a, hipStream_t st)
+{
+  constexpr int MOST = most_decode_waves(D, sizeof(T) == 4 ? 0 : 1);
+  const int w = decode_waves(a);
+  if (MOST >= 16 && w == 16) launch_decode_w<T, D, MOST >= 16 ? 16 : 4>(a, st);
+  else if (MOST >= 8 && w == 8) launch_decode_w<T, D, MOST >= 8 ? 8 : 4>(a, st);
+  else launch_decode_w<T, D, 4>(a, st);
+}
+
+template <typename T, int D>
+void launch_rows_d(const Args &a, hipStream_t st)
+{
+  const dim3 grid((unsigned)(((long)a.T * a.R / kRows + a.S) * a.G)), block(64 * kWaves);
+  BLOSSOM_LAUNCH((rows_kernel<T, D>), grid, block, 0, st, a);
+}
+
+// Calls f with the element type and the head size as compile-time constants.
+template <typename F>
+void with_type(const Args &a, F &&f)
+{
+  auto with_dim = [&](auto type) {
+    switch (a.d) {
+      case 8: f(type, std::integral_constant<int, 8>{}); break;
+      case 16: f(type, std::integral_constant<int, 16>{}); break;
+      case 32: f(type, std::integral_constant<int, 32>{}); break;
+      case 64: f(type, std::integral_constant<int, 64>{}); break;
+      default: f(type, std::integral_constant<int, 128>{}); break;
+    }
+  };
+  if (a.dtype == 0) with_dim(0.0f);
+  else with_dim(bf16_t{});
 }
 
 }  // namespace
 
 void launch_decode(const Args &a, hipStream_t st)
 {
-  if (a.dtype == 0) launch_rows_d<float>(a, false, st);
-  else launch_rows_d<bf16_t>(a, false, st);
+  with_type(a, [&](auto type, auto dim) { launch_decode_d<decltype(type), decltype(dim)::value>(a, st); });
 }
 
 void launch_prompt(const Args &a, hipStream_t st)
 {
   if (prompt_mfma_supported(a)) return launch_prompt_mfma(a, st);
-  if (a.dtype == 0) launch_rows_d<float>(a, true, st);
-  else launch_rows_d<bf16_t>(a, true, st);
+  with_type(a, [&](auto type, auto dim) { launch_rows_d<decltype(type), decltype(dim)::value>(a, st); });
 }
 
 }  // namespace paged

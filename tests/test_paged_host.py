@@ -81,7 +81,8 @@ def test_per_head_tables_are_decodes(lib):
 def test_workspace(lib):
     p = params(S=1, max_pages=4096)
     need = B.paged_workspace_bytes(p, B.WS_DECODE)
-    assert need > 0 and need % (4 * 4 * (64 + 2)) == 0  # parts of four heads' rows: sums, reference, sum of exponentials
+    # parts of four heads' rows: sums, reference, sum of exponentials; and where the sequence's parts begin, and how many
+    assert need > 0 and (need - 8) % (4 * 4 * (64 + 2)) == 0
     assert decode(lib, p, ws=None) == -6 and decode(lib, p, nbytes=need - 1) == -6 and decode(lib, p, ws=vp(4104)) == -5
     assert B.paged_workspace_bytes(p, B.WS_FWD) == 0 and B.paged_workspace_bytes(p, 99) == 0
     assert B.workspace_bytes(B.Params(1, 1, 8, 8, 8, 1, 1), B.WS_DECODE) == 0
