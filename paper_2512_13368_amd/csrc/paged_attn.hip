@@ -17,6 +17,7 @@
 #include "launch.h"
 #include "mfma_common.h"
 #include "paged.h"
+#include "paged_tile.h"
 
 namespace blossom {
 namespace paged {
@@ -26,10 +27,8 @@ namespace {
 using mfma::bf16x8;
 using mfma::kLn2;
 using mfma::kNegInf;
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kRows = 16;   // query rows of a workgroup
-constexpr int kTile = 32;   // keys of a step
 constexpr int kWaves = 4;
 constexpr int kMostParts = 256;   // parts of a key/value head's keys
 constexpr int kFillWaves = 2048;  // decode wavefronts that keep the memory busy: two a SIMD
@@ -333,17 +332,14 @@ __global__ __launch_bounds__(64 * kWaves) void rows_kernel(Args a)
   }
 }
 
-// Registers bound the wavefronts of a decode workgroup.
-constexpr int most_decode_waves(int d, int dtype) { return d == 128 ? 4 : (d == 64 && dtype == 0 ? 8 : 16); }
-
-// Maximum over the four lanes that hold a row's logits.
-__device__ __forceinline__ float row_max(float x)
+// A wavefront of decode holds two tiles of K and of V in LDS, one on its way; of tiles of 16 KB and more one alone, eight wavefronts
+// (or four) to a CU.  (At d = 128, bf16: four wavefronts of two tiles 86.5 us for 131071 keys, eight of one 85.6; two of four
+// 111.)  A workgroup's wavefronts take up to 128 KB.
+constexpr int decode_stages(int row_bytes) { return row_bytes >= 256 ? 1 : 2; }
+constexpr int most_decode_waves(int row_bytes)
 {
-  typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-  const u32x2 a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  const u32x2 b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+  const int held = decode_stages(row_bytes) * 2 * (row_bytes < 32 ? 1024 : 32 * row_bytes);
+  return 131072 / held < 16 ? 131072 / held : 16;
 }
 
 // ---- work of decode, split over a long cache ----
@@ -399,15 +395,16 @@ struct Part {
   }
 };
 
-// One new token a sequence: W wavefronts take the key tiles of up to 16 heads that share keys in turn.  SPLIT: a part of them.
+// One new token a sequence: W wavefronts take a run of key tiles each for up to 16 heads that share keys.  SPLIT: of a part of them.
 template <typename T, int D, int W, bool ONCE, bool SPLIT>
-__global__ __launch_bounds__(64 * W, D == 128 ? 2 : 4) void decode_kernel(Args a)
+__global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
 {
-  typedef Ops<T, D> O_;
-  constexpr int VPT = O_::VPT;
-  constexpr int LDR = D + 4;  // floats of an LDS row
-  constexpr bool AHEAD = D == 128 && sizeof(T) == 2;  // the next tile is on its way while one is worked on
-  extern __shared__ __attribute__((aligned(16))) float lds_d[];
+  typedef Tile<T, D> TL;
+  constexpr int STAGES = decode_stages(TL::RB), HOLD = STAGES * 2 * TL::BYTES;  // LDS of a wavefront
+  constexpr int LDR = D + 4;  // floats of a row of results
+  static_assert(kRows * LDR * 4 <= HOLD, "results go where the tiles were");
+  __shared__ __attribute__((aligned(1024))) char lds[W * HOLD];
+  __shared__ float m_s[W][kRows], l_s[W][kRows];
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, c = lane >> 4;
 
@@ -424,18 +421,18 @@ __global__ __launch_bounds__(64 * W, D == 128 ? 2 : 4) void decode_kernel(Args a
     n_parts = mine.count;
     if (part == 0 && g == 0 && row0 == 0 && threadIdx.x == 0) a.part_of[s] = make_int2(mine.first, n_parts);  // for the join
   }
-  const int rows = min(a.R - row0, kRows), held = min(a.R, kRows);
-  const bool row_ok = n < rows;
+  const int rows = min(a.R - row0, kRows);
 
-  // everything that hangs on nothing is requested before anything is waited for: the length, the query, and the page of what is
-  // this wavefront's first tile if keys are neither split nor windowed
+  // what hangs on nothing is requested before anything is waited for: the length, the query, the first pages
   const int *table = a.page_table + s * a.table_seq + g * a.table_group;
-  const int page_mask = (1 << a.page_shift) - 1;
-  auto entry = [&](int key) { return table[min(key >> a.page_shift, a.max_pages - 1)]; };
+  auto entries = [&](int first) __attribute__((always_inline)) -> int {
+    const int id = table[min(first + lane, a.max_pages - 1)];
+    return id >= 0 && id < a.n_pages ? id : -1;
+  };
   const int raw_len = a.kv_len[s];
-  int id[2] = {entry(wv * kTile + n), entry(wv * kTile + 16 + n)};
-  typename O_::Row q;
-  O_::row(q, static_cast<const T *>(a.Q) + s * a.q_stride + (size_t)(g * a.R + row0 + min(n, rows - 1)) * D, c);
+  int list0 = 0, ids = entries(0);  // pages list0 .. list0 + 63, one a lane
+  typename TL::Query q;
+  TL::load_query(q, static_cast<const T *>(a.Q) + s * a.q_stride + (size_t)(g * a.R + row0 + min(n, rows - 1)) * D, c);
 
   const int len = max(__builtin_amdgcn_readfirstlane(raw_len), 0);
   const Range my = seen_by(a, len - 1, len);
@@ -446,138 +443,89 @@ __global__ __launch_bounds__(64 * W, D == 128 ? 2 : 4) void decode_kernel(Args a
     t_begin = t_lo + min(part * each, t_all);
     t_end = t_lo + min((part + 1) * each, t_all);
   }
-  if (t_begin != 0) {
-    id[0] = entry((t_begin + wv) * kTile + n);
-    id[1] = entry((t_begin + wv) * kTile + 16 + n);
+  const int run = (t_end - t_begin + W - 1) / W;
+  int t = min(t_begin + wv * run, t_end);
+  const int t_stop = min(t + run, t_end);
+
+  char *mine = lds + wv * HOLD;
+  const size_t page_bytes = ((size_t)a.G << a.page_shift) * TL::RB, group_bytes = ((size_t)g << a.page_shift) * TL::RB;
+  auto request = [&](int t, char *to) __attribute__((always_inline)) -> unsigned {
+    const int first = (t * kTile) >> a.page_shift, last = (t * kTile + kTile - 1) >> a.page_shift;
+    if (first < list0 || last >= list0 + 64) {
+      list0 = first;
+      ids = entries(first);
+    }
+    const int key = t * kTile + (lane & 31);
+    const int id = __shfl(ids, (key >> a.page_shift) - list0);
+    const bool ok = id >= 0 && key >= my.lo && key <= my.hi;
+    const unsigned seen = (unsigned)__ballot(ok);
+    const size_t off = max(id, 0) * page_bytes + group_bytes + (size_t)(key & ((1 << a.page_shift) - 1)) * TL::RB;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (what was read from `to` is here)
+    TL::template request<ONCE>(a, to, to + TL::BYTES, off, ok, seen == 0xFFFFFFFFu, lane, 0, 1);
+    return seen;
+  };
+
+  Rows<T, D> r;
+  r.clear();
+  // a ring of STAGES tiles: those of the next STAGES - 1 are on their way while one is worked on
+  unsigned seen[STAGES];
+#pragma unroll
+  for (int k = 0; k < STAGES - 1; ++k) seen[k] = t + k < t_stop ? request(t + k, mine + k * (2 * TL::BYTES)) : 0u;
+  while (t < t_stop) {
+#pragma unroll
+    for (int k = 0; k < STAGES; ++k) {
+      if (t >= t_stop) break;
+      constexpr int AHEAD = STAGES - 1;
+      const int to = (k + AHEAD) % STAGES;
+      if (t + AHEAD < t_stop) {
+        seen[to] = request(t + AHEAD, mine + to * (2 * TL::BYTES));
+        arrived<2 * TL::LOADS * AHEAD>();
+      } else {
+        arrived<0>();
+      }
+      const char *ks = mine + k * (2 * TL::BYTES);
+      r.attend(ks, ks + TL::BYTES, q, a.scale2, seen[k], seen[k] == 0xFFFFFFFFu, lane);
+      ++t;
+    }
   }
 
-  const T *Kc = static_cast<const T *>(a.K_cache), *Vc = static_cast<const T *>(a.V_cache);
-  const size_t page_step = ((size_t)a.G << a.page_shift) * D, group_off = ((size_t)g << a.page_shift) * D;
-
-  f32x4 acc[VPT];
-#pragma unroll
-  for (int j = 0; j < VPT; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  float m = kNegInf, l = 0.0f;
-
-  // requests a tile's rows, whose pages are in `id`, and the pages of the one after
-  auto request = [&](O_ &x, bool (&vok)[2], int t) __attribute__((always_inline)) {
-    const int base = t * kTile;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      id[h] = id[h] >= 0 && id[h] < a.n_pages ? id[h] : -1;
-      const int key = base + 16 * h + n;
-      O_::template row<ONCE>(x.k[h], Kc + max(id[h], 0) * page_step + group_off + (size_t)(key & page_mask) * D, c);
-    }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int vid = __shfl(id[h], 4 * c);  // (four keys of a lane group lie in one page: pages hold 8 positions or more)
-      vok[h] = vid >= 0;
-      const T *v = Vc + max(vid, 0) * page_step + group_off + (size_t)((base + 16 * h + 4 * c) & page_mask) * D;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x.template load_v<ONCE>(4 * h + i, v + i * D, n);
-    }
-    id[0] = entry(base + W * kTile + n);
-    id[1] = entry(base + W * kTile + 16 + n);
-  };
-  auto attend = [&](O_ &x, const bool (&vok)[2], int t) __attribute__((always_inline)) {
-    const int base = t * kTile;
-    float p[8];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const f32x4 sc = x.logits(h, q);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) p[4 * h + i] = sc[i] * a.scale2;
-    }
-    if (!(__all(vok[0] && vok[1]) && base >= my.lo && base + kTile - 1 <= my.hi)) {  // what lies outside may hold anything
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int key = base + 16 * h + 4 * c + i;
-          if (!vok[h] || key < my.lo || key > my.hi) {
-            x.clear_v(4 * h + i);
-            p[4 * h + i] = kNegInf;
-          }
-        }
-    }
-    float mx = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
-    mx = fmaxf(m, row_max(mx));
-    const float ref = mx == kNegInf ? 0.0f : mx;  // no key seen yet: every exponential is 0
-    const float f = __builtin_amdgcn_exp2f(m - ref);
-    m = mx;
-    float sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(p[i] - ref);
-      sum += p[i];
-    }
-    l = l * f + sum;
-#pragma unroll
-    for (int j = 0; j < VPT; ++j) acc[j] *= f;
-    x.product(p, acc);
-  };
-  if constexpr (AHEAD) {
-    O_ x0, x1;
-    bool v0[2], v1[2];
-    int t = t_begin + wv;
-    if (t < t_end) request(x0, v0, t);
-    while (t < t_end) {
-      if (t + W < t_end) request(x1, v1, t + W);
-      attend(x0, v0, t);
-      t += W;
-      if (t >= t_end) break;
-      if (t + W < t_end) request(x0, v0, t + W);
-      attend(x1, v1, t);
-      t += W;
-    }
-  } else {
-    for (int t = t_begin + wv; t < t_end; t += W) {
-      O_ x;
-      bool vok[2];
-      request(x, vok, t);
-      attend(x, vok, t);
-    }
-  }
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
-
-  // ---- the wavefronts' results: [W][held] rows of sums, references, sums of exponentials ----
-  float *acc_s = lds_d, *m_s = lds_d + W * held * LDR, *l_s = m_s + W * held;
-  if (row_ok) {
+  // ---- the wavefronts' results ----
+  const float l = r.total();
+  if (n < rows) {
     if (c == 0) {
-      m_s[wv * held + n] = m;
-      l_s[wv * held + n] = l;
+      m_s[wv][n] = r.m;
+      l_s[wv][n] = l;
     }
-    float *to = acc_s + (wv * held + n) * LDR;
+    float *to = reinterpret_cast<float *>(mine) + n * LDR;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int j = 0; j < TL::NV; ++j)
 #pragma unroll
-      for (int j = 0; j < VPT; ++j)
-        if (VPT * (4 * c + i) + j < D) to[VPT * (4 * c + i) + j] = acc[j][i];
+      for (int i = 0; i < 4; ++i)
+        if (TL::channel(j, c, i) < D) to[TL::channel(j, c, i)] = r.acc[j][i];
   }
   __syncthreads();
   for (int e = threadIdx.x; e < rows * (D / 4); e += 64 * W) {
-    const int r = e / (D / 4), ch = e % (D / 4) * 4;
+    const int row = e / (D / 4), ch = e % (D / 4) * 4;
     float mm = kNegInf;
 #pragma unroll
-    for (int w = 0; w < W; ++w) mm = fmaxf(mm, m_s[w * held + r]);
+    for (int w = 0; w < W; ++w) mm = fmaxf(mm, m_s[w][row]);
     const float ref = mm == kNegInf ? 0.0f : mm;
     float ll = 0.0f;
     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      const float f = __builtin_amdgcn_exp2f(m_s[w * held + r] - ref);
-      const float4 v = *reinterpret_cast<const float4 *>(acc_s + (w * held + r) * LDR + ch);
-      ll = fmaf(l_s[w * held + r], f, ll);
+      const float f = __builtin_amdgcn_exp2f(m_s[w][row] - ref);
+      const float4 v = *reinterpret_cast<const float4 *>(lds + w * HOLD + (row * LDR + ch) * 4);
+      ll = fmaf(l_s[w][row], f, ll);
       o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);
     }
-    const size_t out = (size_t)s * a.H + g * a.R + row0 + r;
+    const size_t out = (size_t)s * a.H + g * a.R + row0 + row;
     if (!SPLIT || n_parts == 1) {
       const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
       store_four(static_cast<T *>(a.O) + out * D + ch, o, inv);
       if (ch == 0 && a.lse) a.lse[out] = ll == 0.0f ? kNegInf : (mm + __log2f(ll)) * kLn2;
     } else {  // [H rows of the token's heads][parts]
-      const size_t at = (size_t)(g * a.R + row0 + r) * a.parts + b;
+      const size_t at = (size_t)(g * a.R + row0 + row) * a.parts + b;
       *reinterpret_cast<float4 *>(a.part_o + at * D + ch) = o;
       if (ch == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(mm, ll);
     }
@@ -658,8 +606,8 @@ long decode_bases(const Args &a) { return (long)a.S * a.G * ((a.R + kRows - 1) /
 // Wavefronts of a decode workgroup: more of them where workgroups are few, as far as registers and keys go.
 int decode_waves(const Args &a)
 {
-  const int most = most_decode_waves(a.d, a.dtype);
-  int w = 4;
+  const int most = most_decode_waves(a.d * (a.dtype == 0 ? 4 : 2));
+  int w = most < 4 ? most : 4;
   while (w < most && decode_bases(a) * w < kFillWaves && most_tiles(a) >= 2 * w) w *= 2;
   return w;
 }
@@ -683,14 +631,9 @@ template <typename T, int D, int W>
 void launch_decode_w(const Args &a, hipStream_t st)
 {
   const dim3 grid((unsigned)(decode_bases(a) / a.S * (a.parts ? a.parts : a.S))), block(64 * W);
-  const size_t lds = (size_t)W * (a.R < kRows ? a.R : kRows) * (D + 6) * sizeof(float);
   // what the last-level cache cannot hold until the next token's call is not kept in the caches at all
   const bool once = a.R <= kRows && (double)a.S * most_tiles(a) * kTile * a.G * D * 2 * sizeof(T) > 256e6;
-  auto go = [&](auto kernel) {
-    if (lds > 65536)  // more than a launch gets unasked
-      (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    BLOSSOM_LAUNCH(kernel, grid, block, lds, st, a);
-  };
+  auto go = [&](auto kernel) { BLOSSOM_LAUNCH(kernel, grid, block, 0, st, a); };
   if (!a.parts) {
     if (once) go(decode_kernel<T, D, W, true, false>);
     else go(decode_kernel<T, D, W, false, false>);
@@ -705,11 +648,13 @@ void launch_decode_w(const Args &a, hipStream_t st)
 template <typename T, int D>
 void launch_decode_d(const Args &a, hipStream_t st)
 {
-  constexpr int MOST = most_decode_waves(D, sizeof(T) == 4 ? 0 : 1);
+  constexpr int MOST = most_decode_waves(D * sizeof(T));
   const int w = decode_waves(a);
-  if (MOST >= 16 && w == 16) launch_decode_w<T, D, MOST >= 16 ? 16 : 4>(a, st);
-  else if (MOST >= 8 && w == 8) launch_decode_w<T, D, MOST >= 8 ? 8 : 4>(a, st);
-  else launch_decode_w<T, D, 4>(a, st);
+  if constexpr (MOST >= 16)
+    if (w == 16) return launch_decode_w<T, D, 16>(a, st);
+  if constexpr (MOST >= 8)
+    if (w == 8) return launch_decode_w<T, D, 8>(a, st);
+  launch_decode_w<T, D, MOST < 4 ? MOST : 4>(a, st);
 }
 
 template <typename T, int D>

@@ -1,0 +1,246 @@
+// Key tiles of a paged cache in LDS: 32 rows of K or V, moved from their pages by direct global->LDS loads, and the operands that
+// 16x16 matrix instructions take from them (gfx950 only).
+//
+// A load moves 1 KB, lane l's 16 bytes to 16*l from its destination on: neighbouring lanes take neighbouring bytes of a row, at 64
+// bytes a clock and CU.  (A lane a row, as the matrix instructions want their operands, gets 18 bytes a clock: the rows of
+// neighbouring lanes are fetched one at a time.)
+#pragma once
+
+#include "common.h"
+#include "mfma_common.h"
+#include "paged.h"
+
+namespace blossom {
+namespace paged {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+constexpr int kTile = 32;  // keys
+
+// what stands in for rows that nobody may see
+static __device__ const uint4 kZeros[64] = {};
+
+// 16 bytes a lane to `lds` + 16 * lane: from a uniform base and 32-bit offsets, or from an address a lane.  ONCE: past the caches.
+template <bool ONCE>
+__device__ __forceinline__ void to_lds(const void *base, unsigned off, unsigned lds)
+{
+  if constexpr (ONCE) asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"{m0}"(lds), "v"(off), "s"(base) : "memory");
+  else asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(lds), "v"(off), "s"(base) : "memory");
+}
+template <bool ONCE>
+__device__ __forceinline__ void to_lds(const void *from, unsigned lds)
+{
+  if constexpr (ONCE) asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"{m0}"(lds), "v"(from) : "memory");
+  else asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(lds), "v"(from) : "memory");
+}
+// at most N of this wavefront's requests are still on their way
+template <int N>
+__device__ __forceinline__ void arrived()
+{
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+template <typename T, int D>
+struct Tile {
+  static constexpr bool BF = sizeof(T) == 2;
+  static constexpr int RB = D * (int)sizeof(T);            // bytes of a row
+  static constexpr int CH = RB / 16;                       // 16-byte chunks of a row
+  static constexpr int RPL = 64 / CH;                      // rows that a load moves
+  static constexpr int LOADS = RPL < kTile ? kTile / RPL : 1;
+  static constexpr int BYTES = LOADS * 1024;               // of LDS (rows of 16 bytes: the second half is not used)
+  static constexpr int NK = BF ? (D >= 32 ? D / 32 : 1) : (D >= 16 ? D / 16 : 1);  // 16-byte pieces of a lane's query and key rows
+  static constexpr int NV = D >= 16 ? D / 16 : 1;          // accumulators: 16 channels each
+
+  // LDS position of chunk c of row r: c ^ swz(r).  The 16 lanes that one clock of a 16-byte read serves (0-3, 12-15 of one lane
+  // group, 4-11 of the next), or the 32 of an 8-byte one, then meet every bank once.
+  static __device__ __forceinline__ int swz_k(int r)
+  {
+    if (RB >= 256) return r & 15;
+    if (RB == 128) return (r >> 1) & 7;
+    if (RB == 64) return (0x78 >> (2 * ((r >> 2) & 3))) & 3;
+    return 0;
+  }
+  static __device__ __forceinline__ int swz_v(int r)
+  {
+    if (!BF) return RB == 512 ? (r >> 2) & 1 : 0;
+    if (RB == 256) return 2 * (r & 7);
+    if (RB == 128) return 2 * ((r >> 1) & 3);
+    if (RB == 64) return 2 * ((r >> 2) & 1);
+    return 0;
+  }
+
+  // Requests loads first, first + step, .. of a tile's K and V.  Lane l < 32 knows where row l of the tile lies (`off`, bytes from
+  // either cache's beginning) and whether it is anybody's (`ok`); `whole`: all are.
+  template <bool ONCE>
+  static __device__ __forceinline__ void request(const Args &a, const char *ks, const char *vs, size_t off, bool ok, bool whole, int lane,
+                                                 int first, int step)
+  {
+    const char *Kc = static_cast<const char *>(a.K_cache), *Vc = static_cast<const char *>(a.V_cache);
+    const unsigned k_to = mfma::lds_address(ks), v_to = mfma::lds_address(vs);
+    const int l_row = lane / CH, l_pos = lane % CH;
+    const unsigned lo = (unsigned)off, hi = (unsigned)(off >> 32);
+    if (RPL <= 8 && whole) {  // (rows that start at a multiple of RPL lie in one page, one after another)
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        if (step > 1 && i % step != first) continue;
+        const int r = RPL * i + l_row;
+        const size_t base = (size_t)(unsigned)__builtin_amdgcn_readlane(hi, RPL * i & 31) << 32 | (unsigned)__builtin_amdgcn_readlane(lo, RPL * i & 31);
+        to_lds<ONCE>(Kc + base, l_row * RB + (l_pos ^ swz_k(r)) * 16, k_to + i * 1024);
+        to_lds<ONCE>(Vc + base, l_row * RB + (l_pos ^ swz_v(r)) * 16, v_to + i * 1024);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        if (step > 1 && i % step != first) continue;
+        const int r = min(RPL * i + l_row, kTile - 1);
+        const size_t mine = (size_t)(unsigned)__shfl((int)hi, r) << 32 | (unsigned)__shfl((int)lo, r);
+        const bool there = __shfl((int)ok, r) != 0;
+        to_lds<ONCE>(there ? Kc + mine + (l_pos ^ swz_k(r)) * 16 : reinterpret_cast<const char *>(kZeros), k_to + i * 1024);
+        to_lds<ONCE>(there ? Vc + mine + (l_pos ^ swz_v(r)) * 16 : reinterpret_cast<const char *>(kZeros), v_to + i * 1024);
+      }
+    }
+  }
+
+  // A row of Q as an operand: lane group c's pieces.  Channels beyond the row are zeros.
+  struct Query {
+    uint4 x[NK];
+  };
+  static __device__ __forceinline__ void load_query(Query &q, const T *p, int c)
+  {
+#pragma unroll
+    for (int i = 0; i < NK; ++i)
+      q.x[i] = (4 * i + c) * 16 < RB ? *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(p) + (4 * i + c) * 16) : make_uint4(0, 0, 0, 0);
+  }
+
+  // Logits of keys 16h .. 16h + 15 (matrix rows) with a lane's query (column n): lane group c gets those of keys 16h + 4c + i.
+  static __device__ __forceinline__ f32x4 logits(const char *ks, int h, int n, int c, const Query &q)
+  {
+    const int r = 16 * h + n;
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      uint4 k = make_uint4(0, 0, 0, 0);
+      if (CH >= 4 || c < CH) k = *reinterpret_cast<const uint4 *>(ks + r * RB + (((4 * i + c) ^ swz_k(r)) * 16));
+      if constexpr (BF) {
+        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(mfma::bf16x8, k), __builtin_bit_cast(mfma::bf16x8, q.x[i]), s, 0, 0, 0);
+      } else {
+        const f32x4 kf = __builtin_bit_cast(f32x4, k), qf = __builtin_bit_cast(f32x4, q.x[i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[e], s, 0, 0, 0);
+      }
+    }
+    return s;
+  }
+
+  // acc += V^T P^T: p[4h + i] is the probability of key 16h + 4c + i.  The sum over keys may run in any order, so lane group c takes
+  // the keys whose probabilities it holds.  bf16: P is rounded as the matrix instruction wants it (its sum is of the unrounded ones),
+  // V^T comes through the transposing LDS read.  Accumulator j, element i holds channel channel(j, c, i) of the lane's query.
+  static __device__ __forceinline__ void product(const char *vs, const float (&p)[8], int lane, f32x4 (&acc)[NV])
+  {
+    const int n = lane & 15, c = lane >> 4;
+    if constexpr (BF) {
+      mfma::bf16x8 pf;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) pf[i] = (__bf16)p[i];
+      const int r = 4 * c + (n >> 2);  // (and 16 on: the same swizzle)
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int ch = CH >= 2 ? 2 * j + ((n >> 1) & 1) : 0;
+        const char *v = vs + r * RB + ((ch ^ swz_v(r)) * 16) + (n & 1) * 8;
+        const mfma::s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((mfma::lds_s16x4 *)(v));
+        const mfma::s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((mfma::lds_s16x4 *)(v + 16 * RB));
+        const mfma::bf16x8 vt = __builtin_bit_cast(mfma::bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pf, acc[j], 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        const int r = 16 * (s >> 2) + 4 * c + (s & 3);
+        const char *row = vs + r * RB;
+        float v[NV];
+        if constexpr (NV >= 4) {
+#pragma unroll
+          for (int e = 0; e < NV; e += 4) {
+            const float4 x = *reinterpret_cast<const float4 *>(row + (((NV * n + e) / 4) ^ swz_v(r)) * 16);
+            v[e] = x.x; v[e + 1] = x.y; v[e + 2] = x.z; v[e + 3] = x.w;
+          }
+        } else if constexpr (NV == 2) {
+          const float2 x = *reinterpret_cast<const float2 *>(row + n * 8);
+          v[0] = x.x; v[1] = x.y;
+        } else {
+          v[0] = *reinterpret_cast<const float *>(row + (D == 8 ? n & 7 : n) * 4);
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j], p[s], acc[j], 0, 0, 0);
+      }
+    }
+  }
+  // (d = 8: channels 8 .. 15 repeat 0 .. 7 and are dropped)
+  static __device__ __forceinline__ int channel(int j, int c, int i) { return BF ? 16 * j + 4 * c + i : NV * (4 * c + i) + j; }
+};
+
+// Maximum over the four lanes that hold a row's logits.
+__device__ __forceinline__ float row_max(float x)
+{
+  typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+  const u32x2 a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const u32x2 b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// A wavefront's 16 rows over the tiles it has met: running maximum (log2 units) and sum in fp32, unnormalised output.
+template <typename T, int D>
+struct Rows {
+  typedef Tile<T, D> TL;
+  f32x4 acc[TL::NV];
+  float m, l;  // (l: this lane's keys alone)
+  __device__ __forceinline__ void clear()
+  {
+    m = mfma::kNegInf;
+    l = 0.0f;
+#pragma unroll
+    for (int j = 0; j < TL::NV; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  // one tile; bit k of `seen`: this lane's row sees key k of the tile (all: no key is masked for any row)
+  __device__ __forceinline__ void attend(const char *ks, const char *vs, const typename TL::Query &q, float scale2, unsigned seen, bool all, int lane)
+  {
+    const int n = lane & 15, c = lane >> 4;
+    float p[8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const f32x4 s = TL::logits(ks, h, n, c, q);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[4 * h + i] = s[i] * scale2;
+    }
+    if (!all) {
+      const int mine = (int)(seen >> (4 * c));
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[4 * h + i] = mine >> (16 * h + i) & 1 ? p[4 * h + i] : mfma::kNegInf;
+    }
+    float mx = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
+    mx = fmaxf(m, row_max(mx));
+    const float ref = mx == mfma::kNegInf ? 0.0f : mx;  // no key seen yet: every exponential is 0
+    const float f = __builtin_amdgcn_exp2f(m - ref);
+    m = mx;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      p[i] = __builtin_amdgcn_exp2f(p[i] - ref);
+      sum += p[i];
+    }
+    l = l * f + sum;
+#pragma unroll
+    for (int j = 0; j < TL::NV; ++j) acc[j] *= f;
+    TL::product(vs, p, lane, acc);
+  }
+  __device__ __forceinline__ float total() const
+  {
+    float x = l + __shfl_xor(l, 16);
+    return x + __shfl_xor(x, 32);
+  }
+};
+
+}  // namespace paged
+}  // namespace blossom
