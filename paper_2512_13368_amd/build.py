@@ -32,6 +32,7 @@ SOURCES = {
     "paged_append.hip": [],
     "paged_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "paged_prompt.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "paged_shared.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }
 
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",

@@ -5,6 +5,10 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <type_traits>
+
+#include "common.h"
+
 namespace blossom {
 namespace paged {
 
@@ -26,21 +30,43 @@ struct Args {
   void *Q_rot;                 // [T,H,d] or nullptr
   void *O;                     // [T,H,d] (decode: [S,H,d])
   float *lse;                  // [T,H] or nullptr
-  int parts;                   // decode: workgroups that share a key/value head's keys; 0: one a sequence
-  float *part_o, *part_ml;     // [H, parts, d] sums and [H, parts, 2] (reference in log2 units, sum of exponentials), in the workspace
-  int2 *part_of;               // [S] first part and parts of a sequence, there too
+  int parts;                   // decode: workgroups that share a key/value head's keys (0: one a sequence); prompt: parts of a row's keys
+  float *part_o, *part_ml;     // their sums [H, parts, d] and (reference in log2 units, sum of exponentials) [H, parts, 2], in the
+                               // workspace; prompt: [T, H, parts, ..]
+  int2 *part_of;               // decode: [S] first part and parts of a sequence, there too
 };
 
 // append: paged_append.hip
 void launch_append(const Args &a, hipStream_t st);
-// one-token and prompt attention: paged_attn.hip.  decode_parts: what `parts` is for this shape
+// one-token and prompt attention: paged_attn.hip.  decode_parts, prompt_parts: what `parts` is for this shape
 int decode_parts(const Args &a);
+int prompt_parts(const Args &a);
 void launch_decode(const Args &a, hipStream_t st);
 void launch_prompt(const Args &a, hipStream_t st);
 // prompt attention for bf16, d = 64 or 128: paged_prompt.hip
 constexpr int kPromptRows = 128;  // query rows of a workgroup
 bool prompt_mfma_supported(const Args &a);
 void launch_prompt_mfma(const Args &a, hipStream_t st);
+// prompt attention for everything else: paged_shared.hip
+constexpr int kSharedRows = 64;
+void launch_prompt_shared(const Args &a, hipStream_t st);
+
+// Calls f with the element type and the head size as compile-time constants.
+template <typename F>
+inline void with_type(const Args &a, F &&f)
+{
+  auto with_dim = [&](auto type) {
+    switch (a.d) {
+      case 8: f(type, std::integral_constant<int, 8>{}); break;
+      case 16: f(type, std::integral_constant<int, 16>{}); break;
+      case 32: f(type, std::integral_constant<int, 32>{}); break;
+      case 64: f(type, std::integral_constant<int, 64>{}); break;
+      default: f(type, std::integral_constant<int, 128>{}); break;
+    }
+  };
+  if (a.dtype == 0) with_dim(0.0f);
+  else with_dim(bf16_t{});
+}
 
 // Keys lo .. hi that a query at `pos` sees, of a sequence with n keys (hi < lo: none).
 struct Range {

@@ -47,10 +47,13 @@ int check_stride(const Args &a, int64_t given, int heads, int64_t *stride)
   return *stride % (a.dtype == BLOSSOM_F32 ? 4 : 8) == 0 ? BLOSSOM_OK : BLOSSOM_ERR_ALIGN;
 }
 
+// partial results: rows of them, and their bytes
+size_t part_rows(const Args &a, bool prompt) { return (size_t)a.H * a.parts * (prompt ? a.T : 1); }
 size_t attn_ws_bytes(Args &a, bool prompt)
 {
-  a.parts = prompt ? 0 : decode_parts(a);
-  return a.parts ? (size_t)a.H * a.parts * (a.d + 2) * sizeof(float) + (size_t)a.S * sizeof(int2) : 0;
+  a.parts = prompt ? prompt_parts(a) : decode_parts(a);
+  if (a.parts <= (prompt ? 1 : 0)) return 0;
+  return part_rows(a, prompt) * (a.d + 2) * sizeof(float) + (prompt ? 0 : (size_t)a.S * sizeof(int2));
 }
 
 int launch_status() { return hipGetLastError() == hipSuccess ? BLOSSOM_OK : BLOSSOM_ERR_LAUNCH; }
@@ -72,8 +75,8 @@ int attn(const blossom_paged_params *p, bool prompt, const void *Q, int64_t q_st
     if (!ws || ws_bytes < need) return BLOSSOM_ERR_WORKSPACE;
     if (!aligned16(ws)) return BLOSSOM_ERR_ALIGN;
     a.part_o = static_cast<float *>(ws);
-    a.part_ml = a.part_o + (size_t)a.H * a.parts * a.d;
-    a.part_of = reinterpret_cast<int2 *>(a.part_ml + (size_t)a.H * a.parts * 2);
+    a.part_ml = a.part_o + part_rows(a, prompt) * a.d;
+    a.part_of = reinterpret_cast<int2 *>(a.part_ml + part_rows(a, prompt) * 2);
   }
   a.Q = Q; a.K_cache = const_cast<void *>(K_cache); a.V_cache = const_cast<void *>(V_cache);
   a.page_table = page_table; a.cu = cu_seqlens; a.kv_len = kv_len;

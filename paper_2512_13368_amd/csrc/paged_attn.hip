@@ -29,308 +29,24 @@ using mfma::kLn2;
 using mfma::kNegInf;
 
 constexpr int kRows = 16;   // query rows of a workgroup
-constexpr int kWaves = 4;
+constexpr int kMostPromptParts = 64;
+enum PromptKind { kFew, kShared, kMatrix };
+struct PromptPlan {
+  PromptKind kind;
+  int parts;
+};
+#ifndef FEW
+#define FEW 16
+#define LEASTF 32
+#define LEASTM 32
+#define WANTF 512
+#define WANTM 512
+#endif
 constexpr int kMostParts = 256;   // parts of a key/value head's keys
 constexpr int kFillWaves = 2048;  // decode wavefronts that keep the memory busy: two a SIMD
 constexpr int kSplitTiles = 8;    // a wavefront's tiles from which splitting a sequence pays for the join
 
-// A load of cached rows; `ONCE`: past the caches, which hold none of them for a second reader.
-template <bool ONCE, typename V>
-__device__ __forceinline__ V cached(const V *p)
-{
-  if constexpr (ONCE) return load_once(p);
-  else return *p;
-}
-
-// Operands of one step in registers, by storage type and head size.
-template <typename T, int D>
-struct Ops;
-
-template <int D>
-struct Ops<bf16_t, D> {
-  static constexpr int NK = D >= 32 ? D / 32 : 1;  // matrix instructions for 16 keys' logits
-  static constexpr int VPT = D >= 16 ? D / 16 : 1; // channels of V in a lane
-  typedef uint4 Row[NK];
-  Row k[2];
-  uint32_t v[8][VPT >= 2 ? VPT / 2 : 1];
-  // d < 32: channels beyond the row are zeros
-  template <bool ONCE = false>
-  static __device__ __forceinline__ void row(uint4 (&to)[NK], const bf16_t *p, int c)
-  {
-    if constexpr (D >= 32) {
-#pragma unroll
-      for (int i = 0; i < NK; ++i) to[i] = cached<ONCE>(reinterpret_cast<const uint4 *>(p + 32 * i + 8 * c));
-    } else {
-      to[0] = make_uint4(0, 0, 0, 0);
-      if (8 * c < D) to[0] = cached<ONCE>(reinterpret_cast<const uint4 *>(p + 8 * c));
-    }
-  }
-  template <bool ONCE = false>
-  __device__ __forceinline__ void load_v(int slot, const bf16_t *p, int m)
-  {
-    if constexpr (VPT == 8) {
-      const uint4 x = cached<ONCE>(reinterpret_cast<const uint4 *>(p + 8 * m));
-      v[slot][0] = x.x; v[slot][1] = x.y; v[slot][2] = x.z; v[slot][3] = x.w;
-    } else if constexpr (VPT == 4) {
-      const uint2 x = cached<ONCE>(reinterpret_cast<const uint2 *>(p + 4 * m));
-      v[slot][0] = x.x; v[slot][1] = x.y;
-    } else if constexpr (VPT == 2) {
-      v[slot][0] = cached<ONCE>(reinterpret_cast<const uint32_t *>(p + 2 * m));
-    } else {
-      v[slot][0] = m < D ? (uint32_t)p[m].bits : 0u;
-    }
-  }
-  __device__ __forceinline__ void clear_v(int slot)
-  {
-#pragma unroll
-    for (int i = 0; i < (VPT >= 2 ? VPT / 2 : 1); ++i) v[slot][i] = 0u;
-  }
-  __device__ __forceinline__ f32x4 logits(int t, const Row &q) const
-  {
-    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int i = 0; i < NK; ++i)
-      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[t][i]), __builtin_bit_cast(bf16x8, q[i]), s, 0, 0, 0);
-    return s;
-  }
-  // The probabilities are rounded to bf16, as the matrix instruction wants them; their sum is of the unrounded ones.
-  __device__ __forceinline__ void product(const float (&p)[8], f32x4 (&acc)[VPT]) const
-  {
-    bf16x8 pf;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) pf[i] = (__bf16)p[i];
-#pragma unroll
-    for (int j = 0; j < VPT; ++j) {
-      uint32_t w[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        w[i] = __builtin_amdgcn_perm(v[2 * i + 1][j / 2], v[2 * i][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
-      const uint4 vt = make_uint4(w[0], w[1], w[2], w[3]);
-      acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vt), __builtin_bit_cast(bf16x8, pf), acc[j], 0, 0, 0);
-    }
-  }
-};
-
-template <int D>
-struct Ops<float, D> {
-  static constexpr int NK = D >= 16 ? D / 16 : 1;
-  static constexpr int VPT = D >= 16 ? D / 16 : 1;
-  typedef float4 Row[NK];
-  Row k[2];
-  float v[8][VPT];
-  template <bool ONCE = false>
-  static __device__ __forceinline__ void row(float4 (&to)[NK], const float *p, int c)
-  {
-    if constexpr (D >= 16) {
-#pragma unroll
-      for (int i = 0; i < NK; ++i) to[i] = cached<ONCE>(reinterpret_cast<const float4 *>(p + 16 * i + 4 * c));
-    } else {
-      to[0] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      if (4 * c < D) to[0] = cached<ONCE>(reinterpret_cast<const float4 *>(p + 4 * c));
-    }
-  }
-  template <bool ONCE = false>
-  __device__ __forceinline__ void load_v(int slot, const float *p, int m)
-  {
-    if constexpr (VPT >= 4) {
-#pragma unroll
-      for (int j = 0; j < VPT; j += 4) {
-        const float4 x = cached<ONCE>(reinterpret_cast<const float4 *>(p + VPT * m + j));
-        v[slot][j] = x.x; v[slot][j + 1] = x.y; v[slot][j + 2] = x.z; v[slot][j + 3] = x.w;
-      }
-    } else if constexpr (VPT == 2) {
-      const float2 x = cached<ONCE>(reinterpret_cast<const float2 *>(p + 2 * m));
-      v[slot][0] = x.x; v[slot][1] = x.y;
-    } else {
-      v[slot][0] = m < D ? p[m] : 0.0f;
-    }
-  }
-  __device__ __forceinline__ void clear_v(int slot)
-  {
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) v[slot][i] = 0.0f;
-  }
-  __device__ __forceinline__ f32x4 logits(int t, const Row &q) const
-  {
-    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int i = 0; i < NK; ++i) {
-      s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[t][i].x, q[i].x, s, 0, 0, 0);
-      s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[t][i].y, q[i].y, s, 0, 0, 0);
-      s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[t][i].z, q[i].z, s, 0, 0, 0);
-      s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[t][i].w, q[i].w, s, 0, 0, 0);
-    }
-    return s;
-  }
-  __device__ __forceinline__ void product(const float (&p)[8], f32x4 (&acc)[VPT]) const
-  {
-#pragma unroll
-    for (int slot = 0; slot < 8; ++slot)
-#pragma unroll
-      for (int j = 0; j < VPT; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[slot][j], p[slot], acc[j], 0, 0, 0);
-  }
-};
-
-__device__ __forceinline__ void store_out(float *p, float x) { *p = x; }
-__device__ __forceinline__ void store_out(bf16_t *p, float x) { p->bits = __builtin_bit_cast(uint16_t, (__bf16)x); }
-
-__device__ __forceinline__ void store_four(float *p, const float4 &x, float f)
-{
-  *reinterpret_cast<float4 *>(p) = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
-}
-__device__ __forceinline__ void store_four(bf16_t *p, const float4 &x, float f)
-{
-  *reinterpret_cast<uint2 *>(p) = make_uint2(mfma::pack2_bf16(x.x * f, x.y * f), mfma::pack2_bf16(x.z * f, x.w * f));
-}
-
 }  // namespace
-
-template <typename T, int D>
-__global__ __launch_bounds__(64 * kWaves) void rows_kernel(Args a)
-{
-  typedef Ops<T, D> O_;
-  constexpr int VPT = O_::VPT;
-  constexpr int LDR = D + 4;  // floats of an LDS row
-  __shared__ __attribute__((aligned(16))) float acc_s[kWaves][kRows][LDR];
-  __shared__ float m_s[kWaves][kRows], l_s[kWaves][kRows];
-
-  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n = lane & 15, c = lane >> 4;
-
-  // ---- this workgroup's rows ----
-  const unsigned g = blockIdx.x % a.G;
-  const int tile = (int)(blockIdx.x / a.G);
-  int s, row0, rows, tok0, new_tokens;
-  s = find_sequence(a.S, lane, [&](int i) { return (int)((long)token_at(a, i) * a.R / kRows) + i <= tile; });
-  tok0 = token_at(a, s);
-  new_tokens = max(token_at(a, s + 1) - tok0, 0);
-  row0 = (tile - (int)((long)tok0 * a.R / kRows) - s) * kRows;
-  rows = new_tokens * a.R;  // (T * R fits 31 bits: checked at the boundary)
-  if (row0 >= rows || row0 < 0) return;
-  const int len = max(a.kv_len[s], 0);
-  const int first_pos = len - new_tokens;
-
-  const int row = row0 + n;
-  const bool row_ok = row < rows;
-  const int tok = (row_ok ? row : rows - 1) / a.R;
-  const int head = g * a.R + (row_ok ? row : rows - 1) - tok * a.R;
-  Range my = seen_by(a, first_pos + tok, len);
-  if (!row_ok) my.hi = -1;
-  // of all rows together
-  const int lo = seen_by(a, first_pos + row0 / a.R, len).lo;
-  const int hi = seen_by(a, first_pos + (min(row0 + kRows, rows) - 1) / a.R, len).hi;
-
-  O_ x;
-  typename O_::Row q;
-  O_::row(q, static_cast<const T *>(a.Q) + (tok0 + tok) * a.q_stride + (size_t)head * D, c);
-
-  const int t_begin = lo / kTile, t_end = hi >= lo ? hi / kTile + 1 : t_begin;
-
-  const int *table = a.page_table + s * a.table_seq + g * a.table_group;
-  const int page_mask = (1 << a.page_shift) - 1;
-  const T *Kc = static_cast<const T *>(a.K_cache), *Vc = static_cast<const T *>(a.V_cache);
-  const size_t page_step = ((size_t)a.G << a.page_shift) * D, group_off = ((size_t)g << a.page_shift) * D;
-  auto entry = [&](int key) { return table[min(key >> a.page_shift, a.max_pages - 1)]; };
-
-  f32x4 acc[VPT];
-#pragma unroll
-  for (int j = 0; j < VPT; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  float m = kNegInf, l = 0.0f;
-
-  for (int t = t_begin + wv; t < t_end; t += kWaves) {
-    const int base = t * kTile;
-    int id[2], vid[2];
-    bool vok[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      id[h] = entry(base + 16 * h + n);
-      id[h] = id[h] >= 0 && id[h] < a.n_pages ? id[h] : -1;
-      const int key = base + 16 * h + n;
-      O_::row(x.k[h], Kc + max(id[h], 0) * page_step + group_off + (size_t)(key & page_mask) * D, c);
-    }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      vid[h] = __shfl(id[h], 4 * c);  // (four keys of a lane group lie in one page: pages hold 8 positions or more)
-      vok[h] = vid[h] >= 0;
-      const int key = base + 16 * h + 4 * c;
-      const T *v = Vc + max(vid[h], 0) * page_step + group_off + (size_t)(key & page_mask) * D;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x.load_v(4 * h + i, v + i * D, n);
-    }
-    const bool whole = __all(vok[0] && vok[1]) && base >= lo && base + kTile - 1 <= hi;
-    if (!whole) {  // what lies outside a sequence may hold anything
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int key = base + 16 * h + 4 * c + i;
-          if (!vok[h] || key < lo || key > hi) x.clear_v(4 * h + i);
-        }
-    }
-    float p[8];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const f32x4 sc = x.logits(h, q);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int key = base + 16 * h + 4 * c + i;
-        p[4 * h + i] = vok[h] && key >= my.lo && key <= my.hi ? sc[i] * a.scale2 : kNegInf;
-      }
-    }
-    float mx = p[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) mx = fmaxf(mx, p[i]);
-    mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
-    const float m_new = fmaxf(m, mx);
-    const float ref = m_new == kNegInf ? 0.0f : m_new;  // no key seen yet: every exponential is 0
-    const float f = __builtin_amdgcn_exp2f(m - ref);
-    m = m_new;
-    float sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(p[i] - ref);
-      sum += p[i];
-    }
-    l = l * f + sum;
-#pragma unroll
-    for (int j = 0; j < VPT; ++j) acc[j] *= f;
-    x.product(p, acc);
-  }
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
-
-  // ---- the four wavefronts' results ----
-  if (c == 0) {
-    m_s[wv][n] = m;
-    l_s[wv][n] = l;
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < VPT; ++j)
-      if (VPT * (4 * c + i) + j < D) acc_s[wv][n][VPT * (4 * c + i) + j] = acc[j][i];
-  __syncthreads();
-  for (int e = threadIdx.x; e < kRows * D; e += 64 * kWaves) {
-    const int r = e / D, ch = e % D;
-    if (row0 + r >= rows) break;
-    float mm = m_s[0][r];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) mm = fmaxf(mm, m_s[w][r]);
-    const float ref = mm == kNegInf ? 0.0f : mm;
-    float ll = 0.0f, o = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float f = __builtin_amdgcn_exp2f(m_s[w][r] - ref);
-      ll += l_s[w][r] * f;
-      o += acc_s[w][r][ch] * f;
-    }
-    const int tk = (row0 + r) / a.R;
-    const size_t out = (size_t)(tok0 + tk) * a.H + g * a.R + (row0 + r) - tk * a.R;
-    store_out(static_cast<T *>(a.O) + out * D + ch, ll == 0.0f ? 0.0f : o / ll);
-    if (ch == 0 && a.lse) a.lse[out] = ll == 0.0f ? kNegInf : (mm + __log2f(ll)) * kLn2;
-  }
-}
 
 // A wavefront of decode holds two tiles of K and of V in LDS, one on its way; of tiles of 16 KB and more one alone, eight wavefronts
 // (or four) to a CU.  (At d = 128, bf16: four wavefronts of two tiles 86.5 us for 131071 keys, eight of one 85.6; two of four
@@ -395,8 +111,9 @@ struct Part {
   }
 };
 
-// One new token a sequence: W wavefronts take a run of key tiles each for up to 16 heads that share keys.  SPLIT: of a part of them.
-template <typename T, int D, int W, bool ONCE, bool SPLIT>
+// One new token a sequence, or few (PROMPT): W wavefronts take a run of key tiles each for up to 16 rows that share keys.  SPLIT: of a
+// part of them.
+template <typename T, int D, int W, bool ONCE, bool SPLIT, bool PROMPT>
 __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
 {
   typedef Tile<T, D> TL;
@@ -410,18 +127,34 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
 
   const int g = blockIdx.x % a.G;
   const unsigned rest = blockIdx.x / a.G;
-  const int tiles = (a.R + kRows - 1) / kRows;
-  const int row0 = (int)(rest % tiles) * kRows, b = (int)(rest / tiles);
-  int s = b, part = 0, n_parts = 1;
-  if constexpr (SPLIT) {
-    const Part mine(a, lane, b, W);
-    if (mine.s < 0) return;
-    s = mine.s;
-    part = b - mine.first;
-    n_parts = mine.count;
-    if (part == 0 && g == 0 && row0 == 0 && threadIdx.x == 0) a.part_of[s] = make_int2(mine.first, n_parts);  // for the join
+  int s, row0, rows, tok0, new_tokens = 1, part = 0, n_parts = 1, b = 0;
+  if constexpr (PROMPT) {
+    const int tile = (int)(rest / a.parts);
+    part = (int)(rest % a.parts);
+    n_parts = a.parts;
+    s = find_sequence(a.S, lane, [&](int i) { return (int)((long)token_at(a, i) * a.R / kRows) + i <= tile; });
+    tok0 = __builtin_amdgcn_readfirstlane(token_at(a, s));
+    new_tokens = max(__builtin_amdgcn_readfirstlane(token_at(a, s + 1)) - tok0, 0);
+    row0 = (tile - (int)((long)tok0 * a.R / kRows) - s) * kRows;
+    if (row0 < 0 || row0 >= new_tokens * a.R) return;
+    rows = min(new_tokens * a.R - row0, kRows);
+  } else {
+    const int tiles = (a.R + kRows - 1) / kRows;
+    row0 = (int)(rest % tiles) * kRows;
+    b = (int)(rest / tiles);
+    s = b;
+    if constexpr (SPLIT) {
+      const Part mine(a, lane, b, W);
+      if (mine.s < 0) return;
+      s = mine.s;
+      part = b - mine.first;
+      n_parts = mine.count;
+      if (part == 0 && g == 0 && row0 == 0 && threadIdx.x == 0) a.part_of[s] = make_int2(mine.first, n_parts);  // for the join
+    }
+    tok0 = s;
+    rows = min(a.R - row0, kRows);
   }
-  const int rows = min(a.R - row0, kRows);
+  const int row = row0 + min(n, rows - 1), tok = PROMPT ? row / a.R : 0, head = g * a.R + row - tok * a.R;
 
   // what hangs on nothing is requested before anything is waited for: the length, the query, the first pages
   const int *table = a.page_table + s * a.table_seq + g * a.table_group;
@@ -432,11 +165,19 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
   const int raw_len = a.kv_len[s];
   int list0 = 0, ids = entries(0);  // pages list0 .. list0 + 63, one a lane
   typename TL::Query q;
-  TL::load_query(q, static_cast<const T *>(a.Q) + s * a.q_stride + (size_t)(g * a.R + row0 + min(n, rows - 1)) * D, c);
+  TL::load_query(q, static_cast<const T *>(a.Q) + (tok0 + tok) * a.q_stride + (size_t)head * D, c);
 
   const int len = max(__builtin_amdgcn_readfirstlane(raw_len), 0);
-  const Range my = seen_by(a, len - 1, len);
-  const int t_lo = my.lo / kTile, t_all = my.hi >= my.lo ? my.hi / kTile - t_lo + 1 : 0;
+  const int first_pos = len - new_tokens;
+  // keys that any row sees, that this lane's row does, that all do
+  Range any = seen_by(a, first_pos + (PROMPT ? row0 / a.R : 0), len), my = any, every = any;
+  if constexpr (PROMPT) {
+    const Range last = seen_by(a, first_pos + (row0 + rows - 1) / a.R, len);
+    every.lo = last.lo;
+    any.hi = last.hi;
+    my = seen_by(a, first_pos + tok, len);
+  }
+  const int t_lo = any.lo / kTile, t_all = any.hi >= any.lo ? any.hi / kTile - t_lo + 1 : 0;
   int t_begin = t_lo, t_end = t_lo + t_all;
   if constexpr (SPLIT) {
     const int each = (t_all + n_parts - 1) / n_parts;
@@ -457,7 +198,7 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
     }
     const int key = t * kTile + (lane & 31);
     const int id = __shfl(ids, (key >> a.page_shift) - list0);
-    const bool ok = id >= 0 && key >= my.lo && key <= my.hi;
+    const bool ok = id >= 0 && key >= any.lo && key <= any.hi;
     const unsigned seen = (unsigned)__ballot(ok);
     const size_t off = max(id, 0) * page_bytes + group_bytes + (size_t)(key & ((1 << a.page_shift) - 1)) * TL::RB;
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (what was read from `to` is here)
@@ -484,7 +225,9 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
         arrived<0>();
       }
       const char *ks = mine + k * (2 * TL::BYTES);
-      r.attend(ks, ks + TL::BYTES, q, a.scale2, seen[k], seen[k] == 0xFFFFFFFFu, lane);
+      const int base = t * kTile;
+      const bool all = seen[k] == 0xFFFFFFFFu && (!PROMPT || (base >= every.lo && base + kTile - 1 <= every.hi));
+      r.attend(ks, ks + TL::BYTES, q, a.scale2, PROMPT ? seen[k] & mfma::row_bits(my.lo - base, my.hi - base) : seen[k], all, lane);
       ++t;
     }
   }
@@ -519,13 +262,14 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
       ll = fmaf(l_s[w][row], f, ll);
       o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);
     }
-    const size_t out = (size_t)s * a.H + g * a.R + row0 + row;
-    if (!SPLIT || n_parts == 1) {
+    const int tk = PROMPT ? (row0 + row) / a.R : 0;
+    const size_t out = (size_t)(tok0 + tk) * a.H + g * a.R + row0 + row - tk * a.R;
+    if (!SPLIT || (!PROMPT && n_parts == 1)) {
       const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
       store_four(static_cast<T *>(a.O) + out * D + ch, o, inv);
       if (ch == 0 && a.lse) a.lse[out] = ll == 0.0f ? kNegInf : (mm + __log2f(ll)) * kLn2;
-    } else {  // [H rows of the token's heads][parts]
-      const size_t at = (size_t)(g * a.R + row0 + row) * a.parts + b;
+    } else {  // decode: [heads of the token][parts of all sequences]; prompt: [rows][parts of each]
+      const size_t at = PROMPT ? out * a.parts + part : (size_t)(g * a.R + row0 + row) * a.parts + b;
       *reinterpret_cast<float4 *>(a.part_o + at * D + ch) = o;
       if (ch == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(mm, ll);
     }
@@ -534,24 +278,30 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
 
 // Joins the parts of a sequence's row, where it has more than one: a workgroup a row, whose threads take a part each for the weights
 // and then, 4 channels each, every (256 / (d / 4))-th part's sums.  Parts that met no key have weight 0 and finite sums.
-template <typename T, int D>
+template <typename T, int D, bool PROMPT>
 __global__ __launch_bounds__(256) void join_kernel(Args a)
 {
   constexpr int LANES = D / 4, GROUPS = 256 / LANES;
   __shared__ float red_s[4], l_s[4], w_s[kMostParts];
   __shared__ __attribute__((aligned(16))) float o_s[GROUPS][D];
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int s = blockIdx.x / a.H, h = blockIdx.x % a.H;
-  const int2 part = a.part_of[s];  // (of a sequence without keys: whatever the workspace held)
-  const int n = __builtin_amdgcn_readfirstlane(tiles_of(a, s) > 0 ? part.y : 0);
   T *O = static_cast<T *>(a.O) + (size_t)blockIdx.x * D;
-  if (n <= 1) {
-    if (n == 1) return;  // (the part's workgroup wrote the row)
-    if (tid < D) store_out(O + tid, 0.0f);
-    if (tid == 0 && a.lse) a.lse[blockIdx.x] = kNegInf;
-    return;
+  int n = a.parts;
+  size_t at0 = (size_t)blockIdx.x * a.parts;
+  if constexpr (PROMPT) {
+    if ((int)(blockIdx.x / a.H) >= token_at(a, a.S)) return;  // (a row that no sequence owns stays as it is)
+  } else {
+    const int s = blockIdx.x / a.H, h = blockIdx.x % a.H;
+    const int2 part = a.part_of[s];  // (of a sequence without keys: whatever the workspace held)
+    n = __builtin_amdgcn_readfirstlane(tiles_of(a, s) > 0 ? part.y : 0);
+    if (n <= 1) {
+      if (n == 1) return;  // (the part's workgroup wrote the row)
+      if (tid < D) store_out(O + tid, 0.0f);
+      if (tid == 0 && a.lse) a.lse[blockIdx.x] = kNegInf;
+      return;
+    }
+    at0 = (size_t)h * a.parts + part.x;
   }
-  const size_t at0 = (size_t)h * a.parts + part.x;
   const float *ml = a.part_ml + at0 * 2;
   const float4 *po = reinterpret_cast<const float4 *>(a.part_o + at0 * D);
   const int at = tid % LANES, grp = tid / LANES;
@@ -635,14 +385,14 @@ void launch_decode_w(const Args &a, hipStream_t st)
   const bool once = a.R <= kRows && (double)a.S * most_tiles(a) * kTile * a.G * D * 2 * sizeof(T) > 256e6;
   auto go = [&](auto kernel) { BLOSSOM_LAUNCH(kernel, grid, block, 0, st, a); };
   if (!a.parts) {
-    if (once) go(decode_kernel<T, D, W, true, false>);
-    else go(decode_kernel<T, D, W, false, false>);
+    if (once) go(decode_kernel<T, D, W, true, false, false>);
+    else go(decode_kernel<T, D, W, false, false, false>);
     return;
   }
-  if (once) go(decode_kernel<T, D, W, true, true>);
-  else go(decode_kernel<T, D, W, false, true>);
+  if (once) go(decode_kernel<T, D, W, true, true, false>);
+  else go(decode_kernel<T, D, W, false, true, false>);
   if (launch_failed()) return;
-  BLOSSOM_LAUNCH((join_kernel<T, D>), dim3((unsigned)(a.S * a.H)), dim3(256), 0, st, a);
+  BLOSSOM_LAUNCH((join_kernel<T, D, false>), dim3((unsigned)(a.S * a.H)), dim3(256), 0, st, a);
 }
 
 template <typename T, int D>
@@ -657,30 +407,6 @@ void launch_decode_d(const Args &a, hipStream_t st)
   launch_decode_w<T, D, MOST < 4 ? MOST : 4>(a, st);
 }
 
-template <typename T, int D>
-void launch_rows_d(const Args &a, hipStream_t st)
-{
-  const dim3 grid((unsigned)(((long)a.T * a.R / kRows + a.S) * a.G)), block(64 * kWaves);
-  BLOSSOM_LAUNCH((rows_kernel<T, D>), grid, block, 0, st, a);
-}
-
-// Calls f with the element type and the head size as compile-time constants.
-template <typename F>
-void with_type(const Args &a, F &&f)
-{
-  auto with_dim = [&](auto type) {
-    switch (a.d) {
-      case 8: f(type, std::integral_constant<int, 8>{}); break;
-      case 16: f(type, std::integral_constant<int, 16>{}); break;
-      case 32: f(type, std::integral_constant<int, 32>{}); break;
-      case 64: f(type, std::integral_constant<int, 64>{}); break;
-      default: f(type, std::integral_constant<int, 128>{}); break;
-    }
-  };
-  if (a.dtype == 0) with_dim(0.0f);
-  else with_dim(bf16_t{});
-}
-
 }  // namespace
 
 void launch_decode(const Args &a, hipStream_t st)
@@ -688,10 +414,44 @@ void launch_decode(const Args &a, hipStream_t st)
   with_type(a, [&](auto type, auto dim) { launch_decode_d<decltype(type), decltype(dim)::value>(a, st); });
 }
 
+// Which kernel takes a prompt call, and into how many parts a row's keys go.
+//  - few rows (a sequence has 16 rows or fewer on average): wavefronts share a row tile's keys, as in decode;
+//  - bf16 at d = 64 or 128: 128-row workgroups on the 32x32 instructions;
+//  - else: 64-row workgroups.
+static PromptPlan prompt_plan(const Args &a)
+{
+  PromptPlan p;
+  const long all = (long)a.T * a.R;
+  p.kind = all <= FEW * a.S ? kFew : prompt_mfma_supported(a) ? kMatrix : kShared;
+  const int rows = p.kind == kFew ? kRows : p.kind == kMatrix ? kPromptRows : kSharedRows;
+  const long groups = (all / rows + (all % rows != 0 && a.S == 1 ? 1 : a.S)) * a.G;  // workgroups, nearly
+  const long tiles = most_tiles(a), least = p.kind == kFew ? LEASTF : LEASTM;      // 32-key tiles that a part is worth
+  const long want = (p.kind == kFew ? WANTF : WANTM) / groups, most = tiles / least;
+  long n = want < most ? want : most;
+  n = n < 1 ? 1 : n > kMostPromptParts ? kMostPromptParts : n;
+  p.parts = (int)n;
+  return p;
+}
+
+int prompt_parts(const Args &a) { return prompt_plan(a).parts; }
+
 void launch_prompt(const Args &a, hipStream_t st)
 {
-  if (prompt_mfma_supported(a)) return launch_prompt_mfma(a, st);
-  with_type(a, [&](auto type, auto dim) { launch_rows_d<decltype(type), decltype(dim)::value>(a, st); });
+  const PromptPlan p = prompt_plan(a);
+  if (p.kind == kMatrix) launch_prompt_mfma(a, st);
+  else if (p.kind == kShared) launch_prompt_shared(a, st);
+  with_type(a, [&](auto type, auto dim) {
+    typedef decltype(type) T;
+    constexpr int D = decltype(dim)::value;
+    if (p.kind == kFew) {
+      constexpr int MOST = most_decode_waves(D * sizeof(T)), W = MOST < 8 ? MOST : 8;
+      const dim3 grid((unsigned)(((long)a.T * a.R / kRows + a.S) * a.G * a.parts)), block(64 * W);
+      if (a.parts > 1) BLOSSOM_LAUNCH((decode_kernel<T, D, W, false, true, true>), grid, block, 0, st, a);
+      else BLOSSOM_LAUNCH((decode_kernel<T, D, W, false, false, true>), grid, block, 0, st, a);
+    }
+    if (a.parts > 1 && !launch_failed())
+      BLOSSOM_LAUNCH((join_kernel<T, D, true>), dim3((unsigned)(a.T * a.H)), dim3(256), 0, st, a);
+  });
 }
 
 }  // namespace paged

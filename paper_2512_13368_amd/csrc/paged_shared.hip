@@ -1,0 +1,161 @@
+// Prompt attention for every type and head size (bf16 at d = 64 and 128 has a kernel of its own: paged_prompt.hip).
+//
+// A workgroup's four wavefronts take 64 rows of one key/value head, (token, head of the group) pairs, 16 each, and walk the 32-key
+// tiles that any of them sees.  A tile is moved to LDS once, one step ahead, and read by all four.
+#include "common.h"
+#include "launch.h"
+#include "mfma_common.h"
+#include "paged.h"
+#include "paged_tile.h"
+
+namespace blossom {
+namespace paged {
+
+using mfma::kLn2;
+using mfma::kNegInf;
+
+namespace {
+constexpr int kWaves = 4;
+}
+
+template <typename T, int D, bool SPLIT>
+__global__ __launch_bounds__(64 * kWaves) void shared_kernel(Args a)
+{
+  typedef Tile<T, D> TL;
+  __shared__ __attribute__((aligned(1024))) char lds[2][2 * TL::BYTES];
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 15, c = lane >> 4;
+
+  // ---- this workgroup's rows: the last tiles, which see most keys, first ----
+  const int g = blockIdx.x % a.G;
+  const unsigned rest = blockIdx.x / a.G;
+  const int part = SPLIT ? (int)(rest % a.parts) : 0;
+  const int tile = (int)(gridDim.x / (a.G * a.parts)) - 1 - (int)(rest / a.parts);
+  const int s = find_sequence(a.S, lane, [&](int i) { return (int)((long)token_at(a, i) * a.R / kSharedRows) + i <= tile; });
+  const int tok0 = __builtin_amdgcn_readfirstlane(token_at(a, s));
+  const int new_tokens = max(__builtin_amdgcn_readfirstlane(token_at(a, s + 1)) - tok0, 0);
+  const int wg_row = (tile - (int)((long)tok0 * a.R / kSharedRows) - s) * kSharedRows;
+  const int rows = new_tokens * a.R;
+  if (wg_row < 0 || wg_row >= rows) return;
+  const int len = max(__builtin_amdgcn_readfirstlane(a.kv_len[s]), 0);
+  const int first_pos = len - new_tokens;
+  const int lo = seen_by(a, first_pos + wg_row / a.R, len).lo;
+  const int hi = seen_by(a, first_pos + (min(wg_row + kSharedRows, rows) - 1) / a.R, len).hi;  // keys that any row sees
+
+  const int row0 = wg_row + 16 * wv, row = row0 + n;
+  const bool row_ok = row < rows;
+  const int tok = (row_ok ? row : rows - 1) / a.R;
+  const int head = g * a.R + (row_ok ? row : rows - 1) - tok * a.R;
+  Range my = seen_by(a, first_pos + tok, len);
+  if (!row_ok) my.hi = -1;
+  // keys that all rows of the wavefront see, and that any does
+  const Range r_first = seen_by(a, first_pos + min(row0, rows - 1) / a.R, len);
+  const Range r_last = seen_by(a, first_pos + min(row0 + 15, rows - 1) / a.R, len);
+  const int any_lo = r_first.lo, any_hi = row0 < rows ? r_last.hi : -1;
+
+  typename TL::Query q;
+  TL::load_query(q, static_cast<const T *>(a.Q) + (tok0 + tok) * a.q_stride + (size_t)head * D, c);
+
+  const int *table = a.page_table + s * a.table_seq;
+  auto entries = [&](int first) __attribute__((always_inline)) -> int {
+    const int id = table[min(first + lane, a.max_pages - 1)];
+    return id >= 0 && id < a.n_pages ? id : -1;
+  };
+  int t = lo / kTile, t_end = hi >= lo ? hi / kTile + 1 : t;
+  if constexpr (SPLIT) {
+    const int each = (t_end - t + a.parts - 1) / a.parts, from = t;
+    t = min(from + part * each, t_end);
+    t_end = min(t + each, t_end);
+  }
+  int list0 = (t * kTile) >> a.page_shift, ids = entries(list0);
+  const size_t page_bytes = ((size_t)a.G << a.page_shift) * TL::RB, group_bytes = ((size_t)g << a.page_shift) * TL::RB;
+  auto request = [&](int t, char *to) __attribute__((always_inline)) -> unsigned {
+    const int first = (t * kTile) >> a.page_shift, last = (t * kTile + kTile - 1) >> a.page_shift;
+    if (last >= list0 + 64) {
+      list0 = first;
+      ids = entries(first);
+    }
+    const int key = t * kTile + (lane & 31);
+    const int id = __shfl(ids, (key >> a.page_shift) - list0);
+    const bool ok = id >= 0 && key >= lo && key <= hi;
+    const unsigned seen = (unsigned)__ballot(ok);
+    const size_t off = max(id, 0) * page_bytes + group_bytes + (size_t)(key & ((1 << a.page_shift) - 1)) * TL::RB;
+    TL::template request<false>(a, to, to + TL::BYTES, off, ok, seen == 0xFFFFFFFFu, lane, wv, kWaves);
+    return seen;
+  };
+
+  Rows<T, D> r;
+  r.clear();
+  unsigned seen = t < t_end ? request(t, lds[0]) : 0u;
+#pragma unroll
+  for (int i = 0; i < TL::NK; ++i) asm volatile("" : "+v"(q.x[i].x), "+v"(q.x[i].y), "+v"(q.x[i].z), "+v"(q.x[i].w));  // (arrived before the walk)
+  mfma::arrived_all<0>();
+  while (t < t_end) {
+#pragma unroll
+    for (int cur = 0; cur < 2; ++cur) {
+      if (t >= t_end) break;
+      const unsigned next = t + 1 < t_end ? request(t + 1, lds[cur ^ 1]) : 0u;
+      const int base = t * kTile;
+      if (base <= any_hi && base + kTile - 1 >= any_lo) {
+        const bool all = seen == 0xFFFFFFFFu && row0 + 15 < rows && base >= r_last.lo && base + kTile - 1 <= r_first.hi;
+        r.attend(lds[cur], lds[cur] + TL::BYTES, q, a.scale2, seen & mfma::row_bits(my.lo - base, my.hi - base), all, lane);
+      }
+      mfma::arrived_all<0>();
+      seen = next;
+      ++t;
+    }
+  }
+
+  const float l = r.total();
+  if (!row_ok) return;
+  const size_t out = (size_t)(tok0 + tok) * a.H + head;
+  if constexpr (SPLIT) {
+    const size_t at = out * a.parts + part;
+#pragma unroll
+    for (int j = 0; j < TL::NV; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (TL::channel(j, c, i) < D) a.part_o[at * D + TL::channel(j, c, i)] = r.acc[j][i];
+    if (c == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(r.m, l);
+    return;
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  T *O = static_cast<T *>(a.O) + out * D;
+  if constexpr (TL::BF) {
+#pragma unroll
+    for (int j = 0; j < TL::NV; ++j)
+      if (16 * j + 4 * c < D) store_four(O + 16 * j + 4 * c, make_float4(r.acc[j][0], r.acc[j][1], r.acc[j][2], r.acc[j][3]), inv);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (TL::NV >= 4) {
+#pragma unroll
+        for (int j = 0; j < TL::NV; j += 4)
+          store_four(O + TL::channel(j, c, i), make_float4(r.acc[j][i], r.acc[j + 1][i], r.acc[j + 2][i], r.acc[j + 3][i]), inv);
+      } else {
+#pragma unroll
+        for (int j = 0; j < TL::NV; ++j)
+          if (TL::channel(j, c, i) < D) O[TL::channel(j, c, i)] = r.acc[j][i] * inv;
+      }
+    }
+  }
+  if (c == 0 && a.lse) a.lse[out] = l == 0.0f ? kNegInf : (r.m + __log2f(l)) * kLn2;
+}
+
+namespace {
+template <typename T, int D>
+void launch_d(const Args &a, hipStream_t st)
+{
+  const dim3 grid((unsigned)(((long)a.T * a.R / kSharedRows + a.S) * a.G * a.parts)), block(64 * kWaves);
+  if (a.parts > 1) BLOSSOM_LAUNCH((shared_kernel<T, D, true>), grid, block, 0, st, a);
+  else BLOSSOM_LAUNCH((shared_kernel<T, D, false>), grid, block, 0, st, a);
+}
+}  // namespace
+
+void launch_prompt_shared(const Args &a, hipStream_t st)
+{
+  with_type(a, [&](auto type, auto dim) { launch_d<decltype(type), decltype(dim)::value>(a, st); });
+}
+
+}  // namespace paged
+}  // namespace blossom

@@ -178,6 +178,18 @@ struct Tile {
   static __device__ __forceinline__ int channel(int j, int c, int i) { return BF ? 16 * j + 4 * c + i : NV * (4 * c + i) + j; }
 };
 
+__device__ __forceinline__ void store_out(float *p, float x) { *p = x; }
+__device__ __forceinline__ void store_out(bf16_t *p, float x) { p->bits = __builtin_bit_cast(uint16_t, (__bf16)x); }
+
+__device__ __forceinline__ void store_four(float *p, const float4 &x, float f)
+{
+  *reinterpret_cast<float4 *>(p) = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
+}
+__device__ __forceinline__ void store_four(bf16_t *p, const float4 &x, float f)
+{
+  *reinterpret_cast<uint2 *>(p) = make_uint2(mfma::pack2_bf16(x.x * f, x.y * f), mfma::pack2_bf16(x.z * f, x.w * f));
+}
+
 // Maximum over the four lanes that hold a row's logits.
 __device__ __forceinline__ float row_max(float x)
 {
