@@ -78,23 +78,31 @@ __device__ __forceinline__ Range seen_by(const Args &a, int pos, int n)
   return {max(pos - a.window + 1, 0), min(pos, min(n, a.cap) - 1)};
 }
 
-// The sequence whose new tokens' tiles hold tile `t`, where sequence s's tiles begin at first(s), which grows with s: all 64 lanes
-// of a wavefront look at one sequence each.
-template <typename F>
-__device__ __forceinline__ int find_sequence(int S, int lane, F &&starts_by)
-{
-  int s = 0;
-  for (int at = 1; at < S; at += 64) {
-    const int mine = at + lane;
-    const unsigned long long in = __ballot(mine < S && starts_by(mine));
-    s += __builtin_popcountll(in);
-    if (in != ~0ull) break;
-  }
-  return __builtin_amdgcn_readfirstlane(s);
-}
-
 // cu[s] inside [0, T], whatever the caller's array holds
 __device__ __forceinline__ int token_at(const Args &a, int s) { return min(max(a.cu[s], 0), a.T); }
+
+// The last sequence s for which begins(s, cu[s]) holds (it does for 0, and up to some s), and its tokens [first, first + count).  64
+// lanes look at one sequence each: one load for up to 63 sequences, two for 4032.
+struct Sequence {
+  int s, first, count;
+  template <typename F>
+  __device__ __forceinline__ Sequence(const Args &a, int lane, F &&begins)
+  {
+    int at = 0, k = 64;
+    for (int block = 0; a.S > 63 && block < a.S && k == 64; block += 63 * 64) {
+      const int i = min(block + 63 * lane, a.S);
+      const bool in = begins(i, token_at(a, i)) && i < a.S;
+      k = __builtin_popcountll(__ballot(in));
+      if (k > 0) at = block + 63 * (k - 1);
+    }
+    const int i = min(at + lane, a.S), cu = token_at(a, i);
+    const bool in = begins(i, cu) && i < a.S && lane < 63;
+    k = max(__builtin_popcountll(__ballot(in)), 1);  // (1 at least, if cu ascends)
+    s = at + k - 1;
+    first = __builtin_amdgcn_readlane(cu, k - 1);
+    count = max(__builtin_amdgcn_readlane(cu, k) - first, 0);
+  }
+};
 
 }  // namespace paged
 }  // namespace blossom

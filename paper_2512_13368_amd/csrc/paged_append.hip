@@ -66,8 +66,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Args a, int share)
   const long wave = (long)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int t = (int)(wave / share), part = (int)(wave % share);
   if (t >= a.T) return;
-  const int s = find_sequence(a.S, lane, [&](int i) { return token_at(a, i) <= t; });
-  const int lo = token_at(a, s), hi = token_at(a, s + 1);
+  const Sequence seq(a, lane, [&](int, int cu) { return cu <= t; });
+  const int s = seq.s, lo = seq.first, hi = seq.first + seq.count;
   if (t < lo || t >= hi) return;  // a row that no sequence owns
   const int n = a.kv_len[s];
   const long pos = (long)n - (hi - lo) + (t - lo);

@@ -35,13 +35,6 @@ struct PromptPlan {
   PromptKind kind;
   int parts;
 };
-#ifndef FEW
-#define FEW 16
-#define LEASTF 32
-#define LEASTM 32
-#define WANTF 512
-#define WANTM 512
-#endif
 constexpr int kMostParts = 256;   // parts of a key/value head's keys
 constexpr int kFillWaves = 2048;  // decode wavefronts that keep the memory busy: two a SIMD
 constexpr int kSplitTiles = 8;    // a wavefront's tiles from which splitting a sequence pays for the join
@@ -132,9 +125,10 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
     const int tile = (int)(rest / a.parts);
     part = (int)(rest % a.parts);
     n_parts = a.parts;
-    s = find_sequence(a.S, lane, [&](int i) { return (int)((long)token_at(a, i) * a.R / kRows) + i <= tile; });
-    tok0 = __builtin_amdgcn_readfirstlane(token_at(a, s));
-    new_tokens = max(__builtin_amdgcn_readfirstlane(token_at(a, s + 1)) - tok0, 0);
+    const Sequence seq(a, lane, [&](int i, int cu) { return (int)((long)cu * a.R / kRows) + i <= tile; });
+    s = seq.s;
+    tok0 = seq.first;
+    new_tokens = seq.count;
     row0 = (tile - (int)((long)tok0 * a.R / kRows) - s) * kRows;
     if (row0 < 0 || row0 >= new_tokens * a.R) return;
     rows = min(new_tokens * a.R - row0, kRows);
@@ -415,21 +409,24 @@ void launch_decode(const Args &a, hipStream_t st)
 }
 
 // Which kernel takes a prompt call, and into how many parts a row's keys go.
-//  - few rows (a sequence has 16 rows or fewer on average): wavefronts share a row tile's keys, as in decode;
-//  - bf16 at d = 64 or 128: 128-row workgroups on the 32x32 instructions;
-//  - else: 64-row workgroups.
+//  - Few 16-row tiles: their keys are shared out over the wavefronts of a workgroup each, as in decode.  That is the shortest way
+//    through a walk, but every tile of keys is moved again for every 16 rows.  (H = 8, G = 2, d = 128, us against the 128-row
+//    kernel: a prompt of 1000 tokens 17 / 25, 64 new tokens over 2000 for 4 sequences 17 / 20; but 500 over 10000 73 / 42, 4 prompts
+//    of 500 24 / 18, 16 of 64 8.6 / 7.6.)
+//  - Otherwise bf16 at d = 64 or 128: 128-row workgroups on the 32x32 instructions; the rest: 64-row workgroups.
+// Keys are split over workgroups where these do not fill the chip and a walk has 64 tiles or more: the join costs 4 us and 1 ns a row
+// (500 tokens over 10000: 42 us against 116; 4 prompts of 500: 33 against 18, hence the limit).
 static PromptPlan prompt_plan(const Args &a)
 {
+  const long all = (long)a.T * a.R, tiles = most_tiles(a);
+  auto groups = [&](int rows) { return (all / rows + (a.S == 1 ? (all % rows != 0) : a.S)) * a.G; };  // workgroups, nearly
   PromptPlan p;
-  const long all = (long)a.T * a.R;
-  p.kind = all <= FEW * a.S ? kFew : prompt_mfma_supported(a) ? kMatrix : kShared;
-  const int rows = p.kind == kFew ? kRows : p.kind == kMatrix ? kPromptRows : kSharedRows;
-  const long groups = (all / rows + (all % rows != 0 && a.S == 1 ? 1 : a.S)) * a.G;  // workgroups, nearly
-  const long tiles = most_tiles(a), least = p.kind == kFew ? LEASTF : LEASTM;      // 32-key tiles that a part is worth
-  const long want = (p.kind == kFew ? WANTF : WANTM) / groups, most = tiles / least;
-  long n = want < most ? want : most;
-  n = n < 1 ? 1 : n > kMostPromptParts ? kMostPromptParts : n;
-  p.parts = (int)n;
+  const long few = groups(kRows);
+  if (few <= 640 && few * tiles <= 24000 && (few <= 128 || tiles >= 8)) p.kind = kFew;
+  else p.kind = prompt_mfma_supported(a) ? kMatrix : kShared;
+  const long want = p.kind == kFew ? 256 / few : 512 / groups(p.kind == kMatrix ? kPromptRows : kSharedRows);
+  const long n = tiles < 64 ? 1 : want < tiles / 16 ? want : tiles / 16;
+  p.parts = (int)(n < 1 ? 1 : n > kMostPromptParts ? kMostPromptParts : n);
   return p;
 }
 

@@ -42,7 +42,7 @@ __device__ __forceinline__ void row_to_lds(const void *base, unsigned off, unsig
 
 }  // namespace
 
-template <int D, int STAGES, int WAVES_EU, bool SPLIT>
+template <int D, int STAGES, int WAVES_EU>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAVES_EU, WAVES_EU))) void prompt_kernel(Args a)
 {
   constexpr int CH = D / 8;              // 16-byte chunks of a row
@@ -59,11 +59,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
   // ---- this workgroup's rows: the last tiles, which see most keys, first ----
   const int g = blockIdx.x % a.G;
   const unsigned rest = blockIdx.x / a.G;
-  const int part = SPLIT ? (int)(rest % a.parts) : 0;
+  const int part = (int)(rest % a.parts);
   const int tile = (int)(gridDim.x / (a.G * a.parts)) - 1 - (int)(rest / a.parts);
-  const int s = find_sequence(a.S, lane, [&](int i) { return (int)((long)token_at(a, i) * a.R / kPromptRows) + i <= tile; });
-  const int tok0 = __builtin_amdgcn_readfirstlane(token_at(a, s));
-  const int new_tokens = max(__builtin_amdgcn_readfirstlane(token_at(a, s + 1)) - tok0, 0);
+  const Sequence seq(a, lane, [&](int i, int cu) { return (int)((long)cu * a.R / kPromptRows) + i <= tile; });
+  const int s = seq.s, tok0 = seq.first, new_tokens = seq.count;
   const int wg_row = (tile - (int)((long)tok0 * a.R / kPromptRows) - s) * kPromptRows;
   const int rows = new_tokens * a.R;
   if (wg_row < 0 || wg_row >= rows) return;
@@ -98,10 +97,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
   const int *table = a.page_table + s * a.table_seq + g * a.table_group;
   const int shift = a.page_shift;
   int t_lo = lo / kKeys, t_hi = hi >= lo ? hi / kKeys : t_lo - 1;
-  if constexpr (SPLIT) {
+  if (a.parts > 1) {
     const int each = (t_hi - t_lo + a.parts) / a.parts, from = t_lo;
-    t_lo = min(from + part * each, t_hi + 1);
-    t_hi = min(t_lo + each - 1, t_hi);
+    t_lo = __builtin_amdgcn_readfirstlane(min(from + part * each, t_hi + 1));
+    t_hi = __builtin_amdgcn_readfirstlane(min(t_lo + each - 1, t_hi));
   }
   const int last_page = min(hi >> shift, a.max_pages - 1);
   int list0 = (t_lo * kKeys) >> shift;  // first page of the chunk
@@ -294,29 +293,21 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
   l_run += __shfl_xor(l_run, 32);
   if (!row_ok) return;
   const size_t out = (size_t)(tok0 + tok) * a.H + head;
-  if constexpr (SPLIT) {
-    const size_t at = out * a.parts + part;
-#pragma unroll
-    for (int mb = 0; mb < NB; ++mb)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<float4 *>(a.part_o + at * D + 32 * mb + 8 * q + 4 * lh) =
-            make_float4(oacc[mb][4 * q], oacc[mb][4 * q + 1], oacc[mb][4 * q + 2], oacc[mb][4 * q + 3]);
-    if (lh == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(fresh ? kNegInf : ref, l_run);
-    return;
-  }
-  const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
-  uint16_t *O = static_cast<uint16_t *>(a.O) + out * D;
+  const bool split = a.parts > 1;
+  const float inv = split ? 1.0f : l_run == 0.0f ? 0.0f : 1.0f / l_run;
+  const size_t at = out * a.parts + part;
 #pragma unroll
   for (int mb = 0; mb < NB; ++mb)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      uint2 w;
-      w.x = mfma::pack2_bf16(oacc[mb][4 * q] * inv, oacc[mb][4 * q + 1] * inv);
-      w.y = mfma::pack2_bf16(oacc[mb][4 * q + 2] * inv, oacc[mb][4 * q + 3] * inv);
-      *reinterpret_cast<uint2 *>(O + 32 * mb + 8 * q + 4 * lh) = w;
+      const float4 x = make_float4(oacc[mb][4 * q] * inv, oacc[mb][4 * q + 1] * inv, oacc[mb][4 * q + 2] * inv, oacc[mb][4 * q + 3] * inv);
+      const size_t to = at * D + 32 * mb + 8 * q + 4 * lh;
+      if (split) *reinterpret_cast<float4 *>(a.part_o + to) = x;
+      else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.O) + to) = make_uint2(mfma::pack2_bf16(x.x, x.y), mfma::pack2_bf16(x.z, x.w));
     }
-  if (lh == 0 && a.lse) a.lse[out] = l_run == 0.0f ? kNegInf : (ref + __log2f(l_run)) * kLn2;
+  if (lh != 0) return;
+  if (split) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(l_run == 0.0f ? kNegInf : ref, l_run);
+  else if (a.lse) a.lse[out] = l_run == 0.0f ? kNegInf : (ref + __log2f(l_run)) * kLn2;
 }
 
 bool prompt_mfma_supported(const Args &a) { return a.dtype == 1 && (a.d == 64 || a.d == 128); }
@@ -325,11 +316,8 @@ void launch_prompt_mfma(const Args &a, hipStream_t st)
 {
   const long tiles = (long)a.T * a.R / kPromptRows + a.S;
   const dim3 grid((unsigned)(tiles * a.G * a.parts)), block(64 * kWaves);
-  auto go = [&](auto kernel) { BLOSSOM_LAUNCH(kernel, grid, block, 0, st, a); };
-  if (a.d == 64 && a.parts > 1) go(prompt_kernel<64, 2, 4, true>);
-  else if (a.d == 64) go(prompt_kernel<64, 2, 4, false>);
-  else if (a.parts > 1) go(prompt_kernel<128, 2, 2, true>);
-  else go(prompt_kernel<128, 2, 2, false>);
+  if (a.d == 64) BLOSSOM_LAUNCH((prompt_kernel<64, 2, 4>), grid, block, 0, st, a);
+  else BLOSSOM_LAUNCH((prompt_kernel<128, 2, 2>), grid, block, 0, st, a);
 }
 
 }  // namespace paged

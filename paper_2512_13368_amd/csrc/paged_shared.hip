@@ -14,6 +14,10 @@ namespace paged {
 using mfma::kLn2;
 using mfma::kNegInf;
 
+#ifndef ST1
+#define ST1 2
+#define ST2 2
+#endif
 namespace {
 constexpr int kWaves = 4;
 }
@@ -22,7 +26,9 @@ template <typename T, int D, bool SPLIT>
 __global__ __launch_bounds__(64 * kWaves) void shared_kernel(Args a)
 {
   typedef Tile<T, D> TL;
-  __shared__ __attribute__((aligned(1024))) char lds[2][2 * TL::BYTES];
+  constexpr int STAGES = TL::RB <= 128 ? ST1 : TL::RB == 256 ? ST2 : 2;
+  constexpr int PER_WAVE = TL::LOADS >= kWaves ? 2 * TL::LOADS / kWaves : 2;  // loads of a tile that a wavefront issues at most
+  __shared__ __attribute__((aligned(1024))) char lds[STAGES][2 * TL::BYTES];
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, c = lane >> 4;
 
@@ -31,21 +37,31 @@ __global__ __launch_bounds__(64 * kWaves) void shared_kernel(Args a)
   const unsigned rest = blockIdx.x / a.G;
   const int part = SPLIT ? (int)(rest % a.parts) : 0;
   const int tile = (int)(gridDim.x / (a.G * a.parts)) - 1 - (int)(rest / a.parts);
-  const int s = find_sequence(a.S, lane, [&](int i) { return (int)((long)token_at(a, i) * a.R / kSharedRows) + i <= tile; });
-  const int tok0 = __builtin_amdgcn_readfirstlane(token_at(a, s));
-  const int new_tokens = max(__builtin_amdgcn_readfirstlane(token_at(a, s + 1)) - tok0, 0);
+  const Sequence seq(a, lane, [&](int i, int cu) { return (int)((long)cu * a.R / kSharedRows) + i <= tile; });
+  const int s = seq.s, tok0 = seq.first, new_tokens = seq.count;
   const int wg_row = (tile - (int)((long)tok0 * a.R / kSharedRows) - s) * kSharedRows;
   const int rows = new_tokens * a.R;
   if (wg_row < 0 || wg_row >= rows) return;
-  const int len = max(__builtin_amdgcn_readfirstlane(a.kv_len[s]), 0);
-  const int first_pos = len - new_tokens;
-  const int lo = seen_by(a, first_pos + wg_row / a.R, len).lo;
-  const int hi = seen_by(a, first_pos + (min(wg_row + kSharedRows, rows) - 1) / a.R, len).hi;  // keys that any row sees
-
+  // (requested together: the length, the first pages, the queries)
+  const int raw_len = a.kv_len[s];
+  const int *table = a.page_table + s * a.table_seq;
+  auto entries = [&](int first) __attribute__((always_inline)) -> int {
+    const int id = table[min(first + lane, a.max_pages - 1)];
+    return id >= 0 && id < a.n_pages ? id : -1;
+  };
+  int list0 = 0, ids = entries(0);  // pages list0 .. list0 + 63, one a lane
   const int row0 = wg_row + 16 * wv, row = row0 + n;
   const bool row_ok = row < rows;
   const int tok = (row_ok ? row : rows - 1) / a.R;
   const int head = g * a.R + (row_ok ? row : rows - 1) - tok * a.R;
+  typename TL::Query q;
+  TL::load_query(q, static_cast<const T *>(a.Q) + (tok0 + tok) * a.q_stride + (size_t)head * D, c);
+
+  const int len = max(__builtin_amdgcn_readfirstlane(raw_len), 0);
+  const int first_pos = len - new_tokens;
+  const int lo = seen_by(a, first_pos + wg_row / a.R, len).lo;
+  const int hi = seen_by(a, first_pos + (min(wg_row + kSharedRows, rows) - 1) / a.R, len).hi;  // keys that any row sees
+
   Range my = seen_by(a, first_pos + tok, len);
   if (!row_ok) my.hi = -1;
   // keys that all rows of the wavefront see, and that any does
@@ -53,25 +69,16 @@ __global__ __launch_bounds__(64 * kWaves) void shared_kernel(Args a)
   const Range r_last = seen_by(a, first_pos + min(row0 + 15, rows - 1) / a.R, len);
   const int any_lo = r_first.lo, any_hi = row0 < rows ? r_last.hi : -1;
 
-  typename TL::Query q;
-  TL::load_query(q, static_cast<const T *>(a.Q) + (tok0 + tok) * a.q_stride + (size_t)head * D, c);
-
-  const int *table = a.page_table + s * a.table_seq;
-  auto entries = [&](int first) __attribute__((always_inline)) -> int {
-    const int id = table[min(first + lane, a.max_pages - 1)];
-    return id >= 0 && id < a.n_pages ? id : -1;
-  };
   int t = lo / kTile, t_end = hi >= lo ? hi / kTile + 1 : t;
   if constexpr (SPLIT) {
     const int each = (t_end - t + a.parts - 1) / a.parts, from = t;
     t = min(from + part * each, t_end);
     t_end = min(t + each, t_end);
   }
-  int list0 = (t * kTile) >> a.page_shift, ids = entries(list0);
   const size_t page_bytes = ((size_t)a.G << a.page_shift) * TL::RB, group_bytes = ((size_t)g << a.page_shift) * TL::RB;
   auto request = [&](int t, char *to) __attribute__((always_inline)) -> unsigned {
     const int first = (t * kTile) >> a.page_shift, last = (t * kTile + kTile - 1) >> a.page_shift;
-    if (last >= list0 + 64) {
+    if (first < list0 || last >= list0 + 64) {
       list0 = first;
       ids = entries(first);
     }
@@ -86,22 +93,27 @@ __global__ __launch_bounds__(64 * kWaves) void shared_kernel(Args a)
 
   Rows<T, D> r;
   r.clear();
-  unsigned seen = t < t_end ? request(t, lds[0]) : 0u;
+  // a ring of STAGES tiles: when tile t is worked on, the next STAGES - 2 may still be on their way and one more is requested
+  unsigned seen[STAGES];
+#pragma unroll
+  for (int k = 0; k < STAGES - 1; ++k) seen[k] = t + k < t_end ? request(t + k, lds[k]) : 0u;
 #pragma unroll
   for (int i = 0; i < TL::NK; ++i) asm volatile("" : "+v"(q.x[i].x), "+v"(q.x[i].y), "+v"(q.x[i].z), "+v"(q.x[i].w));  // (arrived before the walk)
   mfma::arrived_all<0>();
   while (t < t_end) {
 #pragma unroll
-    for (int cur = 0; cur < 2; ++cur) {
+    for (int cur = 0; cur < STAGES; ++cur) {
       if (t >= t_end) break;
-      const unsigned next = t + 1 < t_end ? request(t + 1, lds[cur ^ 1]) : 0u;
+      constexpr int AHEAD = STAGES - 1;
+      const int to = (cur + AHEAD) % STAGES;
+      if (t + AHEAD < t_end) seen[to] = request(t + AHEAD, lds[to]);
       const int base = t * kTile;
       if (base <= any_hi && base + kTile - 1 >= any_lo) {
-        const bool all = seen == 0xFFFFFFFFu && row0 + 15 < rows && base >= r_last.lo && base + kTile - 1 <= r_first.hi;
-        r.attend(lds[cur], lds[cur] + TL::BYTES, q, a.scale2, seen & mfma::row_bits(my.lo - base, my.hi - base), all, lane);
+        const bool all = seen[cur] == 0xFFFFFFFFu && row0 + 15 < rows && base >= r_last.lo && base + kTile - 1 <= r_first.hi;
+        r.attend(lds[cur], lds[cur] + TL::BYTES, q, a.scale2, seen[cur] & mfma::row_bits(my.lo - base, my.hi - base), all, lane);
       }
-      mfma::arrived_all<0>();
-      seen = next;
+      if (t + AHEAD < t_end) mfma::arrived_all<PER_WAVE *(AHEAD - 1)>();
+      else mfma::arrived_all<0>();
       ++t;
     }
   }

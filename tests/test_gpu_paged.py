@@ -418,3 +418,100 @@ def test_prompt_logits_that_grow_along_the_keys(d):
     Q, O, lse = run_prompt(c, Q=Q)
     wO, wl = c.want_prompt(Q)
     check(O, lse, wO, wl, "bf16")
+
+
+# ---- the kernels of large prompt batches (128- or 64-row workgroups), on shapes small enough for the reference: sequences without
+# ---- new tokens make the batch large, a wide page table makes the walks look long (keys are then split over workgroups)
+CROWD = 700
+TYPES = [("bf16", 64), ("bf16", 128), ("fp32", 64), ("fp32", 128), ("fp32", 32), ("bf16", 32), ("fp32", 8), ("bf16", 16), ("bf16", 8), ("fp32", 16)]
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("page,window", [(8, 0), (32, 0), (16, 50), (64, 1)])
+def test_large_batches(dtype, d, page, window):
+    new = [1, 0, 5, 130, 33, 16, 64, 3]
+    kv = [1, 9, 300, 130, 97, 16, 200, 70]
+    c = Cache(kv + [0] * CROWD, 6, 2, d, page, dtype, new=new + [0] * CROWD, window=window, seed=d + page)
+    Q, O, lse = run_prompt(c, strided=True)
+    check(O, lse, *c.want_prompt(Q), dtype)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("H,G", [(1, 1), (5, 1), (12, 4)])
+def test_large_batches_head_layouts(dtype, d, H, G):
+    c = Cache([130, 9, 40] + [0] * CROWD, H, G, d, 16, dtype, new=[130, 2, 40] + [0] * CROWD, seed=H)
+    Q, O, lse = run_prompt(c)
+    check(O, lse, *c.want_prompt(Q), dtype)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_large_batches_pages_out_of_range_and_places_outside(dtype, d):
+    c = Cache([700, 150, 64] + [0] * CROWD, 4, 2, d, 8, dtype, new=[90, 60, 70] + [0] * CROWD, seed=d, max_len=650)
+    c.kv_len[2] = 40  # 30 of its tokens stand before position 0
+    for i in (1, 3, 63, 64, 65, 80):
+        c.table[0, 0, i] = -1
+    c.table[1, 0, 0], c.table[1, 0, 17] = c.p.n_pages, 2**31 - 1
+    Q, O, lse = run_prompt(c)
+    check(O, lse, *c.want_prompt(Q), dtype)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("window", [0, 333])
+def test_large_walks_are_split_and_joined(dtype, d, window):
+    c = Cache([2300, 0, 700, 1300], 8, 2, d, 16, dtype, new=[150, 0, 70, 1], window=window, seed=d, max_pages=40000)
+    if window == 0:
+        assert B.paged_workspace_bytes(c.p, B.WS_PROMPT) > 0
+    Q, O, lse = run_prompt(c)
+    check(O, lse, *c.want_prompt(Q), dtype)
+    _, O2, lse2 = run_prompt(c, Q=Q)
+    assert torch.equal(O, O2) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("dtype,d", [("fp32", 32), ("bf16", 64), ("bf16", 128)])
+def test_split_walks_leave_rows_that_no_sequence_owns(dtype, d):
+    c = Cache([400, 90], 8, 2, d, 16, dtype, new=[40, 9], seed=9, max_pages=40000)
+    c.T += 300
+    c.p.T = c.T
+    Kc, Vc, table, cu, kv_len = c.dev()
+    Q = c.normal(c.T, 8, d)
+    O = torch.full((c.T, 8, d), 5.0, dtype=DTYPES[dtype], device="cuda")
+    lse = torch.full((c.T, 8), 5.0, device="cuda")
+    assert B.paged_workspace_bytes(c.p, B.WS_PROMPT) > 0
+    B.attn_prompt(c.p, Q.cuda(), Kc, Vc, table, cu, kv_len, O=O, lse=lse)
+    torch.cuda.synchronize()
+    assert (O[49:] == 5.0).all() and (lse[49:] == 5.0).all()
+    check(O[:49], lse[:49], *c.want_prompt(Q[:49]), dtype)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("fp32", 32)])
+def test_large_batches_logits_that_grow_along_the_keys(dtype, d):
+    # the softmax's reference has to rise many times, by a little and by a lot
+    c = Cache([900] + [0] * CROWD, 2, 1, d, 16, dtype, new=[200] + [0] * CROWD, seed=d)
+    ids = c.table[0, 0].astype(np.int64)
+    for j in range(900):
+        c.K_cache[int(ids[j // 16]), 0, j % 16] = (j / 900.0) ** 2 * 40.0 * (1.0 if j % 7 else -1.0)
+    Q = (c.normal(200, 2, d).abs() * 0.5 + 0.5).to(DTYPES[dtype])
+    Q, O, lse = run_prompt(c, Q=Q)
+    wO, wl = c.want_prompt(Q)
+    check(O, lse, wO, wl, dtype)
+
+
+def test_many_sequences_find_their_tokens():
+    # more sequences than one look at 63, or 63 at 63, takes
+    rng = np.random.default_rng(5)
+    for S in (63, 64, 65, 127, 4032, 4100):
+        new = [int(x) for x in rng.integers(0, 3, S)]
+        c = Cache(new, 1, 1, 8, 8, "fp32", new=new, seed=S)
+        Q, O, lse = run_prompt(c)
+        check(O, lse, *c.want_prompt(Q), "fp32")
+        run_append(c)
+
+
+@pytest.mark.parametrize("S", [65, 130, 300])
+def test_decode_parts_over_many_sequences(S):
+    # ragged lengths over more sequences than a wavefront has lanes, few heads: split into parts
+    kv = [int(x) for x in np.random.default_rng(S).integers(0, 3000, S)]
+    kv[3], kv[64] = 0, 4000
+    c = Cache(kv, 2, 1, 32, 32, "bf16", seed=S)
+    Q, O, lse = run_decode(c)
+    check(O, lse, *c.want_decode(Q), "bf16")
