@@ -515,3 +515,26 @@ def test_decode_parts_over_many_sequences(S):
     c = Cache(kv, 2, 1, 32, 32, "bf16", seed=S)
     Q, O, lse = run_decode(c)
     check(O, lse, *c.want_decode(Q), "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_append_of_more_than_the_caches_hold(dtype):
+    # written past the caches: 128 MB and more of rows; every row against the same call on a part of the tokens
+    H, G, d, page = 32, 8, 128, 16
+    T = 11000 if dtype == "bf16" else 5500
+    n_pages = T // page + 1
+    p = B.PagedParams(S=1, T=T, H=H, G=G, d=d, page=page, n_pages=n_pages, max_pages=n_pages, dtype=B.F32 if dtype == "fp32" else B.BF16)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    new = lambda *s: torch.randn(s, generator=g, device="cuda").to(DTYPES[dtype])
+    q, k, v = new(T, H, d), new(T, G, d), new(T, G, d)
+    table = torch.randperm(n_pages, generator=g, device="cuda").to(torch.int32)[None]
+    cos, sin = (x.cuda() for x in rope(p.capacity, d))
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    caches = [[torch.zeros(n_pages, G, page, d, dtype=DTYPES[dtype], device="cuda") for _ in range(2)] for _ in range(2)]
+    whole = B.kv_append(p, k, v, *caches[0], table, ints(0, T), ints(T), Q=q, rope=(cos, sin))
+    for lo in range(0, T, 2000):
+        hi = min(T, lo + 2000)
+        part = B.PagedParams(**{**p.__dict__, "T": hi - lo})
+        rows = B.kv_append(part, k[lo:hi], v[lo:hi], *caches[1], table, ints(0, hi - lo), ints(hi), Q=q[lo:hi], rope=(cos, sin))
+        assert torch.equal(rows, whole[lo:hi])
+    assert torch.equal(caches[0][0], caches[1][0]) and torch.equal(caches[0][1], caches[1][1])
