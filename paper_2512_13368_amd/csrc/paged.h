@@ -12,9 +12,23 @@
 namespace blossom {
 namespace paged {
 
+// Division of numbers below 2^31 by one divisor: floor(n m / 2^(31 + s)) with s = ceil(log2 d), m = ceil(2^(31 + s) / d), which is
+// exact because n (m d - 2^(31 + s)) < 2^(31 + s).
+struct Divisor {
+  uint32_t m, s;
+  __device__ __forceinline__ int of(int n) const { return (int)((uint64_t)(uint32_t)n * m >> (31 + s)); }
+};
+inline Divisor divisor(uint32_t d)
+{
+  uint32_t s = 0;
+  while ((1ull << s) < d) ++s;
+  return {(uint32_t)(((1ull << (31 + s)) + d - 1) / d), s};
+}
+
 // One call (passed to kernels by value; device pointers).  Element type of Q, K, V, the caches and O: `dtype`.
 struct Args {
   int S, T, H, G, R, d;        // sequences, packed new tokens, heads, key/value heads, H / G, head size
+  Divisor by_G, by_H, by_R, by_parts;
   int page_shift;              // log2 of the positions a page holds
   int n_pages, max_pages;      // pages of a cache, entries of a page-table row
   int cap;                     // positions a sequence may have: keys at or beyond are never read or written
@@ -33,6 +47,7 @@ struct Args {
   int parts;                   // decode: workgroups that share a key/value head's keys (0: one a sequence); prompt: parts of a row's keys
   float *part_o, *part_ml;     // their sums [H, parts, d] and (reference in log2 units, sum of exponentials) [H, parts, 2], in the
                                // workspace; prompt: [T, H, parts, ..]
+  int row_tiles;               // prompt: workgroups a key/value head and part
   int2 *part_of;               // decode: [S] first part and parts of a sequence, there too
 };
 

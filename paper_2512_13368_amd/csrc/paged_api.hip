@@ -27,6 +27,7 @@ int check_params(const blossom_paged_params *p, Args *a)
   if (held > most || (int64_t)p->T * p->H > most || (int64_t)p->S * p->H > most) return BLOSSOM_ERR_SHAPE;
   *a = Args{};
   a->S = p->S; a->T = p->T; a->H = p->H; a->G = p->G; a->R = p->H / p->G; a->d = p->d;
+  a->by_G = divisor(a->G); a->by_H = divisor(a->H); a->by_R = divisor(a->R);
   a->page_shift = __builtin_ctz((unsigned)p->page);
   a->n_pages = p->n_pages; a->max_pages = p->max_pages;
   a->cap = p->max_len > 0 && p->max_len < held ? p->max_len : (int)held;
@@ -71,6 +72,7 @@ int attn(const blossom_paged_params *p, bool prompt, const void *Q, int64_t q_st
   rc = check_stride(a, q_stride, a.H, &a.q_stride);
   if (rc) return rc;
   const size_t need = attn_ws_bytes(a, prompt);
+  a.by_parts = divisor(a.parts > 0 ? a.parts : 1);
   if (need) {
     if (!ws || ws_bytes < need) return BLOSSOM_ERR_WORKSPACE;
     if (!aligned16(ws)) return BLOSSOM_ERR_ALIGN;

@@ -118,24 +118,23 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, c = lane >> 4;
 
-  const int g = blockIdx.x % a.G;
-  const unsigned rest = blockIdx.x / a.G;
+  const int rest = a.by_G.of(blockIdx.x), g = blockIdx.x - rest * a.G;
   int s, row0, rows, tok0, new_tokens = 1, part = 0, n_parts = 1, b = 0;
   if constexpr (PROMPT) {
-    const int tile = (int)(rest / a.parts);
-    part = (int)(rest % a.parts);
+    const int tile = a.by_parts.of(rest);
+    part = rest - tile * a.parts;
     n_parts = a.parts;
-    const Sequence seq(a, lane, [&](int i, int cu) { return (int)((long)cu * a.R / kRows) + i <= tile; });
+    const Sequence seq(a, lane, [&](int i, int cu) { return (int)((unsigned)(cu * a.R) / kRows) + i <= tile; });
     s = seq.s;
     tok0 = seq.first;
     new_tokens = seq.count;
-    row0 = (tile - (int)((long)tok0 * a.R / kRows) - s) * kRows;
+    row0 = (tile - (int)((unsigned)(tok0 * a.R) / kRows) - s) * kRows;
     if (row0 < 0 || row0 >= new_tokens * a.R) return;
     rows = min(new_tokens * a.R - row0, kRows);
   } else {
     const int tiles = (a.R + kRows - 1) / kRows;
-    row0 = (int)(rest % tiles) * kRows;
-    b = (int)(rest / tiles);
+    b = tiles == 1 ? rest : rest / tiles;
+    row0 = (rest - b * tiles) * kRows;
     s = b;
     if constexpr (SPLIT) {
       const Part mine(a, lane, b, W);
@@ -148,7 +147,7 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
     tok0 = s;
     rows = min(a.R - row0, kRows);
   }
-  const int row = row0 + min(n, rows - 1), tok = PROMPT ? row / a.R : 0, head = g * a.R + row - tok * a.R;
+  const int row = row0 + min(n, rows - 1), tok = PROMPT ? a.by_R.of(row) : 0, head = g * a.R + row - tok * a.R;
 
   // what hangs on nothing is requested before anything is waited for: the length, the query, the first pages
   const int *table = a.page_table + s * a.table_seq + g * a.table_group;
@@ -164,9 +163,9 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
   const int len = max(__builtin_amdgcn_readfirstlane(raw_len), 0);
   const int first_pos = len - new_tokens;
   // keys that any row sees, that this lane's row does, that all do
-  Range any = seen_by(a, first_pos + (PROMPT ? row0 / a.R : 0), len), my = any, every = any;
+  Range any = seen_by(a, first_pos + (PROMPT ? a.by_R.of(row0) : 0), len), my = any, every = any;
   if constexpr (PROMPT) {
-    const Range last = seen_by(a, first_pos + (row0 + rows - 1) / a.R, len);
+    const Range last = seen_by(a, first_pos + a.by_R.of(row0 + rows - 1), len);
     every.lo = last.lo;
     any.hi = last.hi;
     my = seen_by(a, first_pos + tok, len);
@@ -256,7 +255,7 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
       ll = fmaf(l_s[w][row], f, ll);
       o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);
     }
-    const int tk = PROMPT ? (row0 + row) / a.R : 0;
+    const int tk = PROMPT ? a.by_R.of(row0 + row) : 0;
     const size_t out = (size_t)(tok0 + tk) * a.H + g * a.R + row0 + row - tk * a.R;
     if (!SPLIT || (!PROMPT && n_parts == 1)) {
       const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
@@ -283,9 +282,9 @@ __global__ __launch_bounds__(256) void join_kernel(Args a)
   int n = a.parts;
   size_t at0 = (size_t)blockIdx.x * a.parts;
   if constexpr (PROMPT) {
-    if ((int)(blockIdx.x / a.H) >= token_at(a, a.S)) return;  // (a row that no sequence owns stays as it is)
+    if (a.by_H.of(blockIdx.x) >= token_at(a, a.S)) return;  // (a row that no sequence owns stays as it is)
   } else {
-    const int s = blockIdx.x / a.H, h = blockIdx.x % a.H;
+    const int s = a.by_H.of(blockIdx.x), h = blockIdx.x - s * a.H;
     const int2 part = a.part_of[s];  // (of a sequence without keys: whatever the workspace held)
     n = __builtin_amdgcn_readfirstlane(tiles_of(a, s) > 0 ? part.y : 0);
     if (n <= 1) {
@@ -432,9 +431,12 @@ static PromptPlan prompt_plan(const Args &a)
 
 int prompt_parts(const Args &a) { return prompt_plan(a).parts; }
 
-void launch_prompt(const Args &a, hipStream_t st)
+void launch_prompt(const Args &call, hipStream_t st)
 {
+  Args a = call;
   const PromptPlan p = prompt_plan(a);
+  // (sequence s's tiles begin at floor(cu[s] R / rows) + s: enough for the last, partial one of each)
+  a.row_tiles = (int)((long)a.T * a.R / (p.kind == kFew ? kRows : p.kind == kMatrix ? kPromptRows : kSharedRows) + a.S);
   if (p.kind == kMatrix) launch_prompt_mfma(a, st);
   else if (p.kind == kShared) launch_prompt_shared(a, st);
   with_type(a, [&](auto type, auto dim) {
@@ -442,7 +444,7 @@ void launch_prompt(const Args &a, hipStream_t st)
     constexpr int D = decltype(dim)::value;
     if (p.kind == kFew) {
       constexpr int MOST = most_decode_waves(D * sizeof(T)), W = MOST < 8 ? MOST : 8;
-      const dim3 grid((unsigned)(((long)a.T * a.R / kRows + a.S) * a.G * a.parts)), block(64 * W);
+      const dim3 grid((unsigned)((long)a.row_tiles * a.G * a.parts)), block(64 * W);
       if (a.parts > 1) BLOSSOM_LAUNCH((decode_kernel<T, D, W, false, true, true>), grid, block, 0, st, a);
       else BLOSSOM_LAUNCH((decode_kernel<T, D, W, false, false, true>), grid, block, 0, st, a);
     }

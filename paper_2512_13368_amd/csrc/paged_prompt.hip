@@ -57,31 +57,29 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
   const int lq = lane & 31, lh = lane >> 5;
 
   // ---- this workgroup's rows: the last tiles, which see most keys, first ----
-  const int g = blockIdx.x % a.G;
-  const unsigned rest = blockIdx.x / a.G;
-  const int part = (int)(rest % a.parts);
-  const int tile = (int)(gridDim.x / (a.G * a.parts)) - 1 - (int)(rest / a.parts);
-  const Sequence seq(a, lane, [&](int i, int cu) { return (int)((long)cu * a.R / kPromptRows) + i <= tile; });
+  const int rest = a.by_G.of(blockIdx.x), g = blockIdx.x - rest * a.G;
+  const int from_last = a.by_parts.of(rest), part = rest - from_last * a.parts, tile = a.row_tiles - 1 - from_last;
+  const Sequence seq(a, lane, [&](int i, int cu) { return (int)((unsigned)(cu * a.R) / kPromptRows) + i <= tile; });
   const int s = seq.s, tok0 = seq.first, new_tokens = seq.count;
-  const int wg_row = (tile - (int)((long)tok0 * a.R / kPromptRows) - s) * kPromptRows;
+  const int wg_row = (tile - (int)((unsigned)(tok0 * a.R) / kPromptRows) - s) * kPromptRows;
   const int rows = new_tokens * a.R;
   if (wg_row < 0 || wg_row >= rows) return;
   const int len = max(__builtin_amdgcn_readfirstlane(a.kv_len[s]), 0);
   const int first_pos = len - new_tokens;
 
-  const Range all_first = seen_by(a, first_pos + wg_row / a.R, len);
-  const Range all_last = seen_by(a, first_pos + (min(wg_row + kPromptRows, rows) - 1) / a.R, len);
+  const Range all_first = seen_by(a, first_pos + a.by_R.of(wg_row), len);
+  const Range all_last = seen_by(a, first_pos + a.by_R.of(min(wg_row + kPromptRows, rows) - 1), len);
   const int lo = all_first.lo, hi = all_last.hi;  // keys that any row of the workgroup sees
 
   const int row0 = wg_row + 32 * wv, row = row0 + lq;
   const bool row_ok = row < rows;
-  const int tok = (row_ok ? row : rows - 1) / a.R;
+  const int tok = a.by_R.of(row_ok ? row : rows - 1);
   const int head = g * a.R + (row_ok ? row : rows - 1) - tok * a.R;
   Range my = seen_by(a, first_pos + tok, len);
   if (!row_ok) my.hi = -1;
   // keys that all rows of the wavefront see, and that any does (rows ascend with positions)
   const bool wave_on = row0 < rows;
-  const int w_first = first_pos + min(row0, rows - 1) / a.R, w_last = first_pos + min(row0 + 31, rows - 1) / a.R;
+  const int w_first = first_pos + a.by_R.of(min(row0, rows - 1)), w_last = first_pos + a.by_R.of(min(row0 + 31, rows - 1));
   const Range r_first = seen_by(a, w_first, len), r_last = seen_by(a, w_last, len);
   const int every_lo = row0 + 31 < rows ? r_last.lo : 0x7FFFFFFF, every_hi = r_first.hi;
   const int any_lo = r_first.lo, any_hi = wave_on ? r_last.hi : -1;
@@ -314,8 +312,7 @@ bool prompt_mfma_supported(const Args &a) { return a.dtype == 1 && (a.d == 64 ||
 
 void launch_prompt_mfma(const Args &a, hipStream_t st)
 {
-  const long tiles = (long)a.T * a.R / kPromptRows + a.S;
-  const dim3 grid((unsigned)(tiles * a.G * a.parts)), block(64 * kWaves);
+  const dim3 grid((unsigned)((long)a.row_tiles * a.G * a.parts)), block(64 * kWaves);
   if (a.d == 64) BLOSSOM_LAUNCH((prompt_kernel<64, 2, 4>), grid, block, 0, st, a);
   else BLOSSOM_LAUNCH((prompt_kernel<128, 2, 2>), grid, block, 0, st, a);
 }

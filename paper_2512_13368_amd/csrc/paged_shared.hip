@@ -33,13 +33,11 @@ __global__ __launch_bounds__(64 * kWaves) void shared_kernel(Args a)
   const int n = lane & 15, c = lane >> 4;
 
   // ---- this workgroup's rows: the last tiles, which see most keys, first ----
-  const int g = blockIdx.x % a.G;
-  const unsigned rest = blockIdx.x / a.G;
-  const int part = SPLIT ? (int)(rest % a.parts) : 0;
-  const int tile = (int)(gridDim.x / (a.G * a.parts)) - 1 - (int)(rest / a.parts);
-  const Sequence seq(a, lane, [&](int i, int cu) { return (int)((long)cu * a.R / kSharedRows) + i <= tile; });
+  const int rest = a.by_G.of(blockIdx.x), g = blockIdx.x - rest * a.G;
+  const int from_last = a.by_parts.of(rest), part = rest - from_last * a.parts, tile = a.row_tiles - 1 - from_last;
+  const Sequence seq(a, lane, [&](int i, int cu) { return (int)((unsigned)(cu * a.R) / kSharedRows) + i <= tile; });
   const int s = seq.s, tok0 = seq.first, new_tokens = seq.count;
-  const int wg_row = (tile - (int)((long)tok0 * a.R / kSharedRows) - s) * kSharedRows;
+  const int wg_row = (tile - (int)((unsigned)(tok0 * a.R) / kSharedRows) - s) * kSharedRows;
   const int rows = new_tokens * a.R;
   if (wg_row < 0 || wg_row >= rows) return;
   // (requested together: the length, the first pages, the queries)
@@ -52,21 +50,21 @@ __global__ __launch_bounds__(64 * kWaves) void shared_kernel(Args a)
   int list0 = 0, ids = entries(0);  // pages list0 .. list0 + 63, one a lane
   const int row0 = wg_row + 16 * wv, row = row0 + n;
   const bool row_ok = row < rows;
-  const int tok = (row_ok ? row : rows - 1) / a.R;
+  const int tok = a.by_R.of(row_ok ? row : rows - 1);
   const int head = g * a.R + (row_ok ? row : rows - 1) - tok * a.R;
   typename TL::Query q;
   TL::load_query(q, static_cast<const T *>(a.Q) + (tok0 + tok) * a.q_stride + (size_t)head * D, c);
 
   const int len = max(__builtin_amdgcn_readfirstlane(raw_len), 0);
   const int first_pos = len - new_tokens;
-  const int lo = seen_by(a, first_pos + wg_row / a.R, len).lo;
-  const int hi = seen_by(a, first_pos + (min(wg_row + kSharedRows, rows) - 1) / a.R, len).hi;  // keys that any row sees
+  const int lo = seen_by(a, first_pos + a.by_R.of(wg_row), len).lo;
+  const int hi = seen_by(a, first_pos + a.by_R.of(min(wg_row + kSharedRows, rows) - 1), len).hi;  // keys that any row sees
 
   Range my = seen_by(a, first_pos + tok, len);
   if (!row_ok) my.hi = -1;
   // keys that all rows of the wavefront see, and that any does
-  const Range r_first = seen_by(a, first_pos + min(row0, rows - 1) / a.R, len);
-  const Range r_last = seen_by(a, first_pos + min(row0 + 15, rows - 1) / a.R, len);
+  const Range r_first = seen_by(a, first_pos + a.by_R.of(min(row0, rows - 1)), len);
+  const Range r_last = seen_by(a, first_pos + a.by_R.of(min(row0 + 15, rows - 1)), len);
   const int any_lo = r_first.lo, any_hi = row0 < rows ? r_last.hi : -1;
 
   int t = lo / kTile, t_end = hi >= lo ? hi / kTile + 1 : t;
@@ -158,7 +156,7 @@ namespace {
 template <typename T, int D>
 void launch_d(const Args &a, hipStream_t st)
 {
-  const dim3 grid((unsigned)(((long)a.T * a.R / kSharedRows + a.S) * a.G * a.parts)), block(64 * kWaves);
+  const dim3 grid((unsigned)((long)a.row_tiles * a.G * a.parts)), block(64 * kWaves);
   if (a.parts > 1) BLOSSOM_LAUNCH((shared_kernel<T, D, true>), grid, block, 0, st, a);
   else BLOSSOM_LAUNCH((shared_kernel<T, D, false>), grid, block, 0, st, a);
 }
