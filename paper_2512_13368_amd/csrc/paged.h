@@ -63,7 +63,8 @@ constexpr int kPromptRows = 128;  // query rows of a workgroup
 bool prompt_mfma_supported(const Args &a);
 void launch_prompt_mfma(const Args &a, hipStream_t st);
 // prompt attention for everything else: paged_shared.hip
-constexpr int kSharedRows = 64;
+// rows of a workgroup: 16 a wavefront, of which there are as many as it takes to move a tile
+constexpr int shared_waves(int row_bytes) { return row_bytes >= 256 ? 4 : 2; }
 void launch_prompt_shared(const Args &a, hipStream_t st);
 
 // Calls f with the element type and the head size as compile-time constants.
@@ -116,6 +117,87 @@ struct Sequence {
     s = at + k - 1;
     first = __builtin_amdgcn_readlane(cu, k - 1);
     count = max(__builtin_amdgcn_readlane(cu, k) - first, 0);
+  }
+};
+
+// inclusive sums over the lanes of a wavefront
+__device__ __forceinline__ int wave_scan(int x)
+{
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr:1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15 to the second and fourth row, 31 to the last two
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
+__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
+
+// The row tile that workgroup b of a key/value head takes.  A causal walk grows with the tile's place in its sequence, so the tiles of
+// all sequences are taken by their place, the last places first: what sees most keys is begun first, and the workgroups of one round
+// have like work (256 fp32 prompts of 20 to 200 tokens: 21.7 us in the sequences' order, 17.7 so).  C(k) = sum over sequences of
+// max(tiles - k, 0) tiles stand at place k or later: the place is the largest k with C(k) > b, found by halving, 64 sequences' counts
+// a register.  Under `least` sequences, whose tiles are best begun together because they read the same keys, and over kOrdered:
+// in the sequences' order, from the last tile on.
+constexpr int kOrdered = 256;
+struct RowTile {
+  int s, tok0, count, row0;  // sequence, its first token, its tokens; the tile's first row (-1: no tile)
+  __device__ __forceinline__ RowTile(const Args &a, int lane, int b, int rows, int least)
+  {
+    if (a.S < least || a.S > kOrdered) {
+      const int tile = a.row_tiles - 1 - b;
+      const Sequence seq(a, lane, [&](int i, int cu) { return (int)((unsigned)(cu * a.R) / rows) + i <= tile; });
+      s = seq.s;
+      tok0 = seq.first;
+      count = seq.count;
+      row0 = (tile - (int)((unsigned)(tok0 * a.R) / rows) - s) * rows;
+      if (row0 < 0 || row0 >= count * a.R) row0 = -1;
+      return;
+    }
+    constexpr int N = kOrdered / 64;
+    int cu[N], n[N], t[N], most = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      cu[i] = n[i] = t[i] = 0;
+      if (64 * i >= a.S) continue;
+      cu[i] = token_at(a, min(64 * i + lane, a.S));
+      n[i] = max(token_at(a, min(64 * i + lane + 1, a.S)) - cu[i], 0);
+      t[i] = (unsigned)(n[i] * a.R + rows - 1) / rows;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) most = max(most, t[i]);
+    auto beyond = [&](int k) __attribute__((always_inline)) {
+      int x = 0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) x += max(t[i] - k, 0);
+      return wave_sum(x);
+    };
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) most = max(most, __shfl_xor(most, o));
+    int lo = 0, hi = __builtin_amdgcn_readfirstlane(most);
+    s = tok0 = count = 0;
+    row0 = -1;
+    if (beyond(0) <= b) return;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (beyond(mid) > b) lo = mid;
+      else hi = mid;
+    }
+    int nth = b - beyond(lo + 1);  // of the sequences that have a tile at this place
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const unsigned long long has = __ballot(t[i] > lo);
+      const int many = __builtin_popcountll(has);
+      if (nth >= 0 && nth < many) {
+        const int before = __builtin_amdgcn_mbcnt_hi((unsigned)(has >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)has, 0));
+        const int l = __builtin_ctzll(__ballot((has >> lane & 1ull) != 0ull && before == nth));
+        s = 64 * i + l;
+        tok0 = __builtin_amdgcn_readlane(cu[i], l);
+        count = __builtin_amdgcn_readlane(n[i], l);
+        row0 = lo * rows;
+      }
+      nth -= many;
+    }
   }
 };
 

@@ -59,19 +59,6 @@ __device__ __forceinline__ int tiles_of(const Args &a, int s)
   const Range r = seen_by(a, len - 1, len);
   return r.hi >= r.lo ? r.hi / kTile - r.lo / kTile + 1 : 0;
 }
-// inclusive sums over the lanes of a wavefront
-__device__ __forceinline__ int wave_scan(int x)
-{
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr:1, 2, 4, 8
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15 to the second and fourth row, 31 to the last two
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
-  return x;
-}
-__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
-
 // The part of all sequences' keys that workgroup b of a key/value head takes: of a.parts workgroups, a sequence of t tiles is cut into
 // ceil(t / chunk), so that ragged lengths give parts of like size.  Every wavefront finds its own from the lengths, 64 sequences at a
 // time: a chunk of total / (parts - S / 2) nearly always makes few enough parts (half a part a sequence is lost to rounding up), one
@@ -220,7 +207,7 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
       const char *ks = mine + k * (2 * TL::BYTES);
       const int base = t * kTile;
       const bool all = seen[k] == 0xFFFFFFFFu && (!PROMPT || (base >= every.lo && base + kTile - 1 <= every.hi));
-      r.attend(ks, ks + TL::BYTES, q, a.scale2, PROMPT ? seen[k] & mfma::row_bits(my.lo - base, my.hi - base) : seen[k], all, lane);
+      r.attend(ks, ks + TL::BYTES, q, a.scale2, PROMPT ? seen[k] & mfma::row_bits(my.lo - base, my.hi - base) : seen[k], all, true, lane);
       ++t;
     }
   }
@@ -412,9 +399,10 @@ void launch_decode(const Args &a, hipStream_t st)
 //    through a walk, but every tile of keys is moved again for every 16 rows.  (H = 8, G = 2, d = 128, us against the 128-row
 //    kernel: a prompt of 1000 tokens 17 / 25, 64 new tokens over 2000 for 4 sequences 17 / 20; but 500 over 10000 73 / 42, 4 prompts
 //    of 500 24 / 18, 16 of 64 8.6 / 7.6.)
-//  - Otherwise bf16 at d = 64 or 128: 128-row workgroups on the 32x32 instructions; the rest: 64-row workgroups.
+//  - Otherwise bf16 at d = 64 or 128: 128-row workgroups on the 32x32 instructions; the rest: workgroups of 32 or 64 rows.
 // Keys are split over workgroups where these do not fill the chip and a walk has 64 tiles or more: the join costs 4 us and 1 ns a row
 // (500 tokens over 10000: 42 us against 116; 4 prompts of 500: 33 against 18, hence the limit).
+static int shared_rows(const Args &a) { return 16 * shared_waves(a.d * (a.dtype == 0 ? 4 : 2)); }
 static PromptPlan prompt_plan(const Args &a)
 {
   const long all = (long)a.T * a.R, tiles = most_tiles(a);
@@ -423,7 +411,7 @@ static PromptPlan prompt_plan(const Args &a)
   const long few = groups(kRows);
   if (few <= 640 && few * tiles <= 24000 && (few <= 128 || tiles >= 8)) p.kind = kFew;
   else p.kind = prompt_mfma_supported(a) ? kMatrix : kShared;
-  const long want = p.kind == kFew ? 256 / few : 512 / groups(p.kind == kMatrix ? kPromptRows : kSharedRows);
+  const long want = p.kind == kFew ? 256 / few : 512 / groups(p.kind == kMatrix ? kPromptRows : shared_rows(a));
   const long n = tiles < 64 ? 1 : want < tiles / 16 ? want : tiles / 16;
   p.parts = (int)(n < 1 ? 1 : n > kMostPromptParts ? kMostPromptParts : n);
   return p;
@@ -436,7 +424,7 @@ void launch_prompt(const Args &call, hipStream_t st)
   Args a = call;
   const PromptPlan p = prompt_plan(a);
   // (sequence s's tiles begin at floor(cu[s] R / rows) + s: enough for the last, partial one of each)
-  a.row_tiles = (int)((long)a.T * a.R / (p.kind == kFew ? kRows : p.kind == kMatrix ? kPromptRows : kSharedRows) + a.S);
+  a.row_tiles = (int)((long)a.T * a.R / (p.kind == kFew ? kRows : p.kind == kMatrix ? kPromptRows : shared_rows(a)) + a.S);
   if (p.kind == kMatrix) launch_prompt_mfma(a, st);
   else if (p.kind == kShared) launch_prompt_shared(a, st);
   with_type(a, [&](auto type, auto dim) {

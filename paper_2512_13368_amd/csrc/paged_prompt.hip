@@ -58,12 +58,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
 
   // ---- this workgroup's rows: the last tiles, which see most keys, first ----
   const int rest = a.by_G.of(blockIdx.x), g = blockIdx.x - rest * a.G;
-  const int from_last = a.by_parts.of(rest), part = rest - from_last * a.parts, tile = a.row_tiles - 1 - from_last;
-  const Sequence seq(a, lane, [&](int i, int cu) { return (int)((unsigned)(cu * a.R) / kPromptRows) + i <= tile; });
-  const int s = seq.s, tok0 = seq.first, new_tokens = seq.count;
-  const int wg_row = (tile - (int)((unsigned)(tok0 * a.R) / kPromptRows) - s) * kPromptRows;
+  const int nth = a.by_parts.of(rest), part = rest - nth * a.parts;
+  const RowTile mine(a, lane, nth, kPromptRows, 8);
+  const int s = mine.s, tok0 = mine.tok0, new_tokens = mine.count, wg_row = mine.row0;
+  if (wg_row < 0) return;
   const int rows = new_tokens * a.R;
-  if (wg_row < 0 || wg_row >= rows) return;
   const int len = max(__builtin_amdgcn_readfirstlane(a.kv_len[s]), 0);
   const int first_pos = len - new_tokens;
 

@@ -1,7 +1,11 @@
 // Prompt attention for every type and head size (bf16 at d = 64 and 128 has a kernel of its own: paged_prompt.hip).
 //
-// A workgroup's four wavefronts take 64 rows of one key/value head, (token, head of the group) pairs, 16 each, and walk the 32-key
-// tiles that any of them sees.  A tile is moved to LDS once, one step ahead, and read by all four.
+// A workgroup's two wavefronts (four where a row is 256 bytes or more) take 16 rows each of one key/value head, (token, head of the
+// group) pairs, and walk the 32-key tiles that any of them sees.  A tile is moved to LDS once, one step ahead, and read by all.
+// Short ragged prompts are bound by the matrix pipe and the vector ALUs, which do not overlap for fp32 products (256 prompts of 20
+// to 200 tokens, 2 heads, d = 32: 16.6 us, of which the products take 4.6 and the exponentials and the rest 3 at full balance).
+// Tried: rings of 3, 4 and 6 tiles (23.3, 24.6, 25.4 us where 2 took 23.0), results through LDS (no gain), one wavefront a
+// workgroup without barriers (as fast, slower from d = 64 on), two for large rows (d = 64 fp32: 72 us against 61).
 #include "common.h"
 #include "launch.h"
 #include "mfma_common.h"
@@ -14,32 +18,22 @@ namespace paged {
 using mfma::kLn2;
 using mfma::kNegInf;
 
-#ifndef ST1
-#define ST1 2
-#define ST2 2
-#endif
-namespace {
-constexpr int kWaves = 4;
-}
-
 template <typename T, int D, bool SPLIT>
-__global__ __launch_bounds__(64 * kWaves) void shared_kernel(Args a)
+__global__ __launch_bounds__(64 * shared_waves(D * sizeof(T))) void shared_kernel(Args a)
 {
   typedef Tile<T, D> TL;
-  constexpr int STAGES = TL::RB <= 128 ? ST1 : TL::RB == 256 ? ST2 : 2;
-  constexpr int PER_WAVE = TL::LOADS >= kWaves ? 2 * TL::LOADS / kWaves : 2;  // loads of a tile that a wavefront issues at most
-  __shared__ __attribute__((aligned(1024))) char lds[STAGES][2 * TL::BYTES];
+  constexpr int W = shared_waves(TL::RB);
+  __shared__ __attribute__((aligned(1024))) char lds[2][2 * TL::BYTES];
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, c = lane >> 4;
 
   // ---- this workgroup's rows: the last tiles, which see most keys, first ----
   const int rest = a.by_G.of(blockIdx.x), g = blockIdx.x - rest * a.G;
-  const int from_last = a.by_parts.of(rest), part = rest - from_last * a.parts, tile = a.row_tiles - 1 - from_last;
-  const Sequence seq(a, lane, [&](int i, int cu) { return (int)((unsigned)(cu * a.R) / kSharedRows) + i <= tile; });
-  const int s = seq.s, tok0 = seq.first, new_tokens = seq.count;
-  const int wg_row = (tile - (int)((unsigned)(tok0 * a.R) / kSharedRows) - s) * kSharedRows;
+  const int nth = a.by_parts.of(rest), part = rest - nth * a.parts;
+  const RowTile mine(a, lane, nth, 16 * W, 2);
+  const int s = mine.s, tok0 = mine.tok0, new_tokens = mine.count, wg_row = mine.row0;
+  if (wg_row < 0) return;
   const int rows = new_tokens * a.R;
-  if (wg_row < 0 || wg_row >= rows) return;
   // (requested together: the length, the first pages, the queries)
   const int raw_len = a.kv_len[s];
   const int *table = a.page_table + s * a.table_seq;
@@ -58,7 +52,7 @@ __global__ __launch_bounds__(64 * kWaves) void shared_kernel(Args a)
   const int len = max(__builtin_amdgcn_readfirstlane(raw_len), 0);
   const int first_pos = len - new_tokens;
   const int lo = seen_by(a, first_pos + a.by_R.of(wg_row), len).lo;
-  const int hi = seen_by(a, first_pos + a.by_R.of(min(wg_row + kSharedRows, rows) - 1), len).hi;  // keys that any row sees
+  const int hi = seen_by(a, first_pos + a.by_R.of(min(wg_row + 16 * W, rows) - 1), len).hi;  // keys that any row sees
 
   Range my = seen_by(a, first_pos + tok, len);
   if (!row_ok) my.hi = -1;
@@ -85,33 +79,28 @@ __global__ __launch_bounds__(64 * kWaves) void shared_kernel(Args a)
     const bool ok = id >= 0 && key >= lo && key <= hi;
     const unsigned seen = (unsigned)__ballot(ok);
     const size_t off = max(id, 0) * page_bytes + group_bytes + (size_t)(key & ((1 << a.page_shift) - 1)) * TL::RB;
-    TL::template request<false>(a, to, to + TL::BYTES, off, ok, seen == 0xFFFFFFFFu, lane, wv, kWaves);
+    TL::template request<false>(a, to, to + TL::BYTES, off, ok, seen == 0xFFFFFFFFu, lane, wv, W);
     return seen;
   };
 
   Rows<T, D> r;
   r.clear();
-  // a ring of STAGES tiles: when tile t is worked on, the next STAGES - 2 may still be on their way and one more is requested
-  unsigned seen[STAGES];
-#pragma unroll
-  for (int k = 0; k < STAGES - 1; ++k) seen[k] = t + k < t_end ? request(t + k, lds[k]) : 0u;
+  unsigned seen = t < t_end ? request(t, lds[0]) : 0u;
 #pragma unroll
   for (int i = 0; i < TL::NK; ++i) asm volatile("" : "+v"(q.x[i].x), "+v"(q.x[i].y), "+v"(q.x[i].z), "+v"(q.x[i].w));  // (arrived before the walk)
   mfma::arrived_all<0>();
   while (t < t_end) {
 #pragma unroll
-    for (int cur = 0; cur < STAGES; ++cur) {
+    for (int cur = 0; cur < 2; ++cur) {
       if (t >= t_end) break;
-      constexpr int AHEAD = STAGES - 1;
-      const int to = (cur + AHEAD) % STAGES;
-      if (t + AHEAD < t_end) seen[to] = request(t + AHEAD, lds[to]);
+      const unsigned next = t + 1 < t_end ? request(t + 1, lds[cur ^ 1]) : 0u;
       const int base = t * kTile;
       if (base <= any_hi && base + kTile - 1 >= any_lo) {
-        const bool all = seen[cur] == 0xFFFFFFFFu && row0 + 15 < rows && base >= r_last.lo && base + kTile - 1 <= r_first.hi;
-        r.attend(lds[cur], lds[cur] + TL::BYTES, q, a.scale2, seen[cur] & mfma::row_bits(my.lo - base, my.hi - base), all, lane);
+        const bool all = seen == 0xFFFFFFFFu && row0 + 15 < rows && base >= r_last.lo && base + kTile - 1 <= r_first.hi;
+        r.attend(lds[cur], lds[cur] + TL::BYTES, q, a.scale2, seen & mfma::row_bits(my.lo - base, my.hi - base), all, base + 16 <= any_hi, lane);
       }
-      if (t + AHEAD < t_end) mfma::arrived_all<PER_WAVE *(AHEAD - 1)>();
-      else mfma::arrived_all<0>();
+      mfma::arrived_all<0>();
+      seen = next;
       ++t;
     }
   }
@@ -156,7 +145,7 @@ namespace {
 template <typename T, int D>
 void launch_d(const Args &a, hipStream_t st)
 {
-  const dim3 grid((unsigned)((long)a.row_tiles * a.G * a.parts)), block(64 * kWaves);
+  const dim3 grid((unsigned)((long)a.row_tiles * a.G * a.parts)), block(64 * shared_waves(D * sizeof(T)));
   if (a.parts > 1) BLOSSOM_LAUNCH((shared_kernel<T, D, true>), grid, block, 0, st, a);
   else BLOSSOM_LAUNCH((shared_kernel<T, D, false>), grid, block, 0, st, a);
 }

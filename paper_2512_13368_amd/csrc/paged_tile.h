@@ -134,7 +134,8 @@ struct Tile {
   // acc += V^T P^T: p[4h + i] is the probability of key 16h + 4c + i.  The sum over keys may run in any order, so lane group c takes
   // the keys whose probabilities it holds.  bf16: P is rounded as the matrix instruction wants it (its sum is of the unrounded ones),
   // V^T comes through the transposing LDS read.  Accumulator j, element i holds channel channel(j, c, i) of the lane's query.
-  static __device__ __forceinline__ void product(const char *vs, const float (&p)[8], int lane, f32x4 (&acc)[NV])
+  // `both`: the tile's second 16 keys count too.
+  static __device__ __forceinline__ void product(const char *vs, const float (&p)[8], bool both, int lane, f32x4 (&acc)[NV])
   {
     const int n = lane & 15, c = lane >> 4;
     if constexpr (BF) {
@@ -154,6 +155,7 @@ struct Tile {
     } else {
 #pragma unroll
       for (int s = 0; s < 8; ++s) {
+        if (s == 4 && !both) break;
         const int r = 16 * (s >> 2) + 4 * c + (s & 3);
         const char *row = vs + r * RB;
         float v[NV];
@@ -213,16 +215,23 @@ struct Rows {
 #pragma unroll
     for (int j = 0; j < TL::NV; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
-  // one tile; bit k of `seen`: this lane's row sees key k of the tile (all: no key is masked for any row)
-  __device__ __forceinline__ void attend(const char *ks, const char *vs, const typename TL::Query &q, float scale2, unsigned seen, bool all, int lane)
+  // one tile; bit k of `seen`: this lane's row sees key k of the tile (all: no key is masked for any row; both: any row sees one of
+  // the second 16)
+  __device__ __forceinline__ void attend(const char *ks, const char *vs, const typename TL::Query &q, float scale2, unsigned seen, bool all, bool both,
+                                         int lane)
   {
     const int n = lane & 15, c = lane >> 4;
     float p[8];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const f32x4 s = TL::logits(ks, h, n, c, q);
+      if (h == 0 || both) {
+        const f32x4 s = TL::logits(ks, h, n, c, q);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[4 * h + i] = s[i] * scale2;
+        for (int i = 0; i < 4; ++i) p[4 * h + i] = s[i] * scale2;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[4 * h + i] = mfma::kNegInf;
+      }
     }
     if (!all) {
       const int mine = (int)(seen >> (4 * c));
@@ -245,7 +254,7 @@ struct Rows {
     l = l * f + sum;
 #pragma unroll
     for (int j = 0; j < TL::NV; ++j) acc[j] *= f;
-    TL::product(vs, p, lane, acc);
+    TL::product(vs, p, both, lane, acc);
   }
   __device__ __forceinline__ float total() const
   {
