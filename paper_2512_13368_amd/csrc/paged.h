@@ -131,6 +131,17 @@ __device__ __forceinline__ int wave_scan(int x)
   x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
   return x;
 }
+// the largest of numbers >= 0
+__device__ __forceinline__ int wave_max(int x)
+{
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
+  return __builtin_amdgcn_readlane(x, 63);
+}
 __device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
 
 // The row tile that workgroup b of a key/value head takes.  A causal walk grows with the tile's place in its sequence, so the tiles of
@@ -154,30 +165,33 @@ struct RowTile {
       if (row0 < 0 || row0 >= count * a.R) row0 = -1;
       return;
     }
-    constexpr int N = kOrdered / 64;
+    s = tok0 = count = 0;
+    row0 = -1;
+    if (a.S <= 64) find<1>(a, lane, b, rows);
+    else find<kOrdered / 64>(a, lane, b, rows);
+  }
+
+ private:
+  template <int N>
+  __device__ __forceinline__ void find(const Args &a, int lane, int b, int rows)
+  {
     int cu[N], n[N], t[N], most = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      cu[i] = n[i] = t[i] = 0;
-      if (64 * i >= a.S) continue;
-      cu[i] = token_at(a, min(64 * i + lane, a.S));
-      n[i] = max(token_at(a, min(64 * i + lane + 1, a.S)) - cu[i], 0);
+      const int at = 64 * i + lane;
+      cu[i] = token_at(a, min(at, a.S));
+      n[i] = max(token_at(a, min(at + 1, a.S)) - cu[i], 0);
       t[i] = (unsigned)(n[i] * a.R + rows - 1) / rows;
+      most = max(most, t[i]);
     }
-#pragma unroll
-    for (int i = 0; i < N; ++i) most = max(most, t[i]);
     auto beyond = [&](int k) __attribute__((always_inline)) {
       int x = 0;
 #pragma unroll
       for (int i = 0; i < N; ++i) x += max(t[i] - k, 0);
       return wave_sum(x);
     };
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) most = max(most, __shfl_xor(most, o));
-    int lo = 0, hi = __builtin_amdgcn_readfirstlane(most);
-    s = tok0 = count = 0;
-    row0 = -1;
     if (beyond(0) <= b) return;
+    int lo = 0, hi = wave_max(most);
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (beyond(mid) > b) lo = mid;
