@@ -3,16 +3,16 @@
 //   o = sum_j p_j V_j,  p = softmax_j(scale q.K_j)   over the cached positions j that the query sees:
 //   j <= pos, pos - j < window, pos = kv_len - new + i for new token i (decode: pos = kv_len - 1)
 //
-// Query rows are (token, head) pairs that share a key/value head: R = H/G heads of a token read the same keys, so a wavefront
-// takes 16 such rows and 32 keys a step, on 16x16 matrix instructions, with operands straight from memory to registers:
-//  - S^T = K Q^T: a lane's 16 bytes of a key row are an operand as they are.  The result leaves lane (row n, group c) with the
-//    logits of keys 16t + 4c + i (t < 2, i < 4).
-//  - O^T += V^T P^T: the sum over keys may run in any order, so lane group c takes the keys whose probabilities it holds, and P^T
-//    is an operand as it is.  V^T wants 8 keys of one channel in a lane: it loads d/16 channels of its 8 keys and turns that block
-//    in its registers (bf16; fp32 needs no turn).  A lane then holds channels of its own row, so the running maximum and sum
-//    (fp32, log2 units) need no exchange for the rescaling.
-// Four wavefronts of a workgroup take a row tile's key tiles in turn and join their results in LDS; where rows are few, a row's
-// keys are split over workgroups too, whose sums another kernel joins.
+// Query rows are (token, head) pairs that share a key/value head: the R = H/G heads of a token read the same keys, so they stand in
+// one 16-row operand.  This file has the way through a cache that memory bounds, one new token a sequence or a few: the wavefronts
+// of a workgroup take a run of its 32-key tiles each, through LDS that is theirs alone (no barrier in the walk), and join their
+// results there.  Where a sequence is long and workgroups are few, its keys are cut into parts for several, whose results a second
+// kernel joins.  Large prompts: paged_prompt.hip, paged_shared.hip.  The operands and the softmax of a step: paged_tile.h.
+//
+// Measured: one sequence of 131071 keys (32 heads over 8, d = 128, bf16: 537 MB) 85 us, 80 of it in this kernel, where reading as many
+// bytes takes 78; 16 sequences of 4001 to 8191 keys (400 MB) 71 us, the join 3.5 of it; 128 of 100 to 1024 (4 heads, d = 64: 74 MB)
+// 15 us, where a read takes 11 and a launch with its first loads 4; the join inside the kernel would save 3 us of 85 and nothing
+// where sequences are short.
 #include "common.h"
 #include "launch.h"
 #include "mfma_common.h"
@@ -24,20 +24,22 @@ namespace paged {
 
 namespace {
 
-using mfma::bf16x8;
 using mfma::kLn2;
 using mfma::kNegInf;
 
-constexpr int kRows = 16;   // query rows of a workgroup
-constexpr int kMostPromptParts = 64;
+constexpr int kRows = 16;             // query rows of a workgroup
+constexpr int kMostParts = 256;       // parts of a key/value head's keys
+constexpr int kMostPromptParts = 64;  // parts of a row's keys in a prompt
+constexpr int kFillWaves = 2048;      // decode wavefronts that keep the memory busy: two a SIMD (4096: 88 us for 85 at 131071 keys, 16.0 for 15.2 on short ones)
+// A wavefront's tiles from which splitting a sequence pays for the join (8 heads over 2, d = 128, one sequence: 32 tiles over 8
+// wavefronts 8.8 us whole and 10.8 split, 63 tiles 13.9 and 10.8; fp32 at d = 32: 9.4 and 11.0, 16.9 and 12.1).
+constexpr int kSplitTiles = 6;
+
 enum PromptKind { kFew, kShared, kMatrix };
 struct PromptPlan {
   PromptKind kind;
   int parts;
 };
-constexpr int kMostParts = 256;   // parts of a key/value head's keys
-constexpr int kFillWaves = 2048;  // decode wavefronts that keep the memory busy: two a SIMD
-constexpr int kSplitTiles = 8;    // a wavefront's tiles from which splitting a sequence pays for the join
 
 }  // namespace
 
@@ -361,7 +363,8 @@ template <typename T, int D, int W>
 void launch_decode_w(const Args &a, hipStream_t st)
 {
   const dim3 grid((unsigned)(decode_bases(a) / a.S * (a.parts ? a.parts : a.S))), block(64 * W);
-  // what the last-level cache cannot hold until the next token's call is not kept in the caches at all
+  // What the last-level cache cannot hold until the next token's call is not kept in the caches at all: 131071 keys 85 us so, 97 kept;
+  // 74 MB 15.2 us kept, 16.4 so.
   const bool once = a.R <= kRows && (double)a.S * most_tiles(a) * kTile * a.G * D * 2 * sizeof(T) > 256e6;
   auto go = [&](auto kernel) { BLOSSOM_LAUNCH(kernel, grid, block, 0, st, a); };
   if (!a.parts) {
