@@ -402,7 +402,9 @@ void launch_decode(const Args &a, hipStream_t st)
 //    through a walk, but every tile of keys is moved again for every 16 rows.  (H = 8, G = 2, d = 128, us against the 128-row
 //    kernel: a prompt of 1000 tokens 17 / 25, 64 new tokens over 2000 for 4 sequences 17 / 20; but 500 over 10000 73 / 42, 4 prompts
 //    of 500 24 / 18, 16 of 64 8.6 / 7.6.)
-//  - Otherwise bf16 at d = 64 or 128: 128-row workgroups on the 32x32 instructions; the rest: workgroups of 32 or 64 rows.
+//  - Otherwise bf16 at d = 64 or 128: 128-row workgroups on the 32x32 instructions; the rest, and sequences of 64 rows and 128 keys at
+//    most, which would leave those half empty: workgroups of 32 or 64 rows (256 prompts of 16 tokens, 4 heads, d = 128: 8.8 us
+//    for 11.8; of 64: 16.4 for 19.6; of 100: 31.1 for 30.7).
 // Keys are split over workgroups where these do not fill the chip and a walk has 64 tiles or more: the join costs 4 us and 1 ns a row
 // (500 tokens over 10000: 42 us against 116; 4 prompts of 500: 33 against 18, hence the limit).
 static int shared_rows(const Args &a) { return 16 * shared_waves(a.d * (a.dtype == 0 ? 4 : 2)); }
@@ -413,7 +415,7 @@ static PromptPlan prompt_plan(const Args &a)
   PromptPlan p;
   const long few = groups(kRows);
   if (few <= 640 && few * tiles <= 24000 && (few <= 128 || tiles >= 8)) p.kind = kFew;
-  else p.kind = prompt_mfma_supported(a) ? kMatrix : kShared;
+  else p.kind = prompt_mfma_supported(a) && (all > 64 * a.S || tiles > 4) ? kMatrix : kShared;
   const long want = p.kind == kFew ? 256 / few : 512 / groups(p.kind == kMatrix ? kPromptRows : shared_rows(a));
   const long n = tiles < 64 ? 1 : want < tiles / 16 ? want : tiles / 16;
   p.parts = (int)(n < 1 ? 1 : n > kMostPromptParts ? kMostPromptParts : n);

@@ -56,8 +56,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
   constexpr int LOADS = kKeys / (RPI * kWaves);  // such loads of K a wavefront and tile (and as many of V)
   constexpr int TILE = kKeys * D;
   constexpr int NB = D / 32;             // blocks of 32 channels
-  __shared__ __attribute__((aligned(1024))) uint16_t Ks[STAGES][TILE];
-  __shared__ __attribute__((aligned(1024))) uint16_t Vs[STAGES][TILE];
+  __shared__ __attribute__((aligned(1024))) uint16_t lds[2 * STAGES * TILE];
+  uint16_t(*Ks)[TILE] = reinterpret_cast<uint16_t(*)[TILE]>(lds), (*Vs)[TILE] = Ks + STAGES;
 
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lq = lane & 31, lh = lane >> 5;
@@ -294,23 +294,39 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
 
   // ---- results ----
   l_run += __shfl_xor(l_run, 32);
-  if (!row_ok) return;
   const size_t out = (size_t)(tok0 + tok) * a.H + head;
-  const bool split = a.parts > 1;
-  const float inv = split ? 1.0f : l_run == 0.0f ? 0.0f : 1.0f / l_run;
-  const size_t at = out * a.parts + part;
+  if (a.parts > 1) {  // sums as they are, for the join
+    if (!row_ok) return;
+    const size_t at = out * a.parts + part;
+#pragma unroll
+    for (int mb = 0; mb < NB; ++mb)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<float4 *>(a.part_o + at * D + 32 * mb + 8 * q + 4 * lh) =
+            make_float4(oacc[mb][4 * q], oacc[mb][4 * q + 1], oacc[mb][4 * q + 2], oacc[mb][4 * q + 3]);
+    if (lh == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(l_run == 0.0f ? kNegInf : ref, l_run);
+    return;
+  }
+  // A lane holds pieces of a row: they go through LDS, where the tiles were, so that neighbouring lanes store neighbouring bytes.
+  // Chunk c of row r at c ^ (r modulo a row's chunks).
+  const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
+  char *mine_out = reinterpret_cast<char *>(lds) + wv * (32 * D * 2);
 #pragma unroll
   for (int mb = 0; mb < NB; ++mb)
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float4 x = make_float4(oacc[mb][4 * q] * inv, oacc[mb][4 * q + 1] * inv, oacc[mb][4 * q + 2] * inv, oacc[mb][4 * q + 3] * inv);
-      const size_t to = at * D + 32 * mb + 8 * q + 4 * lh;
-      if (split) *reinterpret_cast<float4 *>(a.part_o + to) = x;
-      else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.O) + to) = make_uint2(mfma::pack2_bf16(x.x, x.y), mfma::pack2_bf16(x.z, x.w));
-    }
-  if (lh != 0) return;
-  if (split) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(l_run == 0.0f ? kNegInf : ref, l_run);
-  else if (a.lse) a.lse[out] = l_run == 0.0f ? kNegInf : (ref + __log2f(l_run)) * kLn2;
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<uint2 *>(mine_out + lq * (D * 2) + (((4 * mb + q) ^ (lq & (CH - 1))) * 16) + 8 * lh) =
+          make_uint2(mfma::pack2_bf16(oacc[mb][4 * q] * inv, oacc[mb][4 * q + 1] * inv), mfma::pack2_bf16(oacc[mb][4 * q + 2] * inv, oacc[mb][4 * q + 3] * inv));
+  if (row_ok && lh == 0 && a.lse) a.lse[out] = l_run == 0.0f ? kNegInf : (ref + __log2f(l_run)) * kLn2;
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (a wavefront reads what it wrote itself)
+#pragma unroll
+  for (int i = 0; i < 32 / RPI; ++i) {
+    const int r = RPI * i + l_row;
+    if (row0 + r >= rows) continue;
+    const uint4 x = *reinterpret_cast<const uint4 *>(mine_out + r * (D * 2) + ((l_ch ^ (r & (CH - 1))) * 16));
+    const int tk = a.by_R.of(row0 + r);
+    *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.O) + ((size_t)(tok0 + tk) * a.H + g * a.R + row0 + r - tk * a.R) * D + 8 * l_ch) = x;
+  }
 }
 
 bool prompt_mfma_supported(const Args &a) { return a.dtype == 1 && (a.d == 64 || a.d == 128); }
