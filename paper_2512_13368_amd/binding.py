@@ -674,9 +674,18 @@ def _check_cache(p: PagedParams, K_cache, V_cache, page_table, cu_seqlens, kv_le
     _check_tensor(kv_len, (p.S,), torch.int32, "kv_len")
 
 
+def _on(stream):
+    """For buffers that a call on `stream` needs: the allocator gives their memory on to that stream's work alone, and not to the
+    current stream's while the call still runs."""
+    import contextlib
+    import torch
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
 def kv_append(p: PagedParams, K, V, K_cache, V_cache, page_table, cu_seqlens, kv_len, Q=None, rope=None, Q_rot=None, stream=None):
     """blossom_kv_append: the new tokens' K and V [T,G,d] go into the cache, K rotated with rope=(cos, sin).  Returns Q_rot
-    [T,H,d], the rotated Q (None without Q).  K, V and Q may be slices of one projection: a token's heads are contiguous."""
+    [T,H,d], the rotated Q (None without Q).  K, V and Q may be slices of one projection: a token's heads are contiguous.
+    What the call allocates belongs to `stream` (the current one if None): memory used elsewhere is the caller's to hold."""
     cos, sin = rope if rope is not None else (None, None)
     if Q is None or Q_rot is not None:
         rc = (_fast or fastcall()).kv_append(p, Q, K, V, cos, sin, page_table, cu_seqlens, kv_len, K_cache, V_cache, Q_rot, stream)
@@ -691,7 +700,8 @@ def kv_append(p: PagedParams, K, V, K_cache, V_cache, page_table, cu_seqlens, kv
     if Q is not None:
         qs = _token_stride(Q, p.T, p.H, p.d, dt, "Q")
         if Q_rot is None:
-            Q_rot = torch.empty((p.T, p.H, p.d), dtype=dt, device=Q.device)
+            with _on(stream):
+                Q_rot = torch.empty((p.T, p.H, p.d), dtype=dt, device=Q.device)
     _check_tensor(Q_rot, (p.T, p.H, p.d), dt, "Q_rot")
     if cu_seqlens is None:
         raise ValueError("cu_seqlens is required")
@@ -712,13 +722,14 @@ def _paged_attn(p: PagedParams, which, rows, Q, K_cache, V_cache, page_table, cu
     dt = _torch_dtype(p)
     qs = _token_stride(Q, rows, p.H, p.d, dt, "Q")
     _check_cache(p, K_cache, V_cache, page_table, cu_seqlens, kv_len)
-    if O is None:
-        O = torch.empty((rows, p.H, p.d), dtype=dt, device=Q.device)
+    need = paged_workspace_bytes(p, which)
+    with _on(stream):
+        if O is None:
+            O = torch.empty((rows, p.H, p.d), dtype=dt, device=Q.device)
+        if ws is None and need > 0:
+            ws = torch.empty(need, dtype=torch.uint8, device=Q.device)
     _check_tensor(O, (rows, p.H, p.d), dt, "O")
     _check_tensor(lse, (rows, p.H), torch.float32, "lse")
-    need = paged_workspace_bytes(p, which)
-    if ws is None and need > 0:
-        ws = torch.empty(need, dtype=torch.uint8, device=Q.device)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
     cp = p.c()
     head = (ctypes.byref(cp), _ptr(Q), qs, _ptr(K_cache), _ptr(V_cache), _ptr(page_table))

@@ -376,6 +376,33 @@ def test_other_streams_and_graphs():
         assert torch.equal(O, got[0]) and torch.equal(lse, got[1]), f"replay {k}"
 
 
+def test_buffers_of_a_call_belong_to_its_stream(monkeypatch):
+    """Memory given on to the current stream's work while a call on another still runs would be written twice."""
+    c = Cache([3000, 17, 400], 8, 2, 64, 16, "bf16", seed=5, new=[1, 1, 1])
+    assert B.paged_workspace_bytes(c.p, B.WS_DECODE) > 0
+    Kc, Vc, table, cu, kv_len = c.dev()
+    dq = c.normal(3, 8, 64).cuda()
+    cos, sin = (x.cuda() for x in rope(c.cap, 64))
+    k, v = c.normal(3, 2, 64).cuda(), c.normal(3, 2, 64).cuda()
+    empty, on = torch.empty, []
+
+    def noted(*args, **kw):
+        on.append(torch.cuda.current_stream())
+        return empty(*args, **kw)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    monkeypatch.setattr(torch, "empty", noted)
+    Q_rot = B.kv_append(c.p, k, v, Kc, Vc, table, cu, kv_len, Q=dq, rope=(cos, sin), stream=side)
+    O, _ = B.attn_decode(c.p, Q_rot, Kc, Vc, table, kv_len, stream=side)
+    P, _ = B.attn_prompt(c.p, Q_rot, Kc, Vc, table, cu, kv_len, stream=side)
+    monkeypatch.undo()
+    side.synchronize()
+    assert len(on) >= 4 and all(s == side for s in on)
+    again, _ = B.attn_decode(c.p, Q_rot, Kc, Vc, table, kv_len)
+    assert torch.equal(O, again) and O.shape == P.shape
+
+
 def test_the_python_path_gives_the_same(monkeypatch):
     c = Cache([40, 0, 9], 4, 2, 64, 16, "bf16", new=[5, 0, 9], seed=1)
     Kc, Vc, table, cu, kv_len = c.dev()
