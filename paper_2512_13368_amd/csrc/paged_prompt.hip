@@ -10,11 +10,12 @@
 //  - O^T += V^T P^T with P^T straight from the accumulator registers (rounded to bf16, as the matrix instruction wants them; the
 //    sum is of the unrounded ones) and V^T through the transposing LDS read.
 //
-// Measured: two prompts of 6001 and 8191 tokens, 32 heads over 8, d = 128: 830 us, 1.02 PFLOP/s, where a bf16 product of 8192^3 takes
-// 1.06; chunks of 512 over a window of 4096: 134 us, 850 TFLOP/s; 32 ragged prompts of 7 to 1997, 16 heads over 4, d = 64: 130 us,
-// 680 TFLOP/s.  The matrix pipe is busy 45 % (d = 64: 37 %) and the vector ALUs' issue port 46 % (72 %) of the time: a half tile's 16
-// exponentials alone are 256 cycles beside 512 (256) of products, and the two overlap in part.  Tried: both halves' logits before the
-// exponentials (848 us, 137, 137), three wavefronts a SIMD instead of four at d = 64 (154 us against 143 at the time).
+// Measured: two prompts of 6001 and 8191 tokens, 32 heads over 8, d = 128: 824 to 850 us, 1.0 PFLOP/s, where a bf16 product of 8192^3
+// reaches 1.07; chunks of 512 over a window of 4096: 134 us, 850 TFLOP/s; 32 ragged prompts of 7 to 1997, 16 heads over 4, d = 64:
+// 125 us, 710 TFLOP/s.  The matrix pipe is busy 52 % (d = 64: 40 %) and the vector ALUs' issue port 48 % (77 %) of the time: a half
+// tile's 16 exponentials alone are 256 cycles beside 512 (256) of products, and the two overlap in part.  Tried: both halves' logits
+// before the exponentials (848 against 836 us, 137 against 134 and 129), three wavefronts a SIMD instead of four at d = 64 (154 us
+// against 143 at the time).
 #include "common.h"
 #include "launch.h"
 #include "mfma_common.h"
