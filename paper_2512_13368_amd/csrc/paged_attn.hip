@@ -260,7 +260,7 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
 
 // Joins the parts of a sequence's row, where it has more than one: a workgroup a row, whose threads take a part each for the weights
 // and then, 4 channels each, every (256 / (d / 4))-th part's sums.  Parts that met no key have weight 0 and finite sums.
-template <typename T, int D, bool PROMPT>
+template <typename T, int D>
 __global__ __launch_bounds__(256) void join_kernel(Args a)
 {
   constexpr int LANES = D / 4, GROUPS = 256 / LANES;
@@ -268,22 +268,16 @@ __global__ __launch_bounds__(256) void join_kernel(Args a)
   __shared__ __attribute__((aligned(16))) float o_s[GROUPS][D];
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   T *O = static_cast<T *>(a.O) + (size_t)blockIdx.x * D;
-  int n = a.parts;
-  size_t at0 = (size_t)blockIdx.x * a.parts;
-  if constexpr (PROMPT) {
-    if (a.by_H.of(blockIdx.x) >= token_at(a, a.S)) return;  // (a row that no sequence owns stays as it is)
-  } else {
-    const int s = a.by_H.of(blockIdx.x), h = blockIdx.x - s * a.H;
-    const int2 part = a.part_of[s];  // (of a sequence without keys: whatever the workspace held)
-    n = __builtin_amdgcn_readfirstlane(tiles_of(a, s) > 0 ? part.y : 0);
-    if (n <= 1) {
-      if (n == 1) return;  // (the part's workgroup wrote the row)
-      if (tid < D) store_out(O + tid, 0.0f);
-      if (tid == 0 && a.lse) a.lse[blockIdx.x] = kNegInf;
-      return;
-    }
-    at0 = (size_t)h * a.parts + part.x;
+  const int s = a.by_H.of(blockIdx.x), h = blockIdx.x - s * a.H;
+  const int2 part = a.part_of[s];  // (of a sequence without keys: whatever the workspace held)
+  const int n = __builtin_amdgcn_readfirstlane(tiles_of(a, s) > 0 ? part.y : 0);
+  if (n <= 1) {
+    if (n == 1) return;  // (the part's workgroup wrote the row)
+    if (tid < D) store_out(O + tid, 0.0f);
+    if (tid == 0 && a.lse) a.lse[blockIdx.x] = kNegInf;
+    return;
   }
+  const size_t at0 = (size_t)h * a.parts + part.x;
   const float *ml = a.part_ml + at0 * 2;
   const float4 *po = reinterpret_cast<const float4 *>(a.part_o + at0 * D);
   const int at = tid % LANES, grp = tid / LANES;
@@ -324,6 +318,41 @@ __global__ __launch_bounds__(256) void join_kernel(Args a)
     store_out(O + tid, l == 0.0f ? 0.0f : sum / l);
   }
   if (tid == 0 && a.lse) a.lse[blockIdx.x] = l == 0.0f ? kNegInf : (m + __log2f(l)) * kLn2;
+}
+
+// Joins the parts of prompt rows: D / 4 threads a row, 4 channels each, every part's weight computed by all of them.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void join_rows_kernel(Args a)
+{
+  constexpr int LANES = D / 4, ROWS = 256 / LANES, AHEAD = 8;
+  const int at = threadIdx.x % LANES;
+  const size_t row = (size_t)blockIdx.x * ROWS + threadIdx.x / LANES;
+  if (row >= (size_t)token_at(a, a.S) * a.H) return;  // (a row that no sequence owns stays as it is)
+  const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + row * a.parts;
+  const float4 *po = reinterpret_cast<const float4 *>(a.part_o) + row * a.parts * LANES + at;
+  float m = kNegInf;
+  for (int i = 0; i < a.parts; ++i) m = fmaxf(m, ml[i].x);
+  const float ref = m == kNegInf ? 0.0f : m;
+  float l = 0.0f;
+  float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int i = 0; i < a.parts; i += AHEAD) {
+    float4 v[AHEAD];
+    float2 x[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const int j = min(i + k, a.parts - 1);
+      v[k] = po[(size_t)j * LANES];
+      x[k] = ml[j];
+    }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const float w = i + k < a.parts ? __builtin_amdgcn_exp2f(x[k].x - ref) : 0.0f;
+      l = fmaf(x[k].y, w, l);
+      o.x = fmaf(v[k].x, w, o.x); o.y = fmaf(v[k].y, w, o.y); o.z = fmaf(v[k].z, w, o.z); o.w = fmaf(v[k].w, w, o.w);
+    }
+  }
+  store_four(static_cast<T *>(a.O) + row * D + 4 * at, o, l == 0.0f ? 0.0f : 1.0f / l);
+  if (at == 0 && a.lse) a.lse[row] = l == 0.0f ? kNegInf : (m + __log2f(l)) * kLn2;
 }
 
 namespace {
@@ -375,7 +404,7 @@ void launch_decode_w(const Args &a, hipStream_t st)
   if (once) go(decode_kernel<T, D, W, true, true, false>);
   else go(decode_kernel<T, D, W, false, true, false>);
   if (launch_failed()) return;
-  BLOSSOM_LAUNCH((join_kernel<T, D, false>), dim3((unsigned)(a.S * a.H)), dim3(256), 0, st, a);
+  BLOSSOM_LAUNCH((join_kernel<T, D>), dim3((unsigned)(a.S * a.H)), dim3(256), 0, st, a);
 }
 
 template <typename T, int D>
@@ -399,25 +428,39 @@ void launch_decode(const Args &a, hipStream_t st)
 
 // Which kernel takes a prompt call, and into how many parts a row's keys go.
 //  - Few 16-row tiles: their keys are shared out over the wavefronts of a workgroup each, as in decode.  That is the shortest way
-//    through a walk, but every tile of keys is moved again for every 16 rows.  (H = 8, G = 2, d = 128, us against the 128-row
-//    kernel: a prompt of 1000 tokens 17 / 25, 64 new tokens over 2000 for 4 sequences 17 / 20; but 500 over 10000 73 / 42, 4 prompts
-//    of 500 24 / 18, 16 of 64 8.6 / 7.6.)
+//    through a walk, but every tile of keys is moved again for every 16 rows, and the fewer wavefronts a CU holds (rows of 256 bytes
+//    and more), the sooner that tells.  (H = 8, G = 2, us against the other kernels, split: 500 new tokens over 1500, d = 64: 11 / 16,
+//    d = 128: 16 / 20; 300 over 3700, d = 64: 17 / 18, d = 128: 28 / 24; fp32 at d = 128 200 over 4000: 64 / 53.)
 //  - Otherwise bf16 at d = 64 or 128: 128-row workgroups on the 32x32 instructions; the rest, and sequences of 64 rows and 128 keys at
 //    most, which would leave those half empty: workgroups of 32 or 64 rows (256 prompts of 16 tokens, 4 heads, d = 128: 8.8 us
 //    for 11.8; of 64: 16.4 for 19.6; of 100: 31.1 for 30.7).
-// Keys are split over workgroups where these do not fill the chip and a walk has 64 tiles or more: the join costs 4 us and 1 ns a row
-// (500 tokens over 10000: 42 us against 116; 4 prompts of 500: 33 against 18, hence the limit).
+// Keys are split over workgroups where these do not fill the chip: up to as many as it holds at once (twice, four times as many: 54, 69
+// us for 43 where 500 tokens see 10000 at d = 128), or of the small ones to eight wavefronts a SIMD, which even out ragged walks (one fp32 prompt of 8000 tokens, 2
+// heads, d = 16: 211 us whole, 115, 77, 66 and 63 for 2, 4, 8 and 16 wavefronts a SIMD; 6 of 1408 to 4225, bf16, d = 8: 85 us
+// whole, 85, 35, 22 and 27).  A part has 8 tiles at least (500 over 1500 at d = 64 in the 128-row kernel: 39 us whole, 20 in parts of 16
+// tiles, 16 of 8, 18 of 4), and 64 where parts are many, for the join walks them one after another (16 tokens over 30000, one head,
+// d = 128: 18 us in 32 parts, 20 in 64; over 131000: 36 and 30).
 static int shared_rows(const Args &a) { return 16 * shared_waves(a.d * (a.dtype == 0 ? 4 : 2)); }
 static PromptPlan prompt_plan(const Args &a)
 {
   const long all = (long)a.T * a.R, tiles = most_tiles(a);
   auto groups = [&](int rows) { return (all / rows + (a.S == 1 ? (all % rows != 0) : a.S)) * a.G; };  // workgroups, nearly
+  const int row_bytes = a.d * (a.dtype == 0 ? 4 : 2);
+  const long few = groups(kRows), most_few = row_bytes >= 512 ? 12000 : row_bytes >= 256 ? 16000 : 24000;
   PromptPlan p;
-  const long few = groups(kRows);
-  if (few <= 640 && few * tiles <= 24000 && (few <= 128 || tiles >= 8)) p.kind = kFew;
-  else p.kind = prompt_mfma_supported(a) && (all > 64 * a.S || tiles > 4) ? kMatrix : kShared;
-  const long want = p.kind == kFew ? 256 / few : 512 / groups(p.kind == kMatrix ? kPromptRows : shared_rows(a));
-  const long n = tiles < 64 ? 1 : want < tiles / 16 ? want : tiles / 16;
+  long want;
+  if (few <= 640 && few * tiles <= most_few && (few <= 128 || tiles >= 8)) {
+    p.kind = kFew;
+    want = 256 / few;
+  } else if (prompt_mfma_supported(a) && (all > 64 * a.S || tiles > 4)) {
+    p.kind = kMatrix;
+    want = (a.d == 64 ? 1024 : 512) / groups(kPromptRows);
+  } else {
+    p.kind = kShared;
+    want = 8192 / (groups(shared_rows(a)) * shared_waves(row_bytes));
+  }
+  const long most = tiles < 32 ? 1 : tiles / 64 > 32 ? tiles / 64 : tiles / 8 < 32 ? tiles / 8 : 32;
+  const long n = want < most ? want : most;
   p.parts = (int)(n < 1 ? 1 : n > kMostPromptParts ? kMostPromptParts : n);
   return p;
 }
@@ -442,7 +485,7 @@ void launch_prompt(const Args &call, hipStream_t st)
       else BLOSSOM_LAUNCH((decode_kernel<T, D, W, false, false, true>), grid, block, 0, st, a);
     }
     if (a.parts > 1 && !launch_failed())
-      BLOSSOM_LAUNCH((join_kernel<T, D, true>), dim3((unsigned)(a.T * a.H)), dim3(256), 0, st, a);
+      BLOSSOM_LAUNCH((join_rows_kernel<T, D>), dim3((unsigned)((size_t)a.T * a.H * (D / 4) / 256 + 1)), dim3(256), 0, st, a);
   });
 }
 
