@@ -430,7 +430,9 @@ void launch_decode(const Args &a, hipStream_t st)
 //  - Few 16-row tiles: their keys are shared out over the wavefronts of a workgroup each, as in decode.  That is the shortest way
 //    through a walk, but every tile of keys is moved again for every 16 rows, and the fewer wavefronts a CU holds (rows of 256 bytes
 //    and more), the sooner that tells.  (H = 8, G = 2, us against the other kernels, split: 500 new tokens over 1500, d = 64: 11 / 16,
-//    d = 128: 16 / 20; 300 over 3700, d = 64: 17 / 18, d = 128: 28 / 24; fp32 at d = 128 200 over 4000: 64 / 53.)
+//    d = 128: 16 / 20; 300 over 3700, d = 64: 17 / 18, d = 128: 28 / 24; fp32 at d = 128 200 over 4000: 64 / 53.)  Short walks go that
+//    way where such workgroups are one a CU at most (172 of them, 35 new tokens over 105 for 4 sequences, fp32 at d = 128: 9.7 us / 17.8;
+//    448, 16 prompts of 20 to 60, d = 64: 8.8 / 6.8).
 //  - Otherwise bf16 at d = 64 or 128: 128-row workgroups on the 32x32 instructions; the rest, and sequences of 64 rows and 128 keys at
 //    most, which would leave those half empty: workgroups of 32 or 64 rows (256 prompts of 16 tokens, 4 heads, d = 128: 8.8 us
 //    for 11.8; of 64: 16.4 for 19.6; of 100: 31.1 for 30.7).
@@ -449,7 +451,7 @@ static PromptPlan prompt_plan(const Args &a)
   const long few = groups(kRows), most_few = row_bytes >= 512 ? 12000 : row_bytes >= 256 ? 16000 : 24000;
   PromptPlan p;
   long want;
-  if (few <= 640 && few * tiles <= most_few && (few <= 128 || tiles >= 8)) {
+  if (few <= 640 && few * tiles <= most_few && (few <= 256 || tiles >= 8)) {
     p.kind = kFew;
     want = 256 / few;
   } else if (prompt_mfma_supported(a) && (all > 64 * a.S || tiles > 4)) {
