@@ -84,7 +84,7 @@ __global__ __launch_bounds__(64 * shared_waves(D * sizeof(T))) void shared_kerne
   };
 
   Rows<T, D> r;
-  r.clear();
+  r.clear(row_ok);
   unsigned seen = t < t_end ? request(t, lds[0]) : 0u;
 #pragma unroll
   for (int i = 0; i < TL::NK; ++i) asm volatile("" : "+v"(q.x[i].x), "+v"(q.x[i].y), "+v"(q.x[i].z), "+v"(q.x[i].w));  // (arrived before the walk)

@@ -202,15 +202,19 @@ __device__ __forceinline__ float row_max(float x)
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// A wavefront's 16 rows over the tiles it has met: running maximum (log2 units) and sum in fp32, unnormalised output.
+// A wavefront's 16 rows over the tiles it has met: reference (log2 units) and sum in fp32, unnormalised output.  The reference is a
+// row's maximum over the first keys it met; it is raised only when a lane's eight probabilities of a tile pass kSumLimit in sum, so the
+// usual tile takes no maximum.
+constexpr float kSumLimit = 4096.0f;
 template <typename T, int D>
 struct Rows {
   typedef Tile<T, D> TL;
   f32x4 acc[TL::NV];
-  float m, l;  // (l: this lane's keys alone)
-  __device__ __forceinline__ void clear()
+  float m, l;  // (l: this lane's keys alone; m is -inf while the row has met no key)
+  // (a row that is nobody's, `on` false, never meets one and need not be waited for)
+  __device__ __forceinline__ void clear(bool on = true)
   {
-    m = mfma::kNegInf;
+    m = on ? mfma::kNegInf : 0.0f;
     l = 0.0f;
 #pragma unroll
     for (int j = 0; j < TL::NV; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -221,16 +225,16 @@ struct Rows {
                                          int lane)
   {
     const int n = lane & 15, c = lane >> 4;
-    float p[8];
+    float s[8], p[8];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       if (h == 0 || both) {
-        const f32x4 s = TL::logits(ks, h, n, c, q);
+        const f32x4 x = TL::logits(ks, h, n, c, q);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[4 * h + i] = s[i] * scale2;
+        for (int i = 0; i < 4; ++i) s[4 * h + i] = x[i];
       } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[4 * h + i] = mfma::kNegInf;
+        for (int i = 0; i < 4; ++i) s[4 * h + i] = mfma::kNegInf;
       }
     }
     if (!all) {
@@ -238,22 +242,33 @@ struct Rows {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[4 * h + i] = mine >> (16 * h + i) & 1 ? p[4 * h + i] : mfma::kNegInf;
+        for (int i = 0; i < 4; ++i) s[4 * h + i] = mine >> (16 * h + i) & 1 ? s[4 * h + i] : mfma::kNegInf;
     }
-    float mx = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
-    mx = fmaxf(m, row_max(mx));
-    const float ref = mx == mfma::kNegInf ? 0.0f : mx;  // no key seen yet: every exponential is 0
-    const float f = __builtin_amdgcn_exp2f(m - ref);
-    m = mx;
-    float sum = 0.0f;
+    bool place = __any(m == mfma::kNegInf);
+    float sum;
+#pragma unroll 1
+    for (;;) {
+      float ref = m;
+      if (place) {
+        const float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+        const float to = fmaxf(m, row_max(mx) * scale2);
+        ref = to == mfma::kNegInf ? 0.0f : to;  // no key seen yet: every exponential is 0
+        const float f = __builtin_amdgcn_exp2f(m - ref);
+        m = to;
+        l *= f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(p[i] - ref);
-      sum += p[i];
+        for (int j = 0; j < TL::NV; ++j) acc[j] *= f;
+      }
+      sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale2, -ref));
+        sum += p[i];
+      }
+      if (place || !__any(!(sum <= kSumLimit))) break;
+      place = true;
     }
-    l = l * f + sum;
-#pragma unroll
-    for (int j = 0; j < TL::NV; ++j) acc[j] *= f;
+    l += sum;
     TL::product(vs, p, both, lane, acc);
   }
   __device__ __forceinline__ float total() const
