@@ -30,7 +30,11 @@ using mfma::kNegInf;
 constexpr int kRows = 16;             // query rows of a workgroup
 constexpr int kMostParts = 256;       // parts of a key/value head's keys
 constexpr int kMostPromptParts = 64;  // parts of a row's keys in a prompt
-constexpr int kFillWaves = 2048;      // decode wavefronts that keep the memory busy: two a SIMD (4096: 88 us for 85 at 131071 keys, 16.0 for 15.2 on short ones)
+// Decode wavefronts that keep the memory busy: two a SIMD (four: 88 us for 85 at 131071 keys, 16.0 for 15.2 on short ones).  Four where rows
+// are small, which take as long to work on (67201 keys with a window of 29264, 3 sequences, 8 heads, fp32, d = 8: 20 us for 28.5; 13 of
+// 1462 to 14625, 32 heads over 4, bf16, d = 32: 17.1 for 18.4), one where a CU's LDS holds no more (131000 keys, 8 heads over 2, fp32,
+// d = 128: 59 for 65; 20106 for 2 sequences, 6 over 2: 24 for 35).
+constexpr int fill_waves(int row_bytes) { return row_bytes <= 64 ? 4096 : row_bytes <= 256 ? 2048 : 1024; }
 // A wavefront's tiles from which splitting a sequence pays for the join (8 heads over 2, d = 128, one sequence: 32 tiles over 8
 // wavefronts 8.8 us whole and 10.8 split, 63 tiles 13.9 and 10.8; fp32 at d = 32: 9.4 and 11.0, 16.9 and 12.1).
 constexpr int kSplitTiles = 6;
@@ -364,12 +368,14 @@ long most_tiles(const Args &a)
 }
 long decode_bases(const Args &a) { return (long)a.S * a.G * ((a.R + kRows - 1) / kRows); }
 
+int row_bytes_of(const Args &a) { return a.d * (a.dtype == 0 ? 4 : 2); }
+
 // Wavefronts of a decode workgroup: more of them where workgroups are few, as far as registers and keys go.
 int decode_waves(const Args &a)
 {
-  const int most = most_decode_waves(a.d * (a.dtype == 0 ? 4 : 2));
+  const int most = most_decode_waves(row_bytes_of(a)), fill = fill_waves(row_bytes_of(a));
   int w = most < 4 ? most : 4;
-  while (w < most && decode_bases(a) * w < kFillWaves && most_tiles(a) >= 2 * w) w *= 2;
+  while (w < most && decode_bases(a) * w < fill && most_tiles(a) >= 2 * w) w *= 2;
   return w;
 }
 
@@ -377,11 +383,11 @@ int decode_waves(const Args &a)
 
 int decode_parts(const Args &a)
 {
-  const int w = decode_waves(a);
+  const int w = decode_waves(a), fill = fill_waves(row_bytes_of(a));
   const long heads = (long)a.G * ((a.R + kRows - 1) / kRows);
-  if (decode_bases(a) * w >= kFillWaves || most_tiles(a) < kSplitTiles * w) return 0;
+  if (decode_bases(a) * w >= fill || most_tiles(a) < kSplitTiles * w) return 0;
   if (a.S * most_tiles(a) > 1 << 22) return 0;  // (parts are counted in 32 bits and cut in fp32)
-  const long parts = kFillWaves / w / heads, most = a.S * ((most_tiles(a) + 2 * w - 1) / (2 * w));
+  const long parts = fill / w / heads, most = a.S * ((most_tiles(a) + 2 * w - 1) / (2 * w));
   const long n = parts < most ? parts : most;
   return (int)(n >= 2 * a.S ? (n > kMostParts ? kMostParts : n) : 0);
 }
@@ -442,12 +448,12 @@ void launch_decode(const Args &a, hipStream_t st)
 // whole, 85, 35, 22 and 27).  A part has 8 tiles at least (500 over 1500 at d = 64 in the 128-row kernel: 39 us whole, 20 in parts of 16
 // tiles, 16 of 8, 18 of 4), and 64 where parts are many, for the join walks them one after another (16 tokens over 30000, one head,
 // d = 128: 18 us in 32 parts, 20 in 64; over 131000: 36 and 30).
-static int shared_rows(const Args &a) { return 16 * shared_waves(a.d * (a.dtype == 0 ? 4 : 2)); }
+static int shared_rows(const Args &a) { return 16 * shared_waves(row_bytes_of(a)); }
 static PromptPlan prompt_plan(const Args &a)
 {
   const long all = (long)a.T * a.R, tiles = most_tiles(a);
   auto groups = [&](int rows) { return (all / rows + (a.S == 1 ? (all % rows != 0) : a.S)) * a.G; };  // workgroups, nearly
-  const int row_bytes = a.d * (a.dtype == 0 ? 4 : 2);
+  const int row_bytes = row_bytes_of(a);
   const long few = groups(kRows), most_few = row_bytes >= 512 ? 12000 : row_bytes >= 256 ? 16000 : 24000;
   PromptPlan p;
   long want;
