@@ -10,7 +10,7 @@
 //  - O^T += V^T P^T with P^T straight from the accumulator registers (rounded to bf16, as the matrix instruction wants them; the
 //    sum is of the unrounded ones) and V^T through the transposing LDS read.
 //
-// Measured: two prompts of 6001 and 8191 tokens, 32 heads over 8, d = 128: 824 to 850 us, 1.0 PFLOP/s, where a bf16 product of 8192^3
+// Measured: two prompts of 6001 and 8191 tokens, 32 heads over 8, d = 128: 819 to 850 us, 1.0 PFLOP/s, where a bf16 product of 8192^3
 // reaches 1.07; chunks of 512 over a window of 4096: 134 us, 850 TFLOP/s; 32 ragged prompts of 7 to 1997, 16 heads over 4, d = 64:
 // 125 us, 710 TFLOP/s.  The matrix pipe is busy 52 % (d = 64: 40 %) and the vector ALUs' issue port 48 % (77 %) of the time: a half
 // tile's 16 exponentials alone are 256 cycles beside 512 (256) of products, and the two overlap in part.  Tried: both halves' logits

@@ -3,7 +3,7 @@
 // A workgroup's two wavefronts (four where a row is 256 bytes or more) take 16 rows each of one key/value head, (token, head of the
 // group) pairs, and walk the 32-key tiles that any of them sees.  A tile is moved to LDS once, one step ahead, and read by all.
 // Short ragged prompts are bound by the matrix pipe and the vector ALUs, which do not overlap for fp32 products (256 prompts of 20
-// to 200 tokens, 2 heads, d = 32: 15.7 us, of which the products take 4.6 and the exponentials and the rest 3 at full balance).
+// to 200 tokens, 2 heads, d = 32: 15.4 us, of which the products take 4.6 and the exponentials and the rest 3 at full balance).
 // Tried: rings of 3, 4 and 6 tiles (23.3, 24.6, 25.4 us where 2 took 23.0), results through LDS (no gain), one wavefront a
 // workgroup without barriers (as fast, slower from d = 64 on), two for large rows (d = 64 fp32: 72 us against 61).
 #include "common.h"

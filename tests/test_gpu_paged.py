@@ -565,3 +565,63 @@ def test_append_of_more_than_the_caches_hold(dtype):
         rows = B.kv_append(part, k[lo:hi], v[lo:hi], *caches[1], table, ints(0, hi - lo), ints(hi), Q=q[lo:hi], rope=(cos, sin))
         assert torch.equal(rows, whole[lo:hi])
     assert torch.equal(caches[0][0], caches[1][0]) and torch.equal(caches[0][1], caches[1][1])
+
+
+# ---- walks of middle length: parts of a few tiles, joined by a few threads a row; the running reference of every type
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("window", [0, 1500])
+def test_middle_walks_are_split_and_joined(dtype, d, window):
+    c = Cache([1100, 37, 2047, 0], 6, 2, d, 16, dtype, new=[900, 37, 600, 0], window=window, seed=d + 1)
+    assert B.paged_workspace_bytes(c.p, B.WS_PROMPT) > 0
+    c.table[2, 0, 5] = -1
+    Q, O, lse = run_prompt(c, strided=True)
+    check(O, lse, *c.want_prompt(Q), dtype)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_a_few_tokens_over_middle_pasts(dtype, d):
+    c = Cache([1500, 40, 1030], 4, 2, d, 32, dtype, new=[10, 3, 33], seed=d + 2)
+    assert B.paged_workspace_bytes(c.p, B.WS_PROMPT) > 0
+    Q, O, lse = run_prompt(c)
+    check(O, lse, *c.want_prompt(Q), dtype)
+
+
+def growing(c, n, d):
+    """Keys whose logits grow along a sequence to some 200, every seventh's sign turned."""
+    ids = c.table[0, 0].astype(np.int64)
+    for j in range(n):
+        c.K_cache[int(ids[j // 16]), 0, j % 16] = (j / float(n)) ** 2 * 40.0 * (32 / d) ** 0.5 * (1.0 if j % 7 else -1.0)
+
+
+def check_grown(O, lse, want_O, want_lse, dtype, d):
+    """check(), with room for the logits' own rounding: sums of d products in 32 bits are off by d 2^-24 of a logit at most (its
+    products have one sign), the weights relatively by as much, and with them numerator and denominator of an output."""
+    room = 2 * d * 2.0**-24 * float(want_lse.max()) * float(want_O.abs().max())
+    got = O.double().cpu()
+    near = torch.where((got - want_O).abs() <= room, want_O, got - room * (got - want_O).sign())
+    check(near, lse, want_O, want_lse, dtype)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("tokens", [20, 200])
+def test_logits_that_grow_along_the_keys_in_every_type(dtype, d, tokens):
+    c = Cache([900] + [0] * (CROWD if tokens == 200 else 0), 2, 1, d, 16, dtype, new=[tokens] + [0] * (CROWD if tokens == 200 else 0), seed=d)
+    growing(c, 900, d)
+    Q, O, lse = run_prompt(c, Q=(c.normal(tokens, 2, d).abs() * 0.5 + 0.5).to(DTYPES[dtype]))
+    check_grown(O, lse, *c.want_prompt(Q), dtype, d)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_decode_logits_that_grow_along_the_keys(dtype, d):
+    c = Cache([900], 2, 1, d, 16, dtype, seed=d)
+    growing(c, 900, d)
+    Q, O, lse = run_decode(c, Q=(c.normal(1, 2, d).abs() * 0.5 + 0.5).to(DTYPES[dtype]))
+    check_grown(O, lse, *c.want_decode(Q), dtype, d)
+
+
+@pytest.mark.parametrize("dtype,d", [("fp32", 8), ("bf16", 32), ("fp32", 128)])
+def test_decode_parts_of_small_and_large_rows(dtype, d):
+    c = Cache([9000, 3000], 4, 2, d, 16, dtype, seed=d)
+    assert B.paged_workspace_bytes(c.p, B.WS_DECODE) > 0
+    Q, O, lse = run_decode(c)
+    check(O, lse, *c.want_decode(Q), dtype)
