@@ -10,7 +10,7 @@
 // kernel joins.  Large prompts: paged_prompt.hip, paged_shared.hip.  The operands and the softmax of a step: paged_tile.h.
 //
 // Measured: one sequence of 131071 keys (32 heads over 8, d = 128, bf16: 537 MB) 85 us, 80 of it in this kernel, where reading as many
-// bytes takes 78; 16 sequences of 4001 to 8191 keys (400 MB) 71 us, the join 3.5 of it; 128 of 100 to 1024 (4 heads, d = 64: 74 MB)
+// bytes takes 78; 16 sequences of 4001 to 8191 keys (400 MB) 71 us, the join 4.6 of it; 128 of 100 to 1024 (4 heads, d = 64: 74 MB)
 // 15 us, where a read takes 11 and a launch with its first loads 4; the join inside the kernel would save 3 us of 85 and nothing
 // where sequences are short.
 #include "common.h"
@@ -447,7 +447,9 @@ void launch_decode(const Args &a, hipStream_t st)
 // heads, d = 16: 211 us whole, 115, 77, 66 and 63 for 2, 4, 8 and 16 wavefronts a SIMD; 6 of 1408 to 4225, bf16, d = 8: 85 us
 // whole, 85, 35, 22 and 27).  A part has 8 tiles at least (500 over 1500 at d = 64 in the 128-row kernel: 39 us whole, 20 in parts of 16
 // tiles, 16 of 8, 18 of 4), and 64 where parts are many, for the join walks them one after another (16 tokens over 30000, one head,
-// d = 128: 18 us in 32 parts, 20 in 64; over 131000: 36 and 30).
+// d = 128: 18 us in 32 parts, 20 in 64; over 131000: 36 and 30).  Walks are split from 32 tiles on (from 16: 22 us for 15 at 19 bf16 prompts
+// of 168 to 505, d = 64), of the small workgroups from 24 (8 prompts of 500 to 900, 4 heads, d = 16: 19 us for 27), in fp32, whose
+// tiles take longer, from 16 (4 prompts of 300 to 510, 8 heads, d = 64: 26 for 30; bf16, 30 prompts of 200 to 500, d = 32: 17 for 14).
 static int shared_rows(const Args &a) { return 16 * shared_waves(row_bytes_of(a)); }
 static PromptPlan prompt_plan(const Args &a)
 {
@@ -467,7 +469,7 @@ static PromptPlan prompt_plan(const Args &a)
     p.kind = kShared;
     want = 8192 / (groups(shared_rows(a)) * shared_waves(row_bytes));
   }
-  const long most = tiles < 32 ? 1 : tiles / 64 > 32 ? tiles / 64 : tiles / 8 < 32 ? tiles / 8 : 32;
+  const long most = tiles < (p.kind != kShared ? 32 : a.dtype == 0 ? 16 : 24) ? 1 : tiles / 64 > 32 ? tiles / 64 : tiles / 8 < 32 ? tiles / 8 : 32;
   const long n = want < most ? want : most;
   p.parts = (int)(n < 1 ? 1 : n > kMostPromptParts ? kMostPromptParts : n);
   return p;
