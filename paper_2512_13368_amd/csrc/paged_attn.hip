@@ -36,8 +36,9 @@ constexpr int kMostPromptParts = 64;  // parts of a row's keys in a prompt
 // d = 128: 59 for 65; 20106 for 2 sequences, 6 over 2: 24 for 35).
 constexpr int fill_waves(int row_bytes) { return row_bytes <= 64 ? 4096 : row_bytes <= 256 ? 2048 : 1024; }
 // A wavefront's tiles from which splitting a sequence pays for the join (8 heads over 2, d = 128, one sequence: 32 tiles over 8
-// wavefronts 8.8 us whole and 10.8 split, 63 tiles 13.9 and 10.8; fp32 at d = 32: 9.4 and 11.0, 16.9 and 12.1).
-constexpr int kSplitTiles = 6;
+// wavefronts 8.8 us whole and 10.8 split, 63 tiles 13.9 and 10.8; fp32 at d = 32: 9.4 and 11.0, 16.9 and 12.1).  Large fp32 rows, whose tiles
+// take longest, from 4 on (4 sequences, 8 heads over 4: 500 keys at d = 128 16.8 and 14.4, 1000 at d = 64 14.5 and 13.4).
+constexpr int split_tiles(int dtype, int d) { return dtype == 0 && d >= 64 ? 4 : 6; }
 
 enum PromptKind { kFew, kShared, kMatrix };
 struct PromptPlan {
@@ -385,7 +386,7 @@ int decode_parts(const Args &a)
 {
   const int w = decode_waves(a), fill = fill_waves(row_bytes_of(a));
   const long heads = (long)a.G * ((a.R + kRows - 1) / kRows);
-  if (decode_bases(a) * w >= fill || most_tiles(a) < kSplitTiles * w) return 0;
+  if (decode_bases(a) * w >= fill || most_tiles(a) < split_tiles(a.dtype, a.d) * w) return 0;
   if (a.S * most_tiles(a) > 1 << 22) return 0;  // (parts are counted in 32 bits and cut in fp32)
   const long parts = fill / w / heads, most = a.S * ((most_tiles(a) + 2 * w - 1) / (2 * w));
   const long n = parts < most ? parts : most;
