@@ -658,6 +658,8 @@ def _token_stride(t, rows, heads, d, dtype, name) -> int:
     if tuple(t.shape) != (rows, heads, d) or t.dtype != dtype or not t.is_cuda or t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
         raise ValueError(f"{name}: expected cuda tensor {(rows, heads, d)} {dtype} with contiguous heads and channels, got "
                          f"{tuple(t.shape)} {t.dtype} strides={tuple(t.stride())} cuda={t.is_cuda}")
+    if rows > 1 and t.stride(0) < heads * d:  # (an expanded tensor's 0 would mean rows one after another)
+        raise ValueError(f"{name}: expected tokens that do not overlap, got a token stride of {t.stride(0)} for rows of {heads * d}")
     return t.stride(0) if rows > 1 else 0
 
 

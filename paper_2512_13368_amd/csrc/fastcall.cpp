@@ -161,7 +161,8 @@ struct PagedCall : Arguments {
     T = p.dtype == 0 ? at::kFloat : at::kBFloat16;
     return true;
   }
-  // [rows, heads, d] with contiguous heads and channels; *stride: elements from a row to the next
+  // [rows, heads, d] with contiguous heads and channels, rows that do not overlap (an expanded tensor's 0 would mean rows one after
+  // another); *stride: elements from a row to the next
   void *rows(int64_t count, int64_t heads, int64_t *stride, bool optional = false)
   {
     PyObject *obj = *arg++;
@@ -176,7 +177,7 @@ struct PagedCall : Arguments {
     }
     const at::Tensor &t = THPVariable_Unpack(obj);
     ok = t.is_cuda() && t.scalar_type() == T && t.dim() == 3 && t.size(0) == count && t.size(1) == heads && t.size(2) == p.d &&
-         t.stride(2) == 1 && (heads == 1 || t.stride(1) == p.d);
+         t.stride(2) == 1 && (heads == 1 || t.stride(1) == p.d) && (count <= 1 || t.stride(0) >= heads * p.d);
     if (!ok) return nullptr;
     if (count > 1) *stride = t.stride(0);
     return t.data_ptr();

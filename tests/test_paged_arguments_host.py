@@ -1,0 +1,79 @@
+"""What the paged cache's calls refuse in tensors that look like device tensors of the right shape and type, on both paths of the binding.
+Stand-ins without memory take the tensors' places: a call that gets as far as the library ends with its error of a missing pointer."""
+import types
+
+import pytest
+import torch
+from torch._subclasses.fake_tensor import FakeTensorMode
+
+from paper_2512_13368_amd import binding as B
+
+STREAM = types.SimpleNamespace(cuda_stream=0)
+BF = torch.bfloat16
+P = B.PagedParams(S=2, T=6, H=4, G=2, d=64, page=16, n_pages=10, max_pages=4, dtype=B.BF16)
+
+pytestmark = pytest.mark.filterwarnings("ignore::UserWarning")
+
+
+def dev(*shape, dtype=BF):
+    with FakeTensorMode():
+        return torch.empty(*shape, dtype=dtype, device="cuda")
+
+
+def arguments(p=P):
+    """Every tensor that the three calls take, in order."""
+    i32 = torch.int32
+    return dict(Q=dev(p.T, p.H, p.d), K=dev(p.T, p.G, p.d), V=dev(p.T, p.G, p.d), K_cache=dev(p.n_pages, p.G, p.page, p.d),
+                V_cache=dev(p.n_pages, p.G, p.page, p.d), page_table=dev(p.S, p.max_pages, dtype=i32), cu_seqlens=dev(p.S + 1, dtype=i32),
+                kv_len=dev(p.S, dtype=i32), O=dev(p.T, p.H, p.d), one=dev(p.S, p.H, p.d), one_O=dev(p.S, p.H, p.d),
+                rope=(dev(p.capacity, p.d // 2, dtype=torch.float32), dev(p.capacity, p.d // 2, dtype=torch.float32)))
+
+
+def append(a, p=P):
+    return B.kv_append(p, a["K"], a["V"], a["K_cache"], a["V_cache"], a["page_table"], a["cu_seqlens"], a["kv_len"], Q=a["Q"],
+                       rope=a["rope"], Q_rot=a["O"], stream=STREAM)
+
+
+def decode(a, p=P, ws=None):
+    return B.attn_decode(p, a["one"], a["K_cache"], a["V_cache"], a["page_table"], a["kv_len"], O=a["one_O"], ws=ws, stream=STREAM)
+
+
+def prompt(a, p=P, ws=None):
+    return B.attn_prompt(p, a["Q"], a["K_cache"], a["V_cache"], a["page_table"], a["cu_seqlens"], a["kv_len"], O=a["O"], ws=ws, stream=STREAM)
+
+
+@pytest.fixture(params=["compiled", "python"])
+def path(request, monkeypatch):
+    if request.param == "python":
+        monkeypatch.setattr(B, "_fast", B.PYTHON_PATH)
+    else:
+        assert B.fastcall() is not B.PYTHON_PATH
+    return request.param
+
+
+@pytest.mark.parametrize("call", [append, decode, prompt])
+def test_the_stand_ins_reach_the_library(call):
+    with pytest.raises(B.BlossomError) as e:
+        call(arguments())
+    assert e.value.code == -1
+
+
+@pytest.mark.parametrize("call,name", [(append, "Q"), (append, "K"), (append, "V"), (decode, "one"), (prompt, "Q")])
+@pytest.mark.parametrize("kind", ["expanded", "overlapping"])
+def test_tokens_that_share_memory_are_refused(path, call, name, kind):
+    # a token stride of 0 would be taken for rows one after another, in memory that holds a single one
+    a = arguments()
+    t = a[name]
+    a[name] = t[:1].expand(*t.shape) if kind == "expanded" else t.as_strided(t.shape, (t.shape[2] * (t.shape[1] - 1), t.shape[2], 1))
+    with pytest.raises(ValueError, match="^[QKV]: .* tokens that do not overlap"):
+        call(a)
+
+
+@pytest.mark.parametrize("call,name", [(append, "Q"), (append, "K"), (append, "V"), (decode, "one"), (prompt, "Q")])
+def test_a_single_token_may_have_any_stride(call, name):
+    p = B.PagedParams(**{**P.__dict__, "S": 1, "T": 1})
+    a = arguments(p)
+    a[name] = a[name].as_strided(a[name].shape, (0, p.d, 1))
+    with pytest.raises(B.BlossomError) as e:
+        call(a, p)
+    assert e.value.code == -1
