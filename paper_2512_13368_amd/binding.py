@@ -208,13 +208,22 @@ def _check_tensor(t, shape, dtype, name):
                          f"{tuple(t.shape)} {t.dtype} contiguous={t.is_contiguous()} cuda={t.is_cuda}")
 
 
+def _ws_bytes(ws, need: int) -> int:
+    """Bytes of a caller's workspace, whose address goes to the device where `need` is not 0."""
+    if ws is None:
+        return 0
+    if need and not (ws.is_cuda and ws.is_contiguous()):
+        raise ValueError(f"ws: expected contiguous cuda tensor of {need} bytes or more, got {tuple(ws.shape)} {ws.dtype} "
+                         f"contiguous={ws.is_contiguous()} cuda={ws.is_cuda}")
+    return ws.numel() * ws.element_size()
+
+
 def _workspace(p: Params, which: int, ws, device):
     import torch
     need = workspace_bytes(p, which)
     if ws is None and need > 0:
         ws = torch.empty(need, dtype=torch.uint8, device=device)
-    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
-    return ws, nbytes
+    return ws, _ws_bytes(ws, need)
 
 
 def select_blocks(p: Params, Q, K, valid_len, sel=None, ws=None, stream=None):
@@ -486,8 +495,9 @@ def select_positions(p: Params, kv_groups: int, cmp_block: int, cmp_stride: int,
     need = select_positions_workspace_bytes(p, kv_groups, cmp_block, cmp_stride)
     if ws is None:
         ws = torch.empty(max(need, 16), dtype=torch.uint8, device=Q.device)
+    nbytes = _ws_bytes(ws, need)
     rc = lib().blossom_select_positions(ctypes.byref(cp), kv_groups, cmp_block, cmp_stride, float(score_scale), _ptr(Q),
-                                        _ptr(K), _ptr(valid_len), _ptr(sel_pos), _ptr(ws), ws.numel(), _stream(stream))
+                                        _ptr(K), _ptr(valid_len), _ptr(sel_pos), _ptr(ws), nbytes, _stream(stream))
     if rc:
         raise BlossomError(rc, "blossom_select_positions")
     return sel_pos
@@ -725,6 +735,7 @@ def _paged_attn(p: PagedParams, which, rows, Q, K_cache, V_cache, page_table, cu
     qs = _token_stride(Q, rows, p.H, p.d, dt, "Q")
     _check_cache(p, K_cache, V_cache, page_table, cu_seqlens, kv_len)
     need = paged_workspace_bytes(p, which)
+    _ws_bytes(ws, need)
     with _on(stream):
         if O is None:
             O = torch.empty((rows, p.H, p.d), dtype=dt, device=Q.device)
@@ -732,7 +743,7 @@ def _paged_attn(p: PagedParams, which, rows, Q, K_cache, V_cache, page_table, cu
             ws = torch.empty(need, dtype=torch.uint8, device=Q.device)
     _check_tensor(O, (rows, p.H, p.d), dt, "O")
     _check_tensor(lse, (rows, p.H), torch.float32, "lse")
-    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
+    nbytes = _ws_bytes(ws, need)
     cp = p.c()
     head = (ctypes.byref(cp), _ptr(Q), qs, _ptr(K_cache), _ptr(V_cache), _ptr(page_table))
     tail = (_ptr(kv_len), _ptr(O), _ptr(lse), _ptr(ws), nbytes, _stream(stream))

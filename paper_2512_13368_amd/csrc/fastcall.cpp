@@ -76,7 +76,7 @@ struct Arguments {
     ok = t.is_cuda() && t.scalar_type() == type && t.sizes() == shape && t.is_contiguous();
     return ok ? static_cast<P *>(t.data_ptr()) : nullptr;
   }
-  // any tensor; None only where `need` is 0
+  // a contiguous device tensor; None, or any tensor, only where `need` is 0
   void *workspace(size_t need, size_t *bytes)
   {
     PyObject *obj = *arg++;
@@ -90,6 +90,8 @@ struct Arguments {
       return nullptr;
     }
     const at::Tensor &t = THPVariable_Unpack(obj);
+    ok = need == 0 || (t.is_cuda() && t.is_contiguous());
+    if (!ok) return nullptr;
     *bytes = t.nbytes();
     return t.data_ptr();
   }

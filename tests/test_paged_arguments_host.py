@@ -77,3 +77,42 @@ def test_a_single_token_may_have_any_stride(call, name):
     with pytest.raises(B.BlossomError) as e:
         call(a, p)
     assert e.value.code == -1
+
+
+LONG = B.PagedParams(**{**P.__dict__, "S": 1, "T": 1, "n_pages": 5000, "max_pages": 4096})  # a split, and so a workspace
+
+
+def no_workspaces(need):
+    """Tensors of `need` bytes or more that are not memory of the GPU, or not as much of it as they have elements."""
+    with FakeTensorMode():
+        small = torch.empty(1, dtype=torch.uint8, device="cuda")
+        wide = torch.empty(2 * need, dtype=torch.uint8, device="cuda")
+    return {"host memory": torch.empty(need + 64, dtype=torch.uint8), "expanded": small.expand(need + 64), "every other byte": wide[::2]}
+
+
+@pytest.mark.parametrize("kind", ["host memory", "expanded", "every other byte"])
+@pytest.mark.parametrize("call,which", [(decode, B.WS_DECODE), (prompt, B.WS_PROMPT)])
+def test_workspaces_that_are_no_device_memory_are_refused(path, call, which, kind):
+    need = B.paged_workspace_bytes(LONG, which)
+    assert need > 0
+    with pytest.raises(ValueError, match="^ws: expected contiguous cuda tensor"):
+        call(arguments(LONG), LONG, ws=no_workspaces(need)[kind])
+
+
+@pytest.mark.parametrize("call", [decode, prompt])
+def test_a_workspace_that_nobody_needs_may_be_anything(call):
+    assert B.paged_workspace_bytes(P, B.WS_DECODE) == 0 and B.paged_workspace_bytes(P, B.WS_PROMPT) == 0
+    with pytest.raises(B.BlossomError) as e:
+        call(arguments(), ws=torch.empty(16, dtype=torch.uint8))
+    assert e.value.code == -1
+
+
+@pytest.mark.parametrize("kind", ["host memory", "expanded", "every other byte"])
+def test_selection_refuses_such_workspaces_too(path, kind):
+    p = B.Params(2, 2, 128, 32, 8, 4, 16, B.F32)
+    f = torch.float32
+    Q, K, valid, sel = dev(2, 2, 128, 32, dtype=f), dev(2, 2, 128, 32, dtype=f), dev(2, dtype=torch.int32), dev(2, 2, p.NB, 4, dtype=torch.int32)
+    need = B.workspace_bytes(p, B.WS_SELECT)
+    assert need > 0
+    with pytest.raises(ValueError, match="^ws: expected contiguous cuda tensor"):
+        B.select_blocks(p, Q, K, valid, sel=sel, ws=no_workspaces(need)[kind], stream=STREAM)
