@@ -84,6 +84,19 @@ inline void with_type(const Args &a, F &&f)
   else with_dim(bf16_t{});
 }
 
+// A probability is 2^(scale2 s - ref) with the product unrounded and the reference a rounded one, so the largest key's is 2^e, e the
+// rounding of the reference: what numerator and denominator share and the log of the sum takes back.  Beyond kFar e may be anything
+// (half a unit of a reference of 2^33 is 512), so the products of such rows' tiles are rounded like the reference.  That is no less
+// exact than the logits themselves, and is done where it is needed alone: for a walk of usual logits it is a comparison a tile.
+constexpr float kFar = 1048576.0f;
+__device__ __forceinline__ bool is_far(float ref) { return fabsf(ref) > kFar; }
+// x f in 32 bits, whatever becomes of it
+__device__ __forceinline__ float rounded_product(float x, float f)
+{
+#pragma clang fp contract(off)
+  return x * f;
+}
+
 // Keys lo .. hi that a query at `pos` sees, of a sequence with n keys (hi < lo: none).
 struct Range {
   int lo, hi;

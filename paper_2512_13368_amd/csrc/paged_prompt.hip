@@ -6,7 +6,8 @@
 // of one page), one tile ahead or two; every wavefront reads them whole.
 //  - S^T = K Q^T on v_mfma_f32_32x32x16_bf16: a lane owns one query row and 16 of a half tile's 32 logits.
 //  - softmax in fp32, base 2: p = exp2(scale2 * s - ref).  The reference is a row's maximum over the first keys it meets; it is
-//    raised only when a lane's probabilities of a half tile pass 4096 in sum, so the usual half tile takes no maximum.
+//    raised only when a lane's probabilities of a half tile pass 4096 in sum, so the usual half tile takes no maximum (one far from 0
+//    does: see kFar in paged.h).
 //  - O^T += V^T P^T with P^T straight from the accumulator registers (rounded to bf16, as the matrix instruction wants them; the
 //    sum is of the unrounded ones) and V^T through the transposing LDS read.
 //
@@ -234,16 +235,23 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
     if (base < every_lo || base + 31 > every_hi || pages_ok != 0xFFFFFFFFu)
       mfma::keep_rows(sc, mfma::row_bits(my.lo - base, my.hi - base) & pages_ok, lh, kNegInf);
     bf16x8 pf[2];
-    float sum;
-    bool placed = __any(fresh);
+    float sum, scale = a.scale2;
+    bool placed = __any(fresh || is_far(ref));
 #pragma unroll 1
     for (;;) {
-      if (placed) move_ref(sc);
+      if (placed) {
+        move_ref(sc);
+        if (__any(is_far(ref))) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sc[i] = rounded_product(sc[i], a.scale2);
+          scale = 1.0f;
+        }
+      }
       float sa, sb;
 #pragma unroll
       for (int i = 0; i < 16; i += 2) {
-        const float pa = __builtin_amdgcn_exp2f(fmaf(sc[i], a.scale2, -ref));
-        const float pb = __builtin_amdgcn_exp2f(fmaf(sc[i + 1], a.scale2, -ref));
+        const float pa = __builtin_amdgcn_exp2f(fmaf(sc[i], scale, -ref));
+        const float pb = __builtin_amdgcn_exp2f(fmaf(sc[i + 1], scale, -ref));
         pf[i >> 3][i & 7] = (__bf16)pa;
         pf[i >> 3][(i & 7) + 1] = (__bf16)pb;
         sa = i == 0 ? pa : sa + pa;

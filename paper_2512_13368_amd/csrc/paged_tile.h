@@ -204,7 +204,7 @@ __device__ __forceinline__ float row_max(float x)
 
 // A wavefront's 16 rows over the tiles it has met: reference (log2 units) and sum in fp32, unnormalised output.  The reference is a
 // row's maximum over the first keys it met; it is raised only when a lane's eight probabilities of a tile pass kSumLimit in sum, so the
-// usual tile takes no maximum.
+// usual tile takes no maximum; where it is far from 0 (see kFar), a tile takes one and has its logits scaled before it is subtracted.
 constexpr float kSumLimit = 4096.0f;
 template <typename T, int D>
 struct Rows {
@@ -244,8 +244,8 @@ struct Rows {
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[4 * h + i] = mine >> (16 * h + i) & 1 ? s[4 * h + i] : mfma::kNegInf;
     }
-    bool place = __any(m == mfma::kNegInf);
-    float sum;
+    bool place = __any(is_far(m));  // (-inf too)
+    float sum, scale = scale2;
 #pragma unroll 1
     for (;;) {
       float ref = m;
@@ -258,11 +258,16 @@ struct Rows {
         l *= f;
 #pragma unroll
         for (int j = 0; j < TL::NV; ++j) acc[j] *= f;
+        if (__any(is_far(ref))) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s[i] = rounded_product(s[i], scale2);
+          scale = 1.0f;
+        }
       }
       sum = 0.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale2, -ref));
+        p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale, -ref));
         sum += p[i];
       }
       if (place || !__any(!(sum <= kSumLimit))) break;
