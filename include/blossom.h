@@ -391,7 +391,7 @@ int blossom_dense_causal_fwd(const blossom_params *p, const void *Q, const void 
  * tightly), so that slices of one fused projection can be passed as they are.  Types, ownership, streams and errors as above;
  * pointers and strides are multiples of 16 bytes.  Everything the cache holds outside the visible positions (older rows of a
  * page, pages nobody lists) may be any bits.  A value that is not finite at a cached position may reach every new token of
- * its sequence.  No call synchronises, so all may be captured into a graph.
+ * its sequence, as NaN.  No call synchronises, so all may be captured into a graph.
  */
 typedef struct {
   int32_t S;              /* sequences                                                             */

@@ -193,7 +193,7 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
     return seen;
   };
 
-  Rows<T, D> r;
+  Rows<T, D, true> r;
   r.clear();
   // a ring of STAGES tiles: those of the next STAGES - 1 are on their way while one is worked on
   unsigned seen[STAGES];

@@ -6,6 +6,8 @@
 // to 200 tokens, 2 heads, d = 32: 15.4 us, of which the products take 4.6 and the exponentials and the rest 3 at full balance).
 // Tried: rings of 3, 4 and 6 tiles (23.3, 24.6, 25.4 us where 2 took 23.0), results through LDS (no gain), one wavefront a
 // workgroup without barriers (as fast, slower from d = 64 on), two for large rows (d = 64 fp32: 72 us against 61).
+// bf16 probabilities are rounded once: both terms of them (FINE in paged_tile.h) take 7 to 13 % more time here (11 prompts of 3277, 3 heads
+// over 1, d = 8: 72.4 us for 67.4; 8 of 1000 to 3000, 8 heads over 2, d = 32: 69.3 for 61.2).
 #include "common.h"
 #include "launch.h"
 #include "mfma_common.h"
@@ -83,7 +85,7 @@ __global__ __launch_bounds__(64 * shared_waves(D * sizeof(T))) void shared_kerne
     return seen;
   };
 
-  Rows<T, D> r;
+  Rows<T, D, false> r;
   r.clear(row_ok);
   unsigned seen = t < t_end ? request(t, lds[0]) : 0u;
 #pragma unroll

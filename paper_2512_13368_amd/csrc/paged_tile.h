@@ -132,16 +132,22 @@ struct Tile {
   }
 
   // acc += V^T P^T: p[4h + i] is the probability of key 16h + 4c + i.  The sum over keys may run in any order, so lane group c takes
-  // the keys whose probabilities it holds.  bf16: P is rounded as the matrix instruction wants it (its sum is of the unrounded ones),
-  // V^T comes through the transposing LDS read.  Accumulator j, element i holds channel channel(j, c, i) of the lane's query.
-  // `both`: the tile's second 16 keys count too.
+  // the keys whose probabilities it holds.  bf16: V^T comes through the transposing LDS read, P is rounded as the matrix instruction wants
+  // it (its sum is of the unrounded ones).  FINE: what that leaves of P goes through a second product with the same V, so that of the
+  // output's error its own rounding is all there is (1.6e-3 of its norm; with P rounded once 2.0 to 2.4e-3).  Memory-bound kernels have
+  // the time: 100 to 1024 keys at d = 64 15.1 us without and 15.4 with, 131071 at d = 128 85.6 and 86.0, 16 chosen pages 8.1 and 8.5.
+  // Accumulator j, element i holds channel channel(j, c, i) of the lane's query.  `both`: the tile's second 16 keys count too.
+  template <bool FINE>
   static __device__ __forceinline__ void product(const char *vs, const float (&p)[8], bool both, int lane, f32x4 (&acc)[NV])
   {
     const int n = lane & 15, c = lane >> 4;
     if constexpr (BF) {
-      mfma::bf16x8 pf;
+      mfma::bf16x8 pf, rest;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) pf[i] = (__bf16)p[i];
+      for (int i = 0; i < 8; ++i) {
+        pf[i] = (__bf16)p[i];
+        if constexpr (FINE) rest[i] = (__bf16)(p[i] - (float)pf[i]);
+      }
       const int r = 4 * c + (n >> 2);  // (and 16 on: the same swizzle)
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
@@ -150,6 +156,7 @@ struct Tile {
         const mfma::s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((mfma::lds_s16x4 *)(v));
         const mfma::s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((mfma::lds_s16x4 *)(v + 16 * RB));
         const mfma::bf16x8 vt = __builtin_bit_cast(mfma::bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+        if constexpr (FINE) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, rest, acc[j], 0, 0, 0);
         acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pf, acc[j], 0, 0, 0);
       }
     } else {
@@ -206,7 +213,7 @@ __device__ __forceinline__ float row_max(float x)
 // row's maximum over the first keys it met; it is raised only when a lane's eight probabilities of a tile pass kSumLimit in sum, so the
 // usual tile takes no maximum; where it is far from 0 (see kFar), a tile takes one and has its logits scaled before it is subtracted.
 constexpr float kSumLimit = 4096.0f;
-template <typename T, int D>
+template <typename T, int D, bool FINE>
 struct Rows {
   typedef Tile<T, D> TL;
   f32x4 acc[TL::NV];
@@ -274,7 +281,7 @@ struct Rows {
       place = true;
     }
     l += sum;
-    TL::product(vs, p, both, lane, acc);
+    TL::template product<FINE>(vs, p, both, lane, acc);
   }
   __device__ __forceinline__ float total() const
   {
