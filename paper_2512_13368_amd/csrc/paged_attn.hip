@@ -28,7 +28,7 @@ using mfma::kLn2;
 using mfma::kNegInf;
 
 constexpr int kRows = 16;             // query rows of a workgroup
-constexpr int kMostParts = 256;       // parts of a key/value head's keys
+constexpr int kMostParts = 256;       // parts of a key/value head's keys, of all sequences together
 constexpr int kMostPromptParts = 64;  // parts of a row's keys in a prompt
 // Decode wavefronts that keep the memory busy: two a SIMD (four: 88 us for 85 at 131071 keys, 16.0 for 15.2 on short ones).  Four where rows
 // are small, which take as long to work on (67201 keys with a window of 29264, 3 sequences, 8 heads, fp32, d = 8: 20 us for 28.5; 13 of
@@ -57,6 +57,13 @@ constexpr int most_decode_waves(int row_bytes)
   const int held = decode_stages(row_bytes) * 2 * (row_bytes < 32 ? 1024 : 32 * row_bytes);
   return 131072 / held < 16 ? 131072 / held : 16;
 }
+
+// Four wavefronts at least; one round of workgroups of the most is no more than kMostParts.
+constexpr bool fits_parts(int row_bytes)
+{
+  return most_decode_waves(row_bytes) >= 4 && fill_waves(row_bytes) / most_decode_waves(row_bytes) <= kMostParts;
+}
+static_assert(fits_parts(16) && fits_parts(32) && fits_parts(64) && fits_parts(128) && fits_parts(256) && fits_parts(512), "");
 
 // ---- work of decode, split over a long cache ----
 __device__ __forceinline__ int tiles_of(const Args &a, int s)
@@ -375,7 +382,7 @@ int row_bytes_of(const Args &a) { return a.d * (a.dtype == 0 ? 4 : 2); }
 int decode_waves(const Args &a)
 {
   const int most = most_decode_waves(row_bytes_of(a)), fill = fill_waves(row_bytes_of(a));
-  int w = most < 4 ? most : 4;
+  int w = 4;
   while (w < most && decode_bases(a) * w < fill && most_tiles(a) >= 2 * w) w *= 2;
   return w;
 }
@@ -390,7 +397,7 @@ int decode_parts(const Args &a)
   if (a.S * most_tiles(a) > 1 << 22) return 0;  // (parts are counted in 32 bits and cut in fp32)
   const long parts = fill / w / heads, most = a.S * ((most_tiles(a) + 2 * w - 1) / (2 * w));
   const long n = parts < most ? parts : most;
-  return (int)(n >= 2 * a.S ? (n > kMostParts ? kMostParts : n) : 0);
+  return (int)(n >= 2 * a.S ? n : 0);  // (no more than kMostParts: with so many tiles w is the most there is, see fits_parts)
 }
 
 namespace {
@@ -423,7 +430,7 @@ void launch_decode_d(const Args &a, hipStream_t st)
     if (w == 16) return launch_decode_w<T, D, 16>(a, st);
   if constexpr (MOST >= 8)
     if (w == 8) return launch_decode_w<T, D, 8>(a, st);
-  launch_decode_w<T, D, MOST < 4 ? MOST : 4>(a, st);
+  launch_decode_w<T, D, 4>(a, st);
 }
 
 }  // namespace

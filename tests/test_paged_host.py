@@ -110,3 +110,20 @@ def test_the_binding_names_what_is_wrong():
         B.attn_prompt(p, z(6, 4, 64, dtype=bf), cu_seqlens=None, **ok)
     with pytest.raises(ValueError, match="^K: expected cuda tensor"):
         B.kv_append(p, z(6, 2, 64, dtype=bf), z(6, 2, 64, dtype=bf), cu_seqlens=cu, **ok)
+
+
+@pytest.mark.parametrize("dtype,size", [(B.F32, 4), (B.BF16, 2)])
+@pytest.mark.parametrize("d", [8, 16, 32, 64, 128])
+def test_decode_parts_stay_within_a_round_of_workgroups(dtype, size, d):
+    # the join holds a weight for each of 256 parts; what is lost to rounding up is a part a sequence, so there are two for each at least
+    seen = set()
+    for S in (1, 2, 3, 7, 16, 64, 65, 100, 127, 128, 129, 200, 1000, 5000):
+        for H, G in ((1, 1), (2, 1), (2, 2), (8, 2), (17, 1), (32, 8), (40, 1), (64, 64)):
+            for positions in (32, 128, 512, 1024, 4096, 65536, 1 << 20, 1 << 24):
+                p = params(S=S, H=H, G=G, d=d, dtype=dtype, page=16, n_pages=1, max_pages=positions // 16)
+                need = B.paged_workspace_bytes(p, B.WS_DECODE)
+                if need:
+                    parts, rest = divmod(need - 8 * S, H * (d + 2) * 4)
+                    assert rest == 0 and 2 * S <= parts <= 256, p
+                    seen.add(parts)
+    assert 256 in seen and min(seen) < 64
