@@ -23,6 +23,7 @@
 #include "launch.h"
 #include "mfma_common.h"
 #include "paged.h"
+#include "paged_tile.h"
 
 namespace blossom {
 namespace paged {
@@ -39,17 +40,6 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kKeys = 64;                  // keys of a tile
-constexpr float kSumLimit = 4096.0f;       // a lane's 16 probabilities of a half tile may sum to this
-
-// what stands in for rows that nobody may see
-__device__ const uint4 kZeros[64] = {};
-
-// One direct global->LDS load of 16 bytes a lane (see load_to_lds in mfma_common.h).
-__device__ __forceinline__ void row_to_lds(const void *base, unsigned off, unsigned lds)
-{
-  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(lds), "v"(off), "s"(base) : "memory");
-}
-
 }  // namespace
 
 template <int D, int STAGES, int WAVES_EU>
@@ -164,8 +154,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
           vo += rows_off * (D * 2);
         }
       }
-      row_to_lds(kb, ko, k_to + i * (RPI * kWaves * D * 2));
-      row_to_lds(vb, vo, v_to + i * (RPI * kWaves * D * 2));
+      to_lds<false>(kb, ko, k_to + i * (RPI * kWaves * D * 2));
+      to_lds<false>(vb, vo, v_to + i * (RPI * kWaves * D * 2));
     }
   };
 
