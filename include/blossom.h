@@ -386,6 +386,8 @@ int blossom_dense_causal_fwd(const blossom_params *p, const void *Q, const void 
  *                     sequence s's (none is allowed).  Rows at and beyond cu_seqlens[S] are left as they are.
  *   Capacity          a sequence holds at most max_len positions (0: max_pages * page; never more than that).  What would lie
  *                     beyond, or before position 0, is neither stored nor attended.
+ *   Size              a launch has fewer than 2^32 threads: from 2^26 new tokens on (append), from about 2^24 sequences times key/value
+ *                     heads (decode, prompt), from about 2^30 query rows (prompt) a call is BLOSSOM_ERR_SHAPE and starts nothing.
  * Heads are grouped as in Eq. 4-5: H query heads share G key/value heads, head h uses h / (H/G).  Packed rows are tokens:
  * Q [T,H,d], K and V [T,G,d] with heads and channels contiguous and `*_stride` elements from one token to the next (0: packed
  * tightly), so that slices of one fused projection can be passed as they are.  Types, ownership, streams and errors as above;

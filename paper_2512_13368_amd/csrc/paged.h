@@ -51,15 +51,19 @@ struct Args {
   int2 *part_of;               // decode: [S] first part and parts of a sequence, there too
 };
 
+// HIP counts a launch's threads in 32 bits.  The launchers below start nothing and return false for a call that would have more.
+inline bool countable(long workgroups, int threads) { return workgroups * threads < 1l << 32; }
+
 // append: paged_append.hip
-void launch_append(const Args &a, hipStream_t st);
+bool launch_append(const Args &a, hipStream_t st);
 // one-token and prompt attention: paged_attn.hip.  decode_parts, prompt_parts: what `parts` is for this shape
 int decode_parts(const Args &a);
 int prompt_parts(const Args &a);
-void launch_decode(const Args &a, hipStream_t st);
-void launch_prompt(const Args &a, hipStream_t st);
+bool launch_decode(const Args &a, hipStream_t st);
+bool launch_prompt(const Args &a, hipStream_t st);
 // prompt attention for bf16, d = 64 or 128: paged_prompt.hip
-constexpr int kPromptRows = 128;  // query rows of a workgroup
+constexpr int kPromptRows = 128;  // query rows of a workgroup, which has four wavefronts
+constexpr int kPromptWaves = 4;
 bool prompt_mfma_supported(const Args &a);
 void launch_prompt_mfma(const Args &a, hipStream_t st);
 // prompt attention for everything else: paged_shared.hip

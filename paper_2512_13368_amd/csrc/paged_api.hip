@@ -22,7 +22,7 @@ int check_params(const blossom_paged_params *p, Args *a)
   if (p->H % p->G != 0 || p->window < 0 || p->max_len < 0 || p->table_per_head < 0 || p->table_per_head > 1)
     return BLOSSOM_ERR_PARAM;
   if (!std::isfinite(p->softmax_scale) || p->softmax_scale < 0.0f) return BLOSSOM_ERR_PARAM;
-  // positions and rows are counted in 31 bits, with room for a tile more; workgroups of a launch too
+  // positions and rows are counted in 31 bits, with room for a tile more
   const int64_t most = 0x7FFFFFFFll - 4096, held = (int64_t)p->max_pages * p->page;
   if (held > most || (int64_t)p->T * p->H > most || (int64_t)p->S * p->H > most) return BLOSSOM_ERR_SHAPE;
   *a = Args{};
@@ -84,8 +84,7 @@ int attn(const blossom_paged_params *p, bool prompt, const void *Q, int64_t q_st
   a.page_table = page_table; a.cu = cu_seqlens; a.kv_len = kv_len;
   a.O = O; a.lse = lse;
   (void)hipGetLastError();  // an earlier call's error is not this one's
-  if (prompt) launch_prompt(a, (hipStream_t)hip_stream);
-  else launch_decode(a, (hipStream_t)hip_stream);
+  if (!(prompt ? launch_prompt : launch_decode)(a, (hipStream_t)hip_stream)) return BLOSSOM_ERR_SHAPE;
   return launch_status();
 }
 
@@ -122,7 +121,7 @@ int blossom_kv_append(const blossom_paged_params *p, const void *Q, int64_t q_st
   a.page_table = page_table; a.cu = cu_seqlens; a.kv_len = kv_len;
   a.K_cache = K_cache; a.V_cache = V_cache; a.Q_rot = Q_rot;
   (void)hipGetLastError();
-  launch_append(a, (hipStream_t)hip_stream);
+  if (!launch_append(a, (hipStream_t)hip_stream)) return BLOSSOM_ERR_SHAPE;
   return launch_status();
 }
 

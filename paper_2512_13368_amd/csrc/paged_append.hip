@@ -156,22 +156,24 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Args a, int share)
   }
 }
 
-void launch_append(const Args &a, hipStream_t st)
+bool launch_append(const Args &a, hipStream_t st)
 {
   // few tokens: their rows go to more wavefronts, as far as a wavefront has a load's worth of rows left
   const int rows = (a.Q ? a.H : 0) + 2 * a.G, per = 64 * 16 / (a.d * (a.dtype == 0 ? 4 : 2));
   int share = 1;
   while ((long)a.T * share < 2048 && share * per < rows) share *= 2;
   const long waves = (long)a.T * share;
-  const unsigned blocks = (unsigned)((waves + kThreads / 64 - 1) / (kThreads / 64));
+  const long blocks = (waves + kThreads / 64 - 1) / (kThreads / 64);
+  if (!countable(blocks, kThreads)) return false;
   // More than half the last-level cache is written past it: 16383 tokens of 32 + 2 * 8 heads of 128 channels, 201 MB, take 73 us so and
   // 82 kept.  What is less stays for the attention that follows.
   const bool once = (double)a.T * rows * a.d * (a.dtype == 0 ? 4 : 2) > 128e6;
-  auto go = [&](auto kernel) { BLOSSOM_LAUNCH(kernel, dim3(blocks), dim3(kThreads), 0, st, a, share); };
+  auto go = [&](auto kernel) { BLOSSOM_LAUNCH(kernel, dim3((unsigned)blocks), dim3(kThreads), 0, st, a, share); };
   if (a.dtype == 0 && once) go(append_kernel<float, true>);
   else if (a.dtype == 0) go(append_kernel<float, false>);
   else if (once) go(append_kernel<bf16_t, true>);
   else go(append_kernel<bf16_t, false>);
+  return true;
 }
 
 }  // namespace paged

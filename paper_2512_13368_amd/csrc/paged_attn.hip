@@ -375,6 +375,7 @@ long most_tiles(const Args &a)
   return ((long)(a.window < a.cap ? a.window + kTile - 1 : a.cap) + kTile - 1) / kTile;
 }
 long decode_bases(const Args &a) { return (long)a.S * a.G * ((a.R + kRows - 1) / kRows); }
+long decode_groups(const Args &a) { return decode_bases(a) / a.S * (a.parts ? a.parts : a.S); }
 
 int row_bytes_of(const Args &a) { return a.d * (a.dtype == 0 ? 4 : 2); }
 
@@ -405,7 +406,7 @@ namespace {
 template <typename T, int D, int W>
 void launch_decode_w(const Args &a, hipStream_t st)
 {
-  const dim3 grid((unsigned)(decode_bases(a) / a.S * (a.parts ? a.parts : a.S))), block(64 * W);
+  const dim3 grid((unsigned)decode_groups(a)), block(64 * W);
   // What the last-level cache cannot hold until the next token's call is not kept in the caches at all: 131071 keys 85 us so, 97 kept;
   // 74 MB 15.2 us kept, 16.4 so.
   const bool once = a.R <= kRows && (double)a.S * most_tiles(a) * kTile * a.G * D * 2 * sizeof(T) > 256e6;
@@ -435,9 +436,11 @@ void launch_decode_d(const Args &a, hipStream_t st)
 
 }  // namespace
 
-void launch_decode(const Args &a, hipStream_t st)
+bool launch_decode(const Args &a, hipStream_t st)
 {
+  if (!countable(decode_groups(a), 64 * decode_waves(a))) return false;
   with_type(a, [&](auto type, auto dim) { launch_decode_d<decltype(type), decltype(dim)::value>(a, st); });
+  return true;
 }
 
 // Which kernel takes a prompt call, and into how many parts a row's keys go.
@@ -485,19 +488,24 @@ static PromptPlan prompt_plan(const Args &a)
 
 int prompt_parts(const Args &a) { return prompt_plan(a).parts; }
 
-void launch_prompt(const Args &call, hipStream_t st)
+// wavefronts of a prompt's workgroup where rows are few
+static constexpr int few_waves(int row_bytes) { return most_decode_waves(row_bytes) < 8 ? most_decode_waves(row_bytes) : 8; }
+
+bool launch_prompt(const Args &call, hipStream_t st)
 {
   Args a = call;
   const PromptPlan p = prompt_plan(a);
   // (sequence s's tiles begin at floor(cu[s] R / rows) + s: enough for the last, partial one of each)
   a.row_tiles = (int)((long)a.T * a.R / (p.kind == kFew ? kRows : p.kind == kMatrix ? kPromptRows : shared_rows(a)) + a.S);
+  const int waves = p.kind == kFew ? few_waves(row_bytes_of(a)) : p.kind == kMatrix ? kPromptWaves : shared_waves(row_bytes_of(a));
+  if (!countable((long)a.row_tiles * a.G * a.parts, 64 * waves)) return false;
   if (p.kind == kMatrix) launch_prompt_mfma(a, st);
   else if (p.kind == kShared) launch_prompt_shared(a, st);
   with_type(a, [&](auto type, auto dim) {
     typedef decltype(type) T;
     constexpr int D = decltype(dim)::value;
     if (p.kind == kFew) {
-      constexpr int MOST = most_decode_waves(D * sizeof(T)), W = MOST < 8 ? MOST : 8;
+      constexpr int W = few_waves(D * sizeof(T));
       const dim3 grid((unsigned)((long)a.row_tiles * a.G * a.parts)), block(64 * W);
       if (a.parts > 1) BLOSSOM_LAUNCH((decode_kernel<T, D, W, false, true, true>), grid, block, 0, st, a);
       else BLOSSOM_LAUNCH((decode_kernel<T, D, W, false, false, true>), grid, block, 0, st, a);
@@ -505,6 +513,7 @@ void launch_prompt(const Args &call, hipStream_t st)
     if (a.parts > 1 && !launch_failed())
       BLOSSOM_LAUNCH((join_rows_kernel<T, D>), dim3((unsigned)((size_t)a.T * a.H * (D / 4) / 256 + 1)), dim3(256), 0, st, a);
   });
+  return true;
 }
 
 }  // namespace paged

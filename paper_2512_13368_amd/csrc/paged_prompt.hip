@@ -38,7 +38,7 @@ using mfma::u32x2;
 
 namespace {
 
-constexpr int kWaves = 4;
+constexpr int kWaves = kPromptWaves;
 constexpr int kKeys = 64;                  // keys of a tile
 }  // namespace
 

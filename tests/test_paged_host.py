@@ -127,3 +127,14 @@ def test_decode_parts_stay_within_a_round_of_workgroups(dtype, size, d):
                     assert rest == 0 and 2 * S <= parts <= 256, p
                     seen.add(parts)
     assert 256 in seen and min(seen) < 64
+
+
+def test_calls_of_more_threads_than_a_launch_counts(lib):
+    # a wavefront a token (append), four a sequence and key/value head (decode), two for 32 rows (prompts of small rows), four for 64
+    for T, d in ((1 << 26, 64), (1 << 30, 64), (1 << 26, 8)):
+        assert append(lib, params(T=T, H=1, G=1, d=d)) == -2, T
+    for S, d in ((1 << 24, 64), (1 << 30, 64), (1 << 24, 8)):
+        assert decode(lib, params(S=S, H=1, G=1, d=d, max_pages=2)) == -2, S
+    for T, H, dtype, d in ((1 << 30, 1, B.F32, 8), (1 << 29, 2, B.F32, 64), (1 << 28, 4, B.BF16, 16)):
+        assert prompt(lib, params(T=T, H=H, G=1, d=d, dtype=dtype)) == -2, T
+    assert prompt(lib, params(S=1 << 25, T=1 << 10, H=1, G=1, d=64)) == -2
