@@ -4,7 +4,8 @@
 One attention layer of a sequential recommender with random weights.  Users' histories of different lengths come as one packed
 batch (kv_append, attn_prompt); then every user gets new items, one a step (kv_append, attn_decode).  Beside full attention a step
 shows the two branches of Blossom attention for a single new token: the long-term branch reads the pages whose mean key scores best
-for each key/value head (a page table per head), the short-term branch a window, and a gate blends them.
+for each key/value head (a page table per head), the short-term branch a window, and a gate blends them.  (The pages are chosen in
+plain torch from the whole cache: it shows what the calls take, not how fast a selection can be.)
 
     python examples/serve_paged.py [--users 32] [--history 1000] [--steps 8]
 """
@@ -82,7 +83,9 @@ class Layer:
 
     def select(self, q: torch.Tensor, kv_len: torch.Tensor) -> tuple[torch.Tensor, torch.Tensor]:
         """Per user and key/value head the newest page and the TOPK - 1 best earlier ones, in ascending order, as a table of
-        pages; and how many positions they hold (the listed pages are whole but the newest)."""
+        pages; and how many positions they hold (the listed pages are whole but the newest).  This shows the table's form: it takes
+        every page's mean anew, which reads more than full attention does.  A program that selects for speed keeps the means of whole
+        pages beside the cache."""
         pages = self.table_dev.long().clamp(min=0)
         mean = self.K_cache[pages].float().mean(3).permute(0, 2, 1, 3)                    # [users, G, pages, DIM]
         mine = q.float().view(self.users, GROUPS, HEADS // GROUPS, DIM).sum(2)
