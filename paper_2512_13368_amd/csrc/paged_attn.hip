@@ -9,9 +9,9 @@
 // results there.  Where a sequence is long and workgroups are few, its keys are cut into parts for several, whose results a second
 // kernel joins.  Large prompts: paged_prompt.hip, paged_shared.hip.  The operands and the softmax of a step: paged_tile.h.
 //
-// Measured: one sequence of 131071 keys (32 heads over 8, d = 128, bf16: 537 MB) 85 us, 80 of it in this kernel, where reading as many
-// bytes takes 78; 16 sequences of 4001 to 8191 keys (400 MB) 71 us, the join 4.6 of it; 128 of 100 to 1024 (4 heads, d = 64: 74 MB)
-// 15 us, where a read takes 11 and a launch with its first loads 4; the join inside the kernel would save 3 us of 85 and nothing
+// Measured: one sequence of 131071 keys (32 heads over 8, d = 128, bf16: 537 MB) 86 us, 80 of it in this kernel, where reading as many
+// bytes takes 78; 16 sequences of 4001 to 8191 keys (400 MB) 72 us, the join 4.6 of it; 128 of 100 to 1024 (4 heads, d = 64: 74 MB)
+// 15.4 us, where a read takes 11 and a launch with its first loads 4; the join inside the kernel would save 3 us of 85 and nothing
 // where sequences are short.
 #include "common.h"
 #include "launch.h"
