@@ -111,6 +111,12 @@ __device__ __forceinline__ Range seen_by(const Args &a, int pos, int n)
   return {max(pos - a.window + 1, 0), min(pos, min(n, a.cap) - 1)};
 }
 
+// Rows that see fewer keys than this have large probabilities, whose rounding to bf16 would show beside outputs that are averages over
+// many keys: workgroups that have such rows keep what it leaves (see FINE in paged_tile.h), in every kernel.
+constexpr int kFewKeys = 32;
+// Does any row between two of one sequence see so few?  (The number rises with the position, and falls beyond the capacity.)
+__device__ __forceinline__ bool few_keys(const Range &first, const Range &last) { return min(first.hi - first.lo, last.hi - last.lo) + 1 < kFewKeys; }
+
 // cu[s] inside [0, T], whatever the caller's array holds
 __device__ __forceinline__ int token_at(const Args &a, int s) { return min(max(a.cu[s], 0), a.T); }
 

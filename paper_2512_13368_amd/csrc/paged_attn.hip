@@ -200,7 +200,7 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
     return seen;
   };
 
-  Rows<T, D, true> r;
+  Rows<T, D> r;
   r.clear();
   // a ring of STAGES tiles: those of the next STAGES - 1 are on their way while one is worked on
   unsigned seen[STAGES];
@@ -221,7 +221,7 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
       const char *ks = mine + k * (2 * TL::BYTES);
       const int base = t * kTile;
       const bool all = seen[k] == 0xFFFFFFFFu && (!PROMPT || (base >= every.lo && base + kTile - 1 <= every.hi));
-      r.attend(ks, ks + TL::BYTES, q, a.scale2, PROMPT ? seen[k] & mfma::row_bits(my.lo - base, my.hi - base) : seen[k], all, true, lane);
+      r.template attend<true>(ks, ks + TL::BYTES, q, a.scale2, PROMPT ? seen[k] & mfma::row_bits(my.lo - base, my.hi - base) : seen[k], all, true, lane);
       ++t;
     }
   }

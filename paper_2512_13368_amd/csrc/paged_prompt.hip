@@ -9,9 +9,10 @@
 //    raised only when a lane's probabilities of a half tile pass 4096 in sum, so the usual half tile takes no maximum (one far from 0
 //    does: see kFar in paged.h).
 //  - O^T += V^T P^T with P^T straight from the accumulator registers (rounded to bf16, as the matrix instruction wants them; the
-//    sum is of the unrounded ones) and V^T through the transposing LDS read.  What the rounding leaves of P as a second product, as
-//    decode has it: the error in norm falls from 2.2e-3 to 1.6e-3, for a third more time (long prompts 1075 us for 795, chunks 175 for
-//    128, ragged ones 160 for 121): not taken.
+//    sum is of the unrounded ones) and V^T through the transposing LDS read.  What the rounding leaves of P is a second product in
+//    workgroups with rows that see few keys, which have a walk of their own (as a branch in the one walk it takes 1.3 to 1.6 % of long
+//    prompts).  Everywhere, as in decode, the error in norm falls from 2.2e-3 to 1.6e-3, for a third more time (long prompts 1075 us for
+//    795, chunks 175 for 128, ragged ones 160 for 121): not taken.
 //
 // Measured under steady load: two prompts of 6001 and 8191 tokens, 32 heads over 8, d = 128: 815 us, 1.04 PFLOP/s, where a bf16 product
 // of 8192^3 reaches 1.07; chunks of 512 over a window of 4096: 131 us, 870 TFLOP/s; 32 ragged prompts of 7 to 1997, 16 heads over 4,
@@ -117,12 +118,15 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
     off_hi = (unsigned)(off >> 32);
   };
   take();
+  missing &= ~0ull << max((lo >> shift) - list0, 0);  // (pages of the first tile that end before the first key: anything too)
+  bool fine = few_keys(all_first, all_last) || missing != 0ull;  // few keys: by their number, or because pages are out of range
   auto advance = [&](int page) __attribute__((always_inline)) {
     while (page >= list0 + 64) {
       list0 += 64;
       ids = ids_next;
       ids_next = entries(list0 + 64);
       take();
+      fine = fine || missing != 0ull;
     }
   };
 
@@ -199,7 +203,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
     fresh = fresh && !up;
   };
 
-  auto half = [&](const uint16_t *ks, const uint16_t *vs, int base, unsigned pages_ok) __attribute__((always_inline)) {
+  auto half = [&](const uint16_t *ks, const uint16_t *vs, int base, unsigned pages_ok, auto two) __attribute__((always_inline)) {
     if (base > any_hi || base + 31 < any_lo) return;
     bf16x8 kf[D / 16];
 #pragma unroll
@@ -227,7 +231,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
     }
     if (base < every_lo || base + 31 > every_hi || pages_ok != 0xFFFFFFFFu)
       mfma::keep_rows(sc, mfma::row_bits(my.lo - base, my.hi - base) & pages_ok, lh, kNegInf);
-    bf16x8 pf[2];
+    constexpr bool TWO = decltype(two)::value;
+    bf16x8 pf[2], rest[2];
     float sum, scale = a.scale2;
     bool placed = __any(fresh || is_far(ref));
 #pragma unroll 1
@@ -247,6 +252,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
         const float pb = __builtin_amdgcn_exp2f(fmaf(sc[i + 1], scale, -ref));
         pf[i >> 3][i & 7] = (__bf16)pa;
         pf[i >> 3][(i & 7) + 1] = (__bf16)pb;
+        if constexpr (TWO) {
+          rest[i >> 3][i & 7] = (__bf16)(pa - (float)pf[i >> 3][i & 7]);
+          rest[i >> 3][(i & 7) + 1] = (__bf16)(pb - (float)pf[i >> 3][(i & 7) + 1]);
+        }
         sa = i == 0 ? pa : sa + pa;
         sb = i == 0 ? pb : sb + pb;
       }
@@ -258,7 +267,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int mb = 0; mb < NB; ++mb) oacc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[t][mb], pf[t], oacc[mb], 0, 0, 0);
+      for (int mb = 0; mb < NB; ++mb) {
+        if constexpr (TWO) oacc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[t][mb], rest[t], oacc[mb], 0, 0, 0);
+        oacc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[t][mb], pf[t], oacc[mb], 0, 0, 0);
+      }
   };
 
   // bit k: key base + k has a page
@@ -276,7 +288,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
   for (int kk = 0; kk < D / 16; ++kk) asm volatile("" : "+v"(qf[kk]));
   asm volatile("" : "+v"(ids_next));
   mfma::arrived_all<0>();
-  auto step = [&](int t, auto buffer) __attribute__((always_inline)) {
+  auto step = [&](int t, auto buffer, auto two) __attribute__((always_inline)) {
     constexpr int cur = decltype(buffer)::value;
     unsigned ok0 = 0xFFFFFFFFu, ok1 = 0xFFFFFFFFu;
     if (missing != 0ull) {  // (before the list moves on)
@@ -284,14 +296,18 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(WAV
       ok1 = pages_of(t * kKeys + 32);
     }
     if (t < t_hi) stage(t + 1, Ks[cur ^ 1], Vs[cur ^ 1]);
-    half(Ks[cur], Vs[cur], t * kKeys, ok0);
-    half(Ks[cur] + 32 * D, Vs[cur] + 32 * D, t * kKeys + 32, ok1);
+    half(Ks[cur], Vs[cur], t * kKeys, ok0, two);
+    half(Ks[cur] + 32 * D, Vs[cur] + 32 * D, t * kKeys + 32, ok1, two);
     mfma::arrived_all<0>();
   };
-  for (int t = t_lo; t <= t_hi; t += 2) {
-    step(t, std::integral_constant<int, 0>{});
-    if (t + 1 > t_hi) break;
-    step(t + 1, std::integral_constant<int, 1>{});
+  int t = t_lo;
+  for (; t <= t_hi && !fine; t += 2) {
+    step(t, std::integral_constant<int, 0>{}, std::false_type{});
+    if (t < t_hi) step(t + 1, std::integral_constant<int, 1>{}, std::false_type{});
+  }
+  for (; t <= t_hi; t += 2) {
+    step(t, std::integral_constant<int, 0>{}, std::true_type{});
+    if (t < t_hi) step(t + 1, std::integral_constant<int, 1>{}, std::true_type{});
   }
 
   // ---- results ----

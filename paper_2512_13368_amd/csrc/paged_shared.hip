@@ -6,8 +6,10 @@
 // to 200 tokens, 2 heads, d = 32: 15.4 us, of which the products take 4.6 and the exponentials and the rest 3 at full balance).
 // Tried: rings of 3, 4 and 6 tiles (23.3, 24.6, 25.4 us where 2 took 23.0), results through LDS (no gain), one wavefront a
 // workgroup without barriers (as fast, slower from d = 64 on), two for large rows (d = 64 fp32: 72 us against 61).
-// bf16 probabilities are rounded once: both terms of them (FINE in paged_tile.h) take 7 to 13 % more time here (11 prompts of 3277, 3 heads
-// over 1, d = 8: 72.4 us for 67.4; 8 of 1000 to 3000, 8 heads over 2, d = 32: 69.3 for 61.2).
+// bf16 probabilities are rounded once, but for workgroups with rows that see few keys: both terms of them (FINE in paged_tile.h)
+// everywhere take 7 to 13 % more time here (11 prompts of 3277, 3 heads over 1, d = 8: 72.4 us for 67.4; 8 of 1000 to 3000, 8 heads over
+// 2, d = 32: 69.3 for 61.2), as a branch in the one walk 5 to 6 %, in a walk of their own nothing, or 0.2 of 9 us where all rows see few
+// (256 prompts of 16 tokens, 4 heads, d = 128).
 #include "common.h"
 #include "launch.h"
 #include "mfma_common.h"
@@ -20,8 +22,12 @@ namespace paged {
 using mfma::kLn2;
 using mfma::kNegInf;
 
+// wavefronts a SIMD that registers have to leave room for: bf16 at d = 128 has two registers too many by itself
+template <typename T, int D>
+constexpr int kRoomFor = sizeof(T) == 2 && D == 128 ? 3 : 1;
+
 template <typename T, int D, bool SPLIT>
-__global__ __launch_bounds__(64 * shared_waves(D * sizeof(T))) void shared_kernel(Args a)
+__global__ __launch_bounds__(64 * shared_waves(D * sizeof(T))) __attribute__((amdgpu_waves_per_eu(kRoomFor<T, D>))) void shared_kernel(Args a)
 {
   typedef Tile<T, D> TL;
   constexpr int W = shared_waves(TL::RB);
@@ -53,8 +59,8 @@ __global__ __launch_bounds__(64 * shared_waves(D * sizeof(T))) void shared_kerne
 
   const int len = max(__builtin_amdgcn_readfirstlane(raw_len), 0);
   const int first_pos = len - new_tokens;
-  const int lo = seen_by(a, first_pos + a.by_R.of(wg_row), len).lo;
-  const int hi = seen_by(a, first_pos + a.by_R.of(min(wg_row + 16 * W, rows) - 1), len).hi;  // keys that any row sees
+  const Range wg_first = seen_by(a, first_pos + a.by_R.of(wg_row), len), wg_last = seen_by(a, first_pos + a.by_R.of(min(wg_row + 16 * W, rows) - 1), len);
+  const int lo = wg_first.lo, hi = wg_last.hi;  // keys that any row sees
 
   Range my = seen_by(a, first_pos + tok, len);
   if (!row_ok) my.hi = -1;
@@ -70,11 +76,19 @@ __global__ __launch_bounds__(64 * shared_waves(D * sizeof(T))) void shared_kerne
     t_end = min(t + each, t_end);
   }
   const size_t page_bytes = ((size_t)a.G << a.page_shift) * TL::RB, group_bytes = ((size_t)g << a.page_shift) * TL::RB;
+  // few keys: by their number, or because pages are out of range
+  bool fine = TL::BF && few_keys(wg_first, wg_last);
+  auto look = [&]() __attribute__((always_inline)) {
+    const int page = list0 + lane;
+    if (TL::BF) fine = fine || __any(ids < 0 && page >= lo >> a.page_shift && page <= hi >> a.page_shift);
+  };
+  look();
   auto request = [&](int t, char *to) __attribute__((always_inline)) -> unsigned {
     const int first = (t * kTile) >> a.page_shift, last = (t * kTile + kTile - 1) >> a.page_shift;
     if (first < list0 || last >= list0 + 64) {
       list0 = first;
       ids = entries(first);
+      look();
     }
     const int key = t * kTile + (lane & 31);
     const int id = __shfl(ids, (key >> a.page_shift) - list0);
@@ -85,13 +99,13 @@ __global__ __launch_bounds__(64 * shared_waves(D * sizeof(T))) void shared_kerne
     return seen;
   };
 
-  Rows<T, D, false> r;
+  Rows<T, D> r;
   r.clear(row_ok);
   unsigned seen = t < t_end ? request(t, lds[0]) : 0u;
 #pragma unroll
   for (int i = 0; i < TL::NK; ++i) asm volatile("" : "+v"(q.x[i].x), "+v"(q.x[i].y), "+v"(q.x[i].z), "+v"(q.x[i].w));  // (arrived before the walk)
   mfma::arrived_all<0>();
-  while (t < t_end) {
+  auto pair = [&](auto two) __attribute__((always_inline)) {
 #pragma unroll
     for (int cur = 0; cur < 2; ++cur) {
       if (t >= t_end) break;
@@ -99,13 +113,17 @@ __global__ __launch_bounds__(64 * shared_waves(D * sizeof(T))) void shared_kerne
       const int base = t * kTile;
       if (base <= any_hi && base + kTile - 1 >= any_lo) {
         const bool all = seen == 0xFFFFFFFFu && row0 + 15 < rows && base >= r_last.lo && base + kTile - 1 <= r_first.hi;
-        r.attend(lds[cur], lds[cur] + TL::BYTES, q, a.scale2, seen & mfma::row_bits(my.lo - base, my.hi - base), all, base + 16 <= any_hi, lane);
+        r.template attend<decltype(two)::value>(lds[cur], lds[cur] + TL::BYTES, q, a.scale2, seen & mfma::row_bits(my.lo - base, my.hi - base), all,
+                                                base + 16 <= any_hi, lane);
       }
       mfma::arrived_all<0>();
       seen = next;
       ++t;
     }
-  }
+  };
+  while (t < t_end && !fine) pair(std::false_type{});
+  if constexpr (TL::BF)
+    while (t < t_end) pair(std::true_type{});
 
   const float l = r.total();
   if (!row_ok) return;

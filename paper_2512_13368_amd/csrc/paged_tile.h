@@ -213,7 +213,7 @@ __device__ __forceinline__ float row_max(float x)
 // row's maximum over the first keys it met; it is raised only when a lane's eight probabilities of a tile pass kSumLimit in sum, so the
 // usual tile takes no maximum; where it is far from 0 (see kFar), a tile takes one and has its logits scaled before it is subtracted.
 constexpr float kSumLimit = 4096.0f;
-template <typename T, int D, bool FINE>
+template <typename T, int D>
 struct Rows {
   typedef Tile<T, D> TL;
   f32x4 acc[TL::NV];
@@ -228,6 +228,7 @@ struct Rows {
   }
   // one tile; bit k of `seen`: this lane's row sees key k of the tile (all: no key is masked for any row; both: any row sees one of
   // the second 16)
+  template <bool FINE>
   __device__ __forceinline__ void attend(const char *ks, const char *vs, const typename TL::Query &q, float scale2, unsigned seen, bool all, bool both,
                                          int lane)
   {
