@@ -16,7 +16,7 @@
 //
 // Measured under steady load: two prompts of 6001 and 8191 tokens, 32 heads over 8, d = 128: 815 us, 1.04 PFLOP/s, where a bf16 product
 // of 8192^3 reaches 1.07; chunks of 512 over a window of 4096: 131 us, 870 TFLOP/s; 32 ragged prompts of 7 to 1997, 16 heads over 4,
-// d = 64: 124 us, 720 TFLOP/s.  (In the first milliseconds after a pause the card's clock dips: 884, 1053 and 851 us at the first, fifth
+// d = 64: 124 us, 720 TFLOP/s.  (Other cards: 797 to 850 us for the long ones, one 949.  In the first milliseconds after a pause the card's clock dips: 884, 1053 and 851 us at the first, fifth
 // and twentieth of the long calls.)  The matrix pipe is busy 52 % (d = 64: 41 %) and the vector ALUs' issue port 46 % (75 %) of the
 // time: a half tile's 16 exponentials alone are 256 cycles beside 512 (256) of products, and the two overlap in part.  Tried: both halves' logits
 // before the exponentials (848 against 836 us, 137 against 134 and 129), three wavefronts a SIMD instead of four at d = 64 (154 us
