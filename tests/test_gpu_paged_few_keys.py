@@ -7,6 +7,7 @@ import torch
 from paged_util import Cache, check
 from paper_2512_13368_amd import binding as B
 from test_gpu_paged import CROWD, TYPES, run_prompt
+from test_gpu_paged_paths import widen
 from test_gpu_paged_probabilities import check_fine, coarse, coarse_keys
 
 pytestmark = pytest.mark.gpu
@@ -40,7 +41,7 @@ def test_sequences_begin_with_few_keys(d, H, G, window):
 
 @pytest.mark.parametrize("d", DIMS)
 def test_so_do_walks_that_are_split(d):
-    c = Cache([150, 1, 43, 400], 4, 2, d, 16, "bf16", new=[150, 1, 40, 390], seed=d, scale=0.5 * d**-0.5, max_pages=40000)
+    c = widen(Cache([150, 1, 43, 400], 4, 2, d, 16, "bf16", new=[150, 1, 40, 390], seed=d, scale=0.5 * d**-0.5), 40000)
     assert B.paged_workspace_bytes(c.p, B.WS_PROMPT) > 0
     coarse_keys(c)
     Q, O, _ = run_prompt(c, Q=coarse(c, c.T, 4, d))
