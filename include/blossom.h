@@ -409,9 +409,9 @@ typedef struct {
   int32_t table_per_head; /* decode only: page_table is [S,G,max_pages]                            */
 } blossom_paged_params;
 
-/* Bytes of device workspace of blossom_attn_decode (BLOSSOM_WS_DECODE) and blossom_attn_prompt (BLOSSOM_WS_PROMPT): partial
- * results where a row's keys are split over workgroups.  Host call, no HIP; 0 for invalid params or when none is needed. */
-enum { BLOSSOM_WS_DECODE = 4, BLOSSOM_WS_PROMPT = 5 };
+/* Bytes of device workspace of blossom_attn_decode (BLOSSOM_WS_DECODE), blossom_attn_prompt (BLOSSOM_WS_PROMPT) and
+ * blossom_attn_tree (BLOSSOM_WS_TREE): partial results where a row's keys are split over workgroups.  Host call, no HIP; 0 for invalid params or when none is needed. */
+enum { BLOSSOM_WS_DECODE = 4, BLOSSOM_WS_PROMPT = 5, BLOSSOM_WS_TREE = 6 };
 size_t blossom_paged_workspace_bytes(const blossom_paged_params *p, int which);
 
 /*
@@ -448,6 +448,110 @@ int blossom_attn_decode(const blossom_paged_params *p, const void *Q, int64_t q_
 int blossom_attn_prompt(const blossom_paged_params *p, const void *Q, int64_t q_stride, const void *K_cache,
                         const void *V_cache, const int32_t *page_table, const int32_t *cu_seqlens, const int32_t *kv_len,
                         void *O, float *lse, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * ---- Several ways on from one history ----
+ *
+ * Drafted trees.  Tokens that somebody proposed, in branches, are attended together and the right ones kept.  The n drafted tokens of a
+ * sequence (cu_seqlens, as for a prompt) take the positions past .. past + n - 1 of its pages, past = kv_len[s] - n (kv_len below 0
+ * counts as 0): token i of them the slot past + i, whatever its place in the tree.  What it sees is its mask's business:
+ *   tree_mask         int64 [T]: bit k of a token's mask says that it sees drafted token k of its own sequence, 0 <= k < n, k < 64.
+ *                     For a tree: the token's own bit and its ancestors'.  Any other mask is as good (a later token, not itself, none);
+ *                     bits from n on are ignored, and drafted tokens from the 65th on are seen by none.
+ *   position          past + the number of drafted tokens other than itself that the token sees: in a tree, its depth behind the
+ *                     history.  Rotary angles go by it, and `window`: of the history a token sees positions j < past with
+ *                     position - j < window.  Drafted tokens are seen by the mask alone.
+ */
+
+/*
+ * blossom_kv_append for drafted tokens: keys and values go to the tokens' slots, rotated by their positions in the tree.  A token is
+ * without a place if its slot or its position is outside the capacity.
+ */
+int blossom_kv_append_tree(const blossom_paged_params *p, const void *Q, int64_t q_stride, const void *K, int64_t k_stride,
+                           const void *V, int64_t v_stride, const float *rope_cos, const float *rope_sin,
+                           const int32_t *page_table, const int32_t *cu_seqlens, const int32_t *kv_len,
+                           const int64_t *tree_mask, void *K_cache, void *V_cache, void *Q_rot, void *hip_stream);
+
+/*
+ * Attention of drafted tokens that the cache holds already, over their histories and what their masks name.  A token that sees nothing
+ * gives O = 0 and lse = -inf.
+ *   Q    in   [T,H,d] rows;  O  out  [T,H,d];  lse  out  fp32 [T,H] or NULL
+ *   ws   scratch, >= blossom_paged_workspace_bytes(p, BLOSSOM_WS_TREE), 16-byte aligned (NULL when that is 0)
+ */
+int blossom_attn_tree(const blossom_paged_params *p, const void *Q, int64_t q_stride, const void *K_cache, const void *V_cache,
+                      const int32_t *page_table, const int32_t *cu_seqlens, const int32_t *kv_len, const int64_t *tree_mask,
+                      void *O, float *lse, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Of each sequence's drafted tokens, keeps those that `keep` lists: the rows of slot past + keep[s][i] move to past + i, in both caches
+ * (one layer's; `p` and the lists are the same for all).  What lay between stays where it was, behind the new length.
+ *   keep      in   int32 [S, keep_width]: ascending drafted tokens; the first entry that does not ascend, or is none of 0 .. n - 1, ends it
+ *   new_len   out  int32 [S] or NULL: past + entries kept.  Not kv_len itself, which every layer's call reads.
+ * A row whose old or new slot has no page, or lies outside the capacity, is not moved.
+ */
+int blossom_kv_accept(const blossom_paged_params *p, int32_t keep_width, const int32_t *keep, const int32_t *page_table,
+                      const int32_t *cu_seqlens, const int32_t *kv_len, void *K_cache, void *V_cache, int32_t *new_len,
+                      void *hip_stream);
+
+/*
+ * Forked sequences.  Sequence n of n_new goes on from sequence parent[n] of the S that page_table and kv_len describe: a beam that was
+ * chosen several times is gone on from several times, one that was not is dropped, and its pages with it.  Nothing is moved: whole pages
+ * are shared, and `refs` counts who holds a page.  Entries of page_table outside [0, n_pages) are no pages; all others are held, also
+ * those behind a sequence's length.
+ *   parent      in   int32 [n_new]; an entry outside [0, S) makes an empty sequence
+ *   refs        in   int32 [n_pages]: table entries that hold a page, and whoever else does.  0: free
+ *   new_table   out  int32 [n_new, max_pages]: with L = kv_len[parent[n]] (0 .. capacity) and F = L / page, entries 0 .. F - 1 are the
+ *                    parent's.  From there to the last page that L + grow positions need (no more than the capacity): the eldest
+ *                    (lowest n) of a parent's sequences keeps the parent's page if refs says that nobody else holds it; every
+ *                    other entry is a fresh page.  All further entries are -1.
+ *   new_len     out  int32 [n_new]: L
+ *   new_refs    out  int32 [n_pages]: refs, less the entries of page_table, plus those of new_table
+ *   copies      out  int32 [n_new, 3]: (source, target, rows) where page F holds L mod page rows and is fresh; -1, -1, 0 elsewhere
+ *   missing     out  int32 [1]: fresh pages that there were not; their entries are -1, the last of the sequences go without first
+ * Fresh pages are those that new_refs has at 0 before they are given, but for those that a copy reads; the lowest first, to sequences
+ * and their entries in order.  With every page held by whom refs says, no page is written by two sequences.  No output may be
+ * an input.  grow = 0 makes room for nothing; with parent[n] = n the call lets pages behind shortened sequences go, and makes room.
+ *   ws   scratch, >= blossom_fork_workspace_bytes(p, n_new), 16-byte aligned
+ * H, G, d and dtype are checked and not used.  The copies themselves are done, for each layer's caches, by blossom_kv_copy_pages.
+ */
+size_t blossom_fork_workspace_bytes(const blossom_paged_params *p, int32_t n_new);
+int blossom_kv_fork(const blossom_paged_params *p, int32_t n_new, int32_t grow, const int32_t *parent, const int32_t *page_table,
+                    const int32_t *kv_len, const int32_t *refs, int32_t *new_table, int32_t *new_len, int32_t *new_refs,
+                    int32_t *copies, int32_t *missing, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Copies the first copies[i][2] positions (no more than a page) of page copies[i][0] to page copies[i][1], in both caches.  An entry with a
+ * page outside [0, n_pages), or one page twice, copies nothing.  No target may be a source or a target of another entry.
+ */
+int blossom_kv_copy_pages(const blossom_paged_params *p, int32_t n_copies, const int32_t *copies, void *K_cache, void *V_cache,
+                          void *hip_stream);
+
+/*
+ * Beam search's selection: of the continuations of a history's W beams by any of V items (a row of logits a beam),
+ * the K with the largest
+ *     score[b,w] + logits[bW + w, v] - log sum_u exp(logits[bW + w, u])
+ * in descending order; equal ones by beam, then by logit, then the lower item.  Sums and scores are held in 64 bits.
+ *   logits     in   [B W, V] rows of `dtype`, any element a row's first: logits_stride elements from a row to the next (0: V)
+ *   score      in   fp32 [B, W]: what the beams have come to.  A beam at -inf, or NaN, is not gone on from.
+ *   ended      in   uint8 [B, W] or NULL: beams at their end, which go on in one way: item `eos`, their score as it is
+ *   parent     out  int32 [B, K]: row bW + w of the beam gone on from (as blossom_kv_fork takes it)
+ *   token      out  int32 [B, K];  out_score  out  fp32 [B, K]: the sum above, rounded once
+ *   out_ended  out  uint8 [B, K] or NULL: 1 if the parent had ended or the token is eos
+ * A logit of -inf, or NaN, is no candidate and has no part in the sum; a row with a logit of +inf has none.  Where there are fewer than K
+ * candidates, the last entries are -1, -1, -inf, 0.
+ *   ws   scratch, >= blossom_beam_workspace_bytes(p), 16-byte aligned
+ */
+typedef struct {
+  int32_t B, W;   /* histories, beams of each (1 .. 64)                  */
+  int32_t K;      /* continuations chosen for each (1 .. 64)             */
+  int32_t V;      /* items                                               */
+  int32_t dtype;  /* of the logits                                       */
+  int32_t eos;    /* the item that ends a beam; -1: none (ended is NULL) */
+} blossom_beam_params;
+size_t blossom_beam_workspace_bytes(const blossom_beam_params *p);
+int blossom_beam_select(const blossom_beam_params *p, const void *logits, int64_t logits_stride, const float *score,
+                        const uint8_t *ended, int32_t *parent, int32_t *token, float *out_score, uint8_t *out_ended, void *ws,
+                        size_t ws_bytes, void *hip_stream);
 
 /*
  * Measured ceilings of the matrix-core forward (Eq. 1 as tiled QK^T / softmax / PV for the

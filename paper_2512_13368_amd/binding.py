@@ -15,12 +15,14 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libblossom.so")
 
 F32, BF16 = 0, 1
-WS_SELECT, WS_FWD, WS_BWD, WS_DENSE, WS_DECODE, WS_PROMPT = 0, 1, 2, 3, 4, 5
+WS_SELECT, WS_FWD, WS_BWD, WS_DENSE, WS_DECODE, WS_PROMPT, WS_TREE = 0, 1, 2, 3, 4, 5, 6
 
 EXPORTS = ("blossom_workspace_bytes", "blossom_select_blocks", "blossom_select_blocks_static", "blossom_select_blocks_cmp",
            "blossom_rope_select_blocks", "blossom_attn_bwd_rope", "blossom_select_positions_workspace_bytes",
            "blossom_select_positions", "blossom_attn_fwd_positions", "blossom_attn_bwd_positions", "blossom_out_proj_ln", "blossom_attn_fwd", "blossom_attn_bwd",
            "blossom_attn_bwd_stages", "blossom_paged_workspace_bytes", "blossom_kv_append", "blossom_attn_decode", "blossom_attn_prompt",
+           "blossom_kv_append_tree", "blossom_attn_tree", "blossom_kv_accept", "blossom_fork_workspace_bytes", "blossom_kv_fork",
+           "blossom_kv_copy_pages", "blossom_beam_workspace_bytes", "blossom_beam_select",
            "blossom_dense_causal_fwd", "blossom_probe_bytes", "blossom_probe", "blossom_strerror", "blossom_version")
 PROBE_WORKGROUPS = 4096
 BWD_GATE, BWD_INVERSE, BWD_DQ, BWD_DKV, BWD_ALL = 1, 2, 4, 8, 15
@@ -38,6 +40,10 @@ class BlossomPagedParams(ctypes.Structure):
     _fields_ = [(name, ctypes.c_float if name == "softmax_scale" else ctypes.c_int32)
                 for name in ("S", "T", "H", "G", "d", "page", "n_pages", "max_pages", "dtype", "softmax_scale", "window", "max_len",
                              "table_per_head")]
+
+
+class BlossomBeamParams(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("B", "W", "K", "V", "dtype", "eos")]
 
 
 class BlossomError(RuntimeError):
@@ -103,6 +109,23 @@ def lib() -> ctypes.CDLL:
         L.blossom_attn_decode.argtypes = [gp, vp, i64, vp, vp, i32p, i32p, vp, fp, vp, ctypes.c_size_t, vp]
         L.blossom_attn_prompt.restype = ctypes.c_int
         L.blossom_attn_prompt.argtypes = [gp, vp, i64, vp, vp, i32p, i32p, i32p, vp, fp, vp, ctypes.c_size_t, vp]
+        L.blossom_kv_append_tree.restype = ctypes.c_int
+        L.blossom_kv_append_tree.argtypes = [gp, vp, i64, vp, i64, vp, i64, fp, fp, i32p, i32p, i32p, vp, vp, vp, vp, vp]
+        L.blossom_attn_tree.restype = ctypes.c_int
+        L.blossom_attn_tree.argtypes = [gp, vp, i64, vp, vp, i32p, i32p, i32p, vp, vp, fp, vp, ctypes.c_size_t, vp]
+        L.blossom_kv_accept.restype = ctypes.c_int
+        L.blossom_kv_accept.argtypes = [gp, ctypes.c_int32, i32p, i32p, i32p, i32p, vp, vp, i32p, vp]
+        L.blossom_fork_workspace_bytes.restype = ctypes.c_size_t
+        L.blossom_fork_workspace_bytes.argtypes = [gp, ctypes.c_int32]
+        L.blossom_kv_fork.restype = ctypes.c_int
+        L.blossom_kv_fork.argtypes = [gp, ctypes.c_int32, ctypes.c_int32] + [i32p] * 9 + [vp, ctypes.c_size_t, vp]
+        L.blossom_kv_copy_pages.restype = ctypes.c_int
+        L.blossom_kv_copy_pages.argtypes = [gp, ctypes.c_int32, i32p, vp, vp, vp]
+        bp = ctypes.POINTER(BlossomBeamParams)
+        L.blossom_beam_workspace_bytes.restype = ctypes.c_size_t
+        L.blossom_beam_workspace_bytes.argtypes = [bp]
+        L.blossom_beam_select.restype = ctypes.c_int
+        L.blossom_beam_select.argtypes = [bp, vp, i64, fp, vp, i32p, i32p, fp, vp, vp, ctypes.c_size_t, vp]
         L.blossom_dense_causal_fwd.restype = ctypes.c_int
         L.blossom_dense_causal_fwd.argtypes = [pp, vp, vp, vp, i32p, vp, fp, vp, ctypes.c_size_t, vp]
         L.blossom_probe_bytes.restype = ctypes.c_size_t
@@ -705,6 +728,11 @@ def kv_append(p: PagedParams, K, V, K_cache, V_cache, page_table, cu_seqlens, kv
             if rc:
                 raise BlossomError(rc, "blossom_kv_append")
             return Q_rot
+    return _append(p, "blossom_kv_append", K, V, K_cache, V_cache, page_table, cu_seqlens, kv_len, None, Q, cos, sin, Q_rot, stream)
+
+
+def _append(p: PagedParams, name, K, V, K_cache, V_cache, page_table, cu_seqlens, kv_len, tree_mask, Q, cos, sin, Q_rot, stream):
+    """The Python path of kv_append and kv_append_tree: allocates what is missing, names what is wrong."""
     import torch
     dt = _torch_dtype(p)
     ks, vs = _token_stride(K, p.T, p.G, p.d, dt, "K"), _token_stride(V, p.T, p.G, p.d, dt, "V")
@@ -720,16 +748,18 @@ def kv_append(p: PagedParams, K, V, K_cache, V_cache, page_table, cu_seqlens, kv
     _check_cache(p, K_cache, V_cache, page_table, cu_seqlens, kv_len)
     _check_tensor(cos, (p.capacity, p.d // 2), torch.float32, "rope_cos")
     _check_tensor(sin, (p.capacity, p.d // 2), torch.float32, "rope_sin")
+    _check_tensor(tree_mask, (p.T,), torch.int64, "tree_mask")
     cp = p.c()
-    rc = lib().blossom_kv_append(ctypes.byref(cp), _ptr(Q), qs, _ptr(K), ks, _ptr(V), vs, _ptr(cos), _ptr(sin), _ptr(page_table),
-                                 _ptr(cu_seqlens), _ptr(kv_len), _ptr(K_cache), _ptr(V_cache), _ptr(Q_rot), _stream(stream))
+    mask = () if tree_mask is None else (_ptr(tree_mask),)
+    rc = getattr(lib(), name)(ctypes.byref(cp), _ptr(Q), qs, _ptr(K), ks, _ptr(V), vs, _ptr(cos), _ptr(sin), _ptr(page_table),
+                              _ptr(cu_seqlens), _ptr(kv_len), *mask, _ptr(K_cache), _ptr(V_cache), _ptr(Q_rot), _stream(stream))
     if rc:
-        raise BlossomError(rc, "blossom_kv_append")
+        raise BlossomError(rc, name)
     return Q_rot
 
 
-def _paged_attn(p: PagedParams, which, rows, Q, K_cache, V_cache, page_table, cu_seqlens, kv_len, O, lse, ws, stream):
-    """The Python path of attn_decode and attn_prompt: allocates what is missing, names what is wrong."""
+def _paged_attn(p: PagedParams, which, rows, Q, K_cache, V_cache, page_table, cu_seqlens, kv_len, O, lse, ws, stream, tree_mask=None):
+    """The Python path of attn_decode, attn_prompt and attn_tree: allocates what is missing, names what is wrong."""
     import torch
     dt = _torch_dtype(p)
     qs = _token_stride(Q, rows, p.H, p.d, dt, "Q")
@@ -749,6 +779,8 @@ def _paged_attn(p: PagedParams, which, rows, Q, K_cache, V_cache, page_table, cu
     tail = (_ptr(kv_len), _ptr(O), _ptr(lse), _ptr(ws), nbytes, _stream(stream))
     if which == WS_DECODE:
         name, rc = "blossom_attn_decode", lib().blossom_attn_decode(*head, *tail)
+    elif which == WS_TREE:
+        name, rc = "blossom_attn_tree", lib().blossom_attn_tree(*head, _ptr(cu_seqlens), tail[0], _ptr(tree_mask), *tail[1:])
     else:
         name, rc = "blossom_attn_prompt", lib().blossom_attn_prompt(*head, _ptr(cu_seqlens), *tail)
     if rc:
@@ -780,3 +812,214 @@ def attn_prompt(p: PagedParams, Q, K_cache, V_cache, page_table, cu_seqlens, kv_
     if cu_seqlens is None:
         raise ValueError("cu_seqlens is required")
     return _paged_attn(p, WS_PROMPT, p.T, Q, K_cache, V_cache, page_table, cu_seqlens, kv_len, O, lse, ws, stream)
+
+
+def _here(**tensors):
+    """All of them on the current device, whose stream the call goes to."""
+    import torch
+    now = torch.cuda.current_device() if torch.cuda.is_initialized() else 0
+    for name, t in tensors.items():
+        if t is not None and (not t.is_cuda or (t.device.index or 0) != now):
+            raise ValueError(f"{name}: expected a tensor on the current device, cuda:{now}, got one on {t.device}")
+
+
+def kv_append_tree(p: PagedParams, K, V, K_cache, V_cache, page_table, cu_seqlens, kv_len, tree_mask, Q=None, rope=None, Q_rot=None,
+                   stream=None):
+    """blossom_kv_append_tree: kv_append for drafted tokens, each rotated by its position in its tree.  tree_mask int64 [T]: bit k of
+    a token's says that it sees drafted token k of its sequence.  Returns Q_rot."""
+    cos, sin = rope if rope is not None else (None, None)
+    if Q is None or Q_rot is not None:
+        rc = (_fast or fastcall()).kv_append_tree(p, Q, K, V, cos, sin, page_table, cu_seqlens, kv_len, tree_mask, K_cache, V_cache,
+                                                  Q_rot, stream)
+        if rc is not None:
+            if rc:
+                raise BlossomError(rc, "blossom_kv_append_tree")
+            return Q_rot
+    if tree_mask is None:
+        raise ValueError("tree_mask is required")
+    _here(K=K, V=V, K_cache=K_cache, V_cache=V_cache, page_table=page_table, cu_seqlens=cu_seqlens, kv_len=kv_len, tree_mask=tree_mask,
+          Q=Q, rope_cos=cos, rope_sin=sin, Q_rot=Q_rot)
+    return _append(p, "blossom_kv_append_tree", K, V, K_cache, V_cache, page_table, cu_seqlens, kv_len, tree_mask, Q, cos, sin, Q_rot,
+                   stream)
+
+
+def attn_tree(p: PagedParams, Q, K_cache, V_cache, page_table, cu_seqlens, kv_len, tree_mask, O=None, lse=None, ws=None, stream=None):
+    """blossom_attn_tree: attention of drafted tokens (Q [T,H,d]) over their sequences' histories and the drafted tokens that
+    tree_mask (int64 [T]) names.  Returns (O, lse); lse is written where given."""
+    if O is not None:
+        rc = (_fast or fastcall()).attn_tree(p, Q, K_cache, V_cache, page_table, cu_seqlens, kv_len, tree_mask, O, lse, ws, stream)
+        if rc is not None:
+            if rc:
+                raise BlossomError(rc, "blossom_attn_tree")
+            return O, lse
+    import torch
+    if cu_seqlens is None:
+        raise ValueError("cu_seqlens is required")
+    if tree_mask is None:
+        raise ValueError("tree_mask is required")
+    _check_tensor(tree_mask, (p.T,), torch.int64, "tree_mask")
+    _here(Q=Q, K_cache=K_cache, V_cache=V_cache, page_table=page_table, cu_seqlens=cu_seqlens, kv_len=kv_len, tree_mask=tree_mask, O=O,
+          lse=lse, ws=ws)
+    return _paged_attn(p, WS_TREE, p.T, Q, K_cache, V_cache, page_table, cu_seqlens, kv_len, O, lse, ws, stream, tree_mask)
+
+
+def kv_accept(p: PagedParams, keep, K_cache, V_cache, page_table, cu_seqlens, kv_len, new_len=None, stream=None):
+    """blossom_kv_accept: of each sequence's drafted tokens those that keep (int32 [S, n], ascending, then -1) lists move down behind the
+    history.  Returns new_len int32 [S], the lengths then; kv_len stays, for the other layers' calls."""
+    if new_len is not None:
+        rc = (_fast or fastcall()).kv_accept(p, keep, K_cache, V_cache, page_table, cu_seqlens, kv_len, new_len, stream)
+        if rc is not None:
+            if rc:
+                raise BlossomError(rc, "blossom_kv_accept")
+            return new_len
+    import torch
+    if keep is None or cu_seqlens is None:
+        raise ValueError("keep and cu_seqlens are required")
+    if keep.dim() != 2 or keep.shape[0] != p.S or keep.shape[1] < 1:
+        raise ValueError(f"keep: expected shape ({p.S}, n >= 1), got {tuple(keep.shape)}")
+    _check_tensor(keep, keep.shape, torch.int32, "keep")
+    _check_cache(p, K_cache, V_cache, page_table, cu_seqlens, kv_len)
+    _here(keep=keep, K_cache=K_cache, V_cache=V_cache, page_table=page_table, cu_seqlens=cu_seqlens, kv_len=kv_len, new_len=new_len)
+    if new_len is None:
+        with _on(stream):
+            new_len = torch.empty(p.S, dtype=torch.int32, device=keep.device)
+    _check_tensor(new_len, (p.S,), torch.int32, "new_len")
+    cp = p.c()
+    rc = lib().blossom_kv_accept(ctypes.byref(cp), keep.shape[1], _ptr(keep), _ptr(page_table), _ptr(cu_seqlens), _ptr(kv_len),
+                                 _ptr(K_cache), _ptr(V_cache), _ptr(new_len), _stream(stream))
+    if rc:
+        raise BlossomError(rc, "blossom_kv_accept")
+    return new_len
+
+
+def fork_workspace_bytes(p: PagedParams, n_new: int) -> int:
+    cp = p.c()
+    return int(lib().blossom_fork_workspace_bytes(ctypes.byref(cp), n_new))
+
+
+def kv_fork(p: PagedParams, parent, page_table, kv_len, refs, grow=0, new_table=None, new_len=None, new_refs=None, copies=None,
+            missing=None, ws=None, stream=None):
+    """blossom_kv_fork: parent int32 [N] says which of p.S sequences each of N new ones goes on from, with room for `grow` more
+    positions.  Returns (new_table [N, max_pages], new_len [N], new_refs [n_pages], copies [N, 3], missing [1]): whole pages are shared,
+    `copies` goes to kv_copy_pages for each layer, `missing` counts the pages that there were not."""
+    if new_table is not None:
+        rc = (_fast or fastcall()).kv_fork(p, parent, page_table, kv_len, refs, grow, new_table, new_len, new_refs, copies, missing, ws,
+                                           stream)
+        if rc is not None:
+            if rc:
+                raise BlossomError(rc, "blossom_kv_fork")
+            return new_table, new_len, new_refs, copies, missing
+    import torch
+    for t, nm in ((parent, "parent"), (page_table, "page_table"), (kv_len, "kv_len"), (refs, "refs")):
+        if t is None:
+            raise ValueError(f"{nm} is required")
+    if parent.dim() != 1 or parent.shape[0] < 1:
+        raise ValueError(f"parent: expected shape (n >= 1,), got {tuple(parent.shape)}")
+    N, i32 = parent.shape[0], torch.int32
+    _check_tensor(parent, (N,), i32, "parent")
+    _check_tensor(page_table, (p.S, p.max_pages), i32, "page_table")
+    _check_tensor(kv_len, (p.S,), i32, "kv_len")
+    _check_tensor(refs, (p.n_pages,), i32, "refs")
+    _here(parent=parent, page_table=page_table, kv_len=kv_len, refs=refs, new_table=new_table, new_len=new_len, new_refs=new_refs,
+          copies=copies, missing=missing, ws=ws)
+    need = fork_workspace_bytes(p, N)
+    shapes = ((new_table, (N, p.max_pages), "new_table"), (new_len, (N,), "new_len"), (new_refs, (p.n_pages,), "new_refs"),
+              (copies, (N, 3), "copies"), (missing, (1,), "missing"))
+    with _on(stream):
+        out = [torch.empty(shape, dtype=i32, device=parent.device) if t is None else t for t, shape, _ in shapes]
+        if ws is None:
+            ws = torch.empty(max(need, 16), dtype=torch.uint8, device=parent.device)
+    for t, (_, shape, nm) in zip(out, shapes):
+        _check_tensor(t, shape, i32, nm)
+    nbytes = _ws_bytes(ws, need)
+    cp = p.c()
+    rc = lib().blossom_kv_fork(ctypes.byref(cp), N, grow, _ptr(parent), _ptr(page_table), _ptr(kv_len), _ptr(refs), *map(_ptr, out),
+                               _ptr(ws), nbytes, _stream(stream))
+    if rc:
+        raise BlossomError(rc, "blossom_kv_fork")
+    return tuple(out)
+
+
+def kv_copy_pages(p: PagedParams, copies, K_cache, V_cache, stream=None):
+    """blossom_kv_copy_pages: copies int32 [N, 3] of (source page, target page, positions) in both caches of a layer."""
+    rc = (_fast or fastcall()).kv_copy_pages(p, copies, K_cache, V_cache, stream)
+    if rc is not None:
+        if rc:
+            raise BlossomError(rc, "blossom_kv_copy_pages")
+        return
+    import torch
+    for t, nm in ((copies, "copies"), (K_cache, "K_cache"), (V_cache, "V_cache")):
+        if t is None:
+            raise ValueError(f"{nm} is required")
+    if copies.dim() != 2 or copies.shape[0] < 1 or copies.shape[1] != 3:
+        raise ValueError(f"copies: expected shape (n >= 1, 3), got {tuple(copies.shape)}")
+    _check_tensor(copies, copies.shape, torch.int32, "copies")
+    shp = (p.n_pages, p.G, p.page, p.d)
+    _check_tensor(K_cache, shp, _torch_dtype(p), "K_cache")
+    _check_tensor(V_cache, shp, _torch_dtype(p), "V_cache")
+    _here(copies=copies, K_cache=K_cache, V_cache=V_cache)
+    cp = p.c()
+    rc = lib().blossom_kv_copy_pages(ctypes.byref(cp), copies.shape[0], _ptr(copies), _ptr(K_cache), _ptr(V_cache), _stream(stream))
+    if rc:
+        raise BlossomError(rc, "blossom_kv_copy_pages")
+
+
+@dataclass
+class BeamParams:
+    """blossom_beam_params: B histories of W beams each, of whose continuations by any of V items the K best are chosen."""
+    B: int
+    W: int
+    K: int
+    V: int
+    dtype: int = F32
+    eos: int = -1
+
+    def c(self) -> BlossomBeamParams:
+        return BlossomBeamParams(self.B, self.W, self.K, self.V, self.dtype, self.eos)
+
+
+def beam_workspace_bytes(p: BeamParams) -> int:
+    cp = p.c()
+    return int(lib().blossom_beam_workspace_bytes(ctypes.byref(cp)))
+
+
+def beam_select(p: BeamParams, logits, score, ended=None, parent=None, token=None, out_score=None, out_ended=None, ws=None, stream=None):
+    """blossom_beam_select: logits [B*W, V] (rows may be slices of wider ones), score fp32 [B, W], ended bool or uint8 [B, W] or None.
+    Returns (parent, token, out_score, out_ended), each [B, K], the best first: parent is a row of `logits`."""
+    if parent is not None and out_ended is not None:
+        rc = (_fast or fastcall()).beam_select(p, logits, score, ended, parent, token, out_score, out_ended, ws, stream)
+        if rc is not None:
+            if rc:
+                raise BlossomError(rc, "blossom_beam_select")
+            return parent, token, out_score, out_ended
+    import torch
+    if logits is None or score is None:
+        raise ValueError("logits and score are required")
+    rows = p.B * p.W
+    if tuple(logits.shape) != (rows, p.V) or logits.dtype != _torch_dtype(p) or not logits.is_cuda or (p.V > 1 and logits.stride(1) != 1) or \
+            (rows > 1 and logits.stride(0) < p.V):
+        raise ValueError(f"logits: expected cuda tensor {(rows, p.V)} {_torch_dtype(p)} of contiguous rows that do not overlap, got "
+                         f"{tuple(logits.shape)} {logits.dtype} strides={tuple(logits.stride())} cuda={logits.is_cuda}")
+    _check_tensor(score, (p.B, p.W), torch.float32, "score")
+    flags = (torch.bool, torch.uint8)
+    _check_tensor(ended, (p.B, p.W), ended.dtype if ended is not None and ended.dtype in flags else torch.bool, "ended")
+    _here(logits=logits, score=score, ended=ended, parent=parent, token=token, out_score=out_score, out_ended=out_ended, ws=ws)
+    need = beam_workspace_bytes(p)
+    with _on(stream):
+        def new(t, dtype):
+            return torch.empty((p.B, p.K), dtype=dtype, device=logits.device) if t is None else t
+
+        parent, token, out_score, out_ended = new(parent, torch.int32), new(token, torch.int32), new(out_score, torch.float32), new(out_ended, torch.bool)
+        if ws is None:
+            ws = torch.empty(max(need, 16), dtype=torch.uint8, device=logits.device)
+    _check_tensor(parent, (p.B, p.K), torch.int32, "parent")
+    _check_tensor(token, (p.B, p.K), torch.int32, "token")
+    _check_tensor(out_score, (p.B, p.K), torch.float32, "out_score")
+    _check_tensor(out_ended, (p.B, p.K), out_ended.dtype if out_ended.dtype in flags else torch.bool, "out_ended")
+    nbytes = _ws_bytes(ws, need)
+    cp = p.c()
+    rc = lib().blossom_beam_select(ctypes.byref(cp), _ptr(logits), logits.stride(0) if rows > 1 else 0, _ptr(score), _ptr(ended), _ptr(parent),
+                                   _ptr(token), _ptr(out_score), _ptr(out_ended), _ptr(ws), nbytes, _stream(stream))
+    if rc:
+        raise BlossomError(rc, "blossom_beam_select")
+    return parent, token, out_score, out_ended

@@ -33,6 +33,9 @@ SOURCES = {
     "paged_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "paged_prompt.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "paged_shared.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "paged_pages.hip": [],
+    "beam_api.hip": [],
+    "beam.hip": [],
 }
 
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",

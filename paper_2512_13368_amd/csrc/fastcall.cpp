@@ -24,20 +24,26 @@ PyObject *g_paged_fields[13];
 const char *kPagedFields[13] = {"S", "T", "H", "G", "d", "page", "n_pages", "max_pages", "dtype", "softmax_scale", "window", "max_len",
                                 "table_per_head"};
 
+PyObject *g_beam_fields[6];
+const char *kBeamFields[6] = {"B", "W", "K", "V", "dtype", "eos"};
+
 // One call's arguments, read in order; `ok` falls at the first that is not as expected.
 struct Arguments {
   PyObject *const *arg;
   bool ok = true;
   at::ScalarType T{};
   void *stream = nullptr;
+  int device = -1;     // of the tensors read so far
+  bool mixed = false;  // they are on several
 
   explicit Arguments(PyObject *const *a) : arg(a) {}
 
-  // the 13 fields of a parameter block, the one at `real` a number, the others whole
-  bool fields(PyObject *const *names, int real, long (&v)[13], float *number)
+  // the fields of a parameter block, the one at `real` a number, the others whole
+  template <int N>
+  bool fields(PyObject *const *names, int real, long (&v)[N], float *number)
   {
     PyObject *obj = *arg++;
-    for (int i = 0; i < 13 && ok; ++i) {
+    for (int i = 0; i < N && ok; ++i) {
       PyObject *x = PyObject_GetAttr(obj, names[i]);
       if (!x) return ok = false;
       if (i == real) *number = (float)PyFloat_AsDouble(x);
@@ -47,6 +53,14 @@ struct Arguments {
     }
     return ok;
   }
+  void seen(const at::Tensor &t)
+  {
+    const int d = t.get_device();
+    mixed = mixed || (device >= 0 && d != device);
+    device = d;
+  }
+  // all of them on the current device, whose stream the call goes to
+  void here() { ok = ok && !mixed && (device < 0 || c10::hip::device_count() == 0 || device == c10::hip::current_device()); }
   int32_t whole()
   {
     const long v = PyLong_AsLong(*arg++);
@@ -74,7 +88,28 @@ struct Arguments {
     }
     const at::Tensor &t = THPVariable_Unpack(obj);
     ok = t.is_cuda() && t.scalar_type() == type && t.sizes() == shape && t.is_contiguous();
+    if (ok) seen(t);
     return ok ? static_cast<P *>(t.data_ptr()) : nullptr;
+  }
+  // contiguous int32 rows [rows, *width], or [*width] where `rows` is 0
+  int32_t *table(int64_t rows, int64_t *width)
+  {
+    PyObject *obj = *arg;
+    *width = 0;
+    if (ok && THPVariable_Check(obj)) {
+      const at::Tensor &t = THPVariable_Unpack(obj);
+      if (t.dim() == (rows ? 2 : 1)) *width = t.size(rows ? 1 : 0);
+    }
+    ok = ok && *width >= 1 && *width <= 0x7FFFFFFF;
+    const int64_t two[2] = {rows, *width};
+    return tensor<int32_t>(rows ? at::IntArrayRef(two, 2) : at::IntArrayRef(width, 1), at::kInt);
+  }
+  // [B, W] flags of one byte
+  uint8_t *flags(at::IntArrayRef shape, bool optional)
+  {
+    PyObject *obj = *arg;
+    const bool byte = obj != Py_None && THPVariable_Check(obj) && THPVariable_Unpack(obj).scalar_type() == at::kByte;
+    return tensor<uint8_t>(shape, byte ? at::kByte : at::kBool, optional);
   }
   // a contiguous device tensor; None, or any tensor, only where `need` is 0
   void *workspace(size_t need, size_t *bytes)
@@ -92,6 +127,7 @@ struct Arguments {
     const at::Tensor &t = THPVariable_Unpack(obj);
     ok = need == 0 || (t.is_cuda() && t.is_contiguous());
     if (!ok) return nullptr;
+    if (need) seen(t);
     *bytes = t.nbytes();
     return t.data_ptr();
   }
@@ -181,7 +217,42 @@ struct PagedCall : Arguments {
     ok = t.is_cuda() && t.scalar_type() == T && t.dim() == 3 && t.size(0) == count && t.size(1) == heads && t.size(2) == p.d &&
          t.stride(2) == 1 && (heads == 1 || t.stride(1) == p.d) && (count <= 1 || t.stride(0) >= heads * p.d);
     if (!ok) return nullptr;
+    seen(t);
     if (count > 1) *stride = t.stride(0);
+    return t.data_ptr();
+  }
+};
+
+// Arguments that begin with a beam search's parameter block.
+struct BeamCall : Arguments {
+  blossom_beam_params p{};
+
+  using Arguments::Arguments;
+
+  bool params()
+  {
+    long v[6];
+    if (!fields(g_beam_fields, -1, v, nullptr)) return false;
+    p = {(int32_t)v[0], (int32_t)v[1], (int32_t)v[2], (int32_t)v[3], (int32_t)v[4], (int32_t)v[5]};
+    T = p.dtype == 0 ? at::kFloat : at::kBFloat16;
+    return true;
+  }
+  // [B W, V], contiguous rows that do not overlap
+  void *logits(int64_t *stride)
+  {
+    PyObject *obj = *arg++;
+    *stride = 0;
+    if (!ok || !THPVariable_Check(obj)) {
+      ok = false;
+      return nullptr;
+    }
+    const at::Tensor &t = THPVariable_Unpack(obj);
+    const int64_t rows = (int64_t)p.B * p.W;
+    ok = t.is_cuda() && t.scalar_type() == T && t.dim() == 2 && t.size(0) == rows && t.size(1) == p.V && (p.V <= 1 || t.stride(1) == 1) &&
+         (rows <= 1 || t.stride(0) >= p.V);
+    if (!ok) return nullptr;
+    seen(t);
+    if (rows > 1) *stride = t.stride(0);
     return t.data_ptr();
   }
 };
@@ -474,10 +545,133 @@ FASTCALL_OF(PagedCall, attn_prompt, 11)
   return c.run([&] { return blossom_attn_prompt(&p, Q, qs, t.K, t.V, t.table, t.cu, t.len, O, lse, ws, bytes, c.stream); });
 }
 
+// kv_append_tree(p, Q, K, V, rope_cos, rope_sin, page_table, cu_seqlens, kv_len, tree_mask, K_cache, V_cache, Q_rot, stream)
+FASTCALL_OF(PagedCall, kv_append_tree, 14)
+{
+  const blossom_paged_params &p = c.p;
+  const int64_t held = (int64_t)p.max_pages * p.page, cap = p.max_len > 0 && p.max_len < held ? p.max_len : held;
+  const int64_t x[3] = {p.T, p.H, p.d}, r[2] = {cap, p.d / 2};
+  int64_t qs, ks, vs;
+  void *Q = c.rows(p.T, p.H, &qs, true), *K = c.rows(p.T, p.G, &ks), *V = c.rows(p.T, p.G, &vs);
+  float *cos = c.tensor<float>(r, at::kFloat, true), *sin = c.tensor<float>(r, at::kFloat, true);
+  CacheTensors t;
+  t.table = t.get_table(c);
+  t.cu = t.get_counts(c, (int64_t)p.S + 1);
+  t.len = t.get_counts(c, p.S);
+  int64_t *mask = c.tensor<int64_t>(at::IntArrayRef(x, 1), at::kLong);
+  t.K = t.get_cache(c);
+  t.V = t.get_cache(c);
+  void *Q_rot = c.tensor(x, c.T, true);
+  c.here();
+  c.on_stream();
+  return c.run([&] { return blossom_kv_append_tree(&p, Q, qs, K, ks, V, vs, cos, sin, t.table, t.cu, t.len, mask, t.K, t.V, Q_rot, c.stream); });
+}
+
+// attn_tree(p, Q, K_cache, V_cache, page_table, cu_seqlens, kv_len, tree_mask, O, lse, ws, stream)
+FASTCALL_OF(PagedCall, attn_tree, 12)
+{
+  const blossom_paged_params &p = c.p;
+  const int64_t x[3] = {p.T, p.H, p.d};
+  int64_t qs;
+  void *Q = c.rows(p.T, p.H, &qs);
+  CacheTensors t;
+  t.K = t.get_cache(c);
+  t.V = t.get_cache(c);
+  t.table = t.get_table(c);
+  t.cu = t.get_counts(c, (int64_t)p.S + 1);
+  t.len = t.get_counts(c, p.S);
+  int64_t *mask = c.tensor<int64_t>(at::IntArrayRef(x, 1), at::kLong);
+  void *O = c.tensor(x, c.T);
+  float *lse = c.tensor<float>(at::IntArrayRef(x, 2), at::kFloat, true);
+  size_t bytes;
+  void *ws = c.workspace(blossom_paged_workspace_bytes(&p, BLOSSOM_WS_TREE), &bytes);
+  c.here();
+  c.on_stream();
+  return c.run([&] { return blossom_attn_tree(&p, Q, qs, t.K, t.V, t.table, t.cu, t.len, mask, O, lse, ws, bytes, c.stream); });
+}
+
+// kv_accept(p, keep, K_cache, V_cache, page_table, cu_seqlens, kv_len, new_len, stream)
+FASTCALL_OF(PagedCall, kv_accept, 9)
+{
+  const blossom_paged_params &p = c.p;
+  int64_t width;
+  int32_t *keep = c.table(p.S, &width);
+  CacheTensors t;
+  t.K = t.get_cache(c);
+  t.V = t.get_cache(c);
+  t.table = t.get_table(c);
+  t.cu = t.get_counts(c, (int64_t)p.S + 1);
+  t.len = t.get_counts(c, p.S);
+  int32_t *new_len = t.get_counts(c, p.S);
+  c.here();
+  c.on_stream();
+  return c.run([&] { return blossom_kv_accept(&p, (int32_t)width, keep, t.table, t.cu, t.len, t.K, t.V, new_len, c.stream); });
+}
+
+// kv_fork(p, parent, page_table, kv_len, refs, grow, new_table, new_len, new_refs, copies, missing, ws, stream)
+FASTCALL_OF(PagedCall, kv_fork, 13)
+{
+  const blossom_paged_params &p = c.p;
+  int64_t N;
+  int32_t *parent = c.table(0, &N);
+  const int64_t from[2] = {p.S, p.max_pages}, to[2] = {N, p.max_pages}, three[2] = {N, 3};
+  CacheTensors t;
+  t.table = c.tensor<int32_t>(from, at::kInt);
+  t.len = t.get_counts(c, p.S);
+  int32_t *refs = t.get_counts(c, p.n_pages);
+  const int32_t grow = c.whole();
+  int32_t *new_table = c.tensor<int32_t>(to, at::kInt), *new_len = t.get_counts(c, N), *new_refs = t.get_counts(c, p.n_pages);
+  int32_t *copies = c.tensor<int32_t>(three, at::kInt), *missing = t.get_counts(c, 1);
+  size_t bytes;
+  void *ws = c.workspace(1, &bytes);
+  c.here();
+  c.on_stream();
+  return c.run([&] {
+    return blossom_kv_fork(&p, (int32_t)N, grow, parent, t.table, t.len, refs, new_table, new_len, new_refs, copies, missing, ws, bytes, c.stream);
+  });
+}
+
+// kv_copy_pages(p, copies, K_cache, V_cache, stream)
+FASTCALL_OF(PagedCall, kv_copy_pages, 5)
+{
+  const blossom_paged_params &p = c.p;
+  int64_t n = 0;
+  if (THPVariable_Check(*c.arg) && THPVariable_Unpack(*c.arg).dim() == 2) n = THPVariable_Unpack(*c.arg).size(0);
+  c.ok = c.ok && n >= 1 && n <= 0x7FFFFFFF;
+  const int64_t three[2] = {n, 3};
+  int32_t *copies = c.tensor<int32_t>(three, at::kInt);
+  CacheTensors t;
+  t.K = t.get_cache(c);
+  t.V = t.get_cache(c);
+  c.here();
+  c.on_stream();
+  return c.run([&] { return blossom_kv_copy_pages(&p, (int32_t)n, copies, t.K, t.V, c.stream); });
+}
+
+// beam_select(p, logits, score, ended, parent, token, out_score, out_ended, ws, stream)
+FASTCALL_OF(BeamCall, beam_select, 10)
+{
+  const blossom_beam_params &p = c.p;
+  const int64_t in[2] = {p.B, p.W}, out[2] = {p.B, p.K};
+  int64_t stride;
+  void *logits = c.logits(&stride);
+  float *score = c.tensor<float>(in, at::kFloat);
+  uint8_t *ended = c.flags(in, true);
+  int32_t *parent = c.tensor<int32_t>(out, at::kInt), *token = c.tensor<int32_t>(out, at::kInt);
+  float *out_score = c.tensor<float>(out, at::kFloat);
+  uint8_t *out_ended = c.flags(out, false);
+  size_t bytes;
+  void *ws = c.workspace(1, &bytes);
+  c.here();
+  c.on_stream();
+  return c.run([&] { return blossom_beam_select(&p, logits, stride, score, ended, parent, token, out_score, out_ended, ws, bytes, c.stream); });
+}
+
 #define ENTRY(name) {#name, (PyCFunction)(void *)name, METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {ENTRY(select_blocks), ENTRY(rope_select_blocks), ENTRY(select_positions), ENTRY(attn_fwd),
                           ENTRY(attn_fwd_positions), ENTRY(attn_bwd), ENTRY(attn_bwd_positions), ENTRY(out_proj_ln),
-                          ENTRY(kv_append), ENTRY(attn_decode), ENTRY(attn_prompt),
+                          ENTRY(kv_append), ENTRY(attn_decode), ENTRY(attn_prompt), ENTRY(kv_append_tree), ENTRY(attn_tree),
+                          ENTRY(kv_accept), ENTRY(kv_fork), ENTRY(kv_copy_pages), ENTRY(beam_select),
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
@@ -488,6 +682,8 @@ PyMODINIT_FUNC PyInit__fastcall()
   for (int i = 0; i < 13; ++i)
     if (!(g_fields[i] = PyUnicode_InternFromString(kFields[i])) || !(g_paged_fields[i] = PyUnicode_InternFromString(kPagedFields[i])))
       return nullptr;
+  for (int i = 0; i < 6; ++i)
+    if (!(g_beam_fields[i] = PyUnicode_InternFromString(kBeamFields[i]))) return nullptr;
   if (!(g_cuda_stream = PyUnicode_InternFromString("cuda_stream"))) return nullptr;
   return PyModule_Create(&kModule);
 }

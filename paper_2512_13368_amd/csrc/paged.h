@@ -49,18 +49,45 @@ struct Args {
                                // workspace; prompt: [T, H, parts, ..]
   int row_tiles;               // prompt: workgroups a key/value head and part
   int2 *part_of;               // decode: [S] first part and parts of a sequence, there too
+  const int64_t *tree;         // drafted trees: [T] which of its sequence's drafted tokens a token sees, or nullptr
+  int units;                   // workgroups a key/value head; `parts` of them beyond one a row tile (0: walks are whole).  The partial
+                               // sums are [units, G, rows of a tile, ..] then
+  int4 *part_at;               // [T] of a token's sequence: its first unit, the parts of its walks, its first token; in the workspace
 };
 
 // HIP counts a launch's threads in 32 bits.  The launchers below start nothing and return false for a call that would have more.
 inline bool countable(long workgroups, int threads) { return workgroups * threads < 1l << 32; }
 
-// append: paged_append.hip
+// append: paged_append.hip (a.tree: drafted tokens, turned by their places in their trees)
 bool launch_append(const Args &a, hipStream_t st);
 // one-token and prompt attention: paged_attn.hip.  decode_parts, prompt_parts: what `parts` is for this shape
 int decode_parts(const Args &a);
 int prompt_parts(const Args &a);
 bool launch_decode(const Args &a, hipStream_t st);
 bool launch_prompt(const Args &a, hipStream_t st);
+// attention of drafted trees: paged_attn.hip.  plan_tree sets `parts` and `units`; partial results then have that many rows
+void plan_tree(Args &a);
+size_t tree_part_rows(const Args &a);
+bool launch_tree(const Args &a, hipStream_t st);
+// accepted drafts, forked sequences, copied pages: paged_pages.hip
+struct Accept {
+  const int *keep;             // [S, width] ascending drafted tokens, up to the first entry that is none
+  int width;
+  int *new_len;                // [S] or nullptr
+};
+bool launch_accept(const Args &a, const Accept &x, hipStream_t st);
+struct Fork {
+  int N, grow;                 // new sequences; positions that each gets room for
+  const int *parent;           // [N]
+  const int *refs;             // [n_pages] who holds a page
+  int *table, *len, *new_refs; // [N, max_pages], [N], [n_pages]
+  int *copies, *missing;       // [N, 3] source, target, rows; [1]
+  int *fresh;                  // [N] pages that a sequence gets, in the workspace
+  int *eldest;                 // [S] the first sequence that goes on from this one (N: none), there too
+  int *held;                   // [n_pages] copies that read a page, there too
+};
+bool launch_fork(const Args &a, const Fork &x, hipStream_t st);
+bool launch_copy(const Args &a, const int *copies, int count, hipStream_t st);
 // prompt attention for bf16, d = 64 or 128: paged_prompt.hip
 constexpr int kPromptRows = 128;  // query rows of a workgroup, which has four wavefronts
 constexpr int kPromptWaves = 4;
@@ -235,6 +262,112 @@ struct RowTile {
       }
       nth -= many;
     }
+  }
+};
+
+// ---- drafted trees ----
+//
+// The n drafted tokens of a sequence take the slots past .. past + n - 1 after its history, token i slot past + i; bit k of its mask says
+// that it sees drafted token k (k < 64, k < n).  It stands `depth` positions behind the history, the number of other drafted tokens it sees.
+constexpr int kDrafts = 64;
+__device__ __forceinline__ unsigned long long below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; }
+__device__ __forceinline__ int depth_of(unsigned long long mask, int i, int n)
+{
+  mask &= below(n);
+  if (i < 64) mask &= ~(1ull << i);
+  return __builtin_popcountll(mask);
+}
+
+// What the tokens of one sequence's tree see.
+struct Tree {
+  int past;          // positions before the drafted tokens (below 0 if there are fewer positions than tokens: slots below 0 do not exist)
+  int shown;         // drafted tokens that can be seen
+  Range any, every;  // keys that any token can see; of the history those that all do
+  __device__ __forceinline__ Tree(const Args &a, int raw_len, int n)
+  {
+    past = max(raw_len, 0) - n;
+    shown = min(min(n, kDrafts), past > a.cap - kDrafts ? a.cap - past : kDrafts);
+    any = {first(a, 0), past + shown - 1};
+    every = {first(a, min(n, kDrafts) - 1), min(past, a.cap) - 1};
+  }
+  // the first key that a token sees at this depth
+  __device__ __forceinline__ int first(const Args &a, int depth) const { return max(max(past, 0) + depth - a.window + 1, 0); }
+  __device__ __forceinline__ int tiles() const { return any.hi >= any.lo ? any.hi / 32 - any.lo / 32 + 1 : 0; }
+};
+
+// One token's keys, 32 at a time.
+struct Seen {
+  int lo;                   // of the history
+  unsigned long long mask;  // of the drafted tokens
+  __device__ __forceinline__ Seen(const Args &a, const Tree &t, unsigned long long given, int i, int n)
+  {
+    lo = t.first(a, depth_of(given, i, n));
+    mask = given & below(t.shown);
+  }
+  template <typename F>
+  __device__ __forceinline__ unsigned bits(const Tree &t, int base, F &&row_bits) const
+  {
+    const int to = base - t.past;  // the drafted token at key `base`
+    const unsigned drafted = to >= 64 || to <= -32 ? 0u : to >= 0 ? (unsigned)(mask >> to) : (unsigned)(mask << -to);
+    return row_bits(lo - base, t.every.hi - base) | drafted;
+  }
+};
+
+// The rows and the part of their walk that one workgroup of a key/value head takes.  Whole walks: row tiles at floor(cu[s] R / rows) + s,
+// as for prompts.  Otherwise a sequence's walk of t tiles of 32 keys is cut into ceil(t / chunk) parts, for each of its row tiles: with
+// chunk = ceil(sum of row tiles times tiles / a.parts) there are fewer than a.parts units beyond one a row tile, whatever the lengths are.
+struct TreeUnit {
+  int s = -1, tok0 = 0, count = 0, row0 = 0, part = 0, parts = 1, first = 0;  // (s < 0: none; first: the sequence's first unit)
+  __device__ __forceinline__ TreeUnit(const Args &a, int lane, int unit, int rows, int least)
+  {
+    if (a.parts == 0) {
+      const Sequence seq(a, lane, [&](int i, int cu) { return (int)((unsigned)(cu * a.R) / rows) + i <= unit; });
+      const int at = (unit - (int)((unsigned)(seq.first * a.R) / rows) - seq.s) * rows;
+      if (at < 0 || at >= seq.count * a.R) return;
+      s = seq.s; tok0 = seq.first; count = seq.count; row0 = at;
+      return;
+    }
+    struct One { int cu, n, tiles, row_tiles; };
+    auto look = [&](int i) {
+      One x{token_at(a, min(i, a.S)), 0, 0, 0};
+      if (i >= a.S) return x;
+      x.n = max(token_at(a, i + 1) - x.cu, 0);
+      if (x.n == 0) return x;
+      x.tiles = max(Tree(a, a.kv_len[i], x.n).tiles(), 1);
+      x.row_tiles = (unsigned)(x.n * a.R + rows - 1) / rows;
+      return x;
+    };
+    const One mine0 = look(lane);
+    int total = 0;
+    for (int s0 = 0; s0 < a.S; s0 += 64) {
+      const One x = s0 == 0 ? mine0 : look(s0 + lane);
+      total += wave_sum(x.tiles * x.row_tiles);
+    }
+    const unsigned chunk = max((unsigned)(total + a.parts - 1) / a.parts, (unsigned)least);
+    int done = 0;
+    for (int s0 = 0; s0 < a.S; s0 += 64) {
+      const One x = s0 == 0 ? mine0 : look(s0 + lane);
+      const int cut = (x.tiles + chunk - 1) / chunk, mine = cut * x.row_tiles, upto = done + wave_scan(mine);
+      const int k = __builtin_popcountll(__ballot(upto <= unit));
+      if (k < 64) {
+        s = s0 + k;
+        parts = __builtin_amdgcn_readlane(cut, k);
+        first = __builtin_amdgcn_readlane(upto, k) - __builtin_amdgcn_readlane(mine, k);
+        tok0 = __builtin_amdgcn_readlane(x.cu, k);
+        count = __builtin_amdgcn_readlane(x.n, k);
+        const int tile = (unsigned)(unit - first) / (unsigned)parts;
+        part = unit - first - tile * parts;
+        row0 = tile * rows;
+        return;
+      }
+      done = __builtin_amdgcn_readlane(upto, 63);
+    }
+  }
+  // for the join: by the first workgroup of a sequence
+  __device__ __forceinline__ void tell(const Args &a, int g, int tid, int threads) const
+  {
+    if (a.parts == 0 || part != 0 || row0 != 0 || g != 0) return;
+    for (int i = tid; i < count; i += threads) a.part_at[tok0 + i] = make_int4(first, parts, tok0, 0);
   }
 };
 

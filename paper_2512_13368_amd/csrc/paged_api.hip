@@ -57,6 +57,13 @@ size_t attn_ws_bytes(Args &a, bool prompt)
   return part_rows(a, prompt) * (a.d + 2) * sizeof(float) + (prompt ? 0 : (size_t)a.S * sizeof(int2));
 }
 
+// trees: partial results, then where each token's are
+size_t tree_ws_bytes(const Args &a)
+{
+  const size_t rows = tree_part_rows(a);
+  return rows ? rows * (a.d + 2) * sizeof(float) + (size_t)a.T * sizeof(int4) : 0;
+}
+
 int launch_status() { return hipGetLastError() == hipSuccess ? BLOSSOM_OK : BLOSSOM_ERR_LAUNCH; }
 
 int attn(const blossom_paged_params *p, bool prompt, const void *Q, int64_t q_stride, const void *K_cache, const void *V_cache,
@@ -88,21 +95,9 @@ int attn(const blossom_paged_params *p, bool prompt, const void *Q, int64_t q_st
   return launch_status();
 }
 
-}  // namespace
-
-extern "C" {
-
-size_t blossom_paged_workspace_bytes(const blossom_paged_params *p, int which)
-{
-  Args a;
-  if (check_params(p, &a) != BLOSSOM_OK || (which != BLOSSOM_WS_DECODE && which != BLOSSOM_WS_PROMPT)) return 0;
-  return attn_ws_bytes(a, which == BLOSSOM_WS_PROMPT);
-}
-
-int blossom_kv_append(const blossom_paged_params *p, const void *Q, int64_t q_stride, const void *K, int64_t k_stride,
-                      const void *V, int64_t v_stride, const float *rope_cos, const float *rope_sin,
-                      const int32_t *page_table, const int32_t *cu_seqlens, const int32_t *kv_len, void *K_cache,
-                      void *V_cache, void *Q_rot, void *hip_stream)
+int append(const blossom_paged_params *p, const void *Q, int64_t q_stride, const void *K, int64_t k_stride, const void *V, int64_t v_stride,
+           const float *rope_cos, const float *rope_sin, const int32_t *page_table, const int32_t *cu_seqlens, const int32_t *kv_len,
+           const int64_t *tree_mask, void *K_cache, void *V_cache, void *Q_rot, void *hip_stream)
 {
   Args a;
   int rc = check_params(p, &a);
@@ -118,11 +113,51 @@ int blossom_kv_append(const blossom_paged_params *p, const void *Q, int64_t q_st
   if (!rc) rc = check_stride(a, v_stride, a.G, &a.v_stride);
   if (rc) return rc;
   a.Q = Q; a.K = K; a.V = V; a.rope_cos = rope_cos; a.rope_sin = rope_sin;
-  a.page_table = page_table; a.cu = cu_seqlens; a.kv_len = kv_len;
+  a.page_table = page_table; a.cu = cu_seqlens; a.kv_len = kv_len; a.tree = tree_mask;
   a.K_cache = K_cache; a.V_cache = V_cache; a.Q_rot = Q_rot;
   (void)hipGetLastError();
   if (!launch_append(a, (hipStream_t)hip_stream)) return BLOSSOM_ERR_SHAPE;
   return launch_status();
+}
+
+// the fork's workspace: pages asked for, eldest heirs, reading copies
+size_t fork_ws_bytes(const Args &a, int n_new) { return ((size_t)n_new + a.S + a.n_pages) * sizeof(int); }
+
+bool aligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+}  // namespace
+
+extern "C" {
+
+size_t blossom_paged_workspace_bytes(const blossom_paged_params *p, int which)
+{
+  Args a;
+  if (check_params(p, &a) != BLOSSOM_OK || (which != BLOSSOM_WS_DECODE && which != BLOSSOM_WS_PROMPT && which != BLOSSOM_WS_TREE)) return 0;
+  if (which == BLOSSOM_WS_TREE) {
+    plan_tree(a);
+    return tree_ws_bytes(a);
+  }
+  return attn_ws_bytes(a, which == BLOSSOM_WS_PROMPT);
+}
+
+int blossom_kv_append(const blossom_paged_params *p, const void *Q, int64_t q_stride, const void *K, int64_t k_stride,
+                      const void *V, int64_t v_stride, const float *rope_cos, const float *rope_sin,
+                      const int32_t *page_table, const int32_t *cu_seqlens, const int32_t *kv_len, void *K_cache,
+                      void *V_cache, void *Q_rot, void *hip_stream)
+{
+  return append(p, Q, q_stride, K, k_stride, V, v_stride, rope_cos, rope_sin, page_table, cu_seqlens, kv_len, nullptr, K_cache, V_cache,
+                Q_rot, hip_stream);
+}
+
+int blossom_kv_append_tree(const blossom_paged_params *p, const void *Q, int64_t q_stride, const void *K, int64_t k_stride,
+                           const void *V, int64_t v_stride, const float *rope_cos, const float *rope_sin,
+                           const int32_t *page_table, const int32_t *cu_seqlens, const int32_t *kv_len,
+                           const int64_t *tree_mask, void *K_cache, void *V_cache, void *Q_rot, void *hip_stream)
+{
+  if (!tree_mask) return BLOSSOM_ERR_NULL;
+  if (!aligned(tree_mask, 8)) return BLOSSOM_ERR_ALIGN;
+  return append(p, Q, q_stride, K, k_stride, V, v_stride, rope_cos, rope_sin, page_table, cu_seqlens, kv_len, tree_mask, K_cache, V_cache,
+                Q_rot, hip_stream);
 }
 
 int blossom_attn_decode(const blossom_paged_params *p, const void *Q, int64_t q_stride, const void *K_cache,
@@ -137,6 +172,101 @@ int blossom_attn_prompt(const blossom_paged_params *p, const void *Q, int64_t q_
                         void *O, float *lse, void *ws, size_t ws_bytes, void *hip_stream)
 {
   return attn(p, true, Q, q_stride, K_cache, V_cache, page_table, cu_seqlens, kv_len, O, lse, ws, ws_bytes, hip_stream);
+}
+
+int blossom_attn_tree(const blossom_paged_params *p, const void *Q, int64_t q_stride, const void *K_cache, const void *V_cache,
+                      const int32_t *page_table, const int32_t *cu_seqlens, const int32_t *kv_len, const int64_t *tree_mask,
+                      void *O, float *lse, void *ws, size_t ws_bytes, void *hip_stream)
+{
+  Args a;
+  int rc = check_params(p, &a);
+  if (rc) return rc;
+  if (p->table_per_head) return BLOSSOM_ERR_UNSUPPORTED;
+  if (!Q || !K_cache || !V_cache || !page_table || !cu_seqlens || !kv_len || !tree_mask || !O) return BLOSSOM_ERR_NULL;
+  if (!aligned16(Q) || !aligned16(K_cache) || !aligned16(V_cache) || !aligned16(O) || !aligned(tree_mask, 8)) return BLOSSOM_ERR_ALIGN;
+  rc = check_stride(a, q_stride, a.H, &a.q_stride);
+  if (rc) return rc;
+  plan_tree(a);
+  const size_t need = tree_ws_bytes(a);
+  if (need) {
+    if (!ws || ws_bytes < need) return BLOSSOM_ERR_WORKSPACE;
+    if (!aligned16(ws)) return BLOSSOM_ERR_ALIGN;
+    a.part_at = static_cast<int4 *>(ws);
+    a.part_o = reinterpret_cast<float *>(a.part_at + a.T);
+    a.part_ml = a.part_o + tree_part_rows(a) * a.d;
+  }
+  a.Q = Q; a.K_cache = const_cast<void *>(K_cache); a.V_cache = const_cast<void *>(V_cache);
+  a.page_table = page_table; a.cu = cu_seqlens; a.kv_len = kv_len; a.tree = tree_mask;
+  a.O = O; a.lse = lse;
+  (void)hipGetLastError();
+  if (!launch_tree(a, (hipStream_t)hip_stream)) return BLOSSOM_ERR_SHAPE;
+  return launch_status();
+}
+
+int blossom_kv_accept(const blossom_paged_params *p, int32_t keep_width, const int32_t *keep, const int32_t *page_table,
+                      const int32_t *cu_seqlens, const int32_t *kv_len, void *K_cache, void *V_cache, int32_t *new_len,
+                      void *hip_stream)
+{
+  Args a;
+  const int rc = check_params(p, &a);
+  if (rc) return rc;
+  if (p->table_per_head) return BLOSSOM_ERR_UNSUPPORTED;
+  if (keep_width < 1) return BLOSSOM_ERR_SHAPE;
+  if (!keep || !page_table || !cu_seqlens || !kv_len || !K_cache || !V_cache) return BLOSSOM_ERR_NULL;
+  if (new_len == kv_len) return BLOSSOM_ERR_PARAM;
+  if (!aligned16(K_cache) || !aligned16(V_cache)) return BLOSSOM_ERR_ALIGN;
+  a.page_table = page_table; a.cu = cu_seqlens; a.kv_len = kv_len;
+  a.K_cache = K_cache; a.V_cache = V_cache;
+  (void)hipGetLastError();
+  if (!launch_accept(a, Accept{keep, keep_width, new_len}, (hipStream_t)hip_stream)) return BLOSSOM_ERR_SHAPE;
+  return launch_status();
+}
+
+size_t blossom_fork_workspace_bytes(const blossom_paged_params *p, int32_t n_new)
+{
+  Args a;
+  return check_params(p, &a) == BLOSSOM_OK && n_new >= 1 ? fork_ws_bytes(a, n_new) : 0;
+}
+
+int blossom_kv_fork(const blossom_paged_params *p, int32_t n_new, int32_t grow, const int32_t *parent, const int32_t *page_table,
+                    const int32_t *kv_len, const int32_t *refs, int32_t *new_table, int32_t *new_len, int32_t *new_refs,
+                    int32_t *copies, int32_t *missing, void *ws, size_t ws_bytes, void *hip_stream)
+{
+  Args a;
+  const int rc = check_params(p, &a);
+  if (rc) return rc;
+  if (p->table_per_head) return BLOSSOM_ERR_UNSUPPORTED;
+  if (n_new < 1 || (int64_t)n_new * a.max_pages > 0x7FFFFFFFll || (int64_t)a.S * a.max_pages > 0x7FFFFFFFll) return BLOSSOM_ERR_SHAPE;
+  if (grow < 0) return BLOSSOM_ERR_PARAM;
+  if (!parent || !page_table || !kv_len || !refs || !new_table || !new_len || !new_refs || !copies || !missing) return BLOSSOM_ERR_NULL;
+  if (new_table == page_table || new_len == kv_len || new_refs == refs) return BLOSSOM_ERR_PARAM;
+  if (!ws || ws_bytes < fork_ws_bytes(a, n_new)) return BLOSSOM_ERR_WORKSPACE;
+  if (!aligned16(ws)) return BLOSSOM_ERR_ALIGN;
+  a.page_table = page_table; a.kv_len = kv_len;
+  Fork x{};
+  x.N = n_new; x.grow = grow; x.parent = parent; x.refs = refs;
+  x.table = new_table; x.len = new_len; x.new_refs = new_refs; x.copies = copies; x.missing = missing;
+  x.fresh = static_cast<int *>(ws);
+  x.eldest = x.fresh + n_new;
+  x.held = x.eldest + a.S;
+  (void)hipGetLastError();
+  if (!launch_fork(a, x, (hipStream_t)hip_stream)) return BLOSSOM_ERR_SHAPE;
+  return launch_status();
+}
+
+int blossom_kv_copy_pages(const blossom_paged_params *p, int32_t n_copies, const int32_t *copies, void *K_cache, void *V_cache,
+                          void *hip_stream)
+{
+  Args a;
+  const int rc = check_params(p, &a);
+  if (rc) return rc;
+  if (n_copies < 1) return BLOSSOM_ERR_SHAPE;
+  if (!copies || !K_cache || !V_cache) return BLOSSOM_ERR_NULL;
+  if (!aligned16(K_cache) || !aligned16(V_cache)) return BLOSSOM_ERR_ALIGN;
+  a.K_cache = K_cache; a.V_cache = V_cache;
+  (void)hipGetLastError();
+  if (!launch_copy(a, copies, n_copies, (hipStream_t)hip_stream)) return BLOSSOM_ERR_SHAPE;
+  return launch_status();
 }
 
 }  // extern "C"

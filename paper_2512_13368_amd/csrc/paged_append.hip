@@ -76,8 +76,8 @@ struct Chunk<bf16_t> {
 
 }  // namespace
 
-// `share`: wavefronts that divide a token's rows (a power of two)
-template <typename T, bool ONCE>
+// `share`: wavefronts that divide a token's rows (a power of two).  TREE: drafted tokens, which are turned by their places in their trees.
+template <typename T, bool ONCE, bool TREE>
 __global__ __launch_bounds__(kThreads) void append_kernel(Args a, int share)
 {
   constexpr int E = Chunk<T>::E;
@@ -90,7 +90,9 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Args a, int share)
   if (t < lo || t >= hi) return;  // a row that no sequence owns
   const int n = a.kv_len[s];
   const long pos = (long)n - (hi - lo) + (t - lo);
-  const bool placed = pos >= 0 && pos < a.cap;
+  long angle = pos;
+  if constexpr (TREE) angle = (long)n - (hi - lo) + depth_of(a.tree[t], t - lo, hi - lo);
+  const bool placed = pos >= 0 && pos < a.cap && (!TREE || (angle >= 0 && angle < a.cap));
   int id = -1;
   if (placed) id = a.page_table[s * a.table_seq + (pos >> a.page_shift)];
   const bool stored = id >= 0 && id < a.n_pages;
@@ -102,7 +104,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Args a, int share)
 #pragma unroll
   for (int i = 0; i < E / 2; ++i) { c[i] = 1.0f; sn[i] = 0.0f; }
   if (a.rope_cos && placed) {
-    const float *pc = a.rope_cos + pos * (a.d / 2) + at / 2, *ps = a.rope_sin + pos * (a.d / 2) + at / 2;
+    const float *pc = a.rope_cos + angle * (a.d / 2) + at / 2, *ps = a.rope_sin + angle * (a.d / 2) + at / 2;
 #pragma unroll
     for (int i = 0; i < E / 2; i += 2) {
       const float2 x = *reinterpret_cast<const float2 *>(pc + i), y = *reinterpret_cast<const float2 *>(ps + i);
@@ -169,10 +171,15 @@ bool launch_append(const Args &a, hipStream_t st)
   // 82 kept.  What is less stays for the attention that follows.
   const bool once = (double)a.T * rows * a.d * (a.dtype == 0 ? 4 : 2) > 128e6;
   auto go = [&](auto kernel) { BLOSSOM_LAUNCH(kernel, dim3((unsigned)blocks), dim3(kThreads), 0, st, a, share); };
-  if (a.dtype == 0 && once) go(append_kernel<float, true>);
-  else if (a.dtype == 0) go(append_kernel<float, false>);
-  else if (once) go(append_kernel<bf16_t, true>);
-  else go(append_kernel<bf16_t, false>);
+  auto pick = [&](auto tree) {
+    constexpr bool TREE = decltype(tree)::value;
+    if (a.dtype == 0 && once) go(append_kernel<float, true, TREE>);
+    else if (a.dtype == 0) go(append_kernel<float, false, TREE>);
+    else if (once) go(append_kernel<bf16_t, true, TREE>);
+    else go(append_kernel<bf16_t, false, TREE>);
+  };
+  if (a.tree) pick(std::true_type{});
+  else pick(std::false_type{});
   return true;
 }
 

@@ -105,9 +105,9 @@ struct Part {
   }
 };
 
-// One new token a sequence, or few (PROMPT): W wavefronts take a run of key tiles each for up to 16 rows that share keys.  SPLIT: of a
-// part of them.
-template <typename T, int D, int W, bool ONCE, bool SPLIT, bool PROMPT>
+// One new token a sequence, or few (PROMPT; TREE: drafted ones): W wavefronts take a run of key tiles each for up to 16 rows that share
+// keys.  SPLIT: of a part of them.
+template <typename T, int D, int W, bool ONCE, bool SPLIT, bool PROMPT, bool TREE = false>
 __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
 {
   typedef Tile<T, D> TL;
@@ -121,7 +121,18 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
 
   const int rest = a.by_G.of(blockIdx.x), g = blockIdx.x - rest * a.G;
   int s, row0, rows, tok0, new_tokens = 1, part = 0, n_parts = 1, b = 0;
-  if constexpr (PROMPT) {
+  if constexpr (TREE) {
+    const TreeUnit unit(a, lane, rest, kRows, W);
+    if (unit.s < 0) return;
+    unit.tell(a, g, threadIdx.x, 64 * W);
+    s = unit.s;
+    tok0 = unit.tok0;
+    new_tokens = unit.count;
+    row0 = unit.row0;
+    part = unit.part;
+    n_parts = unit.parts;
+    rows = min(new_tokens * a.R - row0, kRows);
+  } else if constexpr (PROMPT) {
     const int tile = a.by_parts.of(rest);
     part = rest - tile * a.parts;
     n_parts = a.parts;
@@ -160,12 +171,16 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
   int list0 = 0, ids = entries(0);  // pages list0 .. list0 + 63, one a lane
   typename TL::Query q;
   TL::load_query(q, static_cast<const T *>(a.Q) + (tok0 + tok) * a.q_stride + (size_t)head * D, c);
+  unsigned long long mask = 0ull;
+  if constexpr (TREE) mask = a.tree[tok0 + tok];
 
   const int len = max(__builtin_amdgcn_readfirstlane(raw_len), 0);
   const int first_pos = len - new_tokens;
+  const Tree tree(a, len, new_tokens);
+  const Seen sees(a, tree, mask, tok, new_tokens);
   // keys that any row sees, that this lane's row does, that all do
-  Range any = seen_by(a, first_pos + (PROMPT ? a.by_R.of(row0) : 0), len), my = any, every = any;
-  if constexpr (PROMPT) {
+  Range any = TREE ? tree.any : seen_by(a, first_pos + (PROMPT ? a.by_R.of(row0) : 0), len), my = any, every = TREE ? tree.every : any;
+  if constexpr (PROMPT && !TREE) {
     const Range last = seen_by(a, first_pos + a.by_R.of(row0 + rows - 1), len);
     every.lo = last.lo;
     any.hi = last.hi;
@@ -221,7 +236,8 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
       const char *ks = mine + k * (2 * TL::BYTES);
       const int base = t * kTile;
       const bool all = seen[k] == 0xFFFFFFFFu && (!PROMPT || (base >= every.lo && base + kTile - 1 <= every.hi));
-      r.template attend<true>(ks, ks + TL::BYTES, q, a.scale2, PROMPT ? seen[k] & mfma::row_bits(my.lo - base, my.hi - base) : seen[k], all, true, lane);
+      const unsigned row = TREE ? sees.bits(tree, base, mfma::row_bits) : PROMPT ? mfma::row_bits(my.lo - base, my.hi - base) : 0xFFFFFFFFu;
+      r.template attend<true>(ks, ks + TL::BYTES, q, a.scale2, seen[k] & row, all, true, lane);
       ++t;
     }
   }
@@ -258,12 +274,12 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
     }
     const int tk = PROMPT ? a.by_R.of(row0 + row) : 0;
     const size_t out = (size_t)(tok0 + tk) * a.H + g * a.R + row0 + row - tk * a.R;
-    if (!SPLIT || (!PROMPT && n_parts == 1)) {
+    if (!SPLIT || ((!PROMPT || TREE) && n_parts == 1)) {
       const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
       store_four(static_cast<T *>(a.O) + out * D + ch, o, inv);
       if (ch == 0 && a.lse) a.lse[out] = ll == 0.0f ? kNegInf : (mm + __log2f(ll)) * kLn2;
-    } else {  // decode: [heads of the token][parts of all sequences]; prompt: [rows][parts of each]
-      const size_t at = PROMPT ? out * a.parts + part : (size_t)(g * a.R + row0 + row) * a.parts + b;
+    } else {  // decode: [heads of the token][parts of all sequences]; prompt: [rows][parts of each]; trees: [units][heads][rows of a tile]
+      const size_t at = TREE ? ((size_t)rest * a.G + g) * kRows + row : PROMPT ? out * a.parts + part : (size_t)(g * a.R + row0 + row) * a.parts + b;
       *reinterpret_cast<float4 *>(a.part_o + at * D + ch) = o;
       if (ch == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(mm, ll);
     }
@@ -359,6 +375,50 @@ __global__ __launch_bounds__(256) void join_rows_kernel(Args a)
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
       const float w = i + k < a.parts ? __builtin_amdgcn_exp2f(x[k].x - ref) : 0.0f;
+      l = fmaf(x[k].y, w, l);
+      o.x = fmaf(v[k].x, w, o.x); o.y = fmaf(v[k].y, w, o.y); o.z = fmaf(v[k].z, w, o.z); o.w = fmaf(v[k].w, w, o.w);
+    }
+  }
+  store_four(static_cast<T *>(a.O) + row * D + 4 * at, o, l == 0.0f ? 0.0f : 1.0f / l);
+  if (at == 0 && a.lse) a.lse[row] = l == 0.0f ? kNegInf : (m + __log2f(l)) * kLn2;
+}
+
+// Joins the parts of drafted tokens' rows, where a walk has more than one: D / 4 threads a row, 4 channels each, as above.  `rows`: of a
+// workgroup of the walk.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void join_tree_kernel(Args a, int rows)
+{
+  constexpr int LANES = D / 4, ROWS = 256 / LANES, AHEAD = 8;
+  const int at = threadIdx.x % LANES;
+  const size_t row = (size_t)blockIdx.x * ROWS + threadIdx.x / LANES;
+  if (row >= (size_t)token_at(a, a.S) * a.H) return;  // (a row that no sequence owns stays as it is)
+  const int t = a.by_H.of((int)row), h = (int)row - t * a.H;
+  const int4 of = a.part_at[t];
+  const int parts = of.y;
+  if (parts <= 1) return;  // (the walk's workgroup wrote the row)
+  const int g = a.by_R.of(h), r = (t - of.z) * a.R + h - g * a.R, tile = (unsigned)r / (unsigned)rows;
+  const long first = of.x + (long)tile * parts;
+  if (r < 0 || first < 0 || first + parts > a.units) return;  // (cu_seqlens does not ascend: whatever the workspace held)
+  const size_t step = (size_t)a.G * rows, at0 = (first * a.G + g) * rows + (r - tile * rows);
+  const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + at0;
+  const float4 *po = reinterpret_cast<const float4 *>(a.part_o) + at0 * LANES + at;
+  float m = kNegInf;
+  for (int i = 0; i < parts; ++i) m = fmaxf(m, ml[i * step].x);
+  const float ref = m == kNegInf ? 0.0f : m;
+  float l = 0.0f;
+  float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int i = 0; i < parts; i += AHEAD) {
+    float4 v[AHEAD];
+    float2 x[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const size_t j = min(i + k, parts - 1) * step;
+      v[k] = po[j * LANES];
+      x[k] = ml[j];
+    }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const float w = i + k < parts ? __builtin_amdgcn_exp2f(x[k].x - ref) : 0.0f;
       l = fmaf(x[k].y, w, l);
       o.x = fmaf(v[k].x, w, o.x); o.y = fmaf(v[k].y, w, o.y); o.z = fmaf(v[k].z, w, o.z); o.w = fmaf(v[k].w, w, o.w);
     }
@@ -512,6 +572,38 @@ bool launch_prompt(const Args &call, hipStream_t st)
     }
     if (a.parts > 1 && !launch_failed())
       BLOSSOM_LAUNCH((join_rows_kernel<T, D>), dim3((unsigned)((size_t)a.T * a.H * (D / 4) / 256 + 1)), dim3(256), 0, st, a);
+  });
+  return true;
+}
+
+// Drafted trees: 16 rows a workgroup, whose wavefronts take runs of keys as in decode.  Walks are split until the chip is full.
+void plan_tree(Args &a)
+{
+  const int w = few_waves(row_bytes_of(a));
+  const long base = (long)a.T * a.R / kRows + a.S;
+  const long tiles = ((long)(a.window < a.cap ? a.window + kDrafts + kTile - 1 : a.cap) + kTile - 1) / kTile;
+  long extra = fill_waves(row_bytes_of(a)) / w / a.G - base / 2;
+  if (tiles < 2 * w || base * tiles > 1 << 30 || extra < 1) extra = 0;
+  a.parts = (int)extra;
+  a.units = (int)(base + extra);
+}
+
+size_t tree_part_rows(const Args &a) { return a.parts ? (size_t)a.units * a.G * kRows : 0; }
+
+bool launch_tree(const Args &a, hipStream_t st)
+{
+  const dim3 grid((unsigned)((long)a.units * a.G));
+  if (!countable((long)a.units * a.G, 64 * few_waves(row_bytes_of(a)))) return false;
+  with_type(a, [&](auto type, auto dim) {
+    typedef decltype(type) T;
+    constexpr int D = decltype(dim)::value, W = few_waves(D * sizeof(T));
+    if (!a.parts) {
+      BLOSSOM_LAUNCH((decode_kernel<T, D, W, false, false, true, true>), grid, dim3(64 * W), 0, st, a);
+      return;
+    }
+    BLOSSOM_LAUNCH((decode_kernel<T, D, W, false, true, true, true>), grid, dim3(64 * W), 0, st, a);
+    if (launch_failed()) return;
+    BLOSSOM_LAUNCH((join_tree_kernel<T, D>), dim3((unsigned)((size_t)a.T * a.H * (D / 4) / 256 + 1)), dim3(256), 0, st, a, kRows);
   });
   return true;
 }
