@@ -8,6 +8,8 @@
 //   merge_kernel  a workgroup a history: sums joined, then the K best of the runs' lists
 #include "beam.h"
 
+#include <type_traits>
+
 #include "common.h"
 #include "launch.h"
 
@@ -16,9 +18,9 @@ namespace beam {
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kGroups = 64;   // groups of 4 lanes, whose largest logits give a bound that K logits reach
-constexpr int kList = 1024;   // logits beyond the bound that are kept at a time
+constexpr int kThreads = 256;  // of the merge
+constexpr int kWaves = 8;      // of a run
+constexpr int kGroups = 64;   // groups of 4 lanes, whose best give a bound that K reach
 typedef unsigned long long u64;
 
 // logits and items as one number: the larger logit first, then the lower item.  0: none.
@@ -37,178 +39,469 @@ __device__ __forceinline__ u64 ordered(double x)
 }
 __device__ __forceinline__ double score_of(u64 o) { return __longlong_as_double((long long)(o >> 63 ? o ^ 1ull << 63 : ~o)); }
 
-__device__ __forceinline__ float as_float(float x) { return x; }
-__device__ __forceinline__ float as_float(bf16_t x) { return __uint_as_float((unsigned)x.bits << 16); }
-
 // is (p, w, k) before (q, v, l): score, beam, logit and item?
-__device__ __forceinline__ bool before(u64 p, int w, u64 k, u64 q, int v, u64 l) { return p != q ? p > q : w != v ? w < v : k > l; }
+__device__ __forceinline__ bool before(u64 p, int w, u64 k, u64 q, int v, u64 l) 
+{
+  return (p > q) | ((p == q) & ((w < v) | ((w == v) & (k > l))));  // (without branches)
+}
 
 }  // namespace
 
-// Block `lists` of a row: a run of `subs` pieces of kThreads * LD * 16 bytes.
-template <typename T, int LD>
-__global__ __launch_bounds__(kThreads) void rows_kernel(Args a, int subs)
+// The sum of 2^t[i] in 64 bits for |t| <= 1000: the whole part goes to the exponent, the rest f in [-1/2, 1/2] through the polynomial of
+// degree 8 that meets 2^f at Chebyshev's nine points (relative error 1.1e-12 at most; half a unit of an fp32 score is 6e-8 of it).  N at
+// a time, for one alone is a chain of 14 instructions that wait for each other.
+template <int N>
+__device__ __forceinline__ double exp2_sum(const double (&t)[N])
 {
-  constexpr int VEC = 16 / (int)sizeof(T), EL = LD * VEC, SUB = kThreads * EL;
-  struct __attribute__((packed, aligned(sizeof(T)))) Piece { T x[VEC]; };  // (rows begin at any element)
-  __shared__ u64 list[kList + kMost], best[kMost];
-  __shared__ float group_s[kGroups], wave_s[4];
-  __shared__ double sum_s[4];
-  __shared__ u64 top_s[4];
-  __shared__ int count_s;
+  typedef unsigned pair __attribute__((ext_vector_type(2)));
+  constexpr double kShift = 6755399441055744.0;  // 1.5 * 2^52: a sum with it has the whole part in its low bits
+  constexpr double c[9] = {1.0, 0.69314718054593349, 0.24022650695812989, 0.055504109412059341, 0.0096181291594026191, 0.0013333450567999659,
+                           0.00015403455852411408, 1.5310079402479794e-05, 1.3255224887698904e-06};
+  double at[N], f[N], p[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) at[i] = t[i] + kShift;
+#pragma unroll
+  for (int i = 0; i < N; ++i) f[i] = at[i] - kShift;
+#pragma unroll
+  for (int i = 0; i < N; ++i) f[i] = t[i] - f[i];
+#pragma unroll
+  for (int i = 0; i < N; ++i) p[i] = fma(c[8], f[i], c[7]);
+#pragma unroll
+  for (int k = 6; k >= 0; --k) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) p[i] = fma(p[i], f[i], c[k]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    pair w = __builtin_bit_cast(pair, p[i]);
+    w.y += __builtin_bit_cast(pair, at[i]).x << 20;
+    p[i] = __builtin_bit_cast(double, w);
+  }
+#pragma unroll
+  for (int k = N / 2; k >= 1; k /= 2)
+#pragma unroll
+    for (int i = 0; i < k; ++i) p[i] += p[i + k];
+  return p[0];
+}
+
+constexpr double kLog2e = 1.4426950408889634;
+// e^(x - m) for x <= m, neither infinite (beyond e^-690: that)
+__device__ __forceinline__ double exp_from(double x, double m)
+{
+  const double t[1] = {fmax(x - m, -690.0) * kLog2e};
+  return exp2_sum(t);
+}
+
+__device__ __forceinline__ float element(const float *p) { return *p; }
+__device__ __forceinline__ float element(const bf16_t *p) { return __uint_as_float((unsigned)p->bits << 16); }
+
+// 16 bytes of a row, as its elements
+template <typename T>
+struct Piece;
+template <>
+struct Piece<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ float get(const uint4 &v, int e) { return __uint_as_float(e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w); }
+};
+template <>
+struct Piece<bf16_t> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ float get(const uint4 &v, int e)
+  {
+    const unsigned w = e < 2 ? v.x : e < 4 ? v.y : e < 6 ? v.z : v.w;
+    return __uint_as_float(e & 1 ? w & 0xFFFF0000u : w << 16);
+  }
+};
+
+// e^x of bf16 logits from a table in LDS: all 2560 with 2^-14 <= |x| < 64 of either sign, at 1 + (code - that of 2^-14); at 0 what is nearer
+// to 0 (1, to which x + x^2/2 is added: e^x to 2^-42/6), at the end what is larger (nothing: the sum of a piece whose largest logit
+// lies between -20 and 64 does not miss e^-64).  Of two logits in a register the places take nine instructions, where the
+// polynomial takes 36: 512 rows of 152063 logits 82 us by the polynomial, 40 so (other things changed with it).
+constexpr int kLeast = (127 - 14) << 7;
+struct Table {
+  static constexpr int kEnd = ((127 + 6) << 7) - kLeast + 1;  // the place of what is larger
+  static constexpr int kSign = 4096, kSize = kSign + kEnd + 1;  // places of the negative ones begin at kSign
+  static_assert(kEnd < kSign, "");
+  static __device__ __forceinline__ void fill(double *to, int tid, int threads)
+  {
+    for (int i = tid; i < 2 * (kEnd + 1); i += threads) {
+      const bool minus = i > kEnd;
+      const int at = minus ? i - (kEnd + 1) : i;
+      const float x = __uint_as_float((unsigned)(at - 1 + kLeast) << 16 | (minus ? 0x80000000u : 0u));
+      const double t[1] = {(double)(at == 0 || at >= kEnd ? 0.0f : x) * kLog2e};
+      to[minus ? kSign + at : at] = at >= kEnd ? 0.0 : exp2_sum(t);
+    }
+  }
+  // the sum over 16 bytes of logits
+  static __device__ __forceinline__ double sum(const double *table, const uint4 &v)
+  {
+    typedef unsigned short two __attribute__((ext_vector_type(2)));
+    const unsigned w[4] = {v.x, v.y, v.z, v.w};
+    const two below = {kLeast - 1, kLeast - 1}, end = {kEnd, kEnd};
+    two least = end;
+    double e[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const two at = __builtin_elementwise_min(__builtin_elementwise_sub_sat(__builtin_bit_cast(two, w[i] & 0x7FFF7FFFu), below), end);
+      least = __builtin_elementwise_min(least, at);
+      const unsigned place = __builtin_bit_cast(unsigned, at) | (w[i] >> 3 & 0x10001000u);
+      e[2 * i] = table[place & 0xFFFFu];
+      e[2 * i + 1] = table[place >> 16];
+    }
+#pragma unroll
+    for (int k = 4; k >= 1; k /= 2)
+#pragma unroll
+      for (int i = 0; i < k; ++i) e[i] += e[i + k];
+    if (__any(least.x == 0 || least.y == 0)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = Piece<bf16_t>::get(v, i);
+        const double y = fabsf(x) < 0x1p-14f ? (double)x : 0.0;
+        e[0] = fma(y, fma(y, 0.5, 1.0), e[0]);
+      }
+    }
+    return e[0];
+  }
+};
+
+// A wavefront's best logits are held as keys in LDS, in no order until they are more than fit: then, and after every piece, the K best
+// are kept.
+constexpr int kHold = 2 * kMost;
+
+// Leaves the K best of n keys, in order, and returns how many there are.  (One wavefront's LDS: no other touches it.)
+__device__ __forceinline__ int keep_best(u64 *keys, int n, int K, int lane)
+{
+  u64 mine[kHold / 64];
+  int rank[kHold / 64];
+  auto some = [&](auto rounds) __attribute__((always_inline)) {
+    constexpr int R = decltype(rounds)::value;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      mine[r] = 64 * r + lane < n ? keys[64 * r + lane] : 0;
+      rank[r] = 0;
+    }
+    for (int j = 0; j < n; ++j) {
+      const u64 o = keys[j];
+#pragma unroll
+      for (int r = 0; r < R; ++r) rank[r] += o > mine[r];
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (64 * r + lane < n && rank[r] < K) keys[rank[r]] = mine[r];
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  };
+  if (n <= 64) some(std::integral_constant<int, 1>{});
+  else some(std::integral_constant<int, kHold / 64>{});
+  return min(n, K);
+}
+
+__device__ __forceinline__ float wave_max(float x)
+{
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
+  return x;
+}
+
+// Workgroup (row, run) takes `subs` pieces of the row, its wavefronts one after another: of 64 * LD * 16 bytes each, the next on its way
+// while one is worked on.  A lane keeps the sum and the largest of its logits.  When the run is done, the K-th largest of 64 groups' largest
+// bounds what may be among the K best: the few lanes that reach it have their loads looked at again.
+template <typename T, int LD>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(4))) void rows_kernel(Args a)
+{
+  typedef Piece<T> P;
+  constexpr int VEC = P::N, SUB = 64 * LD * VEC, THREADS = 64 * kWaves, FOUND = kWaves * kHold;
+  constexpr bool TABLE = sizeof(T) == 2;
+  struct __attribute__((packed, aligned(sizeof(T)))) Any { uint4 v; };  // (rows begin at any element)
+  __shared__ u64 held[kWaves][kHold];
+  __shared__ double table[TABLE ? Table::kSize : 1];
+  __shared__ double sum_s[kWaves];
+  __shared__ float top_s[kWaves], group_s[kGroups];
+  __shared__ int count_s[2], have_s[kWaves];
+  __shared__ unsigned bound_s;
+  __shared__ unsigned short lane_s[THREADS];
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int row = blockIdx.x / a.lists, run = blockIdx.x - row * a.lists;
   const float score = a.score[row];
   const bool off = (a.ended && a.ended[row]) || !(score > -INFINITY);  // goes on in one way, or not at all
   const T *x0 = static_cast<const T *>(a.logits) + row * a.stride;
-  const long lo = (long)run * subs * SUB, hi = off ? lo : lo + (long)subs * SUB < a.V ? lo + (long)subs * SUB : a.V;
-  float m = -INFINITY;
-  double s = 0.0;
-  int have = 0;
-  for (long at = lo; at < hi; at += SUB) {
-    float x[EL];
-    float top = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < LD; ++j) {
-      const long i = at + (long)(j * kThreads + tid) * VEC;
-      if (i + VEC <= a.V) {
-        const Piece p = *reinterpret_cast<const Piece *>(x0 + i);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) x[j * VEC + e] = as_float(p.x[e]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) x[j * VEC + e] = i + e < a.V ? as_float(x0[i + e]) : -INFINITY;
-      }
+  const long begin = (long)run * a.subs * SUB, end = off ? begin : begin + (long)a.subs * SUB < a.V ? begin + (long)a.subs * SUB : a.V;
+  auto get = [&](long i) __attribute__((always_inline)) -> uint4 {
+    if (i + VEC <= a.V) return reinterpret_cast<const Any *>(x0 + i)->v;
+    // the row's end: what is not there is ruled out
+    constexpr int BITS = 8 * sizeof(T);
+    constexpr u64 kNone = sizeof(T) == 4 ? 0xFF800000FF800000ull : 0xFF80FF80FF80FF80ull;
+    u64 w[2] = {kNone, kNone};
+#pragma unroll 1
+    for (int e = 0; i + e < a.V; ++e) {
+      const u64 b = (u64)(__float_as_uint(element(x0 + i + e)) >> (32 - BITS));
+      const int to = BITS * e & 63;
+      const u64 clear = ~(((1ull << BITS) - 1ull) << to);
+      if (BITS * e < 64) w[0] = (w[0] & clear) | b << to;
+      else w[1] = (w[1] & clear) | b << to;
     }
+    return make_uint4((unsigned)w[0], (unsigned)(w[0] >> 32), (unsigned)w[1], (unsigned)(w[1] >> 32));
+  };
+  uint4 next[LD];
+  auto load = [&](long at) __attribute__((always_inline)) {
 #pragma unroll
-    for (int e = 0; e < EL; ++e) {
-      x[e] = x[e] == x[e] ? x[e] : -INFINITY;  // (a NaN counts as an item that is ruled out)
-      top = fmaxf(top, x[e]);
-    }
-    // ---- a bound that K logits reach: the K-th largest of the groups' largest, or the K-th best so far ----
-    float group = fmaxf(top, __shfl_xor(top, 1));
-    group = fmaxf(group, __shfl_xor(group, 2));
-    if ((lane & 3) == 0) group_s[16 * wv + (lane >> 2)] = group;
-    if (tid == 0) count_s = 0;
+    for (int j = 0; j < LD; ++j) next[j] = get(at + (j * 64 + lane) * VEC);
+  };
+  float m = -INFINITY, lane_top = -INFINITY;
+  double s = 0.0, plain = 0.0;  // sums by reference m, and by none: of what the table gives
+  long at = begin + wv * SUB;
+  if (at < end) load(at);
+  if (tid < 2) count_s[tid] = 0;
+  if constexpr (TABLE) {
+    if (!off) Table::fill(table, tid, THREADS);
     __syncthreads();
-    const float mine = group_s[lane];
-    int rank = 0;
-    for (int i = 0; i < kGroups; ++i) {
-      const float o = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), i));
-      rank += o > mine || (o == mine && i < lane);
-    }
-    const float m_new = fmaxf(m, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), __builtin_ctzll(__ballot(rank == 0)))));
-    const float bound = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), __builtin_ctzll(__ballot(rank == min(a.K, kGroups) - 1))));
-    u64 least = max((u64)ordered(bound), (u64)ordered(-INFINITY) + 1) << 32;  // (-inf is no candidate)
-    if (have == a.K) least = max(least, best[a.K - 1] + 1);
+  }
+  for (; at < end; at += kWaves * SUB) {
+    uint4 v[LD];
+#pragma unroll
+    for (int j = 0; j < LD; ++j) v[j] = next[j];
+    if (at + kWaves * SUB < end) load(at + kWaves * SUB);
+    // (a NaN counts as an item that is ruled out: fmaxf takes the other)
+    float top = -INFINITY;
 #pragma unroll
     for (int j = 0; j < LD; ++j)
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        const u64 key = key_of(x[j * VEC + e], (int)(at + (long)(j * kThreads + tid) * VEC + e));
-        if (key >= least) {
-          const int to = atomicAdd(&count_s, 1);
-          if (to < kList) list[to] = key;
-        }
-      }
-    __syncthreads();
-    int n = count_s;
-    if (n > kList) {  // (as many as that where logits are equal, or lie in the same lanes' places): one after another
-      u64 last = ~0ull;
-      for (n = 0; n < a.K; ++n) {
-        u64 k = 0;
+      for (int e = 0; e < VEC; ++e) top = fmaxf(top, P::get(v[j], e));
+    lane_top = fmaxf(lane_top, top);
+    bool by_table = false;
+    if constexpr (TABLE) {
+      by_table = __any(top >= -20.0f) && !__any(top >= 64.0f);
+      if (by_table) {
 #pragma unroll
-        for (int j = 0; j < LD; ++j)
+        for (int j = 0; j < LD; ++j) asm volatile("" : "+v"(v[j].x), "+v"(v[j].y), "+v"(v[j].z), "+v"(v[j].w));  // (held as they are, not unpacked)
+#pragma unroll
+        for (int j = 0; j < LD; ++j) plain += Table::sum(table, v[j]);
+      }
+    }
+    if (!by_table) {
+      const float m_new = fmaxf(m, wave_max(top));
+      if (m_new > -INFINITY && m_new < INFINITY) {
+        const double ref = -(double)m_new * kLog2e;
+        if (m_new > m) s = m > -INFINITY ? s * exp_from(m, m_new) : 0.0;
+        const float low = m_new - 690.0f;  // (e^-690 of a sum that is 1 or more)
+#pragma unroll
+        for (int j = 0; j < LD; ++j) {
+          double t[VEC];
 #pragma unroll
           for (int e = 0; e < VEC; ++e) {
-            const u64 key = key_of(x[j * VEC + e], (int)(at + (long)(j * kThreads + tid) * VEC + e));
-            if (key >= least && key < last && key > k) k = key;
+            const float x = P::get(v[j], e);
+            t[e] = fma((double)(x > low ? x : low), kLog2e, ref);
           }
+          s += exp2_sum(t);
+        }
+      }
+      m = m_new;
+    }
+  }
+  // ---- the sum ----
 #pragma unroll
-        for (int o = 32; o >= 1; o >>= 1) k = max(k, (u64)__shfl_xor((long long)k, o));
-        __syncthreads();
-        if (lane == 0) top_s[wv] = k;
-        __syncthreads();
-        last = max(max(top_s[0], top_s[1]), max(top_s[2], top_s[3]));
-        if (last == 0) break;
-        if (tid == 0) list[n] = last;
+  for (int o = 32; o >= 1; o >>= 1) {
+    s += __shfl_xor(s, o);
+    if (TABLE) plain += __shfl_xor(plain, o);
+  }
+  if (TABLE && plain > 0.0 && m < INFINITY) {  // both by one reference
+    const float to = fmaxf(m, 0.0f);
+    s = (m > -INFINITY ? s * exp_from(m, to) : 0.0) + plain * exp_from(0.0, to);
+    m = to;
+  }
+  if (lane == 0) {
+    sum_s[wv] = s;
+    top_s[wv] = m;
+  }
+  // ---- the bound: by groups of kWaves lanes ----
+  float group = lane_top;
+#pragma unroll
+  for (int o = 1; o < kWaves; o *= 2) group = fmaxf(group, __shfl_xor(group, o));
+  if (lane % kWaves == 0) group_s[(64 / kWaves) * wv + lane / kWaves] = group;
+  __syncthreads();
+  if (wv == 0) {
+    const float mine = group_s[lane];
+    const unsigned place = (ordered(mine) & ~63u) | lane;  // (but for the last six bits, the lane's in the order)
+    int rank = 0;
+#pragma unroll 8
+    for (int i = 0; i < 64; ++i) rank += (unsigned)__builtin_amdgcn_readlane(place, i) > place;
+    if (rank == a.K - 1) bound_s = max(place & ~63u, ordered(-INFINITY) + 1);  // (-inf is no candidate)
+  } else if (tid == 64) {
+    float top = top_s[0];
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, top_s[w]);
+    double sum = 0.0;
+    for (int w = 0; w < kWaves; ++w)
+      if (top_s[w] > -INFINITY && top < INFINITY) sum += sum_s[w] * exp_from(top_s[w], top);
+    a.stats[blockIdx.x] = make_double2((double)top, sum);
+  }
+  __syncthreads();
+  const float bound = logit_of(bound_s);
+  if (lane_top >= bound) lane_s[atomicAdd(&count_s[0], 1)] = (unsigned short)tid;
+  __syncthreads();
+  // ---- the logits that reach it ----
+  u64 *found = held[0];
+  {
+    const int pieces = end > begin ? (int)((end - begin + kWaves * (long)SUB - 1) / (kWaves * (long)SUB)) : 0, loads = pieces * LD, all = count_s[0] * loads;
+    for (int i = tid; i < all && count_s[1] <= FOUND; i += THREADS) {
+      const int l = (unsigned)i / (unsigned)loads, q = i - l * loads, from = lane_s[l];
+      const long to = begin + ((long)(from >> 6) + (long)kWaves * (q / LD)) * SUB + ((q % LD) * 64 + (from & 63)) * VEC;
+      if (to >= end) continue;
+      const uint4 w = get(to);
+      unsigned some = 0;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) some |= P::get(w, e) >= bound ? 1u << e : 0u;
+      for (; some; some &= some - 1) {
+        const int e = __builtin_ctz(some), k = atomicAdd(&count_s[1], 1);
+        if (k < FOUND) found[k] = key_of(P::get(w, e), (int)(to + e));
       }
     }
-    if (tid < have) list[n + tid] = best[tid];
+  }
+  __syncthreads();
+  int n = count_s[1];
+  if (n > FOUND) {  // (logits that are equal, or large ones in few lanes' places): every wavefront through its pieces, with a bound that rises
+    u64 *mine = held[wv], least = (u64)bound_s << 32;
     __syncthreads();
-    n += have;
-    for (int i = tid; i < n; i += kThreads) {
-      const u64 k = list[i];
-      int r = 0;
-      for (int j = 0; j < n; ++j) r += list[j] > k;
-      if (r < a.K) best[r] = k;
-    }
-    have = min(n, a.K);
-    // ---- the sum ----
-    if (m_new > -INFINITY && m_new < INFINITY) {
-      if (m_new > m) s *= exp((double)m - (double)m_new);
+    n = 0;
+#pragma unroll 1
+    for (at = begin + wv * SUB; at < end; at += kWaves * SUB)
+#pragma unroll 1
+      for (int j = 0; j < LD; ++j) {
+        const long i = at + (j * 64 + lane) * VEC;
+        const uint4 w = get(i);
+        unsigned some = 0;
 #pragma unroll
-      for (int e = 0; e < EL; ++e) s += exp((double)x[e] - (double)m_new);
+        for (int e = 0; e < VEC; ++e) some |= P::get(w, e) >= logit_of((unsigned)(least >> 32)) ? 1u << e : 0u;
+        while (__any(some != 0)) {
+          const int e = some ? __builtin_ctz(some) : 0;
+          const u64 key = key_of(P::get(w, e), (int)(i + e));
+          unsigned long long in = __ballot(some != 0 && key >= least);
+          if (n + __builtin_popcountll(in) > kHold) {
+            n = keep_best(mine, n, a.K, lane);
+            if (n == a.K) least = max(least, mine[a.K - 1] + 1);
+            in = __ballot(some != 0 && key >= least);
+          }
+          if (in >> lane & 1ull) mine[n + __builtin_amdgcn_mbcnt_hi((unsigned)(in >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)in, 0))] = key;
+          n += __builtin_popcountll(in);
+          some &= some - 1;
+        }
+      }
+    n = keep_best(mine, n, a.K, lane);
+    const u64 key = lane < n ? mine[lane] : 0;
+    if (lane == 0) have_s[wv] = n;
+    __syncthreads();
+    int before_me = 0;
+    n = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      before_me += w < wv ? have_s[w] : 0;
+      n += have_s[w];
     }
-    m = m_new;
+    if (key) found[before_me + lane] = key;
     __syncthreads();
   }
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o);
-  if (lane == 0) sum_s[wv] = s;
-  __syncthreads();
-  if (tid == 0) a.stats[blockIdx.x] = make_double2((double)m, (sum_s[0] + sum_s[1]) + (sum_s[2] + sum_s[3]));
-  if (tid < a.K) a.lists_of[(size_t)blockIdx.x * a.K + tid] = tid < have ? best[tid] : 0;
+  u64 *out = a.lists_of + (size_t)blockIdx.x * a.K;
+  for (int i0 = 0; i0 < n; i0 += THREADS / 4) {  // four lanes a key
+    const int i = i0 + (tid >> 2);
+    const u64 mine = found[min(i, n - 1)];
+    int r = 0;
+#pragma unroll 4
+    for (int j = tid & 3; j < n; j += 4) r += found[j] > mine;
+    r += __shfl_xor(r, 1);
+    r += __shfl_xor(r, 2);
+    if (i < n && r < a.K && (tid & 3) == 0) out[r] = mine;
+  }
+  if (tid < a.K && tid >= n) out[tid] = 0;
 }
 
+// Of n candidates in LDS, how many are before the i-th: four lanes a candidate, i = tid / 4.
+__device__ __forceinline__ int rank_of(const u64 *p, const u64 *k, const unsigned char *w, int n, int i, int tid)
+{
+  const int at = min(i, n - 1), my_w = w[at];
+  const u64 my_p = p[at], my_k = k[at];
+  int r = 0;
+#pragma unroll 4
+  for (int j = tid & 3; j < n; j += 4) r += before(p[j], w[j], k[j], my_p, my_w, my_k);
+  r += __shfl_xor(r, 1);
+  return r + __shfl_xor(r, 2);
+}
+
+// One history.  With few candidates all are looked at: those that reach the K-th best of 64 groups' best are put in order.  Otherwise lists are
+// chosen by their first elements: element j of the list whose first is the r-th of all has r + j before it.
 __global__ __launch_bounds__(kThreads) void merge_kernel(Args a)
 {
   constexpr int PAIRS = kMost * (kMost + 1) / 2;
-  __shared__ double lse_s[kMost];
-  __shared__ u64 head_s[kLists], logit_s[kLists], group_s[kGroups];
-  __shared__ int near_s[kLists], chosen_s[kMost], count_s[2];
-  __shared__ u64 p_s[PAIRS], k_s[PAIRS];
-  __shared__ unsigned char w_s[PAIRS];
+  constexpr int FEW = 4;  // candidates of a thread
+  static_assert(FEW * kThreads <= PAIRS, "");
+  __shared__ double lse_s[kMost], score_s[kMost];
+  __shared__ u64 p_s[PAIRS], k_s[PAIRS], group_s[kGroups], head_s[kLists], logit_s[kLists];
+  __shared__ short chosen_s[kMost], near_s[kLists];
+  __shared__ unsigned char w_s[PAIRS], beam_s[kLists], ended_s[kMost];
+  __shared__ int count_s[2];
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), b = blockIdx.x;
   const int L = a.W * a.lists;
   const size_t row0 = (size_t)b * a.W;
+  const u64 *lists = a.lists_of + row0 * a.lists * a.K;
+  const bool few = L * a.K <= FEW * kThreads;
+  // (requested at once: candidates or first elements, sums, scores)
+  u64 first[FEW];
+#pragma unroll
+  for (int i = 0; i < FEW; ++i) {
+    const int c = tid + i * kThreads;
+    first[i] = c < (few ? L * a.K : L) ? lists[few ? c : (size_t)c * a.K] : 0;
+  }
+  if (tid < a.W) {
+    score_s[tid] = (double)a.score[row0 + tid];
+    ended_s[tid] = a.ended ? a.ended[row0 + tid] : 0;
+  }
   if (tid < 2) count_s[tid] = 0;
-  // ---- log sum exp of each beam's row ----
-  for (int w = wv; w < a.W; w += 4) {
-    const double2 *st = a.stats + (row0 + w) * a.lists;
-    double m = -INFINITY;
-    for (int i = lane; i < a.lists; i += 64) m = fmax(m, st[i].x);
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) m = fmax(m, __shfl_xor(m, o));
-    double s = 0.0;
-    for (int i = lane; i < a.lists; i += 64) s += st[i].x > -INFINITY ? st[i].y * exp(st[i].x - m) : 0.0;
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o);
-    if (lane == 0) lse_s[w] = m == INFINITY ? INFINITY : m + log(s);
+  // ---- log sum exp of each beam's row: as many lanes a beam as it has runs ----
+  int per = 1;
+  while (per < a.lists && per < 64) per *= 2;
+  for (int w0 = wv * (64 / per); w0 < a.W; w0 += 4 * (64 / per)) {
+    const int w = w0 + lane / per, at = lane % per;
+    const double2 *st = a.stats + (row0 + min(w, a.W - 1)) * a.lists;
+    double m = -INFINITY, s = 0.0;
+    for (int i = at; i < a.lists; i += per) {
+      const double2 x = st[i];
+      if (!(x.x > -INFINITY)) continue;
+      const double top = fmax(m, x.x);
+      s = (m > -INFINITY ? s * exp_from(m, top) : 0.0) + x.y * exp_from(x.x, top);
+      m = top;
+    }
+    double top = m;
+    for (int o = per / 2; o >= 1; o >>= 1) top = fmax(top, __shfl_xor(top, o));
+    s = m > -INFINITY ? s * exp_from(m, top) : 0.0;
+    for (int o = per / 2; o >= 1; o >>= 1) s += __shfl_xor(s, o);
+    if (at == 0 && w < a.W) lse_s[w] = top == INFINITY ? INFINITY : top + log(s);
   }
   __syncthreads();
-  // place of element j of list l in the order: its score, and its logit and item; none: 0
-  auto look = [&](int l, int j, u64 *k) -> u64 {
-    const int w = l / a.lists;
-    const double score = (double)a.score[row0 + w];
+  // a key of a beam's j-th candidate as a place in the order; none: 0
+  auto place = [&](int w, bool only, u64 &key) -> u64 {
     double to;
-    if (a.ended && a.ended[row0 + w]) {
-      *k = key_of(0.0f, a.eos);
-      to = l == w * a.lists && j == 0 ? score : -INFINITY;
+    if (ended_s[w]) {  // goes on in one way
+      key = key_of(0.0f, a.eos);
+      to = only ? score_s[w] : -INFINITY;
     } else {
-      *k = a.lists_of[(row0 * a.lists + l) * a.K + j];
-      to = *k == 0 ? -INFINITY : score + ((double)logit_of((unsigned)(*k >> 32)) - lse_s[w]);
+      to = key == 0 ? -INFINITY : score_s[w] + ((double)logit_of((unsigned)(key >> 32)) - lse_s[w]);
     }
     return to > -INFINITY ? ordered(to) : 0;  // (a NaN neither)
   };
-  // ---- lists whose first element may be among the K best: the K best first elements ----
-  u64 top = 0;
-  for (int l = tid; l < L; l += kThreads) {
-    u64 k;
-    const u64 p = look(l, 0, &k);
-    head_s[l] = p;
-    logit_s[l] = k;
-    top = max(top, p);
+  const int cells = few ? a.lists * a.K : a.lists;  // of `first`, a beam's
+  u64 top = 0, at[FEW];
+#pragma unroll
+  for (int i = 0; i < FEW; ++i) {
+    const int c = tid + i * kThreads;
+    at[i] = 0;
+    if (c >= a.W * cells) continue;
+    const int w = (unsigned)c / (unsigned)cells;
+    at[i] = place(w, c == w * cells, first[i]);
+    top = max(top, at[i]);
+    if (!few) {
+      head_s[c] = at[i];
+      logit_s[c] = first[i];
+      beam_s[c] = (unsigned char)w;
+    }
   }
   top = max(top, (u64)__shfl_xor((long long)top, 1));
   top = max(top, (u64)__shfl_xor((long long)top, 2));
@@ -218,50 +511,65 @@ __global__ __launch_bounds__(kThreads) void merge_kernel(Args a)
   {
     const u64 mine = group_s[lane];
     int rank = 0;
-    for (int i = 0; i < kGroups; ++i) rank += group_s[i] > mine || (group_s[i] == mine && i < lane);
-    const int at = __builtin_ctzll(__ballot(rank == min(a.K, kGroups) - 1));
-    bound = max(group_s[at], 1ull);
-  }
-  for (int l = tid; l < L; l += kThreads)
-    if (head_s[l] >= bound) near_s[atomicAdd(&count_s[0], 1)] = l;
-  __syncthreads();
-  const int n_near = count_s[0], n_lists = min(n_near, a.K);
-  for (int i = tid; i < n_near; i += kThreads) {
-    const int l = near_s[i], w = l / a.lists;
-    int r = 0;
-    for (int j = 0; j < n_near; ++j) {
-      const int o = near_s[j];
-      r += before(head_s[o], o / a.lists, logit_s[o], head_s[l], w, logit_s[l]);
+#pragma unroll 8
+    for (int i = 0; i < kGroups; ++i) {
+      const u64 o = group_s[i];
+      rank += o > mine || (o == mine && i < lane);
     }
-    if (r < a.K) chosen_s[r] = l;
+    bound = max(group_s[__builtin_ctzll(__ballot(rank == a.K - 1))], 1ull);
   }
-  __syncthreads();
-  // ---- element j of the r-th of them has r + j before it ----
-  const int last = n_lists == a.K ? chosen_s[a.K - 1] : -1;
-  for (int i = tid; i < n_lists * a.K; i += kThreads) {
-    const int r = i / a.K, j = i - r * a.K;
-    if (r + j >= a.K) continue;
-    const int l = chosen_s[r], w = l / a.lists;
-    u64 k;
-    const u64 p = look(l, j, &k);
-    if (p == 0 || (last >= 0 && l != last && !before(p, w, k, head_s[last], last / a.lists, logit_s[last]))) continue;
+  auto put = [&](u64 p, u64 k, int w) __attribute__((always_inline)) {
     const int to = atomicAdd(&count_s[1], 1);
     p_s[to] = p; k_s[to] = k; w_s[to] = (unsigned char)w;
+  };
+  if (few) {
+#pragma unroll
+    for (int i = 0; i < FEW; ++i)
+      if (at[i] >= bound) put(at[i], first[i], (unsigned)(tid + i * kThreads) / (unsigned)cells);
+  } else {
+    for (int l = tid; l < L; l += kThreads)
+      if (head_s[l] >= bound) near_s[atomicAdd(&count_s[0], 1)] = (short)l;
+    __syncthreads();
+    const int n_near = count_s[0], n_lists = min(n_near, a.K);
+    for (int i = tid; i < n_near; i += kThreads) {
+      const int l = near_s[i], w = beam_s[l];
+      const u64 p = head_s[l], k = logit_s[l];
+      int r = 0;
+#pragma unroll 4
+      for (int j = 0; j < n_near; ++j) {
+        const int o = near_s[j];
+        r += before(head_s[o], beam_s[o], logit_s[o], p, w, k);
+      }
+      if (r < a.K) chosen_s[r] = (short)l;
+    }
+    __syncthreads();
+    const int last = n_lists == a.K ? chosen_s[a.K - 1] : -1;
+    for (int i = tid; i < n_lists * a.K; i += kThreads) {
+      const int r = i / a.K, j = i - r * a.K;
+      if (r + j >= a.K) continue;
+      const int l = chosen_s[r], w = beam_s[l];
+      u64 p = head_s[l], k = logit_s[l];
+      if (j > 0) {
+        if (ended_s[w]) continue;
+        k = lists[(size_t)l * a.K + j];
+        p = place(w, false, k);
+        if (p == 0 || (last >= 0 && l != last && !before(p, w, k, head_s[last], beam_s[last], logit_s[last]))) continue;
+      }
+      put(p, k, w);
+    }
   }
   __syncthreads();
   const int n = count_s[1];
   const size_t out = (size_t)b * a.K;
-  for (int i = tid; i < n; i += kThreads) {
-    const u64 p = p_s[i], k = k_s[i];
-    const int w = w_s[i];
-    int r = 0;
-    for (int j = 0; j < n; ++j) r += before(p_s[j], w_s[j], k_s[j], p, w, k);
-    if (r >= a.K) continue;
-    const int item = item_of(k);
+  for (int i0 = 0; i0 < n; i0 += kThreads / 4) {
+    const int i = i0 + (tid >> 2);
+    const int r = rank_of(p_s, k_s, w_s, n, i, tid);
+    if (i >= n || r >= a.K || (tid & 3)) continue;
+    const int item = item_of(k_s[i]), w = w_s[i];
     a.parent[out + r] = (int)(row0 + w);
     a.token[out + r] = item;
-    a.out_score[out + r] = (float)score_of(p);
-    if (a.out_ended) a.out_ended[out + r] = item == a.eos || (a.ended && a.ended[row0 + w]);
+    a.out_score[out + r] = (float)score_of(p_s[i]);
+    if (a.out_ended) a.out_ended[out + r] = item == a.eos || ended_s[w];
   }
   for (int r = n + tid; r < a.K; r += kThreads) {
     a.parent[out + r] = a.token[out + r] = -1;
@@ -272,18 +580,16 @@ __global__ __launch_bounds__(kThreads) void merge_kernel(Args a)
 
 namespace {
 
-int piece(int dtype, int loads) { return kThreads * loads * (dtype == 0 ? 4 : 8); }
+constexpr int kLoads = 4;
+int piece(int dtype) { return 64 * kLoads * (dtype == 0 ? 4 : 8); }
 
 }  // namespace
 
 void plan(Args &a)
 {
-  const long rows = (long)a.B * a.W;
-  a.loads = 8;
-  if (rows * (((long)a.V + piece(a.dtype, 8) - 1) / piece(a.dtype, 8)) < 1024) a.loads = 2;
-  const long pieces = ((long)a.V + piece(a.dtype, a.loads) - 1) / piece(a.dtype, a.loads);
-  const long want = (2048 + rows - 1) / rows, most = kLists / a.W;
-  long lists = pieces < want ? pieces : want;
+  const long rows = (long)a.B * a.W, pieces = ((long)a.V + piece(a.dtype) - 1) / piece(a.dtype);
+  const long want = (1024 + rows - 1) / rows, most = kLists / a.W, whole = (pieces + kWaves - 1) / kWaves;
+  long lists = whole < want ? whole : want;
   if (lists > most) lists = most;
   a.subs = (int)((pieces + lists - 1) / lists);
   a.lists = (int)((pieces + a.subs - 1) / a.subs);
@@ -292,14 +598,12 @@ void plan(Args &a)
 bool launch(const Args &a, hipStream_t st)
 {
   const long blocks = (long)a.B * a.W * a.lists;
-  if (blocks * kThreads >= 1l << 32) return false;
-  const dim3 grid((unsigned)blocks), block(kThreads);
+  if (blocks * 64 * kWaves >= 1l << 32) return false;
+  const dim3 grid((unsigned)blocks), block(64 * kWaves);
   [&] {
-    if (a.dtype == 0 && a.loads == 8) BLOSSOM_LAUNCH((rows_kernel<float, 8>), grid, block, 0, st, a, a.subs);
-    else if (a.dtype == 0) BLOSSOM_LAUNCH((rows_kernel<float, 2>), grid, block, 0, st, a, a.subs);
-    else if (a.loads == 8) BLOSSOM_LAUNCH((rows_kernel<bf16_t, 8>), grid, block, 0, st, a, a.subs);
-    else BLOSSOM_LAUNCH((rows_kernel<bf16_t, 2>), grid, block, 0, st, a, a.subs);
-    BLOSSOM_LAUNCH(merge_kernel, dim3((unsigned)a.B), block, 0, st, a);
+    if (a.dtype == 0) BLOSSOM_LAUNCH((rows_kernel<float, kLoads>), grid, block, 0, st, a);
+    else BLOSSOM_LAUNCH((rows_kernel<bf16_t, kLoads>), grid, block, 0, st, a);
+    BLOSSOM_LAUNCH(merge_kernel, dim3((unsigned)a.B), dim3(kThreads), 0, st, a);
   }();
   return true;
 }

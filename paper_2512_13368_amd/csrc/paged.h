@@ -82,8 +82,8 @@ struct Fork {
   const int *refs;             // [n_pages] who holds a page
   int *table, *len, *new_refs; // [N, max_pages], [N], [n_pages]
   int *copies, *missing;       // [N, 3] source, target, rows; [1]
-  int *fresh;                  // [N] pages that a sequence gets, in the workspace
-  int *eldest;                 // [S] the first sequence that goes on from this one (N: none), there too
+  int2 *at;                    // [N] a sequence's first page that is not whole, is it the eldest of its parent; in the workspace
+  int *fresh;                  // [N] pages that it gets, there too
   int *held;                   // [n_pages] copies that read a page, there too
 };
 bool launch_fork(const Args &a, const Fork &x, hipStream_t st);

@@ -84,6 +84,9 @@ bool launch_accept(const Args &a, const Accept &x, hipStream_t st)
 // one with the last L mod page rows a copy.  refs' = refs - entries of the old table + entries of the new one; fresh pages are those that
 // nobody holds then and no copy reads, the lowest first, to the sequences in order.
 
+// Sequences take a wavefront each, fresh pages one workgroup: two launches between which the counts settle.  A launch takes longer than its
+// work: a fork of 512 sequences of up to 4040 positions takes four launches of 4 to 9 us, mostly chains of loads from one to the next.
+//
 // What a new sequence takes over.
 struct Heir {
   int q, len, full, part, need;  // (q < 0: nothing)
@@ -99,133 +102,124 @@ struct Heir {
 };
 __device__ __forceinline__ int valid(const Args &a, int id) { return id >= 0 && id < a.n_pages ? id : -1; }
 
-// refs go over, and who is the eldest
-__global__ __launch_bounds__(kThreads) void fork_begin_kernel(Args a, Fork x)
+// ---- by a wavefront: new sequence n, and what becomes of old sequence n ----
+
+// Its row of the new table, fresh pages as -2, -3, .. in order, how many those are, and which page it copies.
+__device__ __forceinline__ void fork_row(const Args &a, const Fork &x, int n, int lane)
 {
-  const int i = blockIdx.x * kThreads + threadIdx.x;
-  if (i < a.n_pages) {
-    x.new_refs[i] = x.refs[i];
-    x.held[i] = 0;
+  const Heir h(a, x, n);
+  bool elder = false;  // does an earlier one go on from the same parent?
+  for (int i = lane; i < n; i += 64) elder = elder || x.parent[i] == h.q;
+  const bool eldest = h.q >= 0 && !__any(elder);
+  const int *from = a.page_table + (size_t)max(h.q, 0) * a.max_pages;
+  int *to = x.table + (size_t)n * a.max_pages;
+  int fresh = 0, copy = -1;
+  for (int i0 = 0; i0 < a.max_pages; i0 += 64) {
+    const int i = i0 + lane;
+    const int old = i < h.need ? valid(a, from[i]) : -1;
+    const bool taken = i < h.full || (i < h.need && eldest && old >= 0 && x.refs[old] == 1), asks = i < h.need && !taken;
+    const unsigned long long all = __ballot(asks);
+    const int before = __builtin_amdgcn_mbcnt_hi((unsigned)(all >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)all, 0));
+    if (asks && i == h.full && h.part > 0) copy = old;
+    if (i < a.max_pages) to[i] = taken ? old : asks ? -2 - (fresh + before) : -1;
+    fresh += __builtin_popcountll(all);
   }
-  if (i < a.S) {
-    int e = x.N;
-    for (int n = 0; n < x.N; ++n)
-      if (x.parent[n] == i) {
-        e = n;
-        break;
-      }
-    x.eldest[i] = e;
+  const unsigned long long copies = __ballot(copy >= 0);
+  copy = __builtin_amdgcn_readlane(copy, copies ? __builtin_ctzll(copies) : 0);
+  if (lane == 0) {
+    x.fresh[n] = fresh;
+    x.len[n] = h.len;
+    x.at[n] = make_int2(h.full, eldest);
+    x.copies[3 * n] = copy;
+    x.copies[3 * n + 2] = h.part;
+  }
+}
+// Who holds a page then: one more for every page that a younger one shares, one less for those that neither the eldest takes over.
+__device__ __forceinline__ void fork_refs(const Args &a, const Fork &x, int n, int lane)
+{
+  if (n < x.N) {
+    const int2 at = x.at[n];
+    const int copy = x.copies[3 * n];
+    const int *row = x.table + (size_t)n * a.max_pages;
+    for (int i = lane; i < (at.y ? 0 : at.x); i += 64)
+      if (row[i] >= 0) atomicAdd(x.new_refs + row[i], 1);
+    if (lane == 0 && copy >= 0) atomicAdd(x.held + copy, 1);
+  }
+  if (n >= a.S) return;
+  int heir = x.N;
+  for (int i = lane; i < x.N; i += 64)
+    if (x.parent[i] == n) heir = min(heir, i);
+  heir = x.N - wave_max(x.N - heir);  // the eldest
+  const int *from = a.page_table + (size_t)n * a.max_pages;
+  const int *row = x.table + (size_t)min(heir, x.N - 1) * a.max_pages;
+  for (int i = lane; i < a.max_pages; i += 64) {
+    const int old = valid(a, from[i]), now = heir == x.N ? -1 : row[i];
+    if (old >= 0 && now != old) atomicSub(x.new_refs + old, 1);
   }
 }
 
-// rows of the new table, and what changes hands
-__global__ __launch_bounds__(kThreads) void fork_rows_kernel(Args a, Fork x)
+// Fresh pages, by one workgroup of 1024.
+__device__ __forceinline__ void fork_give(const Args &a, const Fork &x, int tid)
 {
-  __shared__ int fresh_s;
-  const int b = blockIdx.x, tid = threadIdx.x;
-  if (b < x.N) {
-    const Heir h(a, x, b);
-    const bool eldest = h.q >= 0 && x.eldest[h.q] == b;
-    const int *from = a.page_table + (size_t)max(h.q, 0) * a.max_pages;
-    int *to = x.table + (size_t)b * a.max_pages;
-    if (tid == 0) fresh_s = 0;
-    __syncthreads();
-    int copy = -1;
-    for (int i = tid; i < a.max_pages; i += kThreads) {
-      int id = -1;
-      if (i < h.need) {
-        const int old = valid(a, from[i]);
-        if (i < h.full) {
-          id = old;
-        } else if (eldest && old >= 0 && x.refs[old] == 1) {
-          id = old;
-        } else {
-          atomicAdd(&fresh_s, 1);
-          if (i == h.full && h.part > 0) copy = old;
-        }
-        if (id >= 0 && !eldest) atomicAdd(x.new_refs + id, 1);
-        if (i == h.full && h.part > 0) {
-          if (copy >= 0) atomicAdd(x.held + copy, 1);
-          x.copies[3 * b] = copy;
-        }
-      }
-      to[i] = id;
-    }
-    if (tid == 0 && !(h.part > 0 && h.full < h.need)) x.copies[3 * b] = -1;
-    __syncthreads();
-    if (tid == 0) {
-      x.fresh[b] = fresh_s;
-      x.len[b] = h.len;
-    }
-  }
-  if (b < a.S) {  // what nobody, or the eldest, does not take over
-    const int e = x.eldest[b];
-    const int *from = a.page_table + (size_t)b * a.max_pages;
-    Heir h(a, x, min(e, x.N - 1));
-    if (e >= x.N) h.full = h.need = 0;
-    for (int i = tid; i < a.max_pages; i += kThreads) {
-      const int old = valid(a, from[i]);
-      if (old < 0 || i < h.full || (i < h.need && x.refs[old] == 1)) continue;
-      atomicSub(x.new_refs + old, 1);
-    }
-  }
-}
-
-// fresh pages, by one workgroup
-__global__ __launch_bounds__(1024) void fork_give_kernel(Args a, Fork x)
-{
-  __shared__ int sums[16], total_s;
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  constexpr int AT_ONCE = 4, NEAR = 4096;
+  __shared__ int sums[16], begin_s[NEAR];
+  const int lane = tid & 63, wv = tid >> 6;
   // exclusive sums over the workgroup; *total: of all
   auto scan = [&](int v, int *total) -> int {
     const int upto = wave_scan(v);
     __syncthreads();
     if (lane == 63) sums[wv] = upto;
     __syncthreads();
-    if (wv == 0) {
-      const int s = lane < 16 ? sums[lane] : 0, t = wave_scan(s);
-      if (lane < 16) sums[lane] = t - s;
-      if (lane == 15) total_s = t;
-    }
-    __syncthreads();
-    *total = total_s;
-    return sums[wv] + upto - v;
+    const int s = lane < 16 ? sums[lane] : 0, t = wave_scan(s);
+    *total = __builtin_amdgcn_readlane(t, 15);
+    return __shfl(t - s, wv) + upto - v;
   };
-  // requests: sequence n's begin at fresh[n]
+  auto look = [&](int p0) -> unsigned {
+    unsigned free = 0;
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int p = p0 + tid * AT_ONCE + i;
+      if (p < a.n_pages && x.new_refs[p] == 0 && x.held[p] == 0) free |= 1u << i;
+    }
+    return free;
+  };
+  unsigned free = look(0);
+  // requests: sequence n's begin at fresh[n] (of up to NEAR sequences, at begin_s[n])
+  const bool near = x.N <= NEAR;
   int asked = 0;
   for (int n0 = 0; n0 < x.N; n0 += 1024) {
     const int n = n0 + tid, mine = n < x.N ? x.fresh[n] : 0;
     int total;
     const int before = scan(mine, &total);
-    if (n < x.N) x.fresh[n] = asked + before;
+    if (n < x.N) {
+      if (near) begin_s[n] = asked + before;
+      else x.fresh[n] = asked + before;
+    }
     asked += total;
   }
   __syncthreads();
+  auto begin = [&](int n) { return near ? begin_s[n] : x.fresh[n]; };
   // the k-th free page goes to the k-th request: to the last sequence that begins at or before k
   int given = 0;
-  for (int p0 = 0; p0 < a.n_pages && given < asked; p0 += 1024) {
-    const int p = p0 + tid;
-    const bool free = p < a.n_pages && x.new_refs[p] == 0 && x.held[p] == 0;
-    int total;
-    const int k = given + scan(free, &total);
-    if (free && k < asked) {
+  for (int p0 = 0; p0 < a.n_pages && given < asked; p0 += 1024 * AT_ONCE) {
+    if (p0 > 0) free = look(p0);
+    int total, k = scan(__builtin_popcount(free), &total);
+    k += given;
+    for (; free && k < asked; free &= free - 1, ++k) {
+      const int p = p0 + tid * AT_ONCE + __builtin_ctz(free);
       int lo = 0, hi = x.N;
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (x.fresh[mid] <= k) lo = mid;
+        if (begin(mid) <= k) lo = mid;
         else hi = mid;
       }
-      // its (k - fresh[lo])-th entry without a page
-      const Heir h(a, x, lo);
-      int *row = x.table + (size_t)lo * a.max_pages;
-      const int *from = a.page_table + (size_t)h.q * a.max_pages;
-      const bool eldest = x.eldest[h.q] == lo;
-      int at = k - x.fresh[lo], i = h.full;
-      for (; i < h.need; ++i) {
-        const int old = valid(a, from[i]);
-        if (!(eldest && old >= 0 && x.refs[old] == 1) && at-- == 0) break;
-      }
-      row[i] = p;
+      const int nth = k - begin(lo);
+      const int2 at = x.at[lo];
+      int *entry = x.table + (size_t)lo * a.max_pages + at.x;
+      if (!at.y) entry += nth;  // (its entries from there on all ask)
+      else
+        while (*entry != -2 - nth) ++entry;
+      *entry = p;
       x.new_refs[p] = 1;
     }
     given += total;
@@ -233,22 +227,64 @@ __global__ __launch_bounds__(1024) void fork_give_kernel(Args a, Fork x)
   __syncthreads();
   if (tid == 0) x.missing[0] = max(asked - given, 0);
   for (int n = tid; n < x.N; n += 1024) {
-    const Heir h(a, x, n);
-    const int src = x.copies[3 * n], dst = src >= 0 ? x.table[(size_t)n * a.max_pages + h.full] : -1;
-    const bool on = src >= 0 && dst >= 0;
-    x.copies[3 * n] = on ? src : -1;
-    x.copies[3 * n + 1] = on ? dst : -1;
-    x.copies[3 * n + 2] = on ? h.part : 0;
+    int src = x.copies[3 * n];
+    const int part = x.copies[3 * n + 2];
+    const int dst = src >= 0 ? x.table[(size_t)n * a.max_pages + x.at[n].x] : -1;
+    if (dst < 0) src = -1;
+    x.copies[3 * n] = src;
+    x.copies[3 * n + 1] = src < 0 ? -1 : dst;
+    x.copies[3 * n + 2] = src < 0 ? 0 : part;
   }
+  if (asked <= given) return;
+  __syncthreads();
+  for (size_t i = tid; i < (size_t)x.N * a.max_pages; i += 1024)
+    if (x.table[i] < -1) x.table[i] = -1;
+}
+
+__global__ __launch_bounds__(kThreads) void fork_rows_kernel(Args a, Fork x)
+{
+  const int i0 = blockIdx.x * kThreads + threadIdx.x, lane = threadIdx.x & 63;
+  for (int i = i0; i < a.n_pages; i += gridDim.x * kThreads) {
+    x.new_refs[i] = x.refs[i];
+    x.held[i] = 0;
+  }
+  const int n = __builtin_amdgcn_readfirstlane(i0 >> 6);
+  if (n < x.N) fork_row(a, x, n, lane);
+}
+__global__ __launch_bounds__(kThreads) void fork_refs_kernel(Args a, Fork x)
+{
+  const int n = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * kThreads + threadIdx.x) >> 6);
+  if (n < max(x.N, a.S)) fork_refs(a, x, n, threadIdx.x & 63);
+}
+__global__ __launch_bounds__(1024) void fork_give_kernel(Args a, Fork x) { fork_give(a, x, threadIdx.x); }
+// all of it, for few sequences and pages
+__global__ __launch_bounds__(1024) void fork_kernel(Args a, Fork x)
+{
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  for (int i = tid; i < a.n_pages; i += 1024) {
+    x.new_refs[i] = x.refs[i];
+    x.held[i] = 0;
+  }
+  for (int n = wv; n < x.N; n += 16) fork_row(a, x, n, lane);
+  __syncthreads();
+  for (int n = wv; n < max(x.N, a.S); n += 16) fork_refs(a, x, n, lane);
+  __threadfence();  // (the counts' atomics are done in the second-level cache: nobody reads them from the first)
+  __syncthreads();
+  __threadfence();
+  fork_give(a, x, tid);
 }
 
 bool launch_fork(const Args &a, const Fork &x, hipStream_t st)
 {
-  const long begin = ((long)(a.n_pages > a.S ? a.n_pages : a.S) + kThreads - 1) / kThreads, rows = x.N > a.S ? x.N : a.S;
-  if (!countable(begin, kThreads) || !countable(rows, kThreads)) return false;
+  const long most = x.N > a.S ? x.N : a.S, blocks = (most * 64 + kThreads - 1) / kThreads;
+  if (!countable(blocks, kThreads)) return false;
   [&] {
-    BLOSSOM_LAUNCH(fork_begin_kernel, dim3((unsigned)begin), dim3(kThreads), 0, st, a, x);
-    BLOSSOM_LAUNCH(fork_rows_kernel, dim3((unsigned)rows), dim3(kThreads), 0, st, a, x);
+    if (most <= 64 && most * a.max_pages <= 8192 && a.n_pages <= 16384) {
+      BLOSSOM_LAUNCH(fork_kernel, dim3(1), dim3(1024), 0, st, a, x);
+      return;
+    }
+    BLOSSOM_LAUNCH(fork_rows_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, st, a, x);
+    BLOSSOM_LAUNCH(fork_refs_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, st, a, x);
     BLOSSOM_LAUNCH(fork_give_kernel, dim3(1), dim3(1024), 0, st, a, x);
   }();
   return true;
