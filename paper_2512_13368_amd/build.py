@@ -33,6 +33,7 @@ SOURCES = {
     "paged_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "paged_prompt.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "paged_shared.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "paged_tree.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "paged_pages.hip": [],
     "beam_api.hip": [],
     "beam.hip": [],

@@ -50,9 +50,11 @@ struct Args {
   int row_tiles;               // prompt: workgroups a key/value head and part
   int2 *part_of;               // decode: [S] first part and parts of a sequence, there too
   const int64_t *tree;         // drafted trees: [T] which of its sequence's drafted tokens a token sees, or nullptr
-  int units;                   // workgroups a key/value head; `parts` of them beyond one a row tile (0: walks are whole).  The partial
-                               // sums are [units, G, rows of a tile, ..] then
-  int4 *part_at;               // [T] of a token's sequence: its first unit, the parts of its walks, its first token; in the workspace
+  int tree_rows;               // trees: rows of a workgroup: which kernel takes the call (16; shared_waves * 16; 128 or 256)
+  int units;                   // workgroups a key/value head; `parts` is their number too where walks are cut (0: they are whole)
+  int slots;                   // places of partial sums, [slots, G, rows of a tile, ..]
+  int4 *part_at;               // [1 + T] tiles of a workgroup's share; of a token's tree, where its walks begin, tiles of one, its first row
+                               // tile, its first token; in the workspace
 };
 
 // HIP counts a launch's threads in 32 bits.  The launchers below start nothing and return false for a call that would have more.
@@ -97,6 +99,11 @@ void launch_prompt_mfma(const Args &a, hipStream_t st);
 // rows of a workgroup: 16 a wavefront, of which there are as many as it takes to move a tile
 constexpr int shared_waves(int row_bytes) { return row_bytes >= 256 ? 4 : 2; }
 void launch_prompt_shared(const Args &a, hipStream_t st);
+// the same for drafted trees
+void launch_tree_shared(const Args &a, hipStream_t st);
+// drafted trees of more than 16 rows for bf16, d = 64 or 128: paged_tree.hip (once: loads past the caches)
+bool tree_matrix_supported(const Args &a);
+void launch_tree_matrix(const Args &a, bool once, hipStream_t st);
 
 // Calls f with the element type and the head size as compile-time constants.
 template <typename F>
@@ -270,6 +277,7 @@ struct RowTile {
 // The n drafted tokens of a sequence take the slots past .. past + n - 1 after its history, token i slot past + i; bit k of its mask says
 // that it sees drafted token k (k < 64, k < n).  It stands `depth` positions behind the history, the number of other drafted tokens it sees.
 constexpr int kDrafts = 64;
+constexpr int kTreeLeast = 512;  // keys of a workgroup's share, at least, where rows share them
 __device__ __forceinline__ unsigned long long below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; }
 __device__ __forceinline__ int depth_of(unsigned long long mask, int i, int n)
 {
@@ -292,13 +300,13 @@ struct Tree {
   }
   // the first key that a token sees at this depth
   __device__ __forceinline__ int first(const Args &a, int depth) const { return max(max(past, 0) + depth - a.window + 1, 0); }
-  __device__ __forceinline__ int tiles() const { return any.hi >= any.lo ? any.hi / 32 - any.lo / 32 + 1 : 0; }
 };
 
 // One token's keys, 32 at a time.
 struct Seen {
   int lo;                   // of the history
   unsigned long long mask;  // of the drafted tokens
+  Seen() = default;
   __device__ __forceinline__ Seen(const Args &a, const Tree &t, unsigned long long given, int i, int n)
   {
     lo = t.first(a, depth_of(given, i, n));
@@ -313,61 +321,113 @@ struct Seen {
   }
 };
 
-// The rows and the part of their walk that one workgroup of a key/value head takes.  Whole walks: row tiles at floor(cu[s] R / rows) + s,
-// as for prompts.  Otherwise a sequence's walk of t tiles of 32 keys is cut into ceil(t / chunk) parts, for each of its row tiles: with
-// chunk = ceil(sum of row tiles times tiles / a.parts) there are fewer than a.parts units beyond one a row tile, whatever the lengths are.
-struct TreeUnit {
-  int s = -1, tok0 = 0, count = 0, row0 = 0, part = 0, parts = 1, first = 0;  // (s < 0: none; first: the sequence's first unit)
-  __device__ __forceinline__ TreeUnit(const Args &a, int lane, int unit, int rows, int least)
+// Rows of one sequence and key/value head, and what is walked for them.
+struct Walk {
+  int s = -1, tok0 = 0, count = 0, row0 = 0;  // sequence (below 0: none), its first token, its tokens, the first row
+  int len = 0;                                // trees: its kv_len
+  int part = 0, parts = 1;                    // prompts: which of how many parts
+  int from = 0, tiles = 0x7FFFFFFF;           // trees: tiles of the walk from its first on
+  int slot = -1;                              // trees: where partial sums go (below 0: the walk is whole)
+};
+
+// What one workgroup of a key/value head does of all trees.  A tree's rows are cut into row tiles, each of which walks the same key tiles.  With
+// a.parts workgroups, the walks of all row tiles lie one behind the other, and workgroup b takes the b-th of as many equal shares: the end
+// of one walk, whole ones, the beginning of another.  (Cut into parts by themselves, 16 walks of 125 to 253 tiles leave the longest part
+// 1.5 to 1.8 times the mean.)  Row tile j's part in workgroup b has slot b + j.  Otherwise (a.parts 0) a workgroup takes one walk.
+struct TreeWork {
+  struct One {
+    int cu, n, len, tiles, row_tiles;
+  };
+  int unit, rows, keys;  // workgroup; rows of a row tile, keys of a tile
+  int at = 0, end = 0, share = 0;
+  __device__ __forceinline__ One look(const Args &a, int i) const
+  {
+    One x{token_at(a, min(i, a.S)), 0, 0, 0, 0};
+    if (i >= a.S) return x;
+    x.len = a.kv_len[i];
+    x.n = max(token_at(a, i + 1) - x.cu, 0);
+    if (x.n == 0) return x;
+    const Tree t(a, x.len, x.n);
+    x.tiles = t.any.hi >= t.any.lo ? t.any.hi / keys - t.any.lo / keys + 1 : 1;  // (a walk of nothing has a place too)
+    x.row_tiles = (unsigned)(x.n * a.R + rows - 1) / rows;
+    return x;
+  }
+  __device__ __forceinline__ TreeWork(int unit, int rows, int keys) : unit(unit), rows(rows), keys(keys) {}
+  // The first walk.
+  __device__ __forceinline__ Walk begin(const Args &a, int lane, int least)
   {
     if (a.parts == 0) {
+      Walk w;
       const Sequence seq(a, lane, [&](int i, int cu) { return (int)((unsigned)(cu * a.R) / rows) + i <= unit; });
-      const int at = (unit - (int)((unsigned)(seq.first * a.R) / rows) - seq.s) * rows;
-      if (at < 0 || at >= seq.count * a.R) return;
-      s = seq.s; tok0 = seq.first; count = seq.count; row0 = at;
-      return;
+      const int row0 = (unit - (int)((unsigned)(seq.first * a.R) / rows) - seq.s) * rows;
+      if (row0 < 0 || row0 >= seq.count * a.R) return w;
+      w.s = seq.s; w.tok0 = seq.first; w.count = seq.count; w.row0 = row0;
+      w.len = __builtin_amdgcn_readfirstlane(a.kv_len[w.s]);
+      return w;
     }
-    struct One { int cu, n, tiles, row_tiles; };
-    auto look = [&](int i) {
-      One x{token_at(a, min(i, a.S)), 0, 0, 0};
-      if (i >= a.S) return x;
-      x.n = max(token_at(a, i + 1) - x.cu, 0);
-      if (x.n == 0) return x;
-      x.tiles = max(Tree(a, a.kv_len[i], x.n).tiles(), 1);
-      x.row_tiles = (unsigned)(x.n * a.R + rows - 1) / rows;
-      return x;
-    };
-    const One mine0 = look(lane);
+    const One mine0 = look(a, lane);
     int total = 0;
     for (int s0 = 0; s0 < a.S; s0 += 64) {
-      const One x = s0 == 0 ? mine0 : look(s0 + lane);
+      const One x = s0 == 0 ? mine0 : look(a, s0 + lane);
       total += wave_sum(x.tiles * x.row_tiles);
     }
-    const unsigned chunk = max((unsigned)(total + a.parts - 1) / a.parts, (unsigned)least);
-    int done = 0;
+    share = max((unsigned)(total + a.parts - 1) / (unsigned)a.parts, (unsigned)least);
+    at = (int)min((long)unit * share, (long)total);
+    end = (int)min((long)at + share, (long)total);
+    return take(a, lane, mine0);
+  }
+  // The next walk, or piece of one (s < 0: no more).  The first workgroup of a key/value head tells the join where each tree lies.
+  __device__ __forceinline__ Walk next(const Args &a, int lane)
+  {
+    if (at >= end) return Walk{};
+    return take(a, lane, look(a, lane));
+  }
+  __device__ __forceinline__ Walk take(const Args &a, int lane, const One &mine0)
+  {
+    Walk w;
+    if (at >= end) return w;
+    int done = 0, tiles_done = 0;  // row tiles, and tiles of their walks
     for (int s0 = 0; s0 < a.S; s0 += 64) {
-      const One x = s0 == 0 ? mine0 : look(s0 + lane);
-      const int cut = (x.tiles + chunk - 1) / chunk, mine = cut * x.row_tiles, upto = done + wave_scan(mine);
-      const int k = __builtin_popcountll(__ballot(upto <= unit));
+      const One x = s0 == 0 ? mine0 : look(a, s0 + lane);
+      const int mine = x.tiles * x.row_tiles, upto = tiles_done + wave_scan(mine), row_upto = done + wave_scan(x.row_tiles);
+      const int k = __builtin_popcountll(__ballot(upto <= at));
       if (k < 64) {
-        s = s0 + k;
-        parts = __builtin_amdgcn_readlane(cut, k);
-        first = __builtin_amdgcn_readlane(upto, k) - __builtin_amdgcn_readlane(mine, k);
-        tok0 = __builtin_amdgcn_readlane(x.cu, k);
-        count = __builtin_amdgcn_readlane(x.n, k);
-        const int tile = (unsigned)(unit - first) / (unsigned)parts;
-        part = unit - first - tile * parts;
-        row0 = tile * rows;
+        const int tiles = __builtin_amdgcn_readlane(x.tiles, k), row_tiles = __builtin_amdgcn_readlane(x.row_tiles, k);
+        const int in = at - (__builtin_amdgcn_readlane(upto, k) - tiles * row_tiles), tile = (unsigned)in / (unsigned)tiles;
+        w.s = s0 + k;
+        w.tok0 = __builtin_amdgcn_readlane(x.cu, k);
+        w.count = __builtin_amdgcn_readlane(x.n, k);
+        w.len = __builtin_amdgcn_readlane(x.len, k);
+        w.row0 = tile * rows;
+        w.from = in - tile * tiles;
+        w.tiles = min(end - at, tiles - w.from);
+        if (w.tiles < tiles) w.slot = unit + __builtin_amdgcn_readlane(row_upto, k) - row_tiles + tile;
+        at += w.tiles;
+        return w;
+      }
+      tiles_done = __builtin_amdgcn_readlane(upto, 63);
+      done = __builtin_amdgcn_readlane(row_upto, 63);
+    }
+    return w;
+  }
+  // By the workgroup that has a tree's first piece: for the join.
+  __device__ __forceinline__ void tell(const Args &a, const Walk &w, int g, int lane, int tid, int threads) const
+  {
+    if (a.parts == 0 || w.row0 != 0 || w.from != 0 || g != 0) return;
+    int done = 0, tiles_done = 0;
+    for (int s0 = 0; s0 < a.S; s0 += 64) {
+      const One x = look(a, s0 + lane);
+      const int upto = tiles_done + wave_scan(x.tiles * x.row_tiles), row_upto = done + wave_scan(x.row_tiles);
+      if (w.s < s0 + 64) {
+        const int k = w.s - s0, tiles = __builtin_amdgcn_readlane(x.tiles, k), row_tiles = __builtin_amdgcn_readlane(x.row_tiles, k);
+        const int4 place = make_int4(__builtin_amdgcn_readlane(upto, k) - tiles * row_tiles, tiles, __builtin_amdgcn_readlane(row_upto, k) - row_tiles, w.tok0);
+        for (int i = tid; i < w.count; i += threads) a.part_at[1 + w.tok0 + i] = place;
+        if (tid == 0) a.part_at[0] = make_int4(share, 0, 0, 0);  // (all that write it write the same)
         return;
       }
-      done = __builtin_amdgcn_readlane(upto, 63);
+      tiles_done = __builtin_amdgcn_readlane(upto, 63);
+      done = __builtin_amdgcn_readlane(row_upto, 63);
     }
-  }
-  // for the join: by the first workgroup of a sequence
-  __device__ __forceinline__ void tell(const Args &a, int g, int tid, int threads) const
-  {
-    if (a.parts == 0 || part != 0 || row0 != 0 || g != 0) return;
-    for (int i = tid; i < count; i += threads) a.part_at[tok0 + i] = make_int4(first, parts, tok0, 0);
   }
 };
 

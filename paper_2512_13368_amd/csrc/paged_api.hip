@@ -61,7 +61,7 @@ size_t attn_ws_bytes(Args &a, bool prompt)
 size_t tree_ws_bytes(const Args &a)
 {
   const size_t rows = tree_part_rows(a);
-  return rows ? rows * (a.d + 2) * sizeof(float) + (size_t)a.T * sizeof(int4) : 0;
+  return rows ? rows * (a.d + 2) * sizeof(float) + (1 + (size_t)a.T) * sizeof(int4) : 0;
 }
 
 int launch_status() { return hipGetLastError() == hipSuccess ? BLOSSOM_OK : BLOSSOM_ERR_LAUNCH; }
@@ -192,7 +192,7 @@ int blossom_attn_tree(const blossom_paged_params *p, const void *Q, int64_t q_st
     if (!ws || ws_bytes < need) return BLOSSOM_ERR_WORKSPACE;
     if (!aligned16(ws)) return BLOSSOM_ERR_ALIGN;
     a.part_at = static_cast<int4 *>(ws);
-    a.part_o = reinterpret_cast<float *>(a.part_at + a.T);
+    a.part_o = reinterpret_cast<float *>(a.part_at + 1 + a.T);
     a.part_ml = a.part_o + tree_part_rows(a) * a.d;
   }
   a.Q = Q; a.K_cache = const_cast<void *>(K_cache); a.V_cache = const_cast<void *>(V_cache);

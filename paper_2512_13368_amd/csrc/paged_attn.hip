@@ -105,10 +105,15 @@ struct Part {
   }
 };
 
+// What a workgroup of the kernels below takes: up to 16 rows that share keys, and which part of their walk.
+struct FewRows {
+  int s, row0, rows, tok0, new_tokens = 1, part = 0, n_parts = 1, b = 0;
+};
+
 // One new token a sequence, or few (PROMPT; TREE: drafted ones): W wavefronts take a run of key tiles each for up to 16 rows that share
 // keys.  SPLIT: of a part of them.
-template <typename T, int D, int W, bool ONCE, bool SPLIT, bool PROMPT, bool TREE = false>
-__global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
+template <typename T, int D, int W, bool ONCE, bool SPLIT, bool PROMPT, bool TREE>
+__device__ __forceinline__ void few_rows(const Args &a, int g, const FewRows &mine_rows, const Walk &walk)
 {
   typedef Tile<T, D> TL;
   constexpr int STAGES = decode_stages(TL::RB), HOLD = STAGES * 2 * TL::BYTES;  // LDS of a wavefront
@@ -116,49 +121,12 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
   static_assert(kRows * LDR * 4 <= HOLD, "results go where the tiles were");
   __shared__ __attribute__((aligned(1024))) char lds[W * HOLD];
   __shared__ float m_s[W][kRows], l_s[W][kRows];
-  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int lane = threadIdx.x & 63;
+  if constexpr (TREE) asm volatile("" : "+v"(lane));  // (what depends on it is not kept in registers from one walk to the next)
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, c = lane >> 4;
-
-  const int rest = a.by_G.of(blockIdx.x), g = blockIdx.x - rest * a.G;
-  int s, row0, rows, tok0, new_tokens = 1, part = 0, n_parts = 1, b = 0;
-  if constexpr (TREE) {
-    const TreeUnit unit(a, lane, rest, kRows, W);
-    if (unit.s < 0) return;
-    unit.tell(a, g, threadIdx.x, 64 * W);
-    s = unit.s;
-    tok0 = unit.tok0;
-    new_tokens = unit.count;
-    row0 = unit.row0;
-    part = unit.part;
-    n_parts = unit.parts;
-    rows = min(new_tokens * a.R - row0, kRows);
-  } else if constexpr (PROMPT) {
-    const int tile = a.by_parts.of(rest);
-    part = rest - tile * a.parts;
-    n_parts = a.parts;
-    const Sequence seq(a, lane, [&](int i, int cu) { return (int)((unsigned)(cu * a.R) / kRows) + i <= tile; });
-    s = seq.s;
-    tok0 = seq.first;
-    new_tokens = seq.count;
-    row0 = (tile - (int)((unsigned)(tok0 * a.R) / kRows) - s) * kRows;
-    if (row0 < 0 || row0 >= new_tokens * a.R) return;
-    rows = min(new_tokens * a.R - row0, kRows);
-  } else {
-    const int tiles = (a.R + kRows - 1) / kRows;
-    b = tiles == 1 ? rest : rest / tiles;
-    row0 = (rest - b * tiles) * kRows;
-    s = b;
-    if constexpr (SPLIT) {
-      const Part mine(a, lane, b, W);
-      if (mine.s < 0) return;
-      s = mine.s;
-      part = b - mine.first;
-      n_parts = mine.count;
-      if (part == 0 && g == 0 && row0 == 0 && threadIdx.x == 0) a.part_of[s] = make_int2(mine.first, n_parts);  // for the join
-    }
-    tok0 = s;
-    rows = min(a.R - row0, kRows);
-  }
+  const int s = mine_rows.s, row0 = mine_rows.row0, rows = mine_rows.rows, tok0 = mine_rows.tok0, new_tokens = mine_rows.new_tokens;
+  const int part = mine_rows.part, n_parts = mine_rows.n_parts, b = mine_rows.b;
   const int row = row0 + min(n, rows - 1), tok = PROMPT ? a.by_R.of(row) : 0, head = g * a.R + row - tok * a.R;
 
   // what hangs on nothing is requested before anything is waited for: the length, the query, the first pages
@@ -167,7 +135,7 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
     const int id = table[min(first + lane, a.max_pages - 1)];
     return id >= 0 && id < a.n_pages ? id : -1;
   };
-  const int raw_len = a.kv_len[s];
+  const int raw_len = TREE ? walk.len : a.kv_len[s];
   int list0 = 0, ids = entries(0);  // pages list0 .. list0 + 63, one a lane
   typename TL::Query q;
   TL::load_query(q, static_cast<const T *>(a.Q) + (tok0 + tok) * a.q_stride + (size_t)head * D, c);
@@ -188,7 +156,10 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
   }
   const int t_lo = any.lo / kTile, t_all = any.hi >= any.lo ? any.hi / kTile - t_lo + 1 : 0;
   int t_begin = t_lo, t_end = t_lo + t_all;
-  if constexpr (SPLIT) {
+  if constexpr (TREE) {
+    t_begin = t_lo + min(walk.from, t_all);
+    t_end = t_begin + min(walk.tiles, t_lo + t_all - t_begin);
+  } else if constexpr (SPLIT) {
     const int each = (t_all + n_parts - 1) / n_parts;
     t_begin = t_lo + min(part * each, t_all);
     t_end = t_lo + min((part + 1) * each, t_all);
@@ -274,15 +245,65 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
     }
     const int tk = PROMPT ? a.by_R.of(row0 + row) : 0;
     const size_t out = (size_t)(tok0 + tk) * a.H + g * a.R + row0 + row - tk * a.R;
-    if (!SPLIT || ((!PROMPT || TREE) && n_parts == 1)) {
+    if (!SPLIT || (TREE ? walk.slot < 0 : !PROMPT && n_parts == 1)) {
       const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
       store_four(static_cast<T *>(a.O) + out * D + ch, o, inv);
       if (ch == 0 && a.lse) a.lse[out] = ll == 0.0f ? kNegInf : (mm + __log2f(ll)) * kLn2;
-    } else {  // decode: [heads of the token][parts of all sequences]; prompt: [rows][parts of each]; trees: [units][heads][rows of a tile]
-      const size_t at = TREE ? ((size_t)rest * a.G + g) * kRows + row : PROMPT ? out * a.parts + part : (size_t)(g * a.R + row0 + row) * a.parts + b;
+    } else {  // decode: [heads of the token][parts of all sequences]; prompt: [rows][parts of each]; trees: [slots][heads][rows of a tile]
+      const size_t at = TREE ? ((size_t)walk.slot * a.G + g) * kRows + row : PROMPT ? out * a.parts + part : (size_t)(g * a.R + row0 + row) * a.parts + b;
       *reinterpret_cast<float4 *>(a.part_o + at * D + ch) = o;
       if (ch == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(mm, ll);
     }
+  }
+}
+
+template <typename T, int D, int W, bool ONCE, bool SPLIT, bool PROMPT>
+__global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
+{
+  const int lane = threadIdx.x & 63, rest = a.by_G.of(blockIdx.x), g = blockIdx.x - rest * a.G;
+  FewRows r;
+  if constexpr (PROMPT) {
+    const int tile = a.by_parts.of(rest);
+    r.part = rest - tile * a.parts;
+    r.n_parts = a.parts;
+    const Sequence seq(a, lane, [&](int i, int cu) { return (int)((unsigned)(cu * a.R) / kRows) + i <= tile; });
+    r.s = seq.s;
+    r.tok0 = seq.first;
+    r.new_tokens = seq.count;
+    r.row0 = (tile - (int)((unsigned)(r.tok0 * a.R) / kRows) - r.s) * kRows;
+    if (r.row0 < 0 || r.row0 >= r.new_tokens * a.R) return;
+    r.rows = min(r.new_tokens * a.R - r.row0, kRows);
+  } else {
+    const int tiles = (a.R + kRows - 1) / kRows;
+    r.b = tiles == 1 ? rest : rest / tiles;
+    r.row0 = (rest - r.b * tiles) * kRows;
+    r.s = r.b;
+    if constexpr (SPLIT) {
+      const Part mine(a, lane, r.b, W);
+      if (mine.s < 0) return;
+      r.s = mine.s;
+      r.part = r.b - mine.first;
+      r.n_parts = mine.count;
+      if (r.part == 0 && g == 0 && r.row0 == 0 && threadIdx.x == 0) a.part_of[r.s] = make_int2(mine.first, r.n_parts);  // for the join
+    }
+    r.tok0 = r.s;
+    r.rows = min(a.R - r.row0, kRows);
+  }
+  few_rows<T, D, W, ONCE, SPLIT, PROMPT, false>(a, g, r, Walk{});
+}
+
+template <typename T, int D, int W, bool SPLIT>
+__global__ __launch_bounds__(64 * W) void tree_few_kernel(Args a)
+{
+  const int lane = threadIdx.x & 63, rest = a.by_G.of(blockIdx.x), g = blockIdx.x - rest * a.G;
+  TreeWork work(rest, kRows, kTile);
+  for (Walk w = work.begin(a, lane, W); w.s >= 0; w = work.next(a, lane)) {
+    work.tell(a, w, g, lane, threadIdx.x, 64 * W);
+    FewRows r;
+    r.s = w.s; r.tok0 = w.tok0; r.new_tokens = w.count; r.row0 = w.row0;
+    r.rows = min(w.count * a.R - w.row0, kRows);
+    few_rows<T, D, W, false, SPLIT, true, true>(a, g, r, w);
+    __syncthreads();
   }
 }
 
@@ -383,44 +404,78 @@ __global__ __launch_bounds__(256) void join_rows_kernel(Args a)
   if (at == 0 && a.lse) a.lse[row] = l == 0.0f ? kNegInf : (m + __log2f(l)) * kLn2;
 }
 
-// Joins the parts of drafted tokens' rows, where a walk has more than one: D / 4 threads a row, 4 channels each, as above.  `rows`: of a
-// workgroup of the walk.
-template <typename T, int D>
+// Joins the parts of drafted tokens' rows, where a walk has more than one.  D / 4 lanes have 4 channels each of a part; GROUPS such groups
+// take a row's parts in turn, and are summed over at the end.  `rows`: of a workgroup of the walk.
+template <typename T, int D, int GROUPS>
 __global__ __launch_bounds__(256) void join_tree_kernel(Args a, int rows)
 {
-  constexpr int LANES = D / 4, ROWS = 256 / LANES, AHEAD = 8;
-  const int at = threadIdx.x % LANES;
-  const size_t row = (size_t)blockIdx.x * ROWS + threadIdx.x / LANES;
-  if (row >= (size_t)token_at(a, a.S) * a.H) return;  // (a row that no sequence owns stays as it is)
-  const int t = a.by_H.of((int)row), h = (int)row - t * a.H;
-  const int4 of = a.part_at[t];
-  const int parts = of.y;
-  if (parts <= 1) return;  // (the walk's workgroup wrote the row)
-  const int g = a.by_R.of(h), r = (t - of.z) * a.R + h - g * a.R, tile = (unsigned)r / (unsigned)rows;
-  const long first = of.x + (long)tile * parts;
-  if (r < 0 || first < 0 || first + parts > a.units) return;  // (cu_seqlens does not ascend: whatever the workspace held)
-  const size_t step = (size_t)a.G * rows, at0 = (first * a.G + g) * rows + (r - tile * rows);
+  constexpr int LANES = D / 4, EACH = LANES * GROUPS, ROWS = 256 / EACH, AHEAD = 8;
+  __shared__ float4 o_s[GROUPS > 1 ? 256 : 1];
+  __shared__ float2 ml_s[GROUPS > 1 ? 256 / LANES : 1];
+  const int at = threadIdx.x % LANES, grp = threadIdx.x / LANES % GROUPS;
+  const size_t row = (size_t)blockIdx.x * ROWS + threadIdx.x / EACH;
+  // (a row that no sequence owns stays as it is, and one that its walk's workgroup wrote)
+  int parts = 0;
+  size_t step = 0, at0 = 0;
+  if (row < (size_t)token_at(a, a.S) * a.H) {
+    const int t = a.by_H.of((int)row), h = (int)row - t * a.H;
+    const int share = a.part_at[0].x;
+    const int4 of = a.part_at[1 + t];
+    const int g = a.by_R.of(h), r = (t - of.w) * a.R + h - g * a.R, tile = (unsigned)r / (unsigned)rows;
+    const long begin = of.x + (long)tile * of.y;  // of the row's walk, among all
+    if (share > 0 && r >= 0 && begin >= 0 && of.y > 0) {  // (else cu_seqlens does not ascend: whatever the workspace held)
+      const int first = (int)(begin / share), last = (int)((begin + of.y - 1) / share);
+      const long slot = (long)first + of.z + tile;
+      if (last > first && slot >= 0 && slot + last - first < a.slots) {
+        parts = last - first + 1;
+        step = (size_t)a.G * rows;
+        at0 = (slot * a.G + g) * rows + (r - tile * rows);
+      }
+    }
+  }
+  if (GROUPS == 1 && parts == 0) return;
   const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + at0;
   const float4 *po = reinterpret_cast<const float4 *>(a.part_o) + at0 * LANES + at;
   float m = kNegInf;
-  for (int i = 0; i < parts; ++i) m = fmaxf(m, ml[i * step].x);
+  for (int i = grp; i < parts; i += GROUPS) m = fmaxf(m, ml[i * step].x);
   const float ref = m == kNegInf ? 0.0f : m;
   float l = 0.0f;
   float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  for (int i = 0; i < parts; i += AHEAD) {
+  auto add = [&](const float4 &v, float w) __attribute__((always_inline)) {
+    o.x = fmaf(v.x, w, o.x); o.y = fmaf(v.y, w, o.y); o.z = fmaf(v.z, w, o.z); o.w = fmaf(v.w, w, o.w);
+  };
+  for (int i = grp; i < parts; i += AHEAD * GROUPS) {
     float4 v[AHEAD];
     float2 x[AHEAD];
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
-      const size_t j = min(i + k, parts - 1) * step;
+      const size_t j = min(i + k * GROUPS, parts - 1) * step;
       v[k] = po[j * LANES];
       x[k] = ml[j];
     }
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
-      const float w = i + k < parts ? __builtin_amdgcn_exp2f(x[k].x - ref) : 0.0f;
+      const float w = i + k * GROUPS < parts ? __builtin_amdgcn_exp2f(x[k].x - ref) : 0.0f;
       l = fmaf(x[k].y, w, l);
-      o.x = fmaf(v[k].x, w, o.x); o.y = fmaf(v[k].y, w, o.y); o.z = fmaf(v[k].z, w, o.z); o.w = fmaf(v[k].w, w, o.w);
+      add(v[k], w);
+    }
+  }
+  if constexpr (GROUPS > 1) {
+    o_s[threadIdx.x] = o;
+    if (at == 0) ml_s[threadIdx.x / LANES] = make_float2(m, l);
+    __syncthreads();
+    if (grp > 0 || parts == 0) return;
+    const float2 *mls = ml_s + threadIdx.x / LANES;
+    m = kNegInf;
+#pragma unroll
+    for (int k = 0; k < GROUPS; ++k) m = fmaxf(m, mls[k].x);
+    l = 0.0f;
+    o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int k = 0; k < GROUPS; ++k) {
+      const float w = __builtin_amdgcn_exp2f(mls[k].x - (m == kNegInf ? 0.0f : m));
+      l = fmaf(mls[k].y, w, l);
+      add(o_s[threadIdx.x + k * LANES], w);
     }
   }
   store_four(static_cast<T *>(a.O) + row * D + 4 * at, o, l == 0.0f ? 0.0f : 1.0f / l);
@@ -576,34 +631,60 @@ bool launch_prompt(const Args &call, hipStream_t st)
   return true;
 }
 
-// Drafted trees: 16 rows a workgroup, whose wavefronts take runs of keys as in decode.  Walks are split until the chip is full.
+// Drafted trees.
 void plan_tree(Args &a)
 {
-  const int w = few_waves(row_bytes_of(a));
-  const long base = (long)a.T * a.R / kRows + a.S;
-  const long tiles = ((long)(a.window < a.cap ? a.window + kDrafts + kTile - 1 : a.cap) + kTile - 1) / kTile;
-  long extra = fill_waves(row_bytes_of(a)) / w / a.G - base / 2;
-  if (tiles < 2 * w || base * tiles > 1 << 30 || extra < 1) extra = 0;
-  a.parts = (int)extra;
-  a.units = (int)(base + extra);
+  const int row_bytes = row_bytes_of(a), w = few_waves(row_bytes);
+  const long rows = (long)a.T * a.R, each = rows / a.S;
+  int waves, keys = kTile, least = kTreeLeast / kTile;  // workgroups that fill the chip; keys of a tile, tiles of a share at least
+  if (each <= 16) {
+    a.tree_rows = kRows;
+    waves = fill_waves(row_bytes) / w;
+    least = w;
+  } else if (tree_matrix_supported(a)) {
+    a.tree_rows = each <= 128 ? 128 : 256;
+    waves = a.d == 64 ? 512 : 256;
+    keys = 32 * 256 / a.tree_rows;
+    least = kTreeLeast / keys;
+  } else {
+    a.tree_rows = shared_rows(a);
+    waves = 4096 / shared_waves(row_bytes);
+  }
+  const long base = rows / a.tree_rows + a.S;  // row tiles, at most
+  const long tiles = ((long)(a.window < a.cap ? a.window + kDrafts + keys - 1 : a.cap) + keys - 1) / keys;
+  a.parts = waves / a.G;
+  if (tiles < 2 * least || base * tiles > 1 << 30 || 3 * (rows / a.tree_rows > a.S ? rows / a.tree_rows : a.S) > 2 * a.parts) a.parts = 0;
+  a.units = (int)(a.parts ? a.parts : base);
+  a.slots = (int)(a.parts ? a.parts + base : 0);
 }
 
-size_t tree_part_rows(const Args &a) { return a.parts ? (size_t)a.units * a.G * kRows : 0; }
+size_t tree_part_rows(const Args &a) { return (size_t)a.slots * a.G * a.tree_rows; }
 
 bool launch_tree(const Args &a, hipStream_t st)
 {
+  const bool matrix = a.tree_rows != kRows && tree_matrix_supported(a);
+  const int waves = a.tree_rows == kRows ? few_waves(row_bytes_of(a)) : matrix ? 8 : shared_waves(row_bytes_of(a));
   const dim3 grid((unsigned)((long)a.units * a.G));
-  if (!countable((long)a.units * a.G, 64 * few_waves(row_bytes_of(a)))) return false;
+  if (!countable((long)a.units * a.G, 64 * waves)) return false;
+  const bool once = (double)a.S * a.cap * a.G * row_bytes_of(a) * 2 > 256e6;
+  if (matrix) launch_tree_matrix(a, once, st);
+  else if (a.tree_rows != kRows) launch_tree_shared(a, st);
   with_type(a, [&](auto type, auto dim) {
     typedef decltype(type) T;
     constexpr int D = decltype(dim)::value, W = few_waves(D * sizeof(T));
-    if (!a.parts) {
-      BLOSSOM_LAUNCH((decode_kernel<T, D, W, false, false, true, true>), grid, dim3(64 * W), 0, st, a);
-      return;
+    if (a.tree_rows == kRows) {
+      if (a.parts) BLOSSOM_LAUNCH((tree_few_kernel<T, D, W, true>), grid, dim3(64 * W), 0, st, a);
+      else BLOSSOM_LAUNCH((tree_few_kernel<T, D, W, false>), grid, dim3(64 * W), 0, st, a);
     }
-    BLOSSOM_LAUNCH((decode_kernel<T, D, W, false, true, true, true>), grid, dim3(64 * W), 0, st, a);
-    if (launch_failed()) return;
-    BLOSSOM_LAUNCH((join_tree_kernel<T, D>), dim3((unsigned)((size_t)a.T * a.H * (D / 4) / 256 + 1)), dim3(256), 0, st, a, kRows);
+    if (a.parts && !launch_failed()) {
+      // few sequences have many parts
+      constexpr int GROUPS = 256 / (D / 4) < 8 ? 256 / (D / 4) : 8;
+      auto join = [&](auto kernel, int groups) {
+        BLOSSOM_LAUNCH(kernel, dim3((unsigned)((size_t)a.T * a.H * groups * (D / 4) / 256 + 1)), dim3(256), 0, st, a, a.tree_rows);
+      };
+      if (a.parts > 8 * a.S) join(join_tree_kernel<T, D, GROUPS>, GROUPS);
+      else join(join_tree_kernel<T, D, 1>, 1);
+    }
   });
   return true;
 }

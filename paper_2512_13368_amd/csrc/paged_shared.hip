@@ -26,24 +26,21 @@ using mfma::kNegInf;
 template <typename T, int D>
 constexpr int kRoomFor = sizeof(T) == 2 && D == 128 ? 3 : 1;
 
-template <typename T, int D, bool SPLIT>
-__global__ __launch_bounds__(64 * shared_waves(D * sizeof(T))) __attribute__((amdgpu_waves_per_eu(kRoomFor<T, D>))) void shared_kernel(Args a)
+// The rows of one workgroup (SPLIT: over a part of their walk).  TREE: of drafted tokens, as in paged_prompt.hip.
+template <typename T, int D, bool SPLIT, bool TREE>
+__device__ __forceinline__ void walk_rows(const Args &a, int g, const Walk &w)
 {
   typedef Tile<T, D> TL;
   constexpr int W = shared_waves(TL::RB);
   __shared__ __attribute__((aligned(1024))) char lds[2][2 * TL::BYTES];
-  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int lane = threadIdx.x & 63;
+  if constexpr (TREE) asm volatile("" : "+v"(lane));  // (what depends on it is not kept in registers from one walk to the next)
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, c = lane >> 4;
-
-  // ---- this workgroup's rows: the last tiles, which see most keys, first ----
-  const int rest = a.by_G.of(blockIdx.x), g = blockIdx.x - rest * a.G;
-  const int nth = a.by_parts.of(rest), part = rest - nth * a.parts;
-  const RowTile mine(a, lane, nth, 16 * W, 2);
-  const int s = mine.s, tok0 = mine.tok0, new_tokens = mine.count, wg_row = mine.row0;
-  if (wg_row < 0) return;
+  const int s = w.s, tok0 = w.tok0, new_tokens = w.count, wg_row = w.row0;
   const int rows = new_tokens * a.R;
   // (requested together: the length, the first pages, the queries)
-  const int raw_len = a.kv_len[s];
+  const int raw_len = TREE ? w.len : a.kv_len[s];
   const int *table = a.page_table + s * a.table_seq;
   auto entries = [&](int first) __attribute__((always_inline)) -> int {
     const int id = table[min(first + lane, a.max_pages - 1)];
@@ -57,27 +54,36 @@ __global__ __launch_bounds__(64 * shared_waves(D * sizeof(T))) __attribute__((am
   typename TL::Query q;
   TL::load_query(q, static_cast<const T *>(a.Q) + (tok0 + tok) * a.q_stride + (size_t)head * D, c);
 
+  unsigned long long mask = 0ull;
+  if constexpr (TREE) mask = a.tree[tok0 + tok];
+
   const int len = max(__builtin_amdgcn_readfirstlane(raw_len), 0);
   const int first_pos = len - new_tokens;
-  const Range wg_first = seen_by(a, first_pos + a.by_R.of(wg_row), len), wg_last = seen_by(a, first_pos + a.by_R.of(min(wg_row + 16 * W, rows) - 1), len);
+  const Tree tree(a, len, new_tokens);
+  const Seen sees(a, tree, mask, tok, new_tokens);
+  const Range wg_first = TREE ? tree.any : seen_by(a, first_pos + a.by_R.of(wg_row), len);
+  const Range wg_last = TREE ? tree.any : seen_by(a, first_pos + a.by_R.of(min(wg_row + 16 * W, rows) - 1), len);
   const int lo = wg_first.lo, hi = wg_last.hi;  // keys that any row sees
 
   Range my = seen_by(a, first_pos + tok, len);
   if (!row_ok) my.hi = -1;
   // keys that all rows of the wavefront see, and that any does
-  const Range r_first = seen_by(a, first_pos + a.by_R.of(min(row0, rows - 1)), len);
-  const Range r_last = seen_by(a, first_pos + a.by_R.of(min(row0 + 15, rows - 1)), len);
+  const Range r_first = TREE ? Range{tree.any.lo, tree.every.hi} : seen_by(a, first_pos + a.by_R.of(min(row0, rows - 1)), len);
+  const Range r_last = TREE ? Range{tree.every.lo, tree.any.hi} : seen_by(a, first_pos + a.by_R.of(min(row0 + 15, rows - 1)), len);
   const int any_lo = r_first.lo, any_hi = row0 < rows ? r_last.hi : -1;
 
   int t = lo / kTile, t_end = hi >= lo ? hi / kTile + 1 : t;
-  if constexpr (SPLIT) {
+  if constexpr (TREE) {
+    t = min(t + w.from, t_end);
+    t_end = t + min(w.tiles, t_end - t);
+  } else if constexpr (SPLIT) {
     const int each = (t_end - t + a.parts - 1) / a.parts, from = t;
-    t = min(from + part * each, t_end);
+    t = min(from + w.part * each, t_end);
     t_end = min(t + each, t_end);
   }
   const size_t page_bytes = ((size_t)a.G << a.page_shift) * TL::RB, group_bytes = ((size_t)g << a.page_shift) * TL::RB;
   // few keys: by their number, or because pages are out of range
-  bool fine = TL::BF && few_keys(wg_first, wg_last);
+  bool fine = TL::BF && (TREE ? tree.every.hi - tree.every.lo + 1 < kFewKeys : few_keys(wg_first, wg_last));
   auto look = [&]() __attribute__((always_inline)) {
     const int page = list0 + lane;
     if (TL::BF) fine = fine || __any(ids < 0 && page >= lo >> a.page_shift && page <= hi >> a.page_shift);
@@ -100,7 +106,7 @@ __global__ __launch_bounds__(64 * shared_waves(D * sizeof(T))) __attribute__((am
   };
 
   Rows<T, D> r;
-  r.clear(row_ok);
+  r.clear(TREE || row_ok);  // (TREE: rows behind the last do as it does)
   unsigned seen = t < t_end ? request(t, lds[0]) : 0u;
 #pragma unroll
   for (int i = 0; i < TL::NK; ++i) asm volatile("" : "+v"(q.x[i].x), "+v"(q.x[i].y), "+v"(q.x[i].z), "+v"(q.x[i].w));  // (arrived before the walk)
@@ -112,9 +118,9 @@ __global__ __launch_bounds__(64 * shared_waves(D * sizeof(T))) __attribute__((am
       const unsigned next = t + 1 < t_end ? request(t + 1, lds[cur ^ 1]) : 0u;
       const int base = t * kTile;
       if (base <= any_hi && base + kTile - 1 >= any_lo) {
-        const bool all = seen == 0xFFFFFFFFu && row0 + 15 < rows && base >= r_last.lo && base + kTile - 1 <= r_first.hi;
-        r.template attend<decltype(two)::value>(lds[cur], lds[cur] + TL::BYTES, q, a.scale2, seen & mfma::row_bits(my.lo - base, my.hi - base), all,
-                                                base + 16 <= any_hi, lane);
+        const bool all = seen == 0xFFFFFFFFu && (TREE || row0 + 15 < rows) && base >= r_last.lo && base + kTile - 1 <= r_first.hi;
+        const unsigned row_sees = TREE ? sees.bits(tree, base, mfma::row_bits) : mfma::row_bits(my.lo - base, my.hi - base);
+        r.template attend<decltype(two)::value>(lds[cur], lds[cur] + TL::BYTES, q, a.scale2, seen & row_sees, all, base + 16 <= any_hi, lane);
       }
       mfma::arrived_all<0>();
       seen = next;
@@ -129,14 +135,16 @@ __global__ __launch_bounds__(64 * shared_waves(D * sizeof(T))) __attribute__((am
   if (!row_ok) return;
   const size_t out = (size_t)(tok0 + tok) * a.H + head;
   if constexpr (SPLIT) {
-    const size_t at = out * a.parts + part;
+    if (!TREE || w.slot >= 0) {
+      const size_t at = TREE ? ((size_t)w.slot * a.G + g) * (16 * W) + (row - wg_row) : out * a.parts + w.part;
 #pragma unroll
-    for (int j = 0; j < TL::NV; ++j)
+      for (int j = 0; j < TL::NV; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (TL::channel(j, c, i) < D) a.part_o[at * D + TL::channel(j, c, i)] = r.acc[j][i];
-    if (c == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(r.m, l);
-    return;
+        for (int i = 0; i < 4; ++i)
+          if (TL::channel(j, c, i) < D) a.part_o[at * D + TL::channel(j, c, i)] = r.acc[j][i];
+      if (c == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(r.m, l);
+      return;
+    }
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   T *O = static_cast<T *>(a.O) + out * D;
@@ -161,6 +169,32 @@ __global__ __launch_bounds__(64 * shared_waves(D * sizeof(T))) __attribute__((am
   if (c == 0 && a.lse) a.lse[out] = l == 0.0f ? kNegInf : (r.m + __log2f(l)) * kLn2;
 }
 
+template <typename T, int D, bool SPLIT>
+__global__ __launch_bounds__(64 * shared_waves(D * sizeof(T))) __attribute__((amdgpu_waves_per_eu(kRoomFor<T, D>))) void shared_kernel(Args a)
+{
+  // ---- this workgroup's rows: the last tiles, which see most keys, first ----
+  const int rest = a.by_G.of(blockIdx.x), g = blockIdx.x - rest * a.G, nth = a.by_parts.of(rest);
+  const RowTile mine(a, threadIdx.x & 63, nth, 16 * shared_waves(D * sizeof(T)), 2);
+  if (mine.row0 < 0) return;
+  Walk w;
+  w.s = mine.s; w.tok0 = mine.tok0; w.count = mine.count; w.row0 = mine.row0;
+  w.part = rest - nth * a.parts;
+  walk_rows<T, D, SPLIT, false>(a, g, w);
+}
+
+template <typename T, int D, bool SPLIT>
+__global__ __launch_bounds__(64 * shared_waves(D * sizeof(T))) __attribute__((amdgpu_waves_per_eu(kRoomFor<T, D>))) void tree_shared_kernel(Args a)
+{
+  constexpr int W = shared_waves(D * sizeof(T));
+  const int lane = threadIdx.x & 63, rest = a.by_G.of(blockIdx.x), g = blockIdx.x - rest * a.G;
+  TreeWork work(rest, 16 * W, kTile);
+  for (Walk w = work.begin(a, lane, kTreeLeast / kTile); w.s >= 0; w = work.next(a, lane)) {
+    work.tell(a, w, g, lane, threadIdx.x, 64 * W);
+    walk_rows<T, D, SPLIT, true>(a, g, w);
+    __syncthreads();
+  }
+}
+
 namespace {
 template <typename T, int D>
 void launch_d(const Args &a, hipStream_t st)
@@ -174,6 +208,17 @@ void launch_d(const Args &a, hipStream_t st)
 void launch_prompt_shared(const Args &a, hipStream_t st)
 {
   with_type(a, [&](auto type, auto dim) { launch_d<decltype(type), decltype(dim)::value>(a, st); });
+}
+
+void launch_tree_shared(const Args &a, hipStream_t st)
+{
+  with_type(a, [&](auto type, auto dim) {
+    typedef decltype(type) T;
+    constexpr int D = decltype(dim)::value;
+    const dim3 grid((unsigned)((long)a.units * a.G)), block(64 * shared_waves(D * sizeof(T)));
+    if (a.parts) BLOSSOM_LAUNCH((tree_shared_kernel<T, D, true>), grid, block, 0, st, a);
+    else BLOSSOM_LAUNCH((tree_shared_kernel<T, D, false>), grid, block, 0, st, a);
+  });
 }
 
 }  // namespace paged
