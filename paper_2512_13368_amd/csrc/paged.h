@@ -84,9 +84,10 @@ struct Fork {
   const int *refs;             // [n_pages] who holds a page
   int *table, *len, *new_refs; // [N, max_pages], [N], [n_pages]
   int *copies, *missing;       // [N, 3] source, target, rows; [1]
-  int2 *at;                    // [N] a sequence's first page that is not whole, is it the eldest of its parent; in the workspace
+  int4 *at;                    // [N] a sequence's first page that is not whole, is it the eldest of its parent, page and rows that it
+                               // copies (below 0: none); in the workspace
   int *fresh;                  // [N] pages that it gets, there too
-  int *held;                   // [n_pages] copies that read a page, there too
+  int *held;                   // [n_pages] does a copy read a page, there too
 };
 bool launch_fork(const Args &a, const Fork &x, hipStream_t st);
 bool launch_copy(const Args &a, const int *copies, int count, hipStream_t st);

@@ -121,7 +121,7 @@ int append(const blossom_paged_params *p, const void *Q, int64_t q_stride, const
 }
 
 // the fork's workspace: where a sequence's own pages begin, how many it asks for, copies that read a page
-size_t fork_ws_bytes(const Args &a, int n_new) { return (size_t)n_new * (sizeof(int2) + sizeof(int)) + a.n_pages * sizeof(int); }
+size_t fork_ws_bytes(const Args &a, int n_new) { return (size_t)n_new * (sizeof(int4) + sizeof(int)) + a.n_pages * sizeof(int); }
 
 bool aligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
@@ -246,7 +246,7 @@ int blossom_kv_fork(const blossom_paged_params *p, int32_t n_new, int32_t grow, 
   Fork x{};
   x.N = n_new; x.grow = grow; x.parent = parent; x.refs = refs;
   x.table = new_table; x.len = new_len; x.new_refs = new_refs; x.copies = copies; x.missing = missing;
-  x.at = static_cast<int2 *>(ws);
+  x.at = static_cast<int4 *>(ws);
   x.fresh = reinterpret_cast<int *>(x.at + n_new);
   x.held = x.fresh + n_new;
   (void)hipGetLastError();

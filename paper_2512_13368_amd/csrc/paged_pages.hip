@@ -20,52 +20,64 @@ __device__ __forceinline__ int page_of(const Args &a, const int *table, int pos)
 }  // namespace
 
 // Rows past + keep[i] move to past + i, i ascending.  A thread owns 16 bytes of every row (of K or of V, of one key/value head), so what it
-// reads later never lies where it wrote: keep[j] >= j > i for j > i.  No thread waits for another.
+// reads later never lies where it wrote: keep[j] >= j > i for j > i.  No thread waits for another.  64 entries at a time, one a lane, whose
+// pages are looked up together (128 trees of 33 to 64 tokens, up to 12 kept: FIGURES; a chain of loads, length to page to row).
 __global__ __launch_bounds__(kThreads) void accept_kernel(Args a, Accept x, int row_chunks)
 {
   constexpr int AHEAD = 8;
   const int lane = threadIdx.x & 63;
   const int per = 2 * a.G * row_chunks, groups = (per + kThreads - 1) / kThreads;  // threads and workgroups of a sequence
   const int s = blockIdx.x / groups, at = (blockIdx.x - s * groups) * kThreads + threadIdx.x;
-  const int first = token_at(a, s), n = max(token_at(a, s + 1) - first, 0);
-  const int raw = a.kv_len[s], past = max(raw, 0) - n;
   const int *keep = x.keep + (size_t)s * x.width;
   const int *table = a.page_table + s * a.table_seq;
-  // how many are kept: a lane an entry
+  int mine = lane < x.width ? keep[lane] : -1, last = -1;  // (requested with the lengths)
+  const int first = token_at(a, s), n = max(token_at(a, s + 1) - first, 0);
+  const int past = max(a.kv_len[s], 0) - n;
+  const int chunk = at % row_chunks, head = min(at / row_chunks, 2 * a.G - 1);  // K's heads, then V's
+  uint4 *cache = reinterpret_cast<uint4 *>(head < a.G ? a.K_cache : a.V_cache);
+  const int g = head < a.G ? head : head - a.G, page = 1 << a.page_shift;
   int kept = 0;
   for (int i0 = 0; i0 < x.width; i0 += 64) {
     const int i = i0 + lane;
-    const int mine = i < x.width ? keep[i] : -1, before = i == 0 || i >= x.width ? -1 : keep[i - 1];
+    if (i0 > 0) mine = i < x.width ? keep[i] : -1;
+    const int up = __shfl_up(mine, 1), before = lane == 0 ? last : up;
+    last = __builtin_amdgcn_readlane(mine, 63);
     const unsigned long long good = __ballot(mine > before && mine < n && mine >= 0);
     const int run = good == ~0ull ? 64 : __builtin_ctzll(~good);
     kept += run;
+    // where a row of key/value head 0 lies before and after, in positions of a page times heads (below 0: it is not moved)
+    auto place = [&](int pos) __attribute__((always_inline)) -> long {
+      const int id = lane < run ? page_of(a, table, pos) : -1;
+      return id < 0 ? -1 : ((long)id * a.G << a.page_shift) + (pos & (page - 1));
+    };
+    long from = mine == i ? -1 : place(past + mine);
+    const long to = from < 0 ? -1 : place(past + i);
+    if (to < 0) from = -1;
+    unsigned long long moves = __ballot(from >= 0);
+    while (moves) {
+      uint4 v[AHEAD];
+      uint4 *dst[AHEAD];
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        dst[k] = nullptr;
+        if (moves == 0 || at >= per) continue;
+        const int l = __builtin_ctzll(moves);
+        moves &= moves - 1;
+        auto of = [&](long p) __attribute__((always_inline)) {
+          return (long)(unsigned)__builtin_amdgcn_readlane((int)(p >> 32), l) << 32 | (unsigned)__builtin_amdgcn_readlane((int)p, l);
+        };
+        const long step = (long)g << a.page_shift;
+        v[k] = cache[(of(from) + step) * row_chunks + chunk];
+        dst[k] = cache + (of(to) + step) * row_chunks + chunk;
+      }
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k)
+        if (dst[k]) *dst[k] = v[k];
+      if (at >= per) break;
+    }
     if (run < 64) break;
   }
   if (at == 0 && x.new_len) x.new_len[s] = past + kept;
-  if (at >= per) return;
-  const int chunk = at % row_chunks, head = at / row_chunks;  // K's heads, then V's
-  uint4 *cache = reinterpret_cast<uint4 *>(head < a.G ? a.K_cache : a.V_cache);
-  const int g = head < a.G ? head : head - a.G, page = 1 << a.page_shift;
-  auto cell = [&](int id, int pos) __attribute__((always_inline)) {
-    return cache + (((size_t)id * a.G + g) * page + (pos & (page - 1))) * row_chunks + chunk;
-  };
-  for (int i0 = 0; i0 < kept; i0 += AHEAD) {
-    uint4 v[AHEAD];
-    uint4 *to[AHEAD];
-#pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
-      to[k] = nullptr;
-      const int i = i0 + k;
-      if (i >= kept || keep[i] == i) continue;
-      const int src = page_of(a, table, past + keep[i]), dst = page_of(a, table, past + i);
-      if (src < 0 || dst < 0) continue;
-      v[k] = *cell(src, past + keep[i]);
-      to[k] = cell(dst, past + i);
-    }
-#pragma unroll
-    for (int k = 0; k < AHEAD; ++k)
-      if (to[k]) *to[k] = v[k];
-  }
 }
 
 bool launch_accept(const Args &a, const Accept &x, hipStream_t st)
@@ -84,8 +96,9 @@ bool launch_accept(const Args &a, const Accept &x, hipStream_t st)
 // one with the last L mod page rows a copy.  refs' = refs - entries of the old table + entries of the new one; fresh pages are those that
 // nobody holds then and no copy reads, the lowest first, to the sequences in order.
 
-// Sequences take a wavefront each, fresh pages one workgroup: two launches between which the counts settle.  A launch takes longer than its
-// work: a fork of 512 sequences of up to 4040 positions takes four launches of 4 to 9 us, mostly chains of loads from one to the next.
+// Sequences take a wavefront each, which counts pages by atomics (a sum of whole numbers, in any order); fresh pages go out from one
+// workgroup.  It is all chains of loads, each about a microsecond where another die wrote: 512 sequences of up to 4040 positions FIGURES
+// in four launches with the copies; few sequences and pages are done by one workgroup with its counts in LDS.
 //
 // What a new sequence takes over.
 struct Heir {
@@ -102,11 +115,23 @@ struct Heir {
 };
 __device__ __forceinline__ int valid(const Args &a, int id) { return id >= 0 && id < a.n_pages ? id : -1; }
 
-// ---- by a wavefront: new sequence n, and what becomes of old sequence n ----
-
-// Its row of the new table, fresh pages as -2, -3, .. in order, how many those are, and which page it copies.
-__device__ __forceinline__ void fork_row(const Args &a, const Fork &x, int n, int lane)
+// New sequence n, and old sequence n, by a wavefront: its row of the new table, fresh pages as -2, -3, .. in order, how many those are, and
+// which page it copies; who holds a page then.  count(page, change), hold(page): of a page that a copy reads.
+template <typename C, typename H>
+__device__ __forceinline__ void fork_row(const Args &a, const Fork &x, int n, int lane, C &&count, H &&hold)
 {
+  if (n < a.S) {  // dropped by all: its pages go
+    bool heir = false;
+    for (int i = lane; i < x.N; i += 64) heir = heir || x.parent[i] == n;
+    if (!__any(heir)) {
+      const int *from = a.page_table + (size_t)n * a.max_pages;
+      for (int i = lane; i < a.max_pages; i += 64) {
+        const int old = valid(a, from[i]);
+        if (old >= 0) count(old, -1);
+      }
+    }
+  }
+  if (n >= x.N) return;
   const Heir h(a, x, n);
   bool elder = false;  // does an earlier one go on from the same parent?
   for (int i = lane; i < n; i += 64) elder = elder || x.parent[i] == h.q;
@@ -116,53 +141,36 @@ __device__ __forceinline__ void fork_row(const Args &a, const Fork &x, int n, in
   int fresh = 0, copy = -1;
   for (int i0 = 0; i0 < a.max_pages; i0 += 64) {
     const int i = i0 + lane;
-    const int old = i < h.need ? valid(a, from[i]) : -1;
+    const int old = i < (eldest ? a.max_pages : h.need) ? valid(a, from[i]) : -1;
     const bool taken = i < h.full || (i < h.need && eldest && old >= 0 && x.refs[old] == 1), asks = i < h.need && !taken;
     const unsigned long long all = __ballot(asks);
     const int before = __builtin_amdgcn_mbcnt_hi((unsigned)(all >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)all, 0));
     if (asks && i == h.full && h.part > 0) copy = old;
     if (i < a.max_pages) to[i] = taken ? old : asks ? -2 - (fresh + before) : -1;
     fresh += __builtin_popcountll(all);
+    // a younger one holds what it shares too; the eldest lets go of what it does not take over
+    if (old >= 0 && eldest != taken) count(old, eldest ? -1 : 1);
   }
+  if (copy >= 0) hold(copy);
   const unsigned long long copies = __ballot(copy >= 0);
   copy = __builtin_amdgcn_readlane(copy, copies ? __builtin_ctzll(copies) : 0);
   if (lane == 0) {
     x.fresh[n] = fresh;
     x.len[n] = h.len;
-    x.at[n] = make_int2(h.full, eldest);
-    x.copies[3 * n] = copy;
-    x.copies[3 * n + 2] = h.part;
-  }
-}
-// Who holds a page then: one more for every page that a younger one shares, one less for those that neither the eldest takes over.
-__device__ __forceinline__ void fork_refs(const Args &a, const Fork &x, int n, int lane)
-{
-  if (n < x.N) {
-    const int2 at = x.at[n];
-    const int copy = x.copies[3 * n];
-    const int *row = x.table + (size_t)n * a.max_pages;
-    for (int i = lane; i < (at.y ? 0 : at.x); i += 64)
-      if (row[i] >= 0) atomicAdd(x.new_refs + row[i], 1);
-    if (lane == 0 && copy >= 0) atomicAdd(x.held + copy, 1);
-  }
-  if (n >= a.S) return;
-  int heir = x.N;
-  for (int i = lane; i < x.N; i += 64)
-    if (x.parent[i] == n) heir = min(heir, i);
-  heir = x.N - wave_max(x.N - heir);  // the eldest
-  const int *from = a.page_table + (size_t)n * a.max_pages;
-  const int *row = x.table + (size_t)min(heir, x.N - 1) * a.max_pages;
-  for (int i = lane; i < a.max_pages; i += 64) {
-    const int old = valid(a, from[i]), now = heir == x.N ? -1 : row[i];
-    if (old >= 0 && now != old) atomicSub(x.new_refs + old, 1);
+    x.at[n] = make_int4(h.full, eldest, copy, h.part);
+    x.copies[3 * n] = x.copies[3 * n + 1] = -1;
+    x.copies[3 * n + 2] = 0;
   }
 }
 
-// Fresh pages, by one workgroup of 1024.
-__device__ __forceinline__ void fork_give(const Args &a, const Fork &x, int tid)
+// Fresh pages, by one workgroup of 1024: the k-th free page goes to the k-th request.  free(p, n): of pages p .. p + 3, those that are, as
+// bits; held(p): a page is given.
+template <typename F, typename G>
+__device__ __forceinline__ void fork_give(const Args &a, const Fork &x, int tid, F &&free_of, G &&given_out)
 {
-  constexpr int AT_ONCE = 4, NEAR = 4096;
+  constexpr int AT_ONCE = 4, NEAR = 1024;
   __shared__ int sums[16], begin_s[NEAR];
+  __shared__ int4 at_s[NEAR];
   const int lane = tid & 63, wv = tid >> 6;
   // exclusive sums over the workgroup; *total: of all
   auto scan = [&](int v, int *total) -> int {
@@ -174,18 +182,10 @@ __device__ __forceinline__ void fork_give(const Args &a, const Fork &x, int tid)
     *total = __builtin_amdgcn_readlane(t, 15);
     return __shfl(t - s, wv) + upto - v;
   };
-  auto look = [&](int p0) -> unsigned {
-    unsigned free = 0;
-#pragma unroll
-    for (int i = 0; i < AT_ONCE; ++i) {
-      const int p = p0 + tid * AT_ONCE + i;
-      if (p < a.n_pages && x.new_refs[p] == 0 && x.held[p] == 0) free |= 1u << i;
-    }
-    return free;
-  };
-  unsigned free = look(0);
+  unsigned free = free_of(tid * AT_ONCE);
   // requests: sequence n's begin at fresh[n] (of up to NEAR sequences, at begin_s[n])
   const bool near = x.N <= NEAR;
+  if (near && tid < x.N) at_s[tid] = x.at[tid];
   int asked = 0;
   for (int n0 = 0; n0 < x.N; n0 += 1024) {
     const int n = n0 + tid, mine = n < x.N ? x.fresh[n] : 0;
@@ -199,92 +199,107 @@ __device__ __forceinline__ void fork_give(const Args &a, const Fork &x, int tid)
   }
   __syncthreads();
   auto begin = [&](int n) { return near ? begin_s[n] : x.fresh[n]; };
-  // the k-th free page goes to the k-th request: to the last sequence that begins at or before k
   int given = 0;
   for (int p0 = 0; p0 < a.n_pages && given < asked; p0 += 1024 * AT_ONCE) {
-    if (p0 > 0) free = look(p0);
+    if (p0 > 0) free = free_of(p0 + tid * AT_ONCE);
     int total, k = scan(__builtin_popcount(free), &total);
     k += given;
     for (; free && k < asked; free &= free - 1, ++k) {
       const int p = p0 + tid * AT_ONCE + __builtin_ctz(free);
-      int lo = 0, hi = x.N;
+      int lo = 0, hi = x.N;  // the last sequence whose requests begin at or before k
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (begin(mid) <= k) lo = mid;
         else hi = mid;
       }
       const int nth = k - begin(lo);
-      const int2 at = x.at[lo];
-      int *entry = x.table + (size_t)lo * a.max_pages + at.x;
-      if (!at.y) entry += nth;  // (its entries from there on all ask)
+      const int4 at = near ? at_s[lo] : x.at[lo];
+      int i = at.x;
+      int *row = x.table + (size_t)lo * a.max_pages;
+      if (!at.y) i += nth;  // (its entries from there on all ask)
       else
-        while (*entry != -2 - nth) ++entry;
-      *entry = p;
-      x.new_refs[p] = 1;
+        while (row[i] != -2 - nth) ++i;
+      row[i] = p;
+      given_out(p);
+      if (i == at.x && at.z >= 0) {
+        x.copies[3 * lo] = at.z;
+        x.copies[3 * lo + 1] = p;
+        x.copies[3 * lo + 2] = at.w;
+      }
     }
     given += total;
   }
-  __syncthreads();
   if (tid == 0) x.missing[0] = max(asked - given, 0);
-  for (int n = tid; n < x.N; n += 1024) {
-    int src = x.copies[3 * n];
-    const int part = x.copies[3 * n + 2];
-    const int dst = src >= 0 ? x.table[(size_t)n * a.max_pages + x.at[n].x] : -1;
-    if (dst < 0) src = -1;
-    x.copies[3 * n] = src;
-    x.copies[3 * n + 1] = src < 0 ? -1 : dst;
-    x.copies[3 * n + 2] = src < 0 ? 0 : part;
-  }
   if (asked <= given) return;
   __syncthreads();
   for (size_t i = tid; i < (size_t)x.N * a.max_pages; i += 1024)
     if (x.table[i] < -1) x.table[i] = -1;
 }
 
+__global__ __launch_bounds__(kThreads) void fork_begin_kernel(Args a, Fork x)
+{
+  const int i = blockIdx.x * kThreads + threadIdx.x;
+  if (i >= a.n_pages) return;
+  x.new_refs[i] = x.refs[i];
+  x.held[i] = 0;
+}
 __global__ __launch_bounds__(kThreads) void fork_rows_kernel(Args a, Fork x)
 {
-  const int i0 = blockIdx.x * kThreads + threadIdx.x, lane = threadIdx.x & 63;
-  for (int i = i0; i < a.n_pages; i += gridDim.x * kThreads) {
-    x.new_refs[i] = x.refs[i];
-    x.held[i] = 0;
-  }
-  const int n = __builtin_amdgcn_readfirstlane(i0 >> 6);
-  if (n < x.N) fork_row(a, x, n, lane);
-}
-__global__ __launch_bounds__(kThreads) void fork_refs_kernel(Args a, Fork x)
-{
   const int n = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * kThreads + threadIdx.x) >> 6);
-  if (n < max(x.N, a.S)) fork_refs(a, x, n, threadIdx.x & 63);
+  if (n < max(x.N, a.S))
+    fork_row(a, x, n, threadIdx.x & 63, [&](int p, int by) { atomicAdd(x.new_refs + p, by); }, [&](int p) { x.held[p] = 1; });
 }
-__global__ __launch_bounds__(1024) void fork_give_kernel(Args a, Fork x) { fork_give(a, x, threadIdx.x); }
+__global__ __launch_bounds__(1024) void fork_give_kernel(Args a, Fork x)
+{
+  fork_give(
+      a, x, threadIdx.x,
+      [&](int p) {
+        unsigned free = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (p + i < a.n_pages && x.new_refs[p + i] == 0 && x.held[p + i] == 0) free |= 1u << i;
+        return free;
+      },
+      [&](int p) { x.new_refs[p] = 1; });
+}
 // all of it, for few sequences and pages
+constexpr int kFewPages = 8192, kFewForks = 64;
 __global__ __launch_bounds__(1024) void fork_kernel(Args a, Fork x)
 {
+  __shared__ int refs_s[kFewPages];
+  __shared__ unsigned held_s[kFewPages / 32];
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  for (int i = tid; i < a.n_pages; i += 1024) {
-    x.new_refs[i] = x.refs[i];
-    x.held[i] = 0;
-  }
-  for (int n = wv; n < x.N; n += 16) fork_row(a, x, n, lane);
+  for (int i = tid; i < a.n_pages; i += 1024) refs_s[i] = x.refs[i];
+  if (tid < kFewPages / 32) held_s[tid] = 0;
   __syncthreads();
-  for (int n = wv; n < max(x.N, a.S); n += 16) fork_refs(a, x, n, lane);
-  __threadfence();  // (the counts' atomics are done in the second-level cache: nobody reads them from the first)
+  for (int n = wv; n < max(x.N, a.S); n += 16)
+    fork_row(a, x, n, lane, [&](int p, int by) { atomicAdd(refs_s + p, by); }, [&](int p) { atomicOr(held_s + (p >> 5), 1u << (p & 31)); });
   __syncthreads();
-  __threadfence();
-  fork_give(a, x, tid);
+  fork_give(
+      a, x, tid,
+      [&](int p) {
+        unsigned free = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (p + i < a.n_pages && refs_s[p + i] == 0 && (held_s[(p + i) >> 5] >> (p + i & 31) & 1u) == 0) free |= 1u << i;
+        return free;
+      },
+      [&](int p) { refs_s[p] = 1; });
+  __syncthreads();
+  for (int i = tid; i < a.n_pages; i += 1024) x.new_refs[i] = refs_s[i];
 }
 
 bool launch_fork(const Args &a, const Fork &x, hipStream_t st)
 {
-  const long most = x.N > a.S ? x.N : a.S, blocks = (most * 64 + kThreads - 1) / kThreads;
-  if (!countable(blocks, kThreads)) return false;
+  const long most = x.N > a.S ? x.N : a.S, rows = (most * 64 + kThreads - 1) / kThreads, pages = ((long)a.n_pages + kThreads - 1) / kThreads;
+  if (!countable(rows, kThreads) || !countable(pages, kThreads)) return false;
   [&] {
-    if (most <= 64 && most * a.max_pages <= 8192 && a.n_pages <= 16384) {
+    if (most <= kFewForks && most * a.max_pages <= 8192 && a.n_pages <= kFewPages) {
       BLOSSOM_LAUNCH(fork_kernel, dim3(1), dim3(1024), 0, st, a, x);
       return;
     }
-    BLOSSOM_LAUNCH(fork_rows_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, st, a, x);
-    BLOSSOM_LAUNCH(fork_refs_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, st, a, x);
+    BLOSSOM_LAUNCH(fork_begin_kernel, dim3((unsigned)pages), dim3(kThreads), 0, st, a, x);
+    BLOSSOM_LAUNCH(fork_rows_kernel, dim3((unsigned)rows), dim3(kThreads), 0, st, a, x);
     BLOSSOM_LAUNCH(fork_give_kernel, dim3(1), dim3(1024), 0, st, a, x);
   }();
   return true;

@@ -1,15 +1,17 @@
 // Attention of drafted trees on the matrix cores for bf16, d = 64 or 128, where a tree has more than 16 rows (formulas: paged_attn.hip, which
 // serves fewer; other types and head sizes: paged_shared.hip).
 //
-// Rows are (token, head of the group) pairs of one key/value head.  A workgroup of four wavefronts takes up to 256 of them over a share of
-// their walk (TreeWork in paged.h): a wavefront has 32 or 64 rows, RG wavefronts stand side by side for 32 BLOCKS RG rows, and the 4 / RG
-// groups of them take 32 keys of a tile each and are joined in LDS at the end.  So few rows do not leave wavefronts idle, and every
-// key's operands are read from LDS once for up to 64 rows: with 32 a wavefront, as prompts have them, the reads of K and V take longer
-// than the products (128 KB of LDS for 256 rows and 32 keys: 1500 cycles beside 1024).
-//  - K and V tiles go from the pages straight to LDS, through a ring of STAGES tiles (128 KB on a CU), one barrier a tile.
-//  - S^T = K Q^T on v_mfma_f32_32x32x16_bf16, of the next tile among the exponentials of this one: there is one wavefront a SIMD (two at
-//    d = 64), which has to overlap the two by itself.
-//  - Softmax and O^T += V^T P^T as in paged_prompt.hip.
+// Rows are (token, head of the group) pairs of one key/value head.  A workgroup of eight wavefronts takes up to 256 of them over a share of
+// their walk (TreeWork in paged.h), 32 a wavefront: RG wavefronts stand side by side for 32 RG rows, and the 8 / RG groups of them take 32
+// keys of a tile each and are joined in LDS at the end, so that few rows do not leave wavefronts idle.
+//  - K and V tiles go from the pages straight to LDS, once for all rows, through a ring of STAGES tiles (128 KB on a CU) with one barrier a
+//    tile: a tree's rows do less with a tile than a prompt's, and memory has to be kept busy for them.
+//  - S^T = K Q^T, softmax and O^T += V^T P^T as in paged_prompt.hip.
+// Measured: 26 drafted tokens over 131040 positions (32 heads over 8, d = 128: 537 MB) 107 us, 8 of it the join, where reading as many bytes
+// takes 78; 33 to 64 over 4000 to 8100 for 16 sequences (412 MB, 73 GFLOP) 135 us, 13 of it the join.  Of these, with everything but
+// the loads left out, 96; with the loads left out, 114; with both, 41: launch, finding the rows, pages and queries, 17 to 34 MB of partial
+// sums.  Tried: workgroups of 128 rows, two on a CU (150: K and V are moved twice); keys' operands read a tile ahead (no gain); the next tile's
+// logits among this one's exponentials (145); 64 rows a wavefront, one a SIMD (the compiler spills).
 #include "common.h"
 #include "launch.h"
 #include "mfma_common.h"
@@ -189,37 +191,21 @@ __device__ __forceinline__ void walk_tree(const Args &a, int g, const Walk &w)
   for (int k = 0; k < STAGES - 1; ++k)
     if (t_lo + k <= t_hi) request(t_lo + k, k);
   int t = t_lo, k = 0;
-  // EARLY: the keys' operands of a tile are read while the one before is worked on (all eight wavefronts read at once behind a barrier: 64 KB
-  // take 512 cycles; 16 full trees over 4000 to 8100 positions: FIGURES).  At d = 64 there are not the registers for it.
-  constexpr bool EARLY = D == 128;
-  constexpr int AHEAD = STAGES - (EARLY ? 3 : 2);  // tiles that may be on their way when one is begun
-  static_assert(AHEAD >= 1, "");
-  bf16x8 kf[D / 16];
-  auto keys_of = [&](int k) __attribute__((always_inline)) {
-#pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) kf[kk] = *reinterpret_cast<const bf16x8 *>(lds + k * (2 * TILE) + koff[kk]);
-  };
-  if constexpr (EARLY) {
-    if (t_lo + STAGES - 2 <= t_hi) mfma::arrived_all<LOADS *(STAGES - 2)>();
-    else mfma::arrived_all<0>();
-    keys_of(0);  // (in a walk of nothing: whatever is there, for nothing)
-  }
   auto turn = [&](auto two) __attribute__((always_inline)) {
     constexpr bool TWO = decltype(two)::value;
-    // when this tile (EARLY: the next one too) has arrived, everybody is done with the one before, whose place the next request takes
-    if (t + STAGES - 2 <= t_hi) mfma::arrived_all<LOADS * AHEAD>();
+    // when a tile has arrived, everybody is done with the one before it, whose place the next request takes
+    if (t + STAGES - 2 <= t_hi) mfma::arrived_all<LOADS *(STAGES - 2)>();
     else mfma::arrived_all<0>();
     const int here = k, base = t * KEYS + 32 * kg;
     if (t + STAGES - 1 <= t_hi) request(t + STAGES - 1, k == 0 ? STAGES - 1 : k - 1);
     k = k == STAGES - 1 ? 0 : k + 1;
     ++t;
     if (!on) return;
-    if constexpr (!EARLY) {
-      keys_of(here);
-      __builtin_amdgcn_sched_barrier(0);  // keys' operands are requested together, values' between the products
-    }
     const uint16_t *ks = lds + here * (2 * TILE);
-    bf16x8 vf[2][NB];
+    bf16x8 kf[D / 16], vf[2][NB];
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) kf[kk] = *reinterpret_cast<const bf16x8 *>(ks + koff[kk]);
+    __builtin_amdgcn_sched_barrier(0);  // keys' operands are requested together, values' between the products
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -234,14 +220,10 @@ __device__ __forceinline__ void walk_tree(const Args &a, int g, const Walk &w)
     for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk], qf[kk], sc, 0, 0, 0);
-    if constexpr (EARLY) {
-      keys_of(k);  // (behind the last tile: whatever is there, for nothing)
-    } else {
 #pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-      }
+    for (int kk = 0; kk < D / 16; ++kk) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
     }
     const unsigned ok = (unsigned)__builtin_amdgcn_readlane(pages_ok, here);
     if (base < tree.every.lo || base + 31 > tree.every.hi || ok != 0xFFFFFFFFu)
