@@ -18,9 +18,9 @@ namespace beam {
 
 namespace {
 
-constexpr int kThreads = 256;  // of the merge
-constexpr int kWaves = 8;      // of a run
-constexpr int kGroups = 64;   // groups of 4 lanes, whose best give a bound that K reach
+constexpr int kWaves = 8;     // of a run
+constexpr int kFewCandidates = 1024;  // in the lists of a history: four a thread of the merge's small workgroup
+constexpr int kGroups = 64;   // groups of a run's lanes, whose largest logits give a bound that K reach
 typedef unsigned long long u64;
 
 // logits and items as one number: the larger logit first, then the lower item.  0: none.
@@ -207,12 +207,12 @@ __device__ __forceinline__ float wave_max(float x)
 // Workgroup (row, run) takes `subs` pieces of the row, its wavefronts one after another: of 64 * LD * 16 bytes each, the next on its way
 // while one is worked on.  A lane keeps the sum and the largest of its logits.  When the run is done, the K-th largest of 64 groups' largest
 // bounds what may be among the K best: the few lanes that reach it have their loads looked at again.
-template <typename T, int LD>
+template <typename T, int LD, bool TABLE>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(4))) void rows_kernel(Args a)
 {
   typedef Piece<T> P;
   constexpr int VEC = P::N, SUB = 64 * LD * VEC, THREADS = 64 * kWaves, FOUND = kWaves * kHold;
-  constexpr bool TABLE = sizeof(T) == 2;
+  static_assert(!TABLE || sizeof(T) == 2, "");
   struct __attribute__((packed, aligned(sizeof(T)))) Any { uint4 v; };  // (rows begin at any element)
   __shared__ u64 held[kWaves][kHold];
   __shared__ double table[TABLE ? Table::kSize : 1];
@@ -426,39 +426,46 @@ __device__ __forceinline__ int rank_of(const u64 *p, const u64 *k, const unsigne
   return r + __shfl_xor(r, 2);
 }
 
-// One history.  With few candidates all are looked at: those that reach the K-th best of 64 groups' best are put in order.  Otherwise lists are
-// chosen by their first elements: element j of the list whose first is the r-th of all has r + j before it.
-__global__ __launch_bounds__(kThreads) void merge_kernel(Args a)
+// One history: candidates that reach the K-th best of 64 groups' best are put in order.  Candidates are all that the lists hold or, of more than
+// four a thread, those of the K lists with the best first elements.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void merge_kernel(Args a)
 {
-  constexpr int PAIRS = kMost * (kMost + 1) / 2;
-  constexpr int FEW = 4;  // candidates of a thread
-  static_assert(FEW * kThreads <= PAIRS, "");
+  constexpr int FEW = 4, MOST = FEW * THREADS;  // candidates of a thread, and of all
+  constexpr bool CHOOSE = MOST >= kMost * kMost;  // (fewer threads are for fewer candidates)
+  static_assert(!CHOOSE || kLists <= THREADS, "");
   __shared__ double lse_s[kMost], score_s[kMost];
-  __shared__ u64 p_s[PAIRS], k_s[PAIRS], group_s[kGroups], head_s[kLists], logit_s[kLists];
-  __shared__ short chosen_s[kMost], near_s[kLists];
-  __shared__ unsigned char w_s[PAIRS], beam_s[kLists], ended_s[kMost];
-  __shared__ int count_s[2];
+  __shared__ u64 p_s[MOST], k_s[MOST], group_s[THREADS / 64][64];
+  __shared__ short chosen_s[kMost];
+  __shared__ unsigned char w_s[MOST], ended_s[kMost];
+  __shared__ int count_s;
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), b = blockIdx.x;
   const int L = a.W * a.lists;
   const size_t row0 = (size_t)b * a.W;
   const u64 *lists = a.lists_of + row0 * a.lists * a.K;
-  const bool few = L * a.K <= FEW * kThreads;
+  const bool few = !CHOOSE || L * a.K <= MOST;
+  // Candidate tid + i THREADS: each list is turned round by another number of places (see bound_of).
+  auto pick = [&](int i) -> int {
+    const unsigned c = tid + i * THREADS, K = a.K, l = c / K;
+    return (int)(l * K + (c + l + (l * K >> 6)) % K); 
+  };
   // (requested at once: candidates or first elements, sums, scores)
-  u64 first[FEW];
+  u64 key[FEW];
+  int from[FEW];
 #pragma unroll
   for (int i = 0; i < FEW; ++i) {
-    const int c = tid + i * kThreads;
-    first[i] = c < (few ? L * a.K : L) ? lists[few ? c : (size_t)c * a.K] : 0;
+    from[i] = few ? pick(i) : tid + i * THREADS;
+    key[i] = from[i] < (few ? L * a.K : L) ? lists[few ? from[i] : (size_t)from[i] * a.K] : 0;
   }
   if (tid < a.W) {
     score_s[tid] = (double)a.score[row0 + tid];
     ended_s[tid] = a.ended ? a.ended[row0 + tid] : 0;
   }
-  if (tid < 2) count_s[tid] = 0;
+  if (tid == 0) count_s = 0;
   // ---- log sum exp of each beam's row: as many lanes a beam as it has runs ----
   int per = 1;
   while (per < a.lists && per < 64) per *= 2;
-  for (int w0 = wv * (64 / per); w0 < a.W; w0 += 4 * (64 / per)) {
+  for (int w0 = wv * (64 / per); w0 < a.W; w0 += THREADS / per) {
     const int w = w0 + lane / per, at = lane % per;
     const double2 *st = a.stats + (row0 + min(w, a.W - 1)) * a.lists;
     double m = -INFINITY, s = 0.0;
@@ -476,7 +483,7 @@ __global__ __launch_bounds__(kThreads) void merge_kernel(Args a)
     if (at == 0 && w < a.W) lse_s[w] = top == INFINITY ? INFINITY : top + log(s);
   }
   __syncthreads();
-  // a key of a beam's j-th candidate as a place in the order; none: 0
+  // a key of a beam's candidate as a place in the order (only: the beam's first); none: 0
   auto place = [&](int w, bool only, u64 &key) -> u64 {
     double to;
     if (ended_s[w]) {  // goes on in one way
@@ -487,81 +494,83 @@ __global__ __launch_bounds__(kThreads) void merge_kernel(Args a)
     }
     return to > -INFINITY ? ordered(to) : 0;  // (a NaN neither)
   };
-  const int cells = few ? a.lists * a.K : a.lists;  // of `first`, a beam's
+  // The K-th best of 64 groups' best.  Groups are a lane's of all wavefronts, in which first, second, .. elements of many lists meet: then about
+  // as many candidates reach the bound as groups do (without: one beam, 32 lists of 32: 27 us, so 7.6).
+  auto bound_of = [&](u64 top) -> u64 {
+    group_s[wv][lane] = top;
+    __syncthreads();
+    u64 mine = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) mine = max(mine, group_s[w][lane]);
+    int rank = 0;
+#pragma unroll 8
+    for (int i = 0; i < 64; ++i) {
+      const u64 o = (u64)(unsigned)__builtin_amdgcn_readlane((int)(mine >> 32), i) << 32 | (unsigned)__builtin_amdgcn_readlane((int)mine, i);
+      rank += o > mine || (o == mine && i < lane);
+    }
+    const int at = __builtin_ctzll(__ballot(rank == a.K - 1));
+    const u64 bound = (u64)(unsigned)__builtin_amdgcn_readlane((int)(mine >> 32), at) << 32 | (unsigned)__builtin_amdgcn_readlane((int)mine, at);
+    __syncthreads();
+    return max(bound, 1ull);
+  };
+  auto put = [&](u64 p, u64 k, int w) __attribute__((always_inline)) {
+    const int to = atomicAdd(&count_s, 1);
+    p_s[to] = p; k_s[to] = k; w_s[to] = (unsigned char)w;
+  };
+  int n_lists = 0;
+  if constexpr (CHOOSE) {
+    if (!few) {
+      const int w = min((unsigned)tid / (unsigned)a.lists, (unsigned)a.W - 1);
+      const u64 p = tid < L ? place(w, tid == w * a.lists, key[0]) : 0;
+      const u64 bound = bound_of(p);
+      if (tid < L) {
+        if (p >= bound) {
+          const int to = atomicAdd(&count_s, 1);
+          p_s[to] = p; k_s[to] = key[0]; w_s[to] = (unsigned char)w;
+          // (which list it is: where the places of the last candidates will be)
+          reinterpret_cast<int *>(p_s + MOST - kLists / 2)[to] = tid;
+        }
+      }
+      __syncthreads();
+      const int n = count_s;
+      for (int i0 = 0; i0 < n; i0 += THREADS / 4) {
+        const int i = i0 + (tid >> 2), r = rank_of(p_s, k_s, w_s, n, i, tid);
+        if (i < n && r < a.K && (tid & 3) == 0) chosen_s[r] = (short)reinterpret_cast<int *>(p_s + MOST - kLists / 2)[i];
+      }
+      n_lists = min(n, a.K);
+      __syncthreads();
+      if (tid == 0) count_s = 0;
+    }
+  }
+  // ---- the candidates ----
   u64 top = 0, at[FEW];
 #pragma unroll
   for (int i = 0; i < FEW; ++i) {
-    const int c = tid + i * kThreads;
     at[i] = 0;
-    if (c >= a.W * cells) continue;
-    const int w = (unsigned)c / (unsigned)cells;
-    at[i] = place(w, c == w * cells, first[i]);
+    if (!few) from[i] = pick(i);
+    const int c = from[i];
+    if (few) {
+      if (c >= L * a.K) continue;
+      const int w = (unsigned)c / (unsigned)(a.lists * a.K);
+      at[i] = place(w, c == w * a.lists * a.K, key[i]);
+    } else {
+      if (c >= n_lists * a.K) continue;
+      const int r = (unsigned)c / (unsigned)a.K, j = c - r * a.K, l = chosen_s[r], w = (unsigned)l / (unsigned)a.lists;
+      key[i] = r + j < a.K ? lists[(size_t)l * a.K + j] : 0;  // (r + j are before it)
+      at[i] = r + j < a.K ? place(w, j == 0 && l == w * a.lists, key[i]) : 0;
+    }
     top = max(top, at[i]);
-    if (!few) {
-      head_s[c] = at[i];
-      logit_s[c] = first[i];
-      beam_s[c] = (unsigned char)w;
-    }
   }
-  top = max(top, (u64)__shfl_xor((long long)top, 1));
-  top = max(top, (u64)__shfl_xor((long long)top, 2));
-  if ((lane & 3) == 0) group_s[16 * wv + (lane >> 2)] = top;
-  __syncthreads();
-  u64 bound;
-  {
-    const u64 mine = group_s[lane];
-    int rank = 0;
-#pragma unroll 8
-    for (int i = 0; i < kGroups; ++i) {
-      const u64 o = group_s[i];
-      rank += o > mine || (o == mine && i < lane);
-    }
-    bound = max(group_s[__builtin_ctzll(__ballot(rank == a.K - 1))], 1ull);
-  }
-  auto put = [&](u64 p, u64 k, int w) __attribute__((always_inline)) {
-    const int to = atomicAdd(&count_s[1], 1);
-    p_s[to] = p; k_s[to] = k; w_s[to] = (unsigned char)w;
-  };
-  if (few) {
+  const u64 bound = bound_of(top);
 #pragma unroll
-    for (int i = 0; i < FEW; ++i)
-      if (at[i] >= bound) put(at[i], first[i], (unsigned)(tid + i * kThreads) / (unsigned)cells);
-  } else {
-    for (int l = tid; l < L; l += kThreads)
-      if (head_s[l] >= bound) near_s[atomicAdd(&count_s[0], 1)] = (short)l;
-    __syncthreads();
-    const int n_near = count_s[0], n_lists = min(n_near, a.K);
-    for (int i = tid; i < n_near; i += kThreads) {
-      const int l = near_s[i], w = beam_s[l];
-      const u64 p = head_s[l], k = logit_s[l];
-      int r = 0;
-#pragma unroll 4
-      for (int j = 0; j < n_near; ++j) {
-        const int o = near_s[j];
-        r += before(head_s[o], beam_s[o], logit_s[o], p, w, k);
-      }
-      if (r < a.K) chosen_s[r] = (short)l;
-    }
-    __syncthreads();
-    const int last = n_lists == a.K ? chosen_s[a.K - 1] : -1;
-    for (int i = tid; i < n_lists * a.K; i += kThreads) {
-      const int r = i / a.K, j = i - r * a.K;
-      if (r + j >= a.K) continue;
-      const int l = chosen_s[r], w = beam_s[l];
-      u64 p = head_s[l], k = logit_s[l];
-      if (j > 0) {
-        if (ended_s[w]) continue;
-        k = lists[(size_t)l * a.K + j];
-        p = place(w, false, k);
-        if (p == 0 || (last >= 0 && l != last && !before(p, w, k, head_s[last], beam_s[last], logit_s[last]))) continue;
-      }
-      put(p, k, w);
-    }
+  for (int i = 0; i < FEW; ++i) {
+    const int c = from[i];
+    if (at[i] >= bound) put(at[i], key[i], few ? (unsigned)c / (unsigned)(a.lists * a.K) : (unsigned)chosen_s[(unsigned)c / (unsigned)a.K] / (unsigned)a.lists);
   }
   __syncthreads();
-  const int n = count_s[1];
+  const int n = count_s;
   const size_t out = (size_t)b * a.K;
-  for (int i0 = 0; i0 < n; i0 += kThreads / 4) {
+  for (int i0 = 0; i0 < n; i0 += THREADS / 4) {
     const int i = i0 + (tid >> 2);
     const int r = rank_of(p_s, k_s, w_s, n, i, tid);
     if (i >= n || r >= a.K || (tid & 3)) continue;
@@ -571,7 +580,7 @@ __global__ __launch_bounds__(kThreads) void merge_kernel(Args a)
     a.out_score[out + r] = (float)score_of(p_s[i]);
     if (a.out_ended) a.out_ended[out + r] = item == a.eos || ended_s[w];
   }
-  for (int r = n + tid; r < a.K; r += kThreads) {
+  for (int r = n + tid; r < a.K; r += THREADS) {
     a.parent[out + r] = a.token[out + r] = -1;
     a.out_score[out + r] = -INFINITY;
     if (a.out_ended) a.out_ended[out + r] = 0;
@@ -580,17 +589,23 @@ __global__ __launch_bounds__(kThreads) void merge_kernel(Args a)
 
 namespace {
 
-constexpr int kLoads = 4;
-int piece(int dtype) { return 64 * kLoads * (dtype == 0 ? 4 : 8); }
+long piece(int dtype, int loads) { return 64l * loads * (dtype == 0 ? 4 : 8); }
 
 }  // namespace
 
 void plan(Args &a)
 {
-  const long rows = (long)a.B * a.W, pieces = ((long)a.V + piece(a.dtype) - 1) / piece(a.dtype);
-  const long want = (1024 + rows - 1) / rows, most = kLists / a.W, whole = (pieces + kWaves - 1) / kWaves;
-  long lists = whole < want ? whole : want;
+  // Runs: one workgroup a CU's two places, or one a row (2048, 1024 and 512 workgroups for 512 rows of 152063: 52, 49 and 39 us); no more
+  // than the merge's small workgroup takes, unless runs become long (8 rows of 150001, K = 8: merge 6 us with 16 lists a row, 10 with 37).
+  // Four loads a lane and piece of bf16, two of fp32 (400000 logits, K = 32: 9 us, four 23, one 10; 512 rows of 152063: 85, 84, 99); one in
+  // short runs: then a lane's few logits are not worth a table either (1024 rows of 5000: 13 us for 19).
+  const long rows = (long)a.B * a.W, small = kWaves * piece(a.dtype, 1), large = kWaves * piece(a.dtype, 4);
+  const long light = a.W * a.K <= kFewCandidates ? kFewCandidates / (a.W * a.K) : 1;
+  long lists = (512 + rows - 1) / rows, most = a.V <= 8 * large * light ? light : kLists / a.W;
+  if (most > (a.V + small - 1) / small) most = (a.V + small - 1) / small;
   if (lists > most) lists = most;
+  a.loads = (a.V + lists - 1) / lists <= 3 * small ? 1 : a.dtype == 0 ? 2 : 4;
+  const long pieces = (a.V + piece(a.dtype, a.loads) - 1) / piece(a.dtype, a.loads);
   a.subs = (int)((pieces + lists - 1) / lists);
   a.lists = (int)((pieces + a.subs - 1) / a.subs);
 }
@@ -599,11 +614,15 @@ bool launch(const Args &a, hipStream_t st)
 {
   const long blocks = (long)a.B * a.W * a.lists;
   if (blocks * 64 * kWaves >= 1l << 32) return false;
-  const dim3 grid((unsigned)blocks), block(64 * kWaves);
   [&] {
-    if (a.dtype == 0) BLOSSOM_LAUNCH((rows_kernel<float, kLoads>), grid, block, 0, st, a);
-    else BLOSSOM_LAUNCH((rows_kernel<bf16_t, kLoads>), grid, block, 0, st, a);
-    BLOSSOM_LAUNCH(merge_kernel, dim3((unsigned)a.B), dim3(kThreads), 0, st, a);
+    auto rows = [&](auto kernel) { BLOSSOM_LAUNCH(kernel, dim3((unsigned)blocks), dim3(64 * kWaves), 0, st, a); };
+    if (a.dtype == 0 && a.loads > 1) rows(rows_kernel<float, 2, false>);
+    else if (a.dtype == 0) rows(rows_kernel<float, 1, false>);
+    else if (a.loads > 1) rows(rows_kernel<bf16_t, 4, true>);
+    else rows(rows_kernel<bf16_t, 1, false>);
+    if (launch_failed()) return;
+    if (a.W * a.lists * a.K <= kFewCandidates) BLOSSOM_LAUNCH((merge_kernel<256>), dim3((unsigned)a.B), dim3(256), 0, st, a);
+    else BLOSSOM_LAUNCH((merge_kernel<1024>), dim3((unsigned)a.B), dim3(1024), 0, st, a);
   }();
   return true;
 }
