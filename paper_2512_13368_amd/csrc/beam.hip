@@ -20,7 +20,6 @@ namespace {
 
 constexpr int kWaves = 8;     // of a run
 constexpr int kFewCandidates = 1024;  // in the lists of a history: four a thread of the merge's small workgroup
-constexpr int kGroups = 64;   // groups of a run's lanes, whose largest logits give a bound that K reach
 typedef unsigned long long u64;
 
 // logits and items as one number: the larger logit first, then the lower item.  0: none.
@@ -217,7 +216,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(4))
   __shared__ u64 held[kWaves][kHold];
   __shared__ double table[TABLE ? Table::kSize : 1];
   __shared__ double sum_s[kWaves];
-  __shared__ float top_s[kWaves], group_s[kGroups];
+  __shared__ float top_s[kWaves], group_s[kWaves][64];
   __shared__ int count_s[2], have_s[kWaves];
   __shared__ unsigned bound_s;
   __shared__ unsigned short lane_s[THREADS];
@@ -314,14 +313,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(4))
     sum_s[wv] = s;
     top_s[wv] = m;
   }
-  // ---- the bound: by groups of kWaves lanes ----
-  float group = lane_top;
-#pragma unroll
-  for (int o = 1; o < kWaves; o *= 2) group = fmaxf(group, __shfl_xor(group, o));
-  if (lane % kWaves == 0) group_s[(64 / kWaves) * wv + lane / kWaves] = group;
+  // ---- the bound: by groups of a lane of every wavefront (groups of neighbours leave none where a run has few logits: 43 rows of 407 with
+  // K = 17, bf16: 24 us with the merge, so 14) ----
+  group_s[wv][lane] = lane_top;
   __syncthreads();
   if (wv == 0) {
-    const float mine = group_s[lane];
+    float mine = lane_top;
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) mine = fmaxf(mine, group_s[w][lane]);
     const unsigned place = (ordered(mine) & ~63u) | lane;  // (but for the last six bits, the lane's in the order)
     int rank = 0;
 #pragma unroll 8
@@ -595,15 +594,20 @@ long piece(int dtype, int loads) { return 64l * loads * (dtype == 0 ? 4 : 8); }
 
 void plan(Args &a)
 {
-  // Runs: one workgroup a CU's two places, or one a row (2048, 1024 and 512 workgroups for 512 rows of 152063: 52, 49 and 39 us); no more
-  // than the merge's small workgroup takes, unless runs become long (8 rows of 150001, K = 8: merge 6 us with 16 lists a row, 10 with 37).
+  // Runs: a workgroup for each of the CUs' two places, or as comes near (2048, 1024 and 512 workgroups for 512 rows of 152063: 52, 49 and 39
+  // us; 508 and 762 for 254 rows of 108488: 26 and 30 with the merge); no more than the merge's small workgroup takes, unless runs become long (8 rows of 150001, K = 8: merge 6 us with 16 lists a row, 10 with 37).
   // Four loads a lane and piece of bf16, two of fp32 (400000 logits, K = 32: 9 us, four 23, one 10; 512 rows of 152063: 85, 84, 99); one in
   // short runs: then a lane's few logits are not worth a table either (1024 rows of 5000: 13 us for 19).
   const long rows = (long)a.B * a.W, small = kWaves * piece(a.dtype, 1), large = kWaves * piece(a.dtype, 4);
   const long light = a.W * a.K <= kFewCandidates ? kFewCandidates / (a.W * a.K) : 1;
-  long lists = (512 + rows - 1) / rows, most = a.V <= 8 * large * light ? light : kLists / a.W;
+  long lists = 1, most = a.V <= 8 * large * light ? light : kLists / a.W;
   if (most > (a.V + small - 1) / small) most = (a.V + small - 1) / small;
-  if (lists > most) lists = most;
+  // (a round of 512 workgroups takes as long as its logits and 30000 more)
+  for (long n = 2, best = 0; n <= most && (n - 1) * rows < 1024; ++n) {
+    const auto cost = [&](long of) { return (of * rows + 511) / 512 * ((a.V + of - 1) / of + 30000); };
+    if (!best) best = cost(1);
+    if (cost(n) < best) best = cost(n), lists = n;
+  }
   a.loads = (a.V + lists - 1) / lists <= 3 * small ? 1 : a.dtype == 0 ? 2 : 4;
   const long pieces = (a.V + piece(a.dtype, a.loads) - 1) / piece(a.dtype, a.loads);
   a.subs = (int)((pieces + lists - 1) / lists);

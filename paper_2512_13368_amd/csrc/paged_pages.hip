@@ -21,8 +21,8 @@ __device__ __forceinline__ int page_of(const Args &a, const int *table, int pos)
 
 // Rows past + keep[i] move to past + i, i ascending.  A thread owns 16 bytes of every row (of K or of V, of one key/value head), so what it
 // reads later never lies where it wrote: keep[j] >= j > i for j > i.  No thread waits for another.  64 entries at a time, one a lane, whose
-// pages are looked up together
-// (128 trees of 33 to 64 tokens, up to 12 kept: 8.1 us, where a copy of as many rows would take 1; a chain of loads, length to page to row; looked up one by one 11.1).
+// pages are looked up together (128 trees of 33 to 64 tokens, up to 12 kept: 8.1 us, one by one 11.1, where a copy of as many rows would take
+// 1; the rest is a chain of loads, length to page to row).
 __global__ __launch_bounds__(kThreads) void accept_kernel(Args a, Accept x, int row_chunks)
 {
   constexpr int AHEAD = 8;
