@@ -297,10 +297,14 @@ struct Tree {
     past = max(raw_len, 0) - n;
     shown = min(min(n, kDrafts), past > a.cap - kDrafts ? a.cap - past : kDrafts);
     any = {first(a, 0), past + shown - 1};
-    every = {first(a, min(n, kDrafts) - 1), min(past, a.cap) - 1};
+    every = {first(a, min(n - 1, kDrafts)), min(past, a.cap) - 1};  // (a token behind the 64th may see all of these)
   }
   // the first key that a token sees at this depth
-  __device__ __forceinline__ int first(const Args &a, int depth) const { return max(max(past, 0) + depth - a.window + 1, 0); }
+  __device__ __forceinline__ int first(const Args &a, int depth) const
+  {
+    if (a.window == 0x7FFFFFFF) return 0;
+    return (int)min(max((long)max(past, 0) + depth - a.window + 1, 0l), 0x7FFFFFFFl);
+  }
 };
 
 // One token's keys, 32 at a time.
@@ -395,6 +399,11 @@ struct TreeWork {
       if (k < 64) {
         const int tiles = __builtin_amdgcn_readlane(x.tiles, k), row_tiles = __builtin_amdgcn_readlane(x.row_tiles, k);
         const int in = at - (__builtin_amdgcn_readlane(upto, k) - tiles * row_tiles), tile = (unsigned)in / (unsigned)tiles;
+        const int to = unit + __builtin_amdgcn_readlane(row_upto, k) - row_tiles + tile;
+        if ((unsigned)tile >= (unsigned)row_tiles || (unsigned)to >= (unsigned)a.slots) {  // (cu_seqlens does not ascend)
+          at = end;
+          return w;
+        }
         w.s = s0 + k;
         w.tok0 = __builtin_amdgcn_readlane(x.cu, k);
         w.count = __builtin_amdgcn_readlane(x.n, k);
@@ -402,7 +411,7 @@ struct TreeWork {
         w.row0 = tile * rows;
         w.from = in - tile * tiles;
         w.tiles = min(end - at, tiles - w.from);
-        if (w.tiles < tiles) w.slot = unit + __builtin_amdgcn_readlane(row_upto, k) - row_tiles + tile;
+        if (w.tiles < tiles) w.slot = to;
         at += w.tiles;
         return w;
       }

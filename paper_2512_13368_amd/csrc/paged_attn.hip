@@ -651,7 +651,7 @@ void plan_tree(Args &a)
     waves = 4096 / shared_waves(row_bytes);
   }
   const long base = rows / a.tree_rows + a.S;  // row tiles, at most
-  const long tiles = ((long)(a.window < a.cap ? a.window + kDrafts + keys - 1 : a.cap) + keys - 1) / keys;
+  const long tiles = ((a.window < a.cap ? (long)a.window + kDrafts + keys - 1 : a.cap) + keys - 1) / keys;
   a.parts = waves / a.G;
   if (tiles < 2 * least || base * tiles > 1 << 30 || 3 * (rows / a.tree_rows > a.S ? rows / a.tree_rows : a.S) > 2 * a.parts) a.parts = 0;
   a.units = (int)(a.parts ? a.parts : base);

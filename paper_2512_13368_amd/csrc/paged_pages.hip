@@ -293,7 +293,7 @@ __global__ __launch_bounds__(1024) void fork_kernel(Args a, Fork x)
 bool launch_fork(const Args &a, const Fork &x, hipStream_t st)
 {
   const long most = x.N > a.S ? x.N : a.S, rows = (most * 64 + kThreads - 1) / kThreads, pages = ((long)a.n_pages + kThreads - 1) / kThreads;
-  if (!countable(rows, kThreads) || !countable(pages, kThreads)) return false;
+  if (!countable(rows, kThreads) || a.n_pages > 1 << 30) return false;  // (pages are counted past the last)
   [&] {
     if (most <= kFewForks && most * a.max_pages <= 8192 && a.n_pages <= kFewPages) {
       BLOSSOM_LAUNCH(fork_kernel, dim3(1), dim3(1024), 0, st, a, x);

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from paged_util import DTYPES, check, guarded
+from paged_util import DTYPES, LSE_TOL, TOL, check, guarded
 from paper_2512_13368_amd import binding as B
 from test_gpu_paged import rope, rotated
 from tree_util import TreeCache, tree_masks
@@ -86,6 +86,24 @@ def test_tree_of_more_than_64_tokens(dtype, d):
     check(O, lse, *c.want_tree(Q), dtype)
 
 
+@pytest.mark.parametrize("dtype,d,H", [("fp32", 32, 2), ("bf16", 64, 2), ("bf16", 128, 2), ("bf16", 32, 1)])
+def test_tree_windows_of_tokens_that_see_64_others(dtype, d, H):
+    # (the 65th and later stand 64 positions behind the history, one more than any of the first 64 can)
+    for window in range(80, 80 + 33):
+        c = TreeCache([66 + 200, 3], H, 1, d, 16, dtype, new=[66, 1], masks=[[(1 << 64) - 1] * 66, [1]], window=window, seed=4)
+        if window % 8 == 0:
+            Q, O, lse = run_tree(c)
+            check(O, lse, *c.want_tree(Q), dtype)
+            continue
+        Q = c.normal(c.T, H, d)
+        _, O, lse = run_tree(c, Q=Q)
+        for t in (0, 63, 64, 65):
+            for h in range(H):
+                o, x = c.attend_tree(Q[t, h], 0, t, h)
+                assert float((O[t, h].double().cpu() - o).abs().max()) <= 2 * TOL[dtype] * float(o.pow(2).mean().sqrt() + o.abs().max())
+                assert abs(float(lse[t, h]) - x) <= LSE_TOL * (1 + abs(x)), f"window {window} token {t}"
+
+
 @pytest.mark.parametrize("dtype,d,past", [("fp32", 64, 9000), ("bf16", 64, 20011), ("bf16", 128, 30000), ("fp32", 128, 5000), ("bf16", 8, 12000)])
 def test_tree_long_histories_split_and_joined(dtype, d, past):
     c = TreeCache([past, 77, 0, past // 3], 4, 2, d, 32, dtype, new=[21, 30, 0, 1], seed=5)
@@ -103,6 +121,13 @@ def test_tree_capacity_and_short_lengths(dtype, d):
     c.kv_len = [60, 64, -7, 1]
     Q, O, lse = run_tree(c)
     check(O, lse, *c.want_tree(Q), dtype)
+    # (the largest lengths: all of the history, or nothing)
+    c = TreeCache([50] * 4, 2, 1, d, 16, dtype, new=[20, 30, 20, 3], max_len=50, seed=9)
+    c.kv_len = [2**31 - 1, 2**31 - 30, 2**31 - 1, 50]
+    for window in (0, 5, 2**31 - 2):
+        c.window = c.p.window = window
+        Q, O, lse = run_tree(c)
+        check(O, lse, *c.want_tree(Q), dtype)
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])

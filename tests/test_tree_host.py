@@ -111,11 +111,12 @@ def test_outputs_that_are_inputs_are_refused(lib):
 
 
 def test_calls_of_more_threads_than_a_launch_counts(lib):
-    assert tree(lib, params(T=1 << 22, H=64, G=64, max_pages=1)) == -2
+    assert tree(lib, params(T=1 << 24, H=64, G=64, max_pages=1, dtype=0)) == -2
     assert append(lib, params(T=1 << 28, max_pages=1)) == -2
     assert accept(lib, params(S=1 << 24)) == -2
     assert copy(lib, params(), count=1 << 24) == -2
     assert fork(lib, params(max_pages=1), N=1 << 26) == -2
+    assert fork(lib, params(n_pages=(1 << 30) + 1)) == -2
 
 
 BEAM_BAD = [(dict(B=0), -2), (dict(W=0), -2), (dict(K=0), -2), (dict(V=0), -2), (dict(W=65), -3), (dict(K=65), -3), (dict(dtype=2), -3),
