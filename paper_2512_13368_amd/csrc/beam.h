@@ -20,7 +20,7 @@ struct Args {
   int *parent, *token;         // [B, K]
   float *out_score;
   unsigned char *out_ended;    // or nullptr
-  int loads, subs, lists;      // 16-byte loads of a lane and piece, pieces of a run, runs of a row
+  int loads, subs, lists;      // 16-byte loads of a lane and piece, pieces of a run, runs of a row (0: a history is done by one workgroup)
   double2 *stats;              // [B W, lists] largest logit and sum of exponentials, in the workspace
   unsigned long long *lists_of;  // [B W, lists, K] best logits with their items, there too
 };

@@ -6,6 +6,7 @@
 // which is one order whatever the workgroups do.
 //   rows_kernel   a workgroup takes a run of a row: its sum, and its K best logits
 //   merge_kernel  a workgroup a history: sums joined, then the K best of the runs' lists
+//   few_kernel    both, for histories of few logits
 #include "beam.h"
 
 #include <type_traits>
@@ -19,6 +20,7 @@ namespace beam {
 namespace {
 
 constexpr int kWaves = 8;     // of a run
+constexpr int kFewLogits = 8192;  // of a history that one workgroup takes by itself
 constexpr int kFewCandidates = 1024;  // in the lists of a history: four a thread of the merge's small workgroup
 typedef unsigned long long u64;
 
@@ -425,6 +427,110 @@ __device__ __forceinline__ int rank_of(const u64 *p, const u64 *k, const unsigne
   return r + __shfl_xor(r, 2);
 }
 
+// log sum exp of W beams' rows from the `lists` sums of each: as many lanes a beam as it has sums.
+template <int THREADS>
+__device__ __forceinline__ void join_sums(const double2 *stats, int W, int lists, int wv, int lane, double *lse_s)
+{
+  int per = 1;
+  while (per < lists && per < 64) per *= 2;
+  for (int w0 = wv * (64 / per); w0 < W; w0 += THREADS / per) {
+    const int w = w0 + lane / per, at = lane % per;
+    const double2 *st = stats + min(w, W - 1) * lists;
+    double m = -INFINITY, s = 0.0;
+    for (int i = at; i < lists; i += per) {
+      const double2 x = st[i];
+      if (!(x.x > -INFINITY)) continue;
+      const double top = fmax(m, x.x);
+      s = (m > -INFINITY ? s * exp_from(m, top) : 0.0) + x.y * exp_from(x.x, top);
+      m = top;
+    }
+    double top = m;
+    for (int o = per / 2; o >= 1; o >>= 1) top = fmax(top, __shfl_xor(top, o));
+    s = m > -INFINITY ? s * exp_from(m, top) : 0.0;
+    for (int o = per / 2; o >= 1; o >>= 1) s += __shfl_xor(s, o);
+    if (at == 0 && w < W) lse_s[w] = top == INFINITY ? INFINITY : top + log(s);
+  }
+}
+
+// A key of a beam's candidate as a place in the order (only: the beam's first, and what it goes on as if it has ended); none: 0.
+__device__ __forceinline__ u64 place_of(double score, double lse, bool ended, bool only, int eos, u64 &key)
+{
+  double to;
+  if (ended) {  // goes on in one way
+    key = key_of(0.0f, eos);
+    to = only ? score : -INFINITY;
+  } else {
+    to = key == 0 ? -INFINITY : score + ((double)logit_of((unsigned)(key >> 32)) - lse);
+  }
+  return to > -INFINITY ? ordered(to) : 0;  // (a NaN neither)
+}
+
+// The K-th best of 64 groups' best.  Groups are a lane's of all wavefronts, in which first, second, .. elements of many lists meet: then about
+// as many candidates reach the bound as groups do (without: one beam, 32 lists of 32: 27 us, so 7.6).
+// One wavefront finds it: of 16 on a CU, four to a SIMD, each would wait for the other three.
+template <int WAVES>
+__device__ __forceinline__ u64 bound_of(u64 top, int K, int wv, int lane, u64 (*group_s)[64])
+{
+  group_s[wv][lane] = top;
+  __syncthreads();
+  if (wv == 0) {
+    u64 mine = top;
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) mine = max(mine, group_s[w][lane]);
+    int rank = 0;
+#pragma unroll 8
+    for (int i = 0; i < 64; ++i) {
+      const u64 o = (u64)(unsigned)__builtin_amdgcn_readlane((int)(mine >> 32), i) << 32 | (unsigned)__builtin_amdgcn_readlane((int)mine, i);
+      rank += o > mine || (o == mine && i < lane);
+    }
+    if (rank == K - 1) group_s[0][0] = mine;
+  }
+  __syncthreads();
+  return max(group_s[0][0], 1ull);
+}
+// the same of 32 bits, but for the last six of these (which hold the lane's place in the order)
+template <int WAVES>
+__device__ __forceinline__ unsigned bound_of(unsigned top, int K, int wv, int lane, unsigned (*group_s)[64])
+{
+  group_s[wv][lane] = top;
+  __syncthreads();
+  if (wv == 0) {
+    unsigned mine = top;
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) mine = max(mine, group_s[w][lane]);
+    mine = (mine & ~63u) | lane;
+    int rank = 0;
+#pragma unroll 8
+    for (int i = 0; i < 64; ++i) rank += (unsigned)__builtin_amdgcn_readlane(mine, i) > mine;
+    if (rank == K - 1) group_s[0][0] = mine & ~63u;
+  }
+  __syncthreads();
+  return group_s[0][0];
+}
+
+// The K best of n candidates in LDS, in order, for history b.
+template <int THREADS>
+__device__ __forceinline__ void write_best(const Args &a, int b, const u64 *p_s, const u64 *k_s, const unsigned char *w_s, const unsigned char *ended_s,
+                                           int n, int tid)
+{
+  const size_t out = (size_t)b * a.K;
+  for (int i0 = 0; i0 < n; i0 += THREADS / 4) {
+    const int i = i0 + (tid >> 2);
+    const int r = rank_of(p_s, k_s, w_s, n, i, tid);
+    if (i >= n || r >= a.K || (tid & 3)) continue;
+    const int item = item_of(k_s[i]), w = w_s[i];
+    a.parent[out + r] = b * a.W + w;
+    a.token[out + r] = item;
+    a.out_score[out + r] = (float)score_of(p_s[i]);
+    if (a.out_ended) a.out_ended[out + r] = item == a.eos || ended_s[w];
+  }
+  for (int r = n + tid; r < a.K; r += THREADS) {
+    a.parent[out + r] = a.token[out + r] = -1;
+    a.out_score[out + r] = -INFINITY;
+    if (a.out_ended) a.out_ended[out + r] = 0;
+  }
+}
+
 // One history: candidates that reach the K-th best of 64 groups' best are put in order.  Candidates are all that the lists hold or, of more than
 // four a thread, those of the K lists with the best first elements.
 template <int THREADS>
@@ -461,57 +567,9 @@ __global__ __launch_bounds__(THREADS) void merge_kernel(Args a)
     ended_s[tid] = a.ended ? a.ended[row0 + tid] : 0;
   }
   if (tid == 0) count_s = 0;
-  // ---- log sum exp of each beam's row: as many lanes a beam as it has runs ----
-  int per = 1;
-  while (per < a.lists && per < 64) per *= 2;
-  for (int w0 = wv * (64 / per); w0 < a.W; w0 += THREADS / per) {
-    const int w = w0 + lane / per, at = lane % per;
-    const double2 *st = a.stats + (row0 + min(w, a.W - 1)) * a.lists;
-    double m = -INFINITY, s = 0.0;
-    for (int i = at; i < a.lists; i += per) {
-      const double2 x = st[i];
-      if (!(x.x > -INFINITY)) continue;
-      const double top = fmax(m, x.x);
-      s = (m > -INFINITY ? s * exp_from(m, top) : 0.0) + x.y * exp_from(x.x, top);
-      m = top;
-    }
-    double top = m;
-    for (int o = per / 2; o >= 1; o >>= 1) top = fmax(top, __shfl_xor(top, o));
-    s = m > -INFINITY ? s * exp_from(m, top) : 0.0;
-    for (int o = per / 2; o >= 1; o >>= 1) s += __shfl_xor(s, o);
-    if (at == 0 && w < a.W) lse_s[w] = top == INFINITY ? INFINITY : top + log(s);
-  }
+  join_sums<THREADS>(a.stats + row0 * a.lists, a.W, a.lists, wv, lane, lse_s);
   __syncthreads();
-  // a key of a beam's candidate as a place in the order (only: the beam's first); none: 0
-  auto place = [&](int w, bool only, u64 &key) -> u64 {
-    double to;
-    if (ended_s[w]) {  // goes on in one way
-      key = key_of(0.0f, a.eos);
-      to = only ? score_s[w] : -INFINITY;
-    } else {
-      to = key == 0 ? -INFINITY : score_s[w] + ((double)logit_of((unsigned)(key >> 32)) - lse_s[w]);
-    }
-    return to > -INFINITY ? ordered(to) : 0;  // (a NaN neither)
-  };
-  // The K-th best of 64 groups' best.  Groups are a lane's of all wavefronts, in which first, second, .. elements of many lists meet: then about
-  // as many candidates reach the bound as groups do (without: one beam, 32 lists of 32: 27 us, so 7.6).
-  auto bound_of = [&](u64 top) -> u64 {
-    group_s[wv][lane] = top;
-    __syncthreads();
-    u64 mine = 0;
-#pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) mine = max(mine, group_s[w][lane]);
-    int rank = 0;
-#pragma unroll 8
-    for (int i = 0; i < 64; ++i) {
-      const u64 o = (u64)(unsigned)__builtin_amdgcn_readlane((int)(mine >> 32), i) << 32 | (unsigned)__builtin_amdgcn_readlane((int)mine, i);
-      rank += o > mine || (o == mine && i < lane);
-    }
-    const int at = __builtin_ctzll(__ballot(rank == a.K - 1));
-    const u64 bound = (u64)(unsigned)__builtin_amdgcn_readlane((int)(mine >> 32), at) << 32 | (unsigned)__builtin_amdgcn_readlane((int)mine, at);
-    __syncthreads();
-    return max(bound, 1ull);
-  };
+  auto place = [&](int w, bool only, u64 &key) { return place_of(score_s[w], lse_s[w], ended_s[w], only, a.eos, key); };
   auto put = [&](u64 p, u64 k, int w) __attribute__((always_inline)) {
     const int to = atomicAdd(&count_s, 1);
     p_s[to] = p; k_s[to] = k; w_s[to] = (unsigned char)w;
@@ -521,7 +579,7 @@ __global__ __launch_bounds__(THREADS) void merge_kernel(Args a)
     if (!few) {
       const int w = min((unsigned)tid / (unsigned)a.lists, (unsigned)a.W - 1);
       const u64 p = tid < L ? place(w, tid == w * a.lists, key[0]) : 0;
-      const u64 bound = bound_of(p);
+      const u64 bound = bound_of<THREADS / 64>(p, a.K, wv, lane, group_s);
       if (tid < L) {
         if (p >= bound) {
           const int to = atomicAdd(&count_s, 1);
@@ -560,30 +618,115 @@ __global__ __launch_bounds__(THREADS) void merge_kernel(Args a)
     }
     top = max(top, at[i]);
   }
-  const u64 bound = bound_of(top);
+  const u64 bound = bound_of<THREADS / 64>(top, a.K, wv, lane, group_s);
 #pragma unroll
   for (int i = 0; i < FEW; ++i) {
     const int c = from[i];
     if (at[i] >= bound) put(at[i], key[i], few ? (unsigned)c / (unsigned)(a.lists * a.K) : (unsigned)chosen_s[(unsigned)c / (unsigned)a.K] / (unsigned)a.lists);
   }
   __syncthreads();
-  const int n = count_s;
-  const size_t out = (size_t)b * a.K;
-  for (int i0 = 0; i0 < n; i0 += THREADS / 4) {
-    const int i = i0 + (tid >> 2);
-    const int r = rank_of(p_s, k_s, w_s, n, i, tid);
-    if (i >= n || r >= a.K || (tid & 3)) continue;
-    const int item = item_of(k_s[i]), w = w_s[i];
-    a.parent[out + r] = (int)(row0 + w);
-    a.token[out + r] = item;
-    a.out_score[out + r] = (float)score_of(p_s[i]);
-    if (a.out_ended) a.out_ended[out + r] = item == a.eos || ended_s[w];
+  write_best<THREADS>(a, b, p_s, k_s, w_s, ended_s, count_s, tid);
+}
+
+// One history of few logits by itself: all of them are candidates, FEW a thread.
+// Which candidates count is decided in 32 bits, with the bound on what these can be off by on the safe side; the few that may are put in order in
+// 64.  A score in 32 bits is logit + c, c the beam's score less its sum: off by 2^-24 of c and of itself, so by no more than 2^-23 (2 |c| + |logit|).
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void few_kernel(Args a)
+{
+  constexpr int FEW = kFewLogits / 1024, MOST = FEW * THREADS, WAVES = THREADS / 64, N = 4;
+  __shared__ u64 p_s[MOST], k_s[MOST];
+  __shared__ unsigned group_s[WAVES][64];
+  __shared__ double2 stats_s[kMost + WAVES];
+  __shared__ double lse_s[kMost], score_s[kMost];
+  __shared__ float2 off_s[kMost];
+  __shared__ unsigned char w_s[MOST], ended_s[kMost];
+  __shared__ int count_s;
+  float *x_s = reinterpret_cast<float *>(p_s);  // (until candidates are put there)
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), b = blockIdx.x, all = a.W * a.V;
+  const size_t row0 = (size_t)b * a.W;
+  const float by_V = 1.0f / (float)a.V;
+  float x[FEW];
+  int of[FEW];
+#pragma unroll
+  for (int i = 0; i < FEW; ++i) {
+    const int c = tid + i * THREADS;
+    of[i] = (int)(((float)c + 0.5f) * by_V);  // c / V: at least 1/2V from a whole number, and off by 64 * 2^-22
+    x[i] = -INFINITY;
+    if (c < all) {
+      const int64_t at = (int64_t)(row0 + of[i]) * a.stride + (c - of[i] * a.V);
+      x[i] = a.dtype == 0 ? element(static_cast<const float *>(a.logits) + at) : element(static_cast<const bf16_t *>(a.logits) + at);
+    }
   }
-  for (int r = n + tid; r < a.K; r += THREADS) {
-    a.parent[out + r] = a.token[out + r] = -1;
-    a.out_score[out + r] = -INFINITY;
-    if (a.out_ended) a.out_ended[out + r] = 0;
+  if (tid < a.W) {
+    score_s[tid] = (double)a.score[row0 + tid];
+    ended_s[tid] = a.ended ? a.ended[row0 + tid] : 0;
   }
+  if (tid == 0) count_s = 0;
+#pragma unroll
+  for (int i = 0; i < FEW; ++i) x_s[tid + i * THREADS] = x[i];
+  __syncthreads();
+  // ---- the rows' sums: as many threads a row as there are for each, a power of two; up to 64 sum among themselves ----
+  const int each_log2 = 31 - __builtin_clz(THREADS / a.W), lanes = min(1 << each_log2, 64), parts = (1 << each_log2) / lanes;
+  {
+    const int q = tid / lanes, w = q / parts, each = (a.V + parts - 1) / parts, from = (q - w * parts) * each;
+    const int n = w < a.W ? min(each, a.V - from) : 0, i0 = tid % lanes;
+    const float *row = x_s + w * a.V + from;
+    float m = -INFINITY;
+    for (int i = i0; i < n; i += lanes) m = fmaxf(m, row[i]);  // (a NaN is ruled out: fmaxf takes the other)
+    for (int o = lanes / 2; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    double s = 0.0;
+    if (m > -INFINITY && m < INFINITY) {
+      const double ref = -(double)m * kLog2e;
+      const float low = m - 690.0f;  // (e^-690 of a sum that is 1 or more)
+      for (int i = i0; i < n; i += lanes * N) {
+        double t[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const float y = i + lanes * j < n ? row[i + lanes * j] : low;
+          t[j] = fma((double)(y > low ? y : low), kLog2e, ref);
+        }
+        s += exp2_sum(t);
+      }
+    }
+    for (int o = lanes / 2; o >= 1; o >>= 1) s += __shfl_xor(s, o);
+    if (i0 == 0 && w < a.W) stats_s[q] = make_double2((double)m, s);
+  }
+  __syncthreads();
+  join_sums<THREADS>(stats_s, a.W, parts, wv, lane, lse_s);
+  __syncthreads();
+  // ---- the candidates ----
+  if (tid < a.W) {
+    const double c = score_s[tid] - lse_s[tid];
+    // (ended, or beyond 32 bits: each is a candidate, and none bounds the others.  -inf or NaN: none is a candidate)
+    off_s[tid] = ended_s[tid] || fabs(c) > 1e30 ? make_float2(0.0f, INFINITY) : make_float2((float)c, 0x1p-22f * fabsf((float)c));
+    if (!ended_s[tid] && !(c > -INFINITY)) off_s[tid] = make_float2(-INFINITY, 0.0f);
+  }
+  __syncthreads();
+  float upto[FEW], least = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < FEW; ++i) {
+    const int c = tid + i * THREADS, w = min(of[i], a.W - 1);
+    const float2 off = off_s[w];
+    const float near = x[i] + off.x, by = fmaf(fabsf(x[i]), 0x1p-23f, off.y);
+    const bool is = c < all && off.x > -INFINITY && (ended_s[w] ? c == w * a.V : x[i] > -INFINITY);
+    upto[i] = is ? near + by : -INFINITY;
+    if (is && by < INFINITY) least = fmaxf(least, near - by);
+    if (is && !(by < INFINITY)) upto[i] = INFINITY;
+  }
+  const float reach = logit_of(max(bound_of<WAVES>(ordered(least), a.K, wv, lane, group_s), ordered(-INFINITY)));
+#pragma unroll
+  for (int i = 0; i < FEW; ++i) {
+    if (!(upto[i] > -INFINITY && upto[i] >= reach)) continue;
+    const int c = tid + i * THREADS, w = of[i], item = c - w * a.V;
+    u64 key = key_of(x[i], item);
+    const u64 p = place_of(score_s[w], lse_s[w], ended_s[w], item == 0, a.eos, key);
+    if (p == 0) continue;
+    const int to = atomicAdd(&count_s, 1);
+    p_s[to] = p; k_s[to] = key; w_s[to] = (unsigned char)w;
+  }
+  __syncthreads();
+  write_best<THREADS>(a, b, p_s, k_s, w_s, ended_s, count_s, tid);
 }
 
 namespace {
@@ -594,6 +737,12 @@ long piece(int dtype, int loads) { return 64l * loads * (dtype == 0 ? 4 : 8); }
 
 void plan(Args &a)
 {
+  // A history of up to 8192 logits is one workgroup's, but where these are large ones in several rounds for few beams each, which rows by
+  // themselves fill better (4 beams of 1682 logits: 10.5 us, in two kernels 11.3; 160 histories of 26 beams of 42: 9.5, 47; 250 of 4 of 2000:
+  // 11.5, 14.8; 1000: 41, 33; 1000 of one beam of 8000: 48, 23; 300 of 32 of 256: 24, 97).
+  a.lists = 0;
+  const long logits = (long)a.W * a.V;
+  if (logits <= kFewLogits / 4 || (logits <= kFewLogits && (a.B <= 256 || a.W > 5))) return;
   // Runs: a workgroup for each of the CUs' two places, or as comes near (2048, 1024 and 512 workgroups for 512 rows of 152063: 52, 49 and 39
   // us; 508 and 762 for 254 rows of 108488: 26 and 30 with the merge); no more than the merge's small workgroup takes, unless runs become long (8 rows of 150001, K = 8: merge 6 us with 16 lists a row, 10 with 37).
   // Four loads a lane and piece of bf16, two of fp32 (400000 logits, K = 32: 9 us, four 23, one 10; 512 rows of 152063: 85, 84, 99); one in
@@ -616,6 +765,13 @@ void plan(Args &a)
 
 bool launch(const Args &a, hipStream_t st)
 {
+  if (a.lists == 0) {
+    const bool small = a.W * a.V <= kFewLogits / 4;
+    if ((long)a.B * (small ? 256 : 1024) >= 1l << 32) return false;
+    if (small) hipLaunchKernelGGL((few_kernel<256>), dim3((unsigned)a.B), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((few_kernel<1024>), dim3((unsigned)a.B), dim3(1024), 0, st, a);
+    return true;
+  }
   const long blocks = (long)a.B * a.W * a.lists;
   if (blocks * 64 * kWaves >= 1l << 32) return false;
   [&] {

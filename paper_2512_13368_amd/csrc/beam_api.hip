@@ -21,7 +21,8 @@ int check_params(const blossom_beam_params *p, Args *a)
 }
 
 size_t runs(const Args &a) { return (size_t)a.B * a.W * a.lists; }
-size_t ws_bytes_of(const Args &a) { return runs(a) * (sizeof(double2) + a.K * sizeof(unsigned long long)); }
+// (16 where few logits need none: one rule for all callers)
+size_t ws_bytes_of(const Args &a) { return a.lists == 0 ? 16 : runs(a) * (sizeof(double2) + a.K * sizeof(unsigned long long)); }
 bool aligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 }  // namespace

@@ -636,16 +636,18 @@ void plan_tree(Args &a)
 {
   const int row_bytes = row_bytes_of(a), w = few_waves(row_bytes);
   const long rows = (long)a.T * a.R, each = rows / a.S;
-  int waves, keys = kTile, least = kTreeLeast / kTile;  // workgroups that fill the chip; keys of a tile, tiles of a share at least
+  int waves, keys = kTile, least = 2 * kTreeLeast / kTile;  // workgroups that fill the chip; keys of a tile, tiles of a walk that is cut at least
   if (each <= 16) {
+    // (a second launch and second pieces of walks cost as much as 9 tiles a wavefront, where they are large 5: 74 trees of one row over 1937
+    // positions, d = 16, 8.7 us whole and 16.4 cut, 1 over 3205, d = 32, 12.5 and 10.3; 5 over 698, d = 128, fp32, 23.8 and 20.1)
     a.tree_rows = kRows;
     waves = fill_waves(row_bytes) / w;
-    least = w;
+    least = (row_bytes == 512 ? 5 : 9) * w;
   } else if (tree_matrix_supported(a)) {
     a.tree_rows = each <= 128 ? 128 : 256;
     waves = a.d == 64 ? 512 : 256;
     keys = 32 * 256 / a.tree_rows;
-    least = kTreeLeast / keys;
+    least = 2 * kTreeLeast / keys;
   } else {
     a.tree_rows = shared_rows(a);
     waves = 4096 / shared_waves(row_bytes);
@@ -653,7 +655,7 @@ void plan_tree(Args &a)
   const long base = rows / a.tree_rows + a.S;  // row tiles, at most
   const long tiles = ((a.window < a.cap ? (long)a.window + kDrafts + keys - 1 : a.cap) + keys - 1) / keys;
   a.parts = waves / a.G;
-  if (tiles < 2 * least || base * tiles > 1 << 30 || 3 * (rows / a.tree_rows > a.S ? rows / a.tree_rows : a.S) > 2 * a.parts) a.parts = 0;
+  if (tiles < least || base * tiles > 1 << 30 || 3 * (rows / a.tree_rows > a.S ? rows / a.tree_rows : a.S) > 2 * a.parts) a.parts = 0;
   a.units = (int)(a.parts ? a.parts : base);
   a.slots = (int)(a.parts ? a.parts + base : 0);
 }
