@@ -335,6 +335,15 @@ struct Walk {
   int slot = -1;                              // trees: where partial sums go (below 0: the walk is whole)
 };
 
+// Which workgroup of all trees' this one is.  Where a walk is one workgroup's, up to one place a sequence has nothing (launch_tree counts row
+// tiles before it knows them), and with fewer than 8 key/value heads these would lie on the same dies, to which workgroups go in turn: eights
+// are turned by their number (64 trees of 16 rows, 4 heads: every other row tile is nothing; 16.2 us, so 12.1).
+__device__ __forceinline__ int tree_block(const Args &a)
+{
+  const unsigned id = blockIdx.x, eight = id & ~7u;
+  return a.G >= 8 || eight + 8 > gridDim.x ? id : eight | ((id + (id >> 3)) & 7u);
+}
+
 // What one workgroup of a key/value head does of all trees.  A tree's rows are cut into row tiles, each of which walks the same key tiles.  With
 // a.parts workgroups, the walks of all row tiles lie one behind the other, and workgroup b takes the b-th of as many equal shares: the end
 // of one walk, whole ones, the beginning of another.  (Cut into parts by themselves, 16 walks of 125 to 253 tiles leave the longest part

@@ -295,7 +295,7 @@ __global__ __launch_bounds__(64 * W) void decode_kernel(Args a)
 template <typename T, int D, int W, bool SPLIT>
 __global__ __launch_bounds__(64 * W) void tree_few_kernel(Args a)
 {
-  const int lane = threadIdx.x & 63, rest = a.by_G.of(blockIdx.x), g = blockIdx.x - rest * a.G;
+  const int lane = threadIdx.x & 63, block = tree_block(a), rest = a.by_G.of(block), g = block - rest * a.G;
   TreeWork work(rest, kRows, kTile);
   for (Walk w = work.begin(a, lane, W); w.s >= 0; w = work.next(a, lane)) {
     work.tell(a, w, g, lane, threadIdx.x, 64 * W);
@@ -665,7 +665,10 @@ size_t tree_part_rows(const Args &a) { return (size_t)a.slots * a.G * a.tree_row
 bool launch_tree(const Args &a, hipStream_t st)
 {
   const bool matrix = a.tree_rows != kRows && tree_matrix_supported(a);
-  const int waves = a.tree_rows == kRows ? few_waves(row_bytes_of(a)) : matrix ? 8 : shared_waves(row_bytes_of(a));
+  // (whole walks for more than a workgroup a CU: four wavefronts where eight hold more than half a CU's LDS.  43 trees of 1 to 3 rows over 166, 8
+  // heads, d = 64, bf16: 9.0 us with eight, 6.2; 103 of one row over 159 to 318, d = 32, fp32: 23.2 and 16.4; 30 of 4 to 8, d = 16, bf16: 7.8 and 8.6)
+  const int few = a.parts == 0 && (long)a.units * a.G > 256 && row_bytes_of(a) >= 64 ? 4 : few_waves(row_bytes_of(a));
+  const int waves = a.tree_rows == kRows ? few : matrix ? 8 : shared_waves(row_bytes_of(a));
   const dim3 grid((unsigned)((long)a.units * a.G));
   if (!countable((long)a.units * a.G, 64 * waves)) return false;
   const bool once = (double)a.S * a.cap * a.G * row_bytes_of(a) * 2 > 256e6;
@@ -676,7 +679,8 @@ bool launch_tree(const Args &a, hipStream_t st)
     constexpr int D = decltype(dim)::value, W = few_waves(D * sizeof(T));
     if (a.tree_rows == kRows) {
       if (a.parts) BLOSSOM_LAUNCH((tree_few_kernel<T, D, W, true>), grid, dim3(64 * W), 0, st, a);
-      else BLOSSOM_LAUNCH((tree_few_kernel<T, D, W, false>), grid, dim3(64 * W), 0, st, a);
+      else if (few == W) BLOSSOM_LAUNCH((tree_few_kernel<T, D, W, false>), grid, dim3(64 * W), 0, st, a);
+      else BLOSSOM_LAUNCH((tree_few_kernel<T, D, 4, false>), grid, dim3(64 * 4), 0, st, a);
     }
     if (a.parts && !launch_failed()) {
       // few sequences have many parts

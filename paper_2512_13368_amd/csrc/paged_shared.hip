@@ -186,7 +186,7 @@ template <typename T, int D, bool SPLIT>
 __global__ __launch_bounds__(64 * shared_waves(D * sizeof(T))) __attribute__((amdgpu_waves_per_eu(kRoomFor<T, D>))) void tree_shared_kernel(Args a)
 {
   constexpr int W = shared_waves(D * sizeof(T));
-  const int lane = threadIdx.x & 63, rest = a.by_G.of(blockIdx.x), g = blockIdx.x - rest * a.G;
+  const int lane = threadIdx.x & 63, block = tree_block(a), rest = a.by_G.of(block), g = block - rest * a.G;
   TreeWork work(rest, 16 * W, kTile);
   for (Walk w = work.begin(a, lane, kTreeLeast / kTile); w.s >= 0; w = work.next(a, lane)) {
     work.tell(a, w, g, lane, threadIdx.x, 64 * W);

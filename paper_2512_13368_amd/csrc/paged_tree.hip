@@ -322,7 +322,7 @@ __device__ __forceinline__ void walk_tree(const Args &a, int g, const Walk &w)
 template <int D, int RG, int STAGES, int EU, bool ONCE>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(EU, EU))) void tree_kernel(Args a)
 {
-  const int lane = threadIdx.x & 63, rest = a.by_G.of(blockIdx.x), g = blockIdx.x - rest * a.G;
+  const int lane = threadIdx.x & 63, block = tree_block(a), rest = a.by_G.of(block), g = block - rest * a.G;
   constexpr int KEYS = 32 * kWaves / RG;
   TreeWork work(rest, 32 * RG, KEYS);
   for (Walk w = work.begin(a, lane, kTreeLeast / KEYS); w.s >= 0; w = work.next(a, lane)) {
