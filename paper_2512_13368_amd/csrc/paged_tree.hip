@@ -8,10 +8,11 @@
 //    tile: a tree's rows do less with a tile than a prompt's, and memory has to be kept busy for them.
 //  - S^T = K Q^T, softmax and O^T += V^T P^T as in paged_prompt.hip.
 // Measured: 26 drafted tokens over 131040 positions (32 heads over 8, d = 128: 537 MB) 107 us, 8 of it the join, where reading as many bytes
-// takes 78; 33 to 64 over 4000 to 8100 for 16 sequences (412 MB, 73 GFLOP) 135 us, 13 of it the join.  Of these, with everything but
-// the loads left out, 96; with the loads left out, 114; with both, 41: launch, finding the rows, pages and queries, 17 to 34 MB of partial
+// takes 78; 33 to 64 over 4000 to 8100 for 16 sequences (412 MB, 73 GFLOP) 135 us, 10 of it the join.  Of these, with everything but
+// the loads left out, 96; with the loads left out, 114; with both, 41: launch, finding the rows, pages and queries, 17 to 36 MB of partial
 // sums.  Tried: workgroups of 128 rows, two on a CU (150: K and V are moved twice); keys' operands read a tile ahead (no gain); the next tile's
-// logits among this one's exponentials (145); 64 rows a wavefront, one a SIMD (the compiler spills).
+// logits among this one's exponentials (145); a barrier for two tiles at once (139), half the wavefronts at a higher priority (no gain);
+// 64 rows a wavefront, one a SIMD (the compiler spills).
 #include "common.h"
 #include "launch.h"
 #include "mfma_common.h"
