@@ -630,7 +630,8 @@ __global__ __launch_bounds__(THREADS) void merge_kernel(Args a)
 
 // One history of few logits by itself: all of them are candidates, FEW a thread.
 // Which candidates count is decided in 32 bits, with the bound on what these can be off by on the safe side; the few that may are put in order in
-// 64.  A score in 32 bits is logit + c, c the beam's score less its sum: off by 2^-24 of c and of itself, so by no more than 2^-23 (2 |c| + |logit|).
+// 64.  A score in 32 bits is logit + c, c the beam's score less its sum: off by 2^-24 of c, of itself and of its sum with the bound, so by less than 2^-22
+// (|c| + |logit|).
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void few_kernel(Args a)
 {
@@ -699,7 +700,7 @@ __global__ __launch_bounds__(THREADS) void few_kernel(Args a)
   if (tid < a.W) {
     const double c = score_s[tid] - lse_s[tid];
     // (ended, or beyond 32 bits: each is a candidate, and none bounds the others.  -inf or NaN: none is a candidate)
-    off_s[tid] = ended_s[tid] || fabs(c) > 1e30 ? make_float2(0.0f, INFINITY) : make_float2((float)c, 0x1p-22f * fabsf((float)c));
+    off_s[tid] = ended_s[tid] || fabs(c) > 1e30 ? make_float2(0.0f, INFINITY) : make_float2((float)c, fmaf(0x1p-22f, fabsf((float)c), 0x1p-120f));
     if (!ended_s[tid] && !(c > -INFINITY)) off_s[tid] = make_float2(-INFINITY, 0.0f);
   }
   __syncthreads();
@@ -708,7 +709,7 @@ __global__ __launch_bounds__(THREADS) void few_kernel(Args a)
   for (int i = 0; i < FEW; ++i) {
     const int c = tid + i * THREADS, w = min(of[i], a.W - 1);
     const float2 off = off_s[w];
-    const float near = x[i] + off.x, by = fmaf(fabsf(x[i]), 0x1p-23f, off.y);
+    const float near = x[i] + off.x, by = fmaf(fabsf(x[i]), 0x1p-22f, off.y);
     const bool is = c < all && off.x > -INFINITY && (ended_s[w] ? c == w * a.V : x[i] > -INFINITY);
     upto[i] = is ? near + by : -INFINITY;
     if (is && by < INFINITY) least = fmaxf(least, near - by);
