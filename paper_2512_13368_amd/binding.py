@@ -814,6 +814,9 @@ def attn_prompt(p: PagedParams, Q, K_cache, V_cache, page_table, cu_seqlens, kv_
     return _paged_attn(p, WS_PROMPT, p.T, Q, K_cache, V_cache, page_table, cu_seqlens, kv_len, O, lse, ws, stream)
 
 
+_MOST = 2**31 - 1  # of what the library counts in 32 bits
+
+
 def _here(**tensors):
     """All of them on the current device, whose stream the call goes to."""
     import torch
@@ -875,8 +878,8 @@ def kv_accept(p: PagedParams, keep, K_cache, V_cache, page_table, cu_seqlens, kv
     import torch
     if keep is None or cu_seqlens is None:
         raise ValueError("keep and cu_seqlens are required")
-    if keep.dim() != 2 or keep.shape[0] != p.S or keep.shape[1] < 1:
-        raise ValueError(f"keep: expected shape ({p.S}, n >= 1), got {tuple(keep.shape)}")
+    if keep.dim() != 2 or keep.shape[0] != p.S or not 1 <= keep.shape[1] <= _MOST:
+        raise ValueError(f"keep: expected shape ({p.S}, 1 <= n <= {_MOST}), got {tuple(keep.shape)}")
     _check_tensor(keep, keep.shape, torch.int32, "keep")
     _check_cache(p, K_cache, V_cache, page_table, cu_seqlens, kv_len)
     _here(keep=keep, K_cache=K_cache, V_cache=V_cache, page_table=page_table, cu_seqlens=cu_seqlens, kv_len=kv_len, new_len=new_len)
@@ -913,8 +916,10 @@ def kv_fork(p: PagedParams, parent, page_table, kv_len, refs, grow=0, new_table=
     for t, nm in ((parent, "parent"), (page_table, "page_table"), (kv_len, "kv_len"), (refs, "refs")):
         if t is None:
             raise ValueError(f"{nm} is required")
-    if parent.dim() != 1 or parent.shape[0] < 1:
-        raise ValueError(f"parent: expected shape (n >= 1,), got {tuple(parent.shape)}")
+    if parent.dim() != 1 or not 1 <= parent.shape[0] <= _MOST:
+        raise ValueError(f"parent: expected shape (1 <= n <= {_MOST},), got {tuple(parent.shape)}")
+    if not -_MOST <= grow <= _MOST:
+        raise ValueError(f"grow: expected 32 bits, got {grow}")
     N, i32 = parent.shape[0], torch.int32
     _check_tensor(parent, (N,), i32, "parent")
     _check_tensor(page_table, (p.S, p.max_pages), i32, "page_table")
@@ -951,8 +956,8 @@ def kv_copy_pages(p: PagedParams, copies, K_cache, V_cache, stream=None):
     for t, nm in ((copies, "copies"), (K_cache, "K_cache"), (V_cache, "V_cache")):
         if t is None:
             raise ValueError(f"{nm} is required")
-    if copies.dim() != 2 or copies.shape[0] < 1 or copies.shape[1] != 3:
-        raise ValueError(f"copies: expected shape (n >= 1, 3), got {tuple(copies.shape)}")
+    if copies.dim() != 2 or not 1 <= copies.shape[0] <= _MOST or copies.shape[1] != 3:
+        raise ValueError(f"copies: expected shape (1 <= n <= {_MOST}, 3), got {tuple(copies.shape)}")
     _check_tensor(copies, copies.shape, torch.int32, "copies")
     shp = (p.n_pages, p.G, p.page, p.d)
     _check_tensor(K_cache, shp, _torch_dtype(p), "K_cache")

@@ -238,3 +238,14 @@ def test_rows_of_logits_that_overlap_are_refused(path):
     with pytest.raises(B.BlossomError) as e:
         call("beam_select", {**a, "logits": wide})
     assert e.value.code == -1
+
+
+def test_counts_beyond_32_bits_are_refused(path):
+    # (they would wrap round to small ones)
+    a = tensors()
+    for name, key, wrong in (("kv_accept", "keep", i32(P.S, (1 << 32) + 5)), ("kv_copy_pages", "copies", i32((1 << 32) + 7, 3)),
+                             ("kv_fork", "grow", (1 << 32) + 1), ("kv_fork", "grow", -(1 << 32) + 1)):
+        with pytest.raises(ValueError, match=key):
+            call(name, {**a[name], key: wrong})
+    with pytest.raises(ValueError, match="parent"):
+        B.kv_fork(P, i32((1 << 32) + 7), a["kv_fork"]["page_table"], a["kv_fork"]["kv_len"], a["kv_fork"]["refs"])
