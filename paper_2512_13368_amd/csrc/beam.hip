@@ -117,13 +117,14 @@ struct Piece<bf16_t> {
 
 // e^x of bf16 logits from a table in LDS: all 2560 with 2^-14 <= |x| < 64 of either sign, at 1 + (code - that of 2^-14); at 0 what is nearer
 // to 0 (1, to which x + x^2/2 is added: e^x to 2^-42/6), at the end what is larger (nothing: the sum of a piece whose largest logit
-// lies between -20 and 64 does not miss e^-64).  Of two logits in a register the places take nine instructions, where the
-// polynomial takes 36: 512 rows of 152063 logits 82 us by the polynomial, 40 so (other things changed with it).
+// lies between -20 and 64 does not miss e^-64).  Of two logits in a register the places take eight instructions, where the
+// polynomial takes 36: 512 rows of 152063 logits 82 us by the polynomial, 36 so (other things changed with it); a quarter of them by the
+// polynomial, which leaves LDS less to do, 42.
 constexpr int kLeast = (127 - 14) << 7;
 struct Table {
   static constexpr int kEnd = ((127 + 6) << 7) - kLeast + 1;  // the place of what is larger
   static constexpr int kSign = 4096, kSize = kSign + kEnd + 1;  // places of the negative ones begin at kSign
-  static_assert(kEnd < kSign, "");
+  static_assert(kEnd < kSign && kSign * sizeof(double) == 1 << 15, "");
   static __device__ __forceinline__ void fill(double *to, int tid, int threads)
   {
     for (int i = tid; i < 2 * (kEnd + 1); i += threads) {
@@ -139,16 +140,17 @@ struct Table {
   {
     typedef unsigned short two __attribute__((ext_vector_type(2)));
     const unsigned w[4] = {v.x, v.y, v.z, v.w};
-    const two below = {kLeast - 1, kLeast - 1}, end = {kEnd, kEnd};
+    const two below = {kLeast - 1, kLeast - 1}, end = {kEnd, kEnd}, three = {3, 3};
+    const char *bytes = reinterpret_cast<const char *>(table);
     two least = end;
     double e[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const two at = __builtin_elementwise_min(__builtin_elementwise_sub_sat(__builtin_bit_cast(two, w[i] & 0x7FFF7FFFu), below), end);
       least = __builtin_elementwise_min(least, at);
-      const unsigned place = __builtin_bit_cast(unsigned, at) | (w[i] >> 3 & 0x10001000u);
-      e[2 * i] = table[place & 0xFFFFu];
-      e[2 * i + 1] = table[place >> 16];
+      const unsigned place = __builtin_bit_cast(unsigned, at << three) | (w[i] & 0x80008000u);  // in bytes: a logit's sign is that of kSign
+      e[2 * i] = *reinterpret_cast<const double *>(bytes + (place & 0xFFFFu));
+      e[2 * i + 1] = *reinterpret_cast<const double *>(bytes + (place >> 16));
     }
 #pragma unroll
     for (int k = 4; k >= 1; k /= 2)
@@ -265,10 +267,26 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(4))
     if (at + kWaves * SUB < end) load(at + kWaves * SUB);
     // (a NaN counts as an item that is ruled out: fmaxf takes the other)
     float top = -INFINITY;
+    bool exact = true;
+    if constexpr (sizeof(T) == 2) {  // of bf16 the largest as 16-bit whole numbers, two at once, where that is one above 0 and no NaN
+      typedef short two __attribute__((ext_vector_type(2)));
+      two most = __builtin_bit_cast(two, v[0].x);
 #pragma unroll
-    for (int j = 0; j < LD; ++j)
+      for (int j = 0; j < LD; ++j) {
+        most = __builtin_elementwise_max(most, __builtin_elementwise_max(__builtin_bit_cast(two, v[j].x), __builtin_bit_cast(two, v[j].y)));
+        most = __builtin_elementwise_max(most, __builtin_elementwise_max(__builtin_bit_cast(two, v[j].z), __builtin_bit_cast(two, v[j].w)));
+      }
+      const int larger = max((int)most.x, (int)most.y);
+      top = __uint_as_float((unsigned)larger << 16);
+      exact = __any((unsigned)larger > 0x7F80u);
+    }
+    if (exact) {
+      top = -INFINITY;
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) top = fmaxf(top, P::get(v[j], e));
+      for (int j = 0; j < LD; ++j)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) top = fmaxf(top, P::get(v[j], e));
+    }
     lane_top = fmaxf(lane_top, top);
     bool by_table = false;
     if constexpr (TABLE) {
