@@ -99,15 +99,14 @@ bool launch_accept(const Args &a, const Accept &x, hipStream_t st)
 
 // Sequences take a wavefront each, which counts pages by atomics (a sum of whole numbers, in any order); fresh pages go out from one
 // workgroup.  It is all chains of loads, each about a microsecond where another die wrote: 512 sequences of up to 4040 positions 21 us
-// in four launches with the copies; few sequences and pages are done by one workgroup with its counts in LDS.
+// in four launches with the copies; few sequences and pages are done by one workgroup with its counts in LDS.  The eldest counts for all heirs (rows of 512
+// sequences of up to 8208 positions, pages of 8: 23.7 us, each for itself 29.6).
 //
-// What a new sequence takes over.
+// What a new sequence takes over from q.
 struct Heir {
-  int q, len, full, part, need;  // (q < 0: nothing)
-  __device__ __forceinline__ Heir(const Args &a, const Fork &x, int n)
+  int len, full, part, need;  // (q < 0: nothing)
+  __device__ __forceinline__ Heir(const Args &a, const Fork &x, int q)
   {
-    q = x.parent[n];
-    if (q < 0 || q >= a.S) q = -1;
     len = q < 0 ? 0 : min(max(a.kv_len[q], 0), a.cap);
     full = len >> a.page_shift;
     part = len & ((1 << a.page_shift) - 1);
@@ -117,40 +116,46 @@ struct Heir {
 __device__ __forceinline__ int valid(const Args &a, int id) { return id >= 0 && id < a.n_pages ? id : -1; }
 
 // New sequence n, and old sequence n, by a wavefront: its row of the new table, fresh pages as -2, -3, .. in order, how many those are, and
-// which page it copies; who holds a page then.  count(page, change), hold(page): of a page that a copy reads.
+// which page it copies; who holds a page then, of all heirs of a parent by the eldest.  count(page, change), hold(page): of a page that a copy reads.
 template <typename C, typename H>
 __device__ __forceinline__ void fork_row(const Args &a, const Fork &x, int n, int lane, C &&count, H &&hold)
 {
-  if (n < a.S) {  // dropped by all: its pages go
-    bool heir = false;
-    for (int i = lane; i < x.N; i += 64) heir = heir || x.parent[i] == n;
-    if (!__any(heir)) {
-      const int *from = a.page_table + (size_t)n * a.max_pages;
-      for (int i = lane; i < a.max_pages; i += 64) {
-        const int old = valid(a, from[i]);
-        if (old >= 0) count(old, -1);
-      }
+  const int mine = n < x.N ? x.parent[n] : -1, q = mine >= 0 && mine < a.S ? mine : -1;
+  int heirs = 0, younger = 0;  // sequences that go on from the same parent, and that go on from old sequence n
+  bool eldest = q >= 0;
+  for (int i0 = 0; i0 < x.N; i0 += 64) {
+    const int p = i0 + lane < x.N ? x.parent[i0 + lane] : -1;
+    const unsigned long long same = __ballot(p == q && p >= 0);
+    if (heirs == 0 && same) eldest = eldest && i0 + __builtin_ctzll(same) == n;
+    heirs += __builtin_popcountll(same);
+    younger += __builtin_popcountll(__ballot(p == n));
+  }
+  if (n < a.S && younger == 0) {  // dropped by all: its pages go
+    const int *from = a.page_table + (size_t)n * a.max_pages;
+    for (int i = lane; i < a.max_pages; i += 64) {
+      const int old = valid(a, from[i]);
+      if (old >= 0) count(old, -1);
     }
   }
   if (n >= x.N) return;
-  const Heir h(a, x, n);
-  bool elder = false;  // does an earlier one go on from the same parent?
-  for (int i = lane; i < n; i += 64) elder = elder || x.parent[i] == h.q;
-  const bool eldest = h.q >= 0 && !__any(elder);
-  const int *from = a.page_table + (size_t)max(h.q, 0) * a.max_pages;
+  const Heir h(a, x, q);
+  const int *from = a.page_table + (size_t)max(q, 0) * a.max_pages;
   int *to = x.table + (size_t)n * a.max_pages;
   int fresh = 0, copy = -1;
+  const int until = eldest ? a.max_pages : h.need;
+  int next = lane < until ? from[lane] : -1;
   for (int i0 = 0; i0 < a.max_pages; i0 += 64) {
-    const int i = i0 + lane;
-    const int old = i < (eldest ? a.max_pages : h.need) ? valid(a, from[i]) : -1;
+    const int i = i0 + lane, old = valid(a, next);
+    next = i + 64 < until ? from[i + 64] : -1;
     const bool taken = i < h.full || (i < h.need && eldest && old >= 0 && x.refs[old] == 1), asks = i < h.need && !taken;
     const unsigned long long all = __ballot(asks);
     const int before = __builtin_amdgcn_mbcnt_hi((unsigned)(all >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)all, 0));
     if (asks && i == h.full && h.part > 0) copy = old;
     if (i < a.max_pages) to[i] = taken ? old : asks ? -2 - (fresh + before) : -1;
     fresh += __builtin_popcountll(all);
-    // a younger one holds what it shares too; the eldest lets go of what it does not take over
-    if (old >= 0 && eldest != taken) count(old, eldest ? -1 : 1);
+    // whole pages: all heirs for the parent; of the rest the eldest lets go of what it does not take over
+    const int by = i < h.full ? heirs - 1 : taken ? 0 : -1;
+    if (eldest && old >= 0 && by != 0) count(old, by);
   }
   if (copy >= 0) hold(copy);
   const unsigned long long copies = __ballot(copy >= 0);
