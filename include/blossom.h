@@ -538,7 +538,7 @@ int blossom_kv_copy_pages(const blossom_paged_params *p, int32_t n_copies, const
  *   token      out  int32 [B, K];  out_score  out  fp32 [B, K]: the sum above, rounded once
  *   out_ended  out  uint8 [B, K] or NULL: 1 if the parent had ended or the token is eos
  * A logit of -inf, or NaN, is no candidate and has no part in the sum; a row with a logit of +inf has none.  Where there are fewer than K
- * candidates, the last entries are -1, -1, -inf, 0.
+ * candidates, the last entries are -1, -1, -inf, 0.  No output may overlap an input.
  *   ws   scratch, >= blossom_beam_workspace_bytes(p), 16-byte aligned
  */
 typedef struct {
