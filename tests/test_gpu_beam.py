@@ -128,3 +128,23 @@ def test_two_calls_give_the_same_bits(dtype):
     first = [x.clone() for x in run(logits, score, 16)]
     for a, b in zip(first, run(logits, score, 16)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("b,w,k,v", [(300, 2, 3, 700), (300, 1, 4, 5000), (300, 6, 4, 1000), (520, 3, 8, 2731), (513, 1, 2, 3)])
+def test_many_histories(dtype, b, w, k, v):
+    run(*inputs(b, w, v, dtype, b + v), k)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("v", [600, 9000, 100003])
+def test_logits_below_zero(dtype, v):
+    # as log-probabilities are; then with a few NaN of either sign and +-0 among them
+    g = torch.Generator().manual_seed(v)
+    logits = (-torch.rand(2, 3, v, generator=g) * 18 - 0.125).to(DT[dtype])
+    score = -torch.rand(2, 3, generator=g)
+    run(logits, score, 20)
+    logits[0, 0, 5::97], logits[0, 1, 3::89], logits[1, 2, 7::101] = float("nan"), -float("nan"), -0.0
+    logits[1, 0, v // 2] = 0.0
+    run(logits, score, 20)
+    run(logits * 6.0, score, 20)
