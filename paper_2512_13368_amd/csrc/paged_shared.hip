@@ -9,7 +9,8 @@
 // bf16 probabilities are rounded once, but for workgroups with rows that see few keys: both terms of them (FINE in paged_tile.h)
 // everywhere take 7 to 13 % more time here (11 prompts of 3277, 3 heads over 1, d = 8: 72.4 us for 67.4; 8 of 1000 to 3000, 8 heads over
 // 2, d = 32: 69.3 for 61.2), as a branch in the one walk 5 to 6 %, in a walk of their own nothing, or 0.2 of 9 us where all rows see few
-// (256 prompts of 16 tokens, 4 heads, d = 128).
+// (256 prompts of 16 tokens, 4 heads, d = 128).  Trees keep both terms always, as trees of up to 16 rows do (16 trees of 16 to 64 tokens over
+// 2000 to 8000, 8 heads over 2: 27.6 us for 25.7 at d = 8, 32.0 for 30.3 at d = 32; 100 over 300 to 900, 8 over 4, d = 32: 31.1 for 26.6).
 #include "common.h"
 #include "launch.h"
 #include "mfma_common.h"
@@ -82,8 +83,8 @@ __device__ __forceinline__ void walk_rows(const Args &a, int g, const Walk &w)
     t_end = min(t + each, t_end);
   }
   const size_t page_bytes = ((size_t)a.G << a.page_shift) * TL::RB, group_bytes = ((size_t)g << a.page_shift) * TL::RB;
-  // few keys: by their number, or because pages are out of range
-  bool fine = TL::BF && (TREE ? tree.every.hi - tree.every.lo + 1 < kFewKeys : few_keys(wg_first, wg_last));
+  // trees always; few keys: by their number, or because pages are out of range
+  bool fine = TL::BF && (TREE || few_keys(wg_first, wg_last));
   auto look = [&]() __attribute__((always_inline)) {
     const int page = list0 + lane;
     if (TL::BF) fine = fine || __any(ids < 0 && page >= lo >> a.page_shift && page <= hi >> a.page_shift);

@@ -6,13 +6,17 @@
 // keys of a tile each and are joined in LDS at the end, so that few rows do not leave wavefronts idle.
 //  - K and V tiles go from the pages straight to LDS, once for all rows, through a ring of STAGES tiles (128 KB on a CU) with one barrier a
 //    tile: a tree's rows do less with a tile than a prompt's, and memory has to be kept busy for them.
-//  - S^T = K Q^T, softmax and O^T += V^T P^T as in paged_prompt.hip.
-// Measured: 26 drafted tokens over 131040 positions (32 heads over 8, d = 128: 537 MB) 107 us, 8 of it the join, where reading as many bytes
-// takes 78; 33 to 64 over 4000 to 8100 for 16 sequences (412 MB, 73 GFLOP) 135 us, 10 of it the join.  Of these, with everything but
-// the loads left out, 96; with the loads left out, 114; with both, 41: launch, finding the rows, pages and queries, 17 to 36 MB of partial
-// sums.  Tried: workgroups of 128 rows, two on a CU (150: K and V are moved twice); keys' operands read a tile ahead (no gain); the next tile's
-// logits among this one's exponentials (145); a barrier for two tiles at once (139), half the wavefronts at a higher priority (no gain);
-// 64 rows a wavefront, one a SIMD (the compiler spills).
+//  - S^T = K Q^T, softmax and O^T += V^T P^T as in paged_prompt.hip, but both bf16 terms of P always: P rounded to bf16 once leaves outputs off by
+//    2.3e-3 of their norm where their own rounding is 1.6e-3, and trees of up to 16 rows keep both terms too.
+// Measured: 26 drafted tokens over 131040 positions (32 heads over 8, d = 128: 537 MB) 131 us, 8 of it the join, where reading as many bytes
+// takes 78; 33 to 64 over 4000 to 8100 for 16 sequences (412 MB, 73 GFLOP) 164 us, 10 of it the join.  The second term takes 20 and 28 of these (111
+// and 136 without; 26 tokens over 131040, one head over each of 8, 92 and 89; 100 trees of 20 to 64 over 300 to 900, d = 64, 36.6 and 32.2): the matrix
+// pipe does half as much again, and waits for the vector ALUs as before.  Its product after the first one's, so that the remainders are
+// taken meanwhile, gains nothing (132 and 168).
+// Of the walk with P rounded once (111 and 136): with everything but the loads left out, 96; with the loads left out, 114; with both, 41:
+// launch, finding the rows, pages and queries, 17 to 36 MB of partial sums.  Tried there: workgroups of 128 rows, two on a CU (150: K and V are moved
+// twice); keys' operands read a tile ahead (no gain); the next tile's logits among this one's exponentials (145); a barrier for two tiles at
+// once (139), half the wavefronts at a higher priority (no gain); 64 rows a wavefront, one a SIMD (the compiler spills).
 #include "common.h"
 #include "launch.h"
 #include "mfma_common.h"
@@ -93,15 +97,12 @@ __device__ __forceinline__ void walk_tree(const Args &a, int g, const Walk &w)
   };
   take();
   missing &= ~0ull << max((lo >> shift) - list0, 0);  // (pages of the first tile that end before the first key: anything too)
-  // few keys: by their number, or because pages are out of range
-  bool fine = tree.every.hi - tree.every.lo + 1 < kFewKeys || missing != 0ull;
   auto advance = [&](int page) __attribute__((always_inline)) {
     while (page >= list0 + 64) {
       list0 += 64;
       ids = ids_next;
       ids_next = entries(list0 + 64);
       take();
-      fine = fine || missing != 0ull;
     }
   };
 
@@ -192,8 +193,8 @@ __device__ __forceinline__ void walk_tree(const Args &a, int g, const Walk &w)
   for (int k = 0; k < STAGES - 1; ++k)
     if (t_lo + k <= t_hi) request(t_lo + k, k);
   int t = t_lo, k = 0;
-  auto turn = [&](auto two) __attribute__((always_inline)) {
-    constexpr bool TWO = decltype(two)::value;
+#pragma unroll 1
+  while (t <= t_hi) {
     // when a tile has arrived, everybody is done with the one before it, whose place the next request takes
     if (t + STAGES - 2 <= t_hi) mfma::arrived_all<LOADS *(STAGES - 2)>();
     else mfma::arrived_all<0>();
@@ -201,7 +202,7 @@ __device__ __forceinline__ void walk_tree(const Args &a, int g, const Walk &w)
     if (t + STAGES - 1 <= t_hi) request(t + STAGES - 1, k == 0 ? STAGES - 1 : k - 1);
     k = k == STAGES - 1 ? 0 : k + 1;
     ++t;
-    if (!on) return;
+    if (!on) continue;
     const uint16_t *ks = lds + here * (2 * TILE);
     bf16x8 kf[D / 16], vf[2][NB];
 #pragma unroll
@@ -249,10 +250,8 @@ __device__ __forceinline__ void walk_tree(const Args &a, int g, const Walk &w)
         const float pb = __builtin_amdgcn_exp2f(fmaf(sc[i + 1], scale, -ref));
         pf[i >> 3][i & 7] = (__bf16)pa;
         pf[i >> 3][(i & 7) + 1] = (__bf16)pb;
-        if constexpr (TWO) {
-          rest[i >> 3][i & 7] = (__bf16)(pa - (float)pf[i >> 3][i & 7]);
-          rest[i >> 3][(i & 7) + 1] = (__bf16)(pb - (float)pf[i >> 3][(i & 7) + 1]);
-        }
+        rest[i >> 3][i & 7] = (__bf16)(pa - (float)pf[i >> 3][i & 7]);
+        rest[i >> 3][(i & 7) + 1] = (__bf16)(pb - (float)pf[i >> 3][(i & 7) + 1]);
         sa = i == 0 ? pa : sa + pa;
         sb = i == 0 ? pb : sb + pb;
       }
@@ -265,12 +264,10 @@ __device__ __forceinline__ void walk_tree(const Args &a, int g, const Walk &w)
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int mb = 0; mb < NB; ++mb) {
-        if constexpr (TWO) oacc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[h][mb], rest[h], oacc[mb], 0, 0, 0);
+        oacc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[h][mb], rest[h], oacc[mb], 0, 0, 0);
         oacc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[h][mb], pf[h], oacc[mb], 0, 0, 0);
       }
-  };
-  while (t <= t_hi && !fine) turn(std::false_type{});
-  while (t <= t_hi) turn(std::true_type{});
+  }
   mfma::arrived_all<0>();
 
   // ---- results: through LDS, where the key groups are joined and neighbouring lanes get neighbouring channels.  Chunk c (16 bytes) of a row
