@@ -87,12 +87,24 @@ __device__ __forceinline__ double exp2_sum(const double (&t)[N])
 }
 
 constexpr double kLog2e = 1.4426950408889634;
-// e^(x - m) for x <= m, neither infinite (beyond e^-690: that)
+constexpr double kLeastExp = -690.0;  // e^-690 of a sum that is 1 or more: nothing
+// (x - m) log2 e for x <= m, m finite, from e^-690 on (x that is -inf or NaN: that).  The difference is taken in 64 bits, where it is exact or far
+// below -690.
+__device__ __forceinline__ double log2_from(double x, double m) { return fmax(x - m, kLeastExp) * kLog2e; }
 __device__ __forceinline__ double exp_from(double x, double m)
 {
-  const double t[1] = {fmax(x - m, -690.0) * kLog2e};
+  const double t[1] = {log2_from(x, m)};
   return exp2_sum(t);
 }
+// The same as one product and sum, for many logits by one m near 0 (up to kNear: m log2 e is off by 2^-41, and a 32-bit m - 690 by 2^-12).
+// (Farther, m log2 e would be off by as much as differences are, and m - 690 be m.)
+constexpr float kNear = 4096.0f;
+struct FromNear {
+  float least;
+  double ref;
+  __device__ __forceinline__ explicit FromNear(float m) : least(m + (float)kLeastExp), ref(-(double)m * kLog2e) {}
+  __device__ __forceinline__ double log2(float x) const { return fma((double)(x > least ? x : least), kLog2e, ref); }
+};
 
 __device__ __forceinline__ float element(const float *p) { return *p; }
 __device__ __forceinline__ float element(const bf16_t *p) { return __uint_as_float((unsigned)p->bits << 16); }
@@ -301,18 +313,21 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(4))
     if (!by_table) {
       const float m_new = fmaxf(m, wave_max(top));
       if (m_new > -INFINITY && m_new < INFINITY) {
-        const double ref = -(double)m_new * kLog2e;
         if (m_new > m) s = m > -INFINITY ? s * exp_from(m, m_new) : 0.0;
-        const float low = m_new - 690.0f;  // (e^-690 of a sum that is 1 or more)
+        auto add = [&](auto log2) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < LD; ++j) {
-          double t[VEC];
+          for (int j = 0; j < LD; ++j) {
+            double t[VEC];
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) {
-            const float x = P::get(v[j], e);
-            t[e] = fma((double)(x > low ? x : low), kLog2e, ref);
+            for (int e = 0; e < VEC; ++e) t[e] = log2(P::get(v[j], e));
+            s += exp2_sum(t);
           }
-          s += exp2_sum(t);
+        };
+        if (fabsf(m_new) <= kNear) {
+          const FromNear near(m_new);
+          add([&](float x) { return near.log2(x); });
+        } else {
+          add([&](float x) { return log2_from((double)x, (double)m_new); });
         }
       }
       m = m_new;
@@ -445,9 +460,10 @@ __device__ __forceinline__ int rank_of(const u64 *p, const u64 *k, const unsigne
   return r + __shfl_xor(r, 2);
 }
 
-// log sum exp of W beams' rows from the `lists` sums of each: as many lanes a beam as it has sums.
+// log sum exp of W beams' rows from the `lists` sums of each: as many lanes a beam as it has sums.  It is left as the largest logit and the log of
+// the sum by it: their own sum would lose of the log what the largest logit's unit is.
 template <int THREADS>
-__device__ __forceinline__ void join_sums(const double2 *stats, int W, int lists, int wv, int lane, double *lse_s)
+__device__ __forceinline__ void join_sums(const double2 *stats, int W, int lists, int wv, int lane, double2 *lse_s)
 {
   int per = 1;
   while (per < lists && per < 64) per *= 2;
@@ -466,19 +482,19 @@ __device__ __forceinline__ void join_sums(const double2 *stats, int W, int lists
     for (int o = per / 2; o >= 1; o >>= 1) top = fmax(top, __shfl_xor(top, o));
     s = m > -INFINITY ? s * exp_from(m, top) : 0.0;
     for (int o = per / 2; o >= 1; o >>= 1) s += __shfl_xor(s, o);
-    if (at == 0 && w < W) lse_s[w] = top == INFINITY ? INFINITY : top + log(s);
+    if (at == 0 && w < W) lse_s[w] = make_double2(top, top == INFINITY ? 0.0 : log(s));
   }
 }
 
 // A key of a beam's candidate as a place in the order (only: the beam's first, and what it goes on as if it has ended); none: 0.
-__device__ __forceinline__ u64 place_of(double score, double lse, bool ended, bool only, int eos, u64 &key)
+__device__ __forceinline__ u64 place_of(double score, double2 lse, bool ended, bool only, int eos, u64 &key)
 {
   double to;
   if (ended) {  // goes on in one way
     key = key_of(0.0f, eos);
     to = only ? score : -INFINITY;
   } else {
-    to = key == 0 ? -INFINITY : score + ((double)logit_of((unsigned)(key >> 32)) - lse);
+    to = key == 0 ? -INFINITY : score + (((double)logit_of((unsigned)(key >> 32)) - lse.x) - lse.y);
   }
   return to > -INFINITY ? ordered(to) : 0;  // (a NaN neither)
 }
@@ -557,7 +573,8 @@ __global__ __launch_bounds__(THREADS) void merge_kernel(Args a)
   constexpr int FEW = 4, MOST = FEW * THREADS;  // candidates of a thread, and of all
   constexpr bool CHOOSE = MOST >= kMost * kMost;  // (fewer threads are for fewer candidates)
   static_assert(!CHOOSE || kLists <= THREADS, "");
-  __shared__ double lse_s[kMost], score_s[kMost];
+  __shared__ double2 lse_s[kMost];
+  __shared__ double score_s[kMost];
   __shared__ u64 p_s[MOST], k_s[MOST], group_s[THREADS / 64][64];
   __shared__ short chosen_s[kMost];
   __shared__ unsigned char w_s[MOST], ended_s[kMost];
@@ -649,15 +666,15 @@ __global__ __launch_bounds__(THREADS) void merge_kernel(Args a)
 // One history of few logits by itself: all of them are candidates, FEW a thread.
 // Which candidates count is decided in 32 bits, with the bound on what these can be off by on the safe side; the few that may are put in order in
 // 64.  A score in 32 bits is logit + c, c the beam's score less its sum: off by 2^-24 of c, of itself and of its sum with the bound, so by less than 2^-22
-// (|c| + |logit|).
+// (|c| + |logit|); the score in 64 bits, by less than 2^-48 of what c and the logit are differences of.
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void few_kernel(Args a)
 {
   constexpr int FEW = kFewLogits / 1024, MOST = FEW * THREADS, WAVES = THREADS / 64, N = 4;
   __shared__ u64 p_s[MOST], k_s[MOST];
   __shared__ unsigned group_s[WAVES][64];
-  __shared__ double2 stats_s[kMost + WAVES];
-  __shared__ double lse_s[kMost], score_s[kMost];
+  __shared__ double2 stats_s[kMost + WAVES], lse_s[kMost];
+  __shared__ double score_s[kMost];
   __shared__ float2 off_s[kMost];
   __shared__ unsigned char w_s[MOST], ended_s[kMost];
   __shared__ int count_s;
@@ -696,15 +713,10 @@ __global__ __launch_bounds__(THREADS) void few_kernel(Args a)
     for (int o = lanes / 2; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
     double s = 0.0;
     if (m > -INFINITY && m < INFINITY) {
-      const double ref = -(double)m * kLog2e;
-      const float low = m - 690.0f;  // (e^-690 of a sum that is 1 or more)
       for (int i = i0; i < n; i += lanes * N) {
         double t[N];
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-          const float y = i + lanes * j < n ? row[i + lanes * j] : low;
-          t[j] = fma((double)(y > low ? y : low), kLog2e, ref);
-        }
+        for (int j = 0; j < N; ++j) t[j] = log2_from(i + lanes * j < n ? (double)row[i + lanes * j] : -INFINITY, (double)m);
         s += exp2_sum(t);
       }
     }
@@ -716,9 +728,10 @@ __global__ __launch_bounds__(THREADS) void few_kernel(Args a)
   __syncthreads();
   // ---- the candidates ----
   if (tid < a.W) {
-    const double c = score_s[tid] - lse_s[tid];
+    const double c = (score_s[tid] - lse_s[tid].x) - lse_s[tid].y;
+    const float by_64 = fmaf(0x1p-48f, fabsf((float)score_s[tid]) + fabsf((float)lse_s[tid].x), 0x1p-120f);
     // (ended, or beyond 32 bits: each is a candidate, and none bounds the others.  -inf or NaN: none is a candidate)
-    off_s[tid] = ended_s[tid] || fabs(c) > 1e30 ? make_float2(0.0f, INFINITY) : make_float2((float)c, fmaf(0x1p-22f, fabsf((float)c), 0x1p-120f));
+    off_s[tid] = ended_s[tid] || fabs(c) > 1e30 ? make_float2(0.0f, INFINITY) : make_float2((float)c, fmaf(0x1p-22f, fabsf((float)c), by_64));
     if (!ended_s[tid] && !(c > -INFINITY)) off_s[tid] = make_float2(-INFINITY, 0.0f);
   }
   __syncthreads();
