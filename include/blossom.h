@@ -512,7 +512,7 @@ int blossom_kv_accept(const blossom_paged_params *p, int32_t keep_width, const i
  * and their entries in order.  With every page held by whom refs says, no page is written by two sequences.  No output may be
  * an input.  grow = 0 makes room for nothing; with parent[n] = n the call lets pages behind shortened sequences go, and makes room.
  *   ws   scratch, >= blossom_fork_workspace_bytes(p, n_new), 16-byte aligned
- * H, G, d and dtype are checked and not used; n_pages is at most 2^30.  The copies themselves are done, for each layer's caches, by blossom_kv_copy_pages.
+ * H, G, d and dtype are checked and not used; n_pages is at most 2^30, S and n_new are at most 2^20.  The copies themselves are done, for each layer's caches, by blossom_kv_copy_pages.
  */
 size_t blossom_fork_workspace_bytes(const blossom_paged_params *p, int32_t n_new);
 int blossom_kv_fork(const blossom_paged_params *p, int32_t n_new, int32_t grow, const int32_t *parent, const int32_t *page_table,

@@ -268,7 +268,7 @@ __global__ __launch_bounds__(kThreads) void fork_begin_kernel(Args a, Fork x)
 }
 __global__ __launch_bounds__(kThreads) void fork_rows_kernel(Args a, Fork x)
 {
-  const int n = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * kThreads + threadIdx.x) >> 6);
+  const int n = __builtin_amdgcn_readfirstlane((int)((blockIdx.x * kThreads + threadIdx.x) >> 6));
   if (n < max(x.N, a.S))
     fork_row(a, x, n, threadIdx.x & 63, [&](int p, int by) { atomicAdd(x.new_refs + p, by); }, [&](int p) { x.held[p] = 1; });
 }
@@ -281,6 +281,7 @@ __global__ __launch_bounds__(1024) void fork_give_kernel(Args a, Fork x)
 }
 // all of it, for few sequences and pages
 constexpr int kFewPages = 8192, kFewForks = 64;
+constexpr int kMostForks = 1 << 20;  // sequences: each looks through the parents of all
 __global__ __launch_bounds__(1024) void fork_kernel(Args a, Fork x)
 {
   __shared__ int refs_s[kFewPages];
@@ -303,7 +304,7 @@ __global__ __launch_bounds__(1024) void fork_kernel(Args a, Fork x)
 bool launch_fork(const Args &a, const Fork &x, hipStream_t st)
 {
   const long most = x.N > a.S ? x.N : a.S, rows = (most * 64 + kThreads - 1) / kThreads, pages = ((long)a.n_pages + kThreads - 1) / kThreads;
-  if (!countable(rows, kThreads) || a.n_pages > 1 << 30) return false;  // (pages are counted past the last)
+  if (most > kMostForks || a.n_pages > 1 << 30) return false;  // (pages are counted past the last)
   [&] {
     if (most <= kFewForks && most * a.max_pages <= 8192 && a.n_pages <= kFewPages) {
       BLOSSOM_LAUNCH(fork_kernel, dim3(1), dim3(1024), 0, st, a, x);
