@@ -84,8 +84,11 @@ struct Fork {
   const int *refs;             // [n_pages] who holds a page
   int *table, *len, *new_refs; // [N, max_pages], [N], [n_pages]
   int *copies, *missing;       // [N, 3] source, target, rows; [1]
-  int4 *at;                    // [N] a sequence's first page that is not whole, is it the eldest of its parent, page and rows that it
-                               // copies (below 0: none); in the workspace
+  int4 *at;                    // [N] a sequence's first fresh page, its last one where it keeps pages among them (else below 0), page and rows
+                               // that it copies (below 0: none; to its first fresh page); in the workspace
+  uint4 *asks;                 // [N, chunks] of the row of one that does, 64 entries at a time, which are fresh (low, high bits), and how many before
+                               // these are, there too
+  int chunks;
   int *fresh;                  // [N] pages that it gets, there too
   int *held;                   // [n_pages] does a copy read a page, there too
 };

@@ -120,8 +120,12 @@ int append(const blossom_paged_params *p, const void *Q, int64_t q_stride, const
   return launch_status();
 }
 
-// the fork's workspace: where a sequence's own pages begin, how many it asks for, copies that read a page
-size_t fork_ws_bytes(const Args &a, int n_new) { return (size_t)n_new * (sizeof(int4) + sizeof(int)) + a.n_pages * sizeof(int); }
+// the fork's workspace: where a sequence's own pages begin, which of them it asks for and how many, copies that read a page
+int fork_chunks(const Args &a) { return (a.max_pages + 63) / 64; }
+size_t fork_ws_bytes(const Args &a, int n_new)
+{
+  return (size_t)n_new * (sizeof(int4) + fork_chunks(a) * sizeof(uint4) + sizeof(int)) + a.n_pages * sizeof(int);
+}
 
 bool aligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
@@ -247,7 +251,9 @@ int blossom_kv_fork(const blossom_paged_params *p, int32_t n_new, int32_t grow, 
   x.N = n_new; x.grow = grow; x.parent = parent; x.refs = refs;
   x.table = new_table; x.len = new_len; x.new_refs = new_refs; x.copies = copies; x.missing = missing;
   x.at = static_cast<int4 *>(ws);
-  x.fresh = reinterpret_cast<int *>(x.at + n_new);
+  x.asks = reinterpret_cast<uint4 *>(x.at + n_new);
+  x.chunks = fork_chunks(a);
+  x.fresh = reinterpret_cast<int *>(x.asks + (size_t)n_new * x.chunks);
   x.held = x.fresh + n_new;
   (void)hipGetLastError();
   if (!launch_fork(a, x, (hipStream_t)hip_stream)) return BLOSSOM_ERR_SHAPE;

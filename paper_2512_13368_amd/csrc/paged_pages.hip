@@ -141,7 +141,7 @@ __device__ __forceinline__ void fork_row(const Args &a, const Fork &x, int n, in
   const Heir h(a, x, q);
   const int *from = a.page_table + (size_t)max(q, 0) * a.max_pages;
   int *to = x.table + (size_t)n * a.max_pages;
-  int fresh = 0, copy = -1;
+  int fresh = 0, copy = -1, first = 0, last = -1;  // (entries that ask: how many, the first and last of them)
   const int until = eldest ? a.max_pages : h.need;
   int next = lane < until ? from[lane] : -1;
   for (int i0 = 0; i0 < a.max_pages; i0 += 64) {
@@ -150,6 +150,10 @@ __device__ __forceinline__ void fork_row(const Args &a, const Fork &x, int n, in
     const bool taken = i < h.full || (i < h.need && eldest && old >= 0 && x.refs[old] == 1), asks = i < h.need && !taken;
     const unsigned long long all = __ballot(asks);
     const int before = __builtin_amdgcn_mbcnt_hi((unsigned)(all >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)all, 0));
+    if (all != 0ull) {
+      if (fresh == 0) first = i0 + __builtin_ctzll(all);
+      last = i0 + 63 - __builtin_clzll(all);
+    }
     if (asks && i == h.full && h.part > 0) copy = old;
     if (i < a.max_pages) to[i] = taken ? old : asks ? -2 - (fresh + before) : -1;
     fresh += __builtin_popcountll(all);
@@ -157,13 +161,22 @@ __device__ __forceinline__ void fork_row(const Args &a, const Fork &x, int n, in
     const int by = i < h.full ? heirs - 1 : taken ? 0 : -1;
     if (eldest && old >= 0 && by != 0) count(old, by);
   }
+  const bool apart = last - first + 1 != fresh;
+  if (apart) {  // pages that are kept lie among the fresh ones: where these are
+    int before = 0;
+    for (int i0 = first & ~63; i0 <= last; i0 += 64) {
+      const unsigned long long all = __ballot(i0 + lane <= last && to[i0 + lane] < -1);
+      if (lane == 0) x.asks[(size_t)n * x.chunks + (i0 >> 6)] = make_uint4((unsigned)all, (unsigned)(all >> 32), before, 0);
+      before += __builtin_popcountll(all);
+    }
+  }
   if (copy >= 0) hold(copy);
   const unsigned long long copies = __ballot(copy >= 0);
   copy = __builtin_amdgcn_readlane(copy, copies ? __builtin_ctzll(copies) : 0);
   if (lane == 0) {
     x.fresh[n] = fresh;
     x.len[n] = h.len;
-    x.at[n] = make_int4(h.full, eldest, copy, h.part);
+    x.at[n] = make_int4(first, apart ? last : -1, copy, h.part);
     x.copies[3 * n] = x.copies[3 * n + 1] = -1;
     x.copies[3 * n + 2] = 0;
   }
@@ -171,7 +184,9 @@ __device__ __forceinline__ void fork_row(const Args &a, const Fork &x, int n, in
 
 // Fresh pages, by one workgroup of 1024: the k-th free page goes to the k-th request.  Pages are looked at 1024 EACH at a time, a wavefront 64 by
 // 64, and listed; then every thread has a request.  (2000 free pages behind a million that are held: 200 us; 4096 pages at a time, each thread's
-// own given out by itself, 512 sequences 7.6 us, so 5.8.)  (held_of(p): 0 if page p is free; given_out(p): it is given.)
+// own given out by itself, 512 sequences 7.6 us, so 5.8.)  An eldest's requests may lie among pages that it keeps: then fork_row leaves in x.asks
+// which 64 entries at a time ask.  (Found by looking from the row's first on, 65536 pages for 64 rows took 4.8 ms, for 8 rows
+// 19; so 0.08 and 0.09.)  (held_of(p): 0 if page p is free; given_out(p): it is given.)
 template <int EACH, typename F, typename G>
 __device__ __forceinline__ void fork_give(const Args &a, const Fork &x, int tid, F &&held_of, G &&given_out)
 {
@@ -239,9 +254,20 @@ __device__ __forceinline__ void fork_give(const Args &a, const Fork &x, int tid,
       const int4 at = near ? at_s[lo] : x.at[lo];
       int i = at.x;
       int *row = x.table + (size_t)lo * a.max_pages;
-      if (!at.y) i += nth;  // (its entries from there on all ask)
-      else
-        while (row[i] != -2 - nth) ++i;
+      if (at.y < 0) i += nth;
+      else {  // the last 64 entries before which no more than nth ask, and of those that ask here the one
+        int c = at.x >> 6, end = (at.y >> 6) + 1;
+        const uint4 *asks = x.asks + (size_t)lo * x.chunks;
+        while (end - c > 1) {
+          const int mid = (c + end) >> 1;
+          if ((int)asks[mid].z <= nth) c = mid;
+          else end = mid;
+        }
+        const uint4 here = asks[c];
+        unsigned long long all = (unsigned long long)here.y << 32 | here.x;
+        for (int left = nth - (int)here.z; left > 0; --left) all &= all - 1;
+        i = 64 * c + __builtin_ctzll(all);
+      }
       row[i] = p;
       given_out(p);
       if (i == at.x && at.z >= 0) {
