@@ -632,7 +632,10 @@ bool launch_prompt(const Args &call, hipStream_t st)
   return true;
 }
 
-// Drafted trees.
+// Drafted trees.  Which kernel goes by the mean of a sequence's rows, for the host knows no more: sequences with one token or none count too (one
+// tree of 64 tokens among 63 of one, over 4000 positions each, 32 heads over 8, d = 128: 192 us by the 16-row kernel, which walks the one
+// tree's keys once for each 16 rows; that tree alone takes 41 and the others 180).  17 rows and more are the 128-row kernel's, in which
+// wavefronts without rows move tiles alone (26 rows over 2000, 20000 and 131040 positions, 8 heads: 19, 26 and 92 us, the last 5.8 TB/s).
 void plan_tree(Args &a)
 {
   const int row_bytes = row_bytes_of(a), w = few_waves(row_bytes);

@@ -8,12 +8,12 @@
 //    tile: a tree's rows do less with a tile than a prompt's, and memory has to be kept busy for them.
 //  - S^T = K Q^T, softmax and O^T += V^T P^T as in paged_prompt.hip, but both bf16 terms of P always: P rounded to bf16 once leaves outputs off by
 //    2.3e-3 of their norm where their own rounding is 1.6e-3, and trees of up to 16 rows keep both terms too.
-// Measured: 26 drafted tokens over 131040 positions (32 heads over 8, d = 128: 537 MB) 131 us, 8 of it the join, where reading as many bytes
-// takes 78; 33 to 64 over 4000 to 8100 for 16 sequences (412 MB, 73 GFLOP) 164 us, 10 of it the join.  The second term takes 20 and 28 of these (111
-// and 136 without; 26 tokens over 131040, one head over each of 8, 92 and 89; 100 trees of 20 to 64 over 300 to 900, d = 64, 36.6 and 32.2): the matrix
-// pipe does half as much again, and waits for the vector ALUs as before.  Its product after the first one's, so that the remainders are
-// taken meanwhile, gains nothing (132 and 168).
-// Of the walk with P rounded once (111 and 136): with everything but the loads left out, 96; with the loads left out, 114; with both, 41:
+// Measured: 26 drafted tokens over 131040 positions (32 heads over 8, d = 128: 537 MB) 129 us, 8 of it the join, where reading as many bytes
+// takes 78; 33 to 64 over 4000 to 8100 for 16 sequences (412 MB, 73 GFLOP) 166 us, 10 of it the join.  The second term takes 21 and 30 of these (108
+// and 136 without; 26 tokens over 131040, one head over each of 8, 92 and 89; 100 trees of 20 to 64 over 300 to 900, d = 64, 36.6 and 32.2): half as
+// many matrix instructions again, and three vector instructions more a probability.  Its product after the first one's, so that the
+// remainders are taken meanwhile, gains nothing.
+// Of the walk with P rounded once, 136: with everything but the loads left out, 96; with the loads left out, 114; with both, 41:
 // launch, finding the rows, pages and queries, 17 to 36 MB of partial sums.  Tried there: workgroups of 128 rows, two on a CU (150: K and V are moved
 // twice); keys' operands read a tile ahead (no gain); the next tile's logits among this one's exponentials (145); a barrier for two tiles at
 // once (139), half the wavefronts at a higher priority (no gain); 64 rows a wavefront, one a SIMD (the compiler spills).
