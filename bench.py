@@ -39,12 +39,12 @@ CSRC = os.path.join(ROOT, "paper_2512_13368_amd", "csrc")
 
 
 def sources_sha256():
-    """Hash of the kernel sources that the workloads run (the paged cache's serve no workload here): a stored
-    profile figure is only quoted for the code it was measured on."""
+    """Hash of the kernel sources that the workloads run (the paged cache's and beam search's serve no workload here): a
+    stored profile figure is only quoted for the code it was measured on."""
     import hashlib
     h = hashlib.sha256()
     for name in sorted(os.listdir(CSRC)):
-        if name.endswith((".hip", ".h")) and not name.startswith("paged"):
+        if name.endswith((".hip", ".h")) and not name.startswith(("paged", "beam")):
             h.update(name.encode())
             h.update(open(os.path.join(CSRC, name), "rb").read())
     return h.hexdigest()
