@@ -55,7 +55,7 @@ def test_long_rows_take_no_longer():
         out = B.kv_fork(p, parent, table, n, refs, grow=8 * width)
         ws = torch.empty(B.fork_workspace_bytes(p, S), dtype=torch.uint8, device="cuda")
         times = []
-        for _ in range(5):
+        for _ in range(20):
             a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
             a.record()
             B.kv_fork(p, parent, table, n, refs, grow=8 * width, new_table=out[0], new_len=out[1], new_refs=out[2], copies=out[3], missing=out[4], ws=ws)
